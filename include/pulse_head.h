@@ -1,0 +1,87 @@
+/*
+ * pulse_head.h -- C ABI of libpulse's operators at a model's output end.
+ *
+ * The weights whose changes the codec of pulse.h carries are trained and used
+ * here: the trainer normalises the last hidden states, takes the cross entropy
+ * of the head's logits and its gradient; a receiver multiplies its current
+ * tokens with weights that it holds as FP8 or MXFP4 codes.
+ *
+ * Conventions: those of pulse.h (device pointers, a hipStream_t passed as
+ * void*, work enqueued and not waited for, no device memory allocated,
+ * PULSE_OK or a negative pulse_status with pulse_last_error()).  Unless said
+ * otherwise:
+ *   - matrices are row-major; a stride is the number of elements from one row
+ *     to the next and at least the row's length;
+ *   - dense pointers are 16-byte aligned (else PULSE_EALIGN);
+ *   - outputs do not overlap inputs;
+ *   - a workspace is 256-byte aligned, needs no initialisation, holds nothing
+ *     between calls, and serves any calls ordered on one stream;
+ *   - results are the same bits for the same inputs: no atomics, a fixed order
+ *     of every sum.
+ * Sums, statistics and products are accumulated in FP32.
+ */
+#ifndef PULSE_HEAD_H
+#define PULSE_HEAD_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "pulse.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Element types beside PULSE_DTYPE_FP8_E4M3 and PULSE_DTYPE_MXFP4. */
+#define PULSE_DTYPE_F32 3
+#define PULSE_DTYPE_BF16 4
+
+/* The largest row that the norm handles. */
+#define PULSE_NORM_MAX_COLS 16384
+
+/* Flag of the norm: no mean is taken off and none is written (RMS norm). */
+#define PULSE_NORM_RMS 1u
+
+/*
+ * pulse_layer_norm_forward -- per row of x, with n = cols:
+ *   mean = sum(x) / n (0 with PULSE_NORM_RMS),
+ *   rstd = 1 / sqrt(sum((x - mean)^2) / n + eps),
+ *   y = (x - mean) * rstd * weight + bias, rounded once to y's type.
+ *   dtype         of x and y: PULSE_DTYPE_F32 or PULSE_DTYPE_BF16.
+ *   weight, bias  [cols] of `param_dtype` (F32 or BF16); bias may be NULL.
+ *   mean          FP32 [rows]; ignored with PULSE_NORM_RMS (may be NULL then).
+ *   rstd          FP32 [rows].
+ *   x_stride, y_stride   elements from row to row.
+ * cols is 1 to PULSE_NORM_MAX_COLS.  Rows of 16-byte groups (cols and strides
+ * multiples of 8) are moved 16 bytes at a time; any other row element by
+ * element.
+ */
+int pulse_layer_norm_forward(int dtype, const void *x, uint64_t x_stride, int param_dtype,
+                             const void *weight, const void *bias, void *y, uint64_t y_stride,
+                             float *mean, float *rstd, uint64_t rows, uint32_t cols, float eps,
+                             uint32_t flags, void *stream);
+
+/* Workspace of pulse_layer_norm_backward for rows of `cols` elements. */
+size_t pulse_layer_norm_workspace_bytes(uint32_t cols);
+
+/*
+ * pulse_layer_norm_backward -- the gradient of a forward pass that gave mean
+ * and rstd.  With xh = (x - mean) * rstd and a = dy * weight, per row
+ *   dx = rstd * (a - sum(a)/n - xh * sum(a * xh)/n)
+ * (without the middle term with PULSE_NORM_RMS), rounded once to dx's type, and
+ *   dweight = sum over rows of dy * xh,   dbias = sum over rows of dy.
+ *   dweight, dbias  FP32 [cols]; dbias may be NULL.
+ * rows == 0 sets dweight and dbias to zero.
+ */
+int pulse_layer_norm_backward(int dtype, const void *dy, uint64_t dy_stride, const void *x,
+                              uint64_t x_stride, int param_dtype, const void *weight,
+                              const float *mean, const float *rstd, void *dx, uint64_t dx_stride,
+                              float *dweight, float *dbias, uint64_t rows, uint32_t cols,
+                              uint32_t flags, void *workspace, size_t workspace_bytes,
+                              void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* PULSE_HEAD_H */

@@ -1,0 +1,70 @@
+// head.hpp -- parameter blocks, launchers and device helpers of the operators
+// at a model's output end (include/pulse_head.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+namespace pulse {
+
+// ---------------------------------------------------------------- norm
+
+constexpr uint32_t kNormMaxCols = 16384;
+constexpr uint32_t kNormBlocks = 512;  // blocks of the backward pass, each with its column sums
+
+struct NormParams {
+  const void* x;
+  uint64_t x_stride;
+  const void* weight;
+  const void* bias;  // may be null
+  void* y;
+  uint64_t y_stride;
+  float* mean;  // null: RMS form
+  float* rstd;
+  uint64_t rows;
+  uint32_t cols;
+  float eps;
+  int param_bf16;
+};
+
+struct NormGradParams {
+  const void* dy;
+  uint64_t dy_stride;
+  const void* x;
+  uint64_t x_stride;
+  const void* weight;
+  const float* mean;  // null: RMS form
+  const float* rstd;
+  void* dx;
+  uint64_t dx_stride;
+  float* dweight;
+  float* dbias;    // may be null
+  float* partial;  // [blocks][cols] of dweight, then of dbias
+  uint64_t rows;
+  uint32_t cols;
+  int param_bf16;
+};
+
+hipError_t launch_layer_norm(bool bf16, const NormParams& p, hipStream_t stream);
+hipError_t launch_layer_norm_grad(bool bf16, const NormGradParams& p, hipStream_t stream);
+
+// ---------------------------------------------------------------- device helpers
+
+// The wave's sum in every lane: within rows of 16 lanes by DPP, then the four
+// rows' sums through scalar registers.  A fixed order, no LDS.
+__device__ __forceinline__ float wave_sum(float v) {
+  auto add = [&](auto ctrl) {
+    v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xF,
+                                                    0xF, true));
+  };
+  add(std::integral_constant<int, 0xB1>{});   // quad_perm 1,0,3,2
+  add(std::integral_constant<int, 0x4E>{});   // quad_perm 2,3,0,1
+  add(std::integral_constant<int, 0x141>{});  // row_half_mirror
+  add(std::integral_constant<int, 0x140>{});  // row_mirror
+  auto row = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+  return (row(0) + row(16)) + (row(32) + row(48));
+}
+
+}  // namespace pulse

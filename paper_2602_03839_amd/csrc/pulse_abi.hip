@@ -1,8 +1,6 @@
 // pulse_abi.hip -- the extern "C" entry points of libpulse (declared in
 // include/pulse.h): argument validation on the host, splitting of batches
 // into launches, and kernel launch on the caller's stream.
-#include <stdarg.h>
-#include <stdio.h>
 #include <string.h>
 
 #include <algorithm>
@@ -10,33 +8,18 @@
 #include <vector>
 
 #include "../../include/pulse.h"
+#include "abi_status.hpp"
 #include "device_common.hpp"
 #include "launch.hpp"
 
 namespace {
 
-thread_local char g_last_error[512];
-
-int fail(int status, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_last_error, sizeof g_last_error, fmt, ap);
-  va_end(ap);
-  return status;
-}
-
-int ok() {
-  g_last_error[0] = '\0';
-  return PULSE_OK;
-}
-
-bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
-bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-
-int hip_status(hipError_t e, const char* what) {
-  if (e != hipSuccess) return fail(PULSE_EHIP, "%s: %s", what, hipGetErrorString(e));
-  return ok();
-}
+using pulse::aligned;
+using pulse::aligned16;
+using pulse::fail;
+using pulse::g_last_error;
+using pulse::hip_status;
+using pulse::ok;
 
 int check_workspace(void* ws, size_t bytes) {
   if (!ws) return fail(PULSE_EINVAL, "workspace is NULL");

@@ -1,0 +1,164 @@
+"""ctypes binding to libpulse.so's operators at a model's output end (C ABI in
+include/pulse_head.h).
+
+Argument marshalling only, like ``pulse``: every call takes torch tensors that
+already live on the GPU, passes their device pointers and the current HIP
+stream to the C entry point, and raises ``pulse.PulseError`` on a non-zero
+status.  A class holds what a program keeps beside its weights (the weight
+itself and the call's workspace); one object's calls must be ordered on one
+stream.  Matrices are two-dimensional with rows of adjacent elements; rows may
+lie further apart than their length (a view's stride), weights may not.
+
+Outputs are allocated on the stream that the call runs on unless they are given.
+"""
+from __future__ import annotations
+
+import ctypes
+import threading
+from typing import Optional
+
+import torch
+
+from . import pulse
+from .pulse import PulseError, _check, _f32, _p, _stream
+
+F32, BF16 = 3, 4  # PULSE_DTYPE_F32, PULSE_DTYPE_BF16
+NORM_RMS = 1      # PULSE_NORM_RMS
+NORM_MAX_COLS = 16384
+
+EXPORTS = ("pulse_layer_norm_workspace_bytes", "pulse_layer_norm_forward",
+           "pulse_layer_norm_backward")
+
+_lock = threading.Lock()
+_lib = None
+
+
+def lib():
+    """libpulse.so with this module's entry points declared."""
+    global _lib
+    if _lib is not None:
+        return _lib
+    L = pulse.lib()
+    with _lock:
+        if _lib is None:
+            vp, u64, u32, f32, i32 = (ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32,
+                                      ctypes.c_float, ctypes.c_int)
+            sz = ctypes.c_size_t
+            L.pulse_layer_norm_workspace_bytes.argtypes = [u32]
+            L.pulse_layer_norm_forward.argtypes = [i32, vp, u64, i32, vp, vp, vp, u64, vp, vp, u64,
+                                                   u32, f32, u32, vp]
+            L.pulse_layer_norm_backward.argtypes = [i32, vp, u64, vp, u64, i32, vp, vp, vp, vp, u64,
+                                                    vp, vp, u64, u32, u32, vp, sz, vp]
+            for name in EXPORTS:
+                getattr(L, name).restype = sz if name.endswith("_workspace_bytes") else i32
+            _lib = L
+    return _lib
+
+
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _dtype(t: torch.Tensor, name: str) -> int:
+    code = _DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if code is None:
+        raise PulseError(f"{name} must be float32 or bfloat16, got {getattr(t, 'dtype', type(t).__name__)}")
+    return code
+
+
+def _matrix(t: torch.Tensor, name: str, cols: int, rows: Optional[int] = None, dtype=None, device=None):
+    """(pointer, row stride) of a device matrix whose rows are adjacent elements."""
+    if not isinstance(t, torch.Tensor):
+        raise PulseError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
+    if not t.is_cuda:
+        raise PulseError(f"{name} must be a device tensor (got {t.device})")
+    if t.dim() != 2 or t.shape[1] != cols or (rows is not None and t.shape[0] != rows):
+        want = f"[{'rows' if rows is None else rows}, {cols}]"
+        raise PulseError(f"{name} must have the shape {want}, got {list(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise PulseError(f"{name} must be {dtype}, got {t.dtype}")
+    if device is not None and t.device != device:
+        raise PulseError(f"{name} is on {t.device}, the call's other tensors on {device}")
+    stride = t.stride(0) if t.shape[0] > 1 else cols
+    if (cols > 1 and t.stride(1) != 1) or stride < cols:
+        raise PulseError(f"{name} must have rows of adjacent elements that do not overlap "
+                         f"(strides {t.stride()})")
+    return t.data_ptr(), stride
+
+
+def _new(shape, dtype, device, stream):
+    """An output on the stream that will write it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class LayerNorm:
+    """Layer norm, or RMS norm with ``rms``, over the last axis.
+
+    ``weight`` and ``bias`` (may be None) are [cols], both float32 or both
+    bfloat16; activations are float32 or bfloat16 of their own.
+    """
+
+    def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                 eps: float = 1e-6, rms: bool = False):
+        self._dt = _dtype(weight, "weight")
+        self.device, self.cols = weight.device, weight.numel()
+        _p(weight, "weight", optional=False)
+        _p(bias, "bias", dtype=weight.dtype, numel=self.cols, device=self.device)
+        if not 1 <= self.cols <= NORM_MAX_COLS:
+            raise PulseError(f"weight has {self.cols} elements, 1 to {NORM_MAX_COLS} are handled")
+        self.weight, self.bias, self.eps, self.rms = weight, bias, float(eps), bool(rms)
+        self.ws = torch.empty(int(lib().pulse_layer_norm_workspace_bytes(self.cols)),
+                              dtype=torch.uint8, device=self.device)
+
+    def __call__(self, x: torch.Tensor, y: Optional[torch.Tensor] = None,
+                 mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None):
+        """(y, mean, rstd) of x [rows, cols]; mean is None for the RMS form."""
+        dev, dt = self.device, _dtype(x, "x")
+        px, sx = _matrix(x, "x", self.cols, device=dev)
+        rows = x.shape[0]
+        if y is None:
+            y = _new((rows, self.cols), x.dtype, dev, stream)
+        py, sy = _matrix(y, "y", self.cols, rows, x.dtype, dev)
+        if self.rms:
+            mean = None
+        elif mean is None:
+            mean = _new((rows,), torch.float32, dev, stream)
+        if rstd is None:
+            rstd = _new((rows,), torch.float32, dev, stream)
+        _check(lib().pulse_layer_norm_forward(
+            dt, px, sx, self._dt, self.weight.data_ptr(),
+            None if self.bias is None else self.bias.data_ptr(), py, sy,
+            _f32(mean, "mean", rows, dev, optional=True), _f32(rstd, "rstd", rows, dev), rows,
+            self.cols, self.eps, NORM_RMS if self.rms else 0, _stream(stream, dev)),
+            "pulse_layer_norm_forward")
+        return y, mean, rstd
+
+    def backward(self, dy: torch.Tensor, x: torch.Tensor, mean: Optional[torch.Tensor],
+                 rstd: torch.Tensor, dx: Optional[torch.Tensor] = None,
+                 dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                 stream=None):
+        """(dx, dweight, dbias) for the upstream gradient dy and the forward
+        pass's x, mean and rstd; dbias is None where there is no bias."""
+        dev, dt = self.device, _dtype(x, "x")
+        px, sx = _matrix(x, "x", self.cols, device=dev)
+        rows = x.shape[0]
+        pdy, sdy = _matrix(dy, "dy", self.cols, rows, x.dtype, dev)
+        if dx is None:
+            dx = _new((rows, self.cols), x.dtype, dev, stream)
+        pdx, sdx = _matrix(dx, "dx", self.cols, rows, x.dtype, dev)
+        if dweight is None:
+            dweight = _new((self.cols,), torch.float32, dev, stream)
+        if self.bias is None:
+            dbias = None
+        elif dbias is None:
+            dbias = _new((self.cols,), torch.float32, dev, stream)
+        _check(lib().pulse_layer_norm_backward(
+            dt, pdy, sdy, px, sx, self._dt, self.weight.data_ptr(),
+            None if self.rms else _f32(mean, "mean", rows, dev), _f32(rstd, "rstd", rows, dev), pdx,
+            sdx, _f32(dweight, "dweight", self.cols, dev),
+            _f32(dbias, "dbias", self.cols, dev, optional=True), rows, self.cols,
+            NORM_RMS if self.rms else 0, self.ws.data_ptr(), self.ws.numel(), _stream(stream, dev)),
+            "pulse_layer_norm_backward")
+        return dx, dweight, dbias
