@@ -80,6 +80,25 @@ int pulse_layer_norm_backward(int dtype, const void *dy, uint64_t dy_stride, con
                               uint32_t flags, void *workspace, size_t workspace_bytes,
                               void *stream);
 
+/*
+ * pulse_lowp_matmul -- y = x W^T, W the receiver's copy of a [rows, cols]
+ * weight as pulse_cast_lowp and pulse_apply_lowp_batch leave it (codes flat in
+ * row order, an MXFP4 block any 32 consecutive values, so a block may span two
+ * rows):
+ *   W = code * 2^(scale - 127)  (MXFP4; a block with scale 0xFF is NaN),
+ *   W = code / inv_scale        (FP8 E4M3, inv_scale as it was cast with).
+ * Meant for the few tokens of a decoding step: the weight is read once for
+ * every 64 tokens.  Products are exact, summed in FP32, rounded once to y.
+ *   dtype    PULSE_DTYPE_MXFP4 (codes 4-byte aligned) or PULSE_DTYPE_FP8_E4M3
+ *            (codes 8-byte aligned; scales unused).
+ *   x        BF16 [tokens, cols]; y [tokens, rows] of `y_dtype` (F32 or BF16).
+ * rows and cols are at least 1 and below 2^31; tokens at most 2^20; inv_scale
+ * is finite and not zero for FP8.
+ */
+int pulse_lowp_matmul(int dtype, const uint8_t *codes, const uint8_t *scales, float inv_scale,
+                      uint32_t rows, uint32_t cols, const uint16_t *x, uint64_t x_stride,
+                      uint32_t tokens, int y_dtype, void *y, uint64_t y_stride, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

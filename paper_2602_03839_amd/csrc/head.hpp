@@ -50,7 +50,28 @@ struct NormGradParams {
 hipError_t launch_layer_norm(bool bf16, const NormParams& p, hipStream_t stream);
 hipError_t launch_layer_norm_grad(bool bf16, const NormGradParams& p, hipStream_t stream);
 
+// ---------------------------------------------------------------- low-bit products
+
+struct LowpMatmulParams {
+  const uint8_t* codes;
+  const uint8_t* scales;  // MXFP4
+  float inv_scale;        // FP8
+  uint32_t rows, cols;
+  uint64_t code_bytes, scale_bytes;
+  const uint16_t* x;
+  uint64_t x_stride;
+  uint32_t tokens;
+  void* y;
+  uint64_t y_stride;
+  int y_bf16;
+};
+
+hipError_t launch_lowp_matmul(bool mxfp4, const LowpMatmulParams& p, hipStream_t stream);
+
 // ---------------------------------------------------------------- device helpers
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
 // The wave's sum in every lane: within rows of 16 lanes by DPP, then the four
 // rows' sums through scalar registers.  A fixed order, no LDS.

@@ -99,4 +99,30 @@ int pulse_layer_norm_backward(int dtype, const void* dy, uint64_t dy_stride, con
                     "layer_norm backward launch");
 }
 
+int pulse_lowp_matmul(int dtype, const uint8_t* codes, const uint8_t* scales, float inv_scale,
+                      uint32_t rows, uint32_t cols, const uint16_t* x, uint64_t x_stride,
+                      uint32_t tokens, int y_dtype, void* y, uint64_t y_stride, void* stream) {
+  const char* who = "lowp matmul";
+  const bool mx = dtype == PULSE_DTYPE_MXFP4;
+  if (!mx && dtype != PULSE_DTYPE_FP8_E4M3)
+    return fail(PULSE_EINVAL, "%s: dtype %d is neither FP8_E4M3 nor MXFP4", who, dtype);
+  if (y_dtype != PULSE_DTYPE_F32 && y_dtype != PULSE_DTYPE_BF16)
+    return fail(PULSE_EINVAL, "%s: y_dtype %d is neither F32 nor BF16", who, y_dtype);
+  if (rows == 0 || rows > 0x7FFFFFFFu || cols == 0 || cols > 0x7FFFFFFFu)
+    return fail(PULSE_EINVAL, "%s: a weight of %u x %u", who, rows, cols);
+  if (tokens > 1u << 20) return fail(PULSE_EINVAL, "%s: more than 2^20 tokens", who);
+  if (tokens == 0) return ok();
+  if (!codes) return fail(PULSE_EINVAL, "%s: codes is NULL", who);
+  if (mx && !scales) return fail(PULSE_EINVAL, "%s: scales is NULL", who);
+  if (!aligned(codes, mx ? 4 : 8)) return fail(PULSE_EALIGN, "%s: codes not %d-byte aligned", who, mx ? 4 : 8);
+  if (!mx && !(inv_scale - inv_scale == 0.0f && inv_scale != 0.0f))
+    return fail(PULSE_EINVAL, "%s: inv_scale is zero or not finite", who);
+  if (int rc = check_matrix(who, "x", x, x_stride, tokens, cols)) return rc;
+  if (int rc = check_matrix(who, "y", y, y_stride, tokens, rows)) return rc;
+  const uint64_t n = (uint64_t)rows * cols;
+  pulse::LowpMatmulParams p = {codes, scales, inv_scale, rows, cols, mx ? (n + 1) / 2 : n, (n + 31) / 32,
+                               x, x_stride, tokens, y, y_stride, y_dtype == PULSE_DTYPE_BF16};
+  return hip_status(pulse::launch_lowp_matmul(mx, p, (hipStream_t)stream), "lowp matmul launch");
+}
+
 }  // extern "C"

@@ -27,7 +27,7 @@ NORM_RMS = 1      # PULSE_NORM_RMS
 NORM_MAX_COLS = 16384
 
 EXPORTS = ("pulse_layer_norm_workspace_bytes", "pulse_layer_norm_forward",
-           "pulse_layer_norm_backward")
+           "pulse_layer_norm_backward", "pulse_lowp_matmul")
 
 _lock = threading.Lock()
 _lib = None
@@ -49,6 +49,7 @@ def lib():
                                                    u32, f32, u32, vp]
             L.pulse_layer_norm_backward.argtypes = [i32, vp, u64, vp, u64, i32, vp, vp, vp, vp, u64,
                                                     vp, vp, u64, u32, u32, vp, sz, vp]
+            L.pulse_lowp_matmul.argtypes = [i32, vp, vp, f32, u32, u32, vp, u64, u32, i32, vp, u64, vp]
             for name in EXPORTS:
                 getattr(L, name).restype = sz if name.endswith("_workspace_bytes") else i32
             _lib = L
@@ -160,5 +161,34 @@ class LayerNorm:
             sdx, _f32(dweight, "dweight", self.cols, dev),
             _f32(dbias, "dbias", self.cols, dev, optional=True), rows, self.cols,
             NORM_RMS if self.rms else 0, self.ws.data_ptr(), self.ws.numel(), _stream(stream, dev)),
-            "pulse_layer_norm_backward")
+            "pulse_layer_norm_backward", "pulse_lowp_matmul")
         return dx, dweight, dbias
+
+
+class LowpLinear:
+    """Products with a [rows, cols] weight that a receiver holds as MXFP4 or FP8
+    codes (the tensors that ``pulse.ApplyLowpBatch`` patches in place)."""
+
+    def __init__(self, dtype: int, codes: torch.Tensor, scales: Optional[torch.Tensor], rows: int,
+                 cols: int, inv_scale: float = 1.0):
+        nc, ns = pulse.lowp_sizes(dtype, rows * cols)
+        self.device = codes.device
+        self._codes = _p(codes, "codes", esize=1, min_numel=nc, optional=False)
+        self._scales = _p(scales, "scales", esize=1, min_numel=ns, device=self.device,
+                          optional=dtype != pulse.MXFP4)
+        self.dtype, self.rows, self.cols, self.inv_scale = dtype, rows, cols, float(inv_scale)
+        self.keep = (codes, scales)
+
+    def __call__(self, x: torch.Tensor, out: Optional[torch.Tensor] = None,
+                 out_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
+        """x W^T for BF16 x [tokens, cols]: [tokens, rows], float32 or bfloat16."""
+        dev = self.device
+        px, sx = _matrix(x, "x", self.cols, dtype=torch.bfloat16, device=dev)
+        if out is None:
+            out = _new((x.shape[0], self.rows), out_dtype, dev, stream)
+        dt = _dtype(out, "out")
+        py, sy = _matrix(out, "out", self.rows, x.shape[0], device=dev)
+        _check(lib().pulse_lowp_matmul(self.dtype, self._codes, self._scales, self.inv_scale, self.rows,
+                                       self.cols, px, sx, x.shape[0], dt, py, sy,
+                                       _stream(stream, dev)), "pulse_lowp_matmul")
+        return out
