@@ -81,6 +81,52 @@ int pulse_layer_norm_backward(int dtype, const void *dy, uint64_t dy_stride, con
                               void *stream);
 
 /*
+ * Softmax cross entropy of a head's logits, which are never stored: with
+ *   z[t][v] = logit_scale * sum_k x[t][k] weight[v][k]      (products exact,
+ *             summed in FP32),
+ *   lse[t]  = log sum_v exp(z[t][v]),
+ *   loss[t] = lse[t] - z[t][targets[t]];  0 where the target is ignored.
+ * A target outside [0, vocab) is ignored, whatever its value: such a token has
+ * an lse, no loss and no gradient, and what is in its row of x (NaN, say) reaches
+ * no gradient of another token or of the weight.
+ *   x         BF16 [tokens, hidden], rows x_stride apart.
+ *   weight    BF16 [vocab, hidden], rows adjacent.
+ *   targets   device int64 [tokens].
+ * hidden is 1 to PULSE_CE_MAX_HIDDEN; tokens and vocab are below 2^31, vocab at
+ * least 1; logit_scale is finite.  tokens == 0 writes no loss or lse (and a
+ * zero dweight).  A hidden that is no multiple of 8 costs a copy of the weight
+ * with padded rows in the workspace.
+ */
+#define PULSE_CE_MAX_HIDDEN 65536
+
+/* Workspace of both calls for up to `tokens` tokens. */
+size_t pulse_linear_ce_workspace_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden);
+
+/* loss and lse: FP32 [tokens]. */
+int pulse_linear_ce_forward(const uint16_t *x, uint64_t x_stride, const uint16_t *weight,
+                            const int64_t *targets, uint32_t tokens, uint32_t vocab,
+                            uint32_t hidden, float logit_scale, float *loss, float *lse,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * pulse_linear_ce_backward -- the gradient for the upstream dloss (FP32
+ * [tokens], e.g. a token's advantage over the number of tokens), with the
+ * forward pass's lse.  Piece by piece of the vocabulary the logits are computed
+ * again and G[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - [v == targets[t]]) is
+ * rounded to BF16 for the two products
+ *   dx = logit_scale * G weight,   dweight = logit_scale * G^T x,
+ * which are summed in FP32 and rounded once to BF16.
+ *   dx       BF16 [tokens, hidden], rows dx_stride apart.
+ *   dweight  BF16 [vocab, hidden].
+ */
+int pulse_linear_ce_backward(const uint16_t *x, uint64_t x_stride, const uint16_t *weight,
+                             const int64_t *targets, uint32_t tokens, uint32_t vocab,
+                             uint32_t hidden, float logit_scale, const float *lse,
+                             const float *dloss, uint16_t *dx, uint64_t dx_stride,
+                             uint16_t *dweight, void *workspace, size_t workspace_bytes,
+                             void *stream);
+
+/*
  * pulse_lowp_matmul -- y = x W^T, W the receiver's copy of a [rows, cols]
  * weight as pulse_cast_lowp and pulse_apply_lowp_batch leave it (codes flat in
  * row order, an MXFP4 block any 32 consecutive values, so a block may span two

@@ -1,0 +1,217 @@
+// gemm_tile.hpp -- one block's tile of out[m][n] = sum_k A[m][k] B[n][k] on BF16
+// operands with FP32 sums, for the products of the cross entropy.
+//
+// Each operand is either k-contiguous (row m or n holds adjacent k) or k-major
+// (row k holds adjacent m or n), so that no operand has to be transposed in
+// memory first.  64 k at a time go straight from global memory to LDS
+// (16 bytes a lane, no registers), into one of NST buffers, while the matrix
+// cores work on an earlier one.
+//
+// LDS layout.  Such a load writes a wave's 64 groups of 16 bytes side by side, so
+// any permutation has to be made on the global side: which lane loads
+// which group.
+//   k-contiguous: rows of 128 bytes (8 groups).  Group c of row r lies at
+//     place c ^ ((r >> 1) & 7): the 16 rows that a fragment read touches at
+//     one c then cover all 64 banks once.
+//   k-major: rows of all the tile's m (or n).  Pairs of groups (16 elements, one
+//     fragment's width) are permuted by k: the transposing read takes 4
+//     rows of 32 bytes for each of its lane groups, 8 rows apart, which then
+//     lie in different banks.
+//
+// A fragment of v_mfma_f32_16x16x32_bf16 is 8 adjacent k of one m (or n) per lane:
+// lane l has m = l & 15 and k = 8 (l >> 4) + 0..7.  From a k-major tile two
+// ds_read_b64_tr_b16 give 4 of those k each.
+#pragma once
+
+#include "head.hpp"
+
+namespace pulse {
+
+// One operand as the block sees it: `p` points to its first row (m or n) at
+// k = 0, or, k-major, to its first column at k = 0.  `limit` counts the rows (or
+// columns, a multiple of 8) from there to the matrix's end: what lies past it is
+// read from the last one and dropped by the epilogue.
+struct GemmOperand {
+  const uint16_t* p;
+  uint64_t ld;  // elements from row to row
+  uint32_t limit;
+};
+
+namespace {
+__device__ __align__(16) uint32_t gemm_zeros[4];  // what k past the end is read from
+}
+
+// Waits until at most N of the wave's loads into LDS are on their way and its LDS
+// reads are done, then for the block's other waves.
+template <int N>
+__device__ __forceinline__ void wait_and_meet() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
+
+constexpr int kGemmK = 64;  // k per buffer
+
+template <int ROWS, int WAVES, bool KMAJOR>
+struct GemmTile {
+  static constexpr int kBytes = ROWS * kGemmK * 2;
+  static constexpr int kLoads = kBytes / 1024 / WAVES;  // per wave and buffer
+  static_assert(kBytes % (1024 * WAVES) == 0, "whole wave loads");
+
+  static __device__ __forceinline__ uint32_t mix(uint32_t k) {
+    return ROWS >= 128 ? (k & 3) | ((k >> 3) & 1) << 2 : ((k >> 1) & 1) | ((k >> 3) & 1) << 1;
+  }
+
+  uint32_t off[kLoads];  // byte offset from the operand's k position
+  uint32_t k_of[kLoads];
+  const char* at;
+  uint64_t step;
+
+  __device__ __forceinline__ void init(const GemmOperand& o, uint32_t k0, int wave, int lane) {
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t load = i * WAVES + wave;
+      if constexpr (!KMAJOR) {
+        uint32_t r = load * 8 + (lane >> 3);
+        const uint32_t c = (lane & 7) ^ ((r >> 1) & 7);
+        if (r >= o.limit) r = o.limit - 1;
+        off[i] = (uint32_t)(r * o.ld * 2 + c * 16);
+        k_of[i] = c * 8;
+      } else {
+        constexpr uint32_t kGroups = ROWS / 8;
+        const uint32_t k = load * (64 / kGroups) + lane / kGroups, g = lane % kGroups;
+        uint32_t c = (((g >> 1) ^ mix(k)) << 1 | (g & 1)) * 8;
+        if (c >= o.limit) c = o.limit - 8;
+        off[i] = (uint32_t)(k * o.ld * 2 + c * 2);
+        k_of[i] = k;
+      }
+    }
+    at = (const char*)o.p + (KMAJOR ? k0 * o.ld * 2 : (uint64_t)k0 * 2);
+    step = KMAJOR ? kGemmK * o.ld * 2 : kGemmK * 2;
+  }
+
+  // The next 64 k, of which `left` lie in the matrix, into `lds`.
+  __device__ __forceinline__ void load(char* lds, int32_t left, int wave) {
+    typedef const __attribute__((address_space(1))) void* global_t;
+    typedef __attribute__((address_space(3))) void* lds_t;
+    if (left >= kGemmK) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        __builtin_amdgcn_global_load_lds((global_t)(at + off[i]), (lds_t)(lds + (i * WAVES + wave) * 1024),
+                                         16, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const char* from = (int32_t)k_of[i] < left ? at + off[i] : (const char*)gemm_zeros;
+        __builtin_amdgcn_global_load_lds((global_t)from, (lds_t)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
+      }
+    }
+    at += step;
+  }
+
+  // The lane's fragment of the 16 rows from `first` (a multiple of 16), k = 32 ks ...
+  static __device__ __forceinline__ bf16x8_t fragment(const char* lds, uint32_t first, int ks, int lane) {
+    const uint32_t r = lane & 15, g = lane >> 4;
+    if constexpr (!KMAJOR) {
+      return *(const bf16x8_t*)(lds + (first + r) * 128 + (((ks * 4 + g) ^ ((r >> 1) & 7)) << 4));
+    } else {
+      const uint32_t k = ks * 32 + g * 8 + (r >> 2);
+      const uint32_t at = k * (ROWS * 2) + (((first >> 4) ^ mix(k)) << 5) + (r & 3) * 8;
+      s16x4_t v[2];
+      v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(lds + at));
+      v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(lds + at + 4 * ROWS * 2));
+      return __builtin_bit_cast(bf16x8_t, *(const uint4*)v);
+    }
+  }
+};
+
+template <int BM_, int BN_, int WM_, int WN_, int NST_, bool AK_, bool BK_>
+struct Gemm {
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NST = NST_;
+  static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
+  static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;  // fragments of a wave
+  typedef GemmTile<BM, kWaves, AK_> A;
+  typedef GemmTile<BN, kWaves, BK_> B;
+  static constexpr int kStage = A::kBytes + B::kBytes;
+  static constexpr int kLds = NST * kStage;
+  typedef f32x4_t Acc[FM][FN];
+
+  // acc[i][j][e] of lane (l & 15, l >> 4): m = wave's m + 16 i + 4 (l >> 4) + e,
+  // n = wave's n + 16 j + (l & 15).
+  static __device__ __forceinline__ uint32_t m_of(int i, int lane, int wave) {
+    return (wave / WN) * (FM * 16) + i * 16 + (lane >> 4) * 4;
+  }
+  static __device__ __forceinline__ uint32_t n_of(int j, int lane, int wave) {
+    return (wave % WN) * (FN * 16) + j * 16 + (lane & 15);
+  }
+
+  // Sums over k0 <= k < k1 (k0 a multiple of 64).  Every wave calls it; ends with
+  // a barrier, after which `lds` is free.
+  static __device__ __forceinline__ void run(char* lds, const GemmOperand& a, const GemmOperand& b, uint32_t k0,
+                                             uint32_t k1, Acc& acc) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    A la;
+    B lb;
+    la.init(a, k0, wave, lane);
+    lb.init(b, k0, wave, lane);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    const int32_t steps = (int32_t)((k1 - k0 + kGemmK - 1) / kGemmK);
+    int32_t left = (int32_t)(k1 - k0);
+    const uint32_t m = (wave / WN) * (FM * 16), n = (wave % WN) * (FN * 16);
+    int fill = 0;
+    auto issue = [&] {
+      la.load(lds + fill * kStage, left, wave);
+      lb.load(lds + fill * kStage + A::kBytes, left, wave);
+      left -= kGemmK;
+      fill = fill + 1 == NST ? 0 : fill + 1;
+    };
+#pragma unroll
+    for (int s = 0; s < NST - 1; ++s)
+      if (s < steps) issue();
+    int use = 0;
+    for (int32_t s = 0; s < steps; ++s) {
+      // buffer `use` has landed for every wave, and every wave is done with the
+      // one that is filled next
+      if (NST > 2 && s + NST - 1 <= steps) wait_and_meet<(NST - 2) * (A::kLoads + B::kLoads)>();
+      else wait_and_meet<0>();
+      if (s + NST - 1 < steps) issue();
+      const char* la_ = lds + use * kStage;
+      const char* lb_ = la_ + A::kBytes;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks) {
+        bf16x8_t fb[FN];
+#pragma unroll
+        for (int j = 0; j < FN; ++j) fb[j] = B::fragment(lb_, n + j * 16, ks, lane);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+          const bf16x8_t fa = A::fragment(la_, m + i * 16, ks, lane);
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
+        }
+      }
+      use = use + 1 == NST ? 0 : use + 1;
+    }
+    __syncthreads();
+  }
+};
+
+// Tile (m, n) of block `id`: each of the 8 XCDs, to which blocks go in turn, gets
+// a run of adjacent tiles, 8 in m by as many in n as are in flight, so that its
+// L2 serves each operand row several times.
+__device__ __forceinline__ void gemm_tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t& m,
+                                             uint32_t& n) {
+  const uint32_t all = tiles_m * tiles_n, per = all / 8, rest = all % 8;
+  const uint32_t x = id % 8, at = id / 8;
+  const uint32_t t = x * per + (x < rest ? x : rest) + at;
+  const uint32_t band = t / (8 * tiles_n), in = t % (8 * tiles_n);
+  const uint32_t high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
+  m = band * 8 + in % high;
+  n = in / high;
+}
+
+}  // namespace pulse

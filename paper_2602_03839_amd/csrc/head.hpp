@@ -68,6 +68,40 @@ struct LowpMatmulParams {
 
 hipError_t launch_lowp_matmul(bool mxfp4, const LowpMatmulParams& p, hipStream_t stream);
 
+// ---------------------------------------------------------------- cross entropy
+
+constexpr uint32_t kCeMaxHidden = 65536;
+
+struct LinearCeParams {
+  const uint16_t* x;
+  uint64_t x_stride;
+  const uint16_t* weight;
+  const int64_t* targets;
+  uint32_t tokens, vocab, hidden;
+  float logit_scale;
+  float* loss;
+  float* lse;
+};
+
+struct LinearCeGradParams {
+  const uint16_t* x;
+  uint64_t x_stride;
+  const uint16_t* weight;
+  const int64_t* targets;
+  uint32_t tokens, vocab, hidden;
+  float logit_scale;
+  const float* lse;
+  const float* dloss;
+  uint16_t* dx;
+  uint64_t dx_stride;
+  uint16_t* dweight;
+};
+
+hipError_t launch_zero_bytes(void* p, uint64_t bytes, hipStream_t stream);  // an even number of them
+uint64_t linear_ce_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden);
+hipError_t launch_linear_ce(const LinearCeParams& p, char* ws, hipStream_t stream);
+hipError_t launch_linear_ce_grad(const LinearCeGradParams& p, char* ws, hipStream_t stream);
+
 // ---------------------------------------------------------------- device helpers
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));

@@ -51,6 +51,22 @@ int check_matrix(const char* who, const char* name, const void* p, uint64_t stri
   return PULSE_OK;
 }
 
+int check_ce(const char* who, const void* x, uint64_t x_stride, const void* weight, const void* targets,
+             uint32_t tokens, uint32_t vocab, uint32_t hidden, float logit_scale, const void* ws,
+             size_t ws_bytes) {
+  if (vocab == 0 || vocab > 0x7FFFFFFFu || tokens > 0x7FFFFFFFu)
+    return fail(PULSE_EINVAL, "%s: %u tokens, vocabulary of %u", who, tokens, vocab);
+  if (hidden == 0 || hidden > PULSE_CE_MAX_HIDDEN)
+    return fail(PULSE_EINVAL, "%s: hidden size %u, 1 to %d are handled", who, hidden, PULSE_CE_MAX_HIDDEN);
+  if (!(logit_scale - logit_scale == 0.0f)) return fail(PULSE_EINVAL, "%s: logit_scale is not finite", who);
+  if (tokens == 0) return PULSE_OK;
+  if (int rc = check_matrix(who, "x", x, x_stride, tokens, hidden)) return rc;
+  if (!weight || !targets) return fail(PULSE_EINVAL, "%s: weight or targets is NULL", who);
+  if (!aligned16(weight)) return fail(PULSE_EALIGN, "%s: weight not 16-byte aligned", who);
+  if (!aligned(targets, 8)) return fail(PULSE_EALIGN, "%s: targets not 8-byte aligned", who);
+  return check_space(who, ws, ws_bytes, pulse::linear_ce_bytes(tokens, vocab, hidden));
+}
+
 }  // namespace
 
 extern "C" {
@@ -97,6 +113,48 @@ int pulse_layer_norm_backward(int dtype, const void* dy, uint64_t dy_stride, con
                              (float*)workspace, rows, cols, param_dtype == PULSE_DTYPE_BF16};
   return hip_status(pulse::launch_layer_norm_grad(dtype == PULSE_DTYPE_BF16, p, (hipStream_t)stream),
                     "layer_norm backward launch");
+}
+
+size_t pulse_linear_ce_workspace_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
+  return tokens && vocab && hidden ? pulse::linear_ce_bytes(tokens, vocab, hidden) : 0;
+}
+
+int pulse_linear_ce_forward(const uint16_t* x, uint64_t x_stride, const uint16_t* weight,
+                            const int64_t* targets, uint32_t tokens, uint32_t vocab, uint32_t hidden,
+                            float logit_scale, float* loss, float* lse, void* workspace,
+                            size_t workspace_bytes, void* stream) {
+  const char* who = "linear_ce forward";
+  if (int rc = check_ce(who, x, x_stride, weight, targets, tokens, vocab, hidden, logit_scale, workspace,
+                        workspace_bytes))
+    return rc;
+  if (tokens == 0) return ok();
+  if (!loss || !lse) return fail(PULSE_EINVAL, "%s: loss or lse is NULL", who);
+  if (!aligned(loss, 4) || !aligned(lse, 4)) return fail(PULSE_EALIGN, "%s: loss/lse not 4-byte aligned", who);
+  pulse::LinearCeParams p = {x, x_stride, weight, targets, tokens, vocab, hidden, logit_scale, loss, lse};
+  return hip_status(pulse::launch_linear_ce(p, (char*)workspace, (hipStream_t)stream), "linear_ce launch");
+}
+
+int pulse_linear_ce_backward(const uint16_t* x, uint64_t x_stride, const uint16_t* weight,
+                             const int64_t* targets, uint32_t tokens, uint32_t vocab, uint32_t hidden,
+                             float logit_scale, const float* lse, const float* dloss, uint16_t* dx,
+                             uint64_t dx_stride, uint16_t* dweight, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+  const char* who = "linear_ce backward";
+  if (int rc = check_ce(who, x, x_stride, weight, targets, tokens, vocab, hidden, logit_scale, workspace,
+                        workspace_bytes))
+    return rc;
+  if (!dweight) return fail(PULSE_EINVAL, "%s: dweight is NULL", who);
+  if (!aligned16(dweight)) return fail(PULSE_EALIGN, "%s: dweight not 16-byte aligned", who);
+  if (tokens == 0)
+    return hip_status(pulse::launch_zero_bytes(dweight, (uint64_t)vocab * hidden * 2, (hipStream_t)stream),
+                      "linear_ce launch");
+  if (!lse || !dloss) return fail(PULSE_EINVAL, "%s: lse or dloss is NULL", who);
+  if (!aligned(lse, 4) || !aligned(dloss, 4)) return fail(PULSE_EALIGN, "%s: lse/dloss not 4-byte aligned", who);
+  if (int rc = check_matrix(who, "dx", dx, dx_stride, tokens, hidden)) return rc;
+  pulse::LinearCeGradParams p = {x, x_stride, weight, targets, tokens, vocab, hidden, logit_scale, lse, dloss,
+                                 dx, dx_stride, dweight};
+  return hip_status(pulse::launch_linear_ce_grad(p, (char*)workspace, (hipStream_t)stream),
+                    "linear_ce backward launch");
 }
 
 int pulse_lowp_matmul(int dtype, const uint8_t* codes, const uint8_t* scales, float inv_scale,

@@ -1,0 +1,525 @@
+// linear_ce.hip -- softmax cross entropy of z = s x W^T over a large vocabulary,
+// forward and backward, with the logits in registers only.
+//
+// Forward: a block computes a tile of 256 vocabulary entries by its tokens
+// (gemm_tile.hpp), reduces it per token to the largest logit and the sum of
+// exponentials below it, and writes those two numbers; a second kernel joins a
+// token's pairs.  The logit of the target is written by the lane that has it.
+//
+// Backward: the vocabulary is taken in pieces.  For a piece, the logits are
+// computed again and turned into G[t][v] = g_t s (e^(z - lse) - [v = y_t]) in
+// BF16, and two products follow: dx += G W (FP32 sums, kept across pieces) and
+// dw = G^T X.  G of one piece is all that is ever stored.  It is the one
+// rounding to BF16 besides the outputs' own: the products need a BF16 operand,
+// and the rounding is relative to each entry, like the rounding of W and X
+// that the model already has.
+//
+// The three products of the backward pass and the one of the forward pass are
+// bound by the matrix cores for many tokens, by reading W for few.
+#include "device_common.hpp"
+#include "gemm_tile.hpp"
+#include "head.hpp"
+
+namespace pulse {
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+
+// 2^x (v_exp_f32, 1 ulp).
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// ---------------------------------------------------------------- logits
+
+struct LogitParams {
+  const uint16_t* w;
+  uint64_t w_ld;
+  const uint16_t* x;
+  uint64_t x_ld;
+  const int64_t* targets;
+  uint32_t tokens, hidden;
+  uint32_t v_begin, v_end;  // the piece; forward: the whole vocabulary
+  uint32_t tiles_m, tiles_n;
+  float scale;
+  // forward
+  float2* part;  // [tokens][tiles_m]: largest logit, sum of exponentials below it
+  float* hit;    // [tokens]: the target's logit
+  // backward
+  const float* lse;
+  const float* dloss;
+  uint32_t vocab;
+  uint16_t* g;  // [tokens][g_ld]
+  uint64_t g_ld;
+};
+
+template <typename T>
+__global__ __launch_bounds__(T::kThreads) void ce_forward_kernel(LogitParams p) {
+  __shared__ alignas(1024) char lds[T::kLds];
+  uint32_t tm, tn;
+  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+  const uint32_t m0 = p.v_begin + tm * T::BM, n0 = tn * T::BN;
+  typename T::Acc acc;
+  const GemmOperand a = {p.w + (uint64_t)m0 * p.w_ld, p.w_ld, p.v_end - m0};
+  const GemmOperand b = {p.x + (uint64_t)n0 * p.x_ld, p.x_ld, p.tokens - n0};
+  T::run(lds, a, b, 0, p.hidden, acc);
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float2(*s_part)[T::BN] = (float2(*)[T::BN])lds;  // [WM][BN]
+#pragma unroll
+  for (int j = 0; j < T::FN; ++j) {
+    const uint32_t n = T::n_of(j, lane, wave), t = n0 + n;
+    const int64_t y = t < p.tokens ? p.targets[t] : -1;
+    float top = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t v = m0 + T::m_of(i, lane, wave) + e;
+        float z = acc[i][j][e] * p.scale;
+        if (v >= p.v_end) z = -INFINITY;
+        if ((int64_t)v == y) p.hit[t] = z;
+        acc[i][j][e] = z;
+        top = z > top || z != z ? z : top;  // a NaN stays
+      }
+#pragma unroll
+    for (int x = 16; x < 64; x *= 2) {
+      const float o = __shfl_xor(top, x);
+      top = o > top || o != o ? o : top;
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += exp2_fast((acc[i][j][e] - top) * kLog2e);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (lane < 16) s_part[wave / T::WN][n] = make_float2(top, top == -INFINITY ? 0.0f : sum);
+  }
+  __syncthreads();
+  for (uint32_t n = threadIdx.x; n < T::BN; n += T::kThreads) {
+    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < T::WM; ++w) {
+      const float o = s_part[w][n].x;
+      top = o > top || o != o ? o : top;
+    }
+#pragma unroll
+    for (int w = 0; w < T::WM; ++w) {
+      const float2 q = s_part[w][n];
+      sum += q.x == -INFINITY ? 0.0f : q.y * exp2_fast((q.x - top) * kLog2e);
+    }
+    if (n0 + n < p.tokens) p.part[(uint64_t)(n0 + n) * p.tiles_m + tm] = make_float2(top, sum);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
+  __shared__ alignas(1024) char lds[T::kLds];
+  uint32_t tm, tn;
+  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+  const uint32_t m0 = p.v_begin + tm * T::BM, n0 = tn * T::BN;
+  typename T::Acc acc;
+  const GemmOperand a = {p.w + (uint64_t)m0 * p.w_ld, p.w_ld, p.v_end - m0};
+  const GemmOperand b = {p.x + (uint64_t)n0 * p.x_ld, p.x_ld, p.tokens - n0};
+  T::run(lds, a, b, 0, p.hidden, acc);
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int j = 0; j < T::FN; ++j) {
+    const uint32_t t = n0 + T::n_of(j, lane, wave);
+    if (t >= p.tokens) continue;
+    const int64_t y = p.targets[t];
+    const bool kept = y >= 0 && y < (int64_t)p.vocab;
+    const float by = p.dloss[t] * p.scale, lse = p.lse[t];
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+      float g[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t v = m0 + T::m_of(i, lane, wave) + e;
+        const float pr = exp2_fast((acc[i][j][e] * p.scale - lse) * kLog2e);
+        const float d = (int64_t)v == y ? pr - 1.0f : pr;
+        g[e] = kept && v < p.v_end ? d * by : 0.0f;
+      }
+      uint2 o;
+      o.x = bf16x2_rne(__float_as_uint(g[0]), __float_as_uint(g[1]));
+      o.y = bf16x2_rne(__float_as_uint(g[2]), __float_as_uint(g[3]));
+      *(uint2*)(p.g + t * p.g_ld + (m0 - p.v_begin + T::m_of(i, lane, wave))) = o;
+    }
+  }
+}
+
+// A token's pairs joined, one wave each.
+__global__ __launch_bounds__(256) void ce_join_kernel(const float2* part, const float* hit,
+                                                      const int64_t* targets, uint32_t tokens,
+                                                      uint32_t vocab, uint32_t tiles, float* loss,
+                                                      float* lse) {
+  const uint32_t t = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (t >= tokens) return;
+  const int lane = threadIdx.x & 63;
+  const float2* mine = part + (uint64_t)t * tiles;
+  float top = -INFINITY;
+  for (uint32_t i = lane; i < tiles; i += 64) {
+    const float o = mine[i].x;
+    top = o > top || o != o ? o : top;
+  }
+#pragma unroll
+  for (int x = 1; x < 64; x *= 2) {
+    const float o = __shfl_xor(top, x);
+    top = o > top || o != o ? o : top;
+  }
+  float sum = 0.0f;
+  for (uint32_t i = lane; i < tiles; i += 64) {
+    const float2 q = mine[i];
+    sum += q.x == -INFINITY ? 0.0f : q.y * exp2_fast((q.x - top) * kLog2e);
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) {
+    const float rest = logf(sum);
+    const int64_t y = targets[t];
+    lse[t] = top + rest;
+    // the difference first: a target that is the largest logit leaves log(sum)
+    loss[t] = y >= 0 && y < (int64_t)vocab ? (top - hit[t]) + rest : 0.0f;
+  }
+}
+
+// ---------------------------------------------------------------- products of the gradient
+
+struct GradParams {
+  GemmOperand a, b;  // at the first tile
+  uint32_t m, n, k;  // sizes
+  uint32_t tiles_m, tiles_n;
+  uint32_t k_split;  // k per blockIdx.y, a multiple of 64
+  float* sums;       // dx: [splits][n][m]
+  int add;           // dx: onto what is there
+  uint16_t* out;     // dw: [n][out_ld]
+  uint64_t out_ld;
+};
+
+template <typename T, bool AK, bool BK>
+__device__ __forceinline__ void grad_tile(const GradParams& p, char* lds, uint32_t& m0, uint32_t& n0,
+                                          typename T::Acc& acc) {
+  uint32_t tm, tn;
+  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+  m0 = tm * T::BM;
+  n0 = tn * T::BN;
+  const GemmOperand a = {p.a.p + (AK ? (uint64_t)m0 : m0 * p.a.ld), p.a.ld, p.a.limit - m0};
+  const GemmOperand b = {p.b.p + (BK ? (uint64_t)n0 : n0 * p.b.ld), p.b.ld, p.b.limit - n0};
+  const uint32_t k0 = blockIdx.y * p.k_split;
+  // a split past the end has no k and gives zeros
+  const uint32_t k1 = k0 >= p.k ? k0 : p.k - k0 < p.k_split ? p.k : k0 + p.k_split;
+  T::run(lds, a, b, k0, k1, acc);
+}
+
+template <typename T>
+__global__ __launch_bounds__(T::kThreads) void ce_dx_kernel(GradParams p) {
+  __shared__ alignas(1024) char lds[T::kLds];
+  uint32_t m0, n0;
+  typename T::Acc acc;
+  grad_tile<T, true, false>(p, lds, m0, n0, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float* sums = p.sums + (uint64_t)blockIdx.y * p.n * p.m;
+#pragma unroll
+  for (int j = 0; j < T::FN; ++j) {
+    const uint32_t n = n0 + T::n_of(j, lane, wave);
+    if (n >= p.n) continue;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+      const uint32_t m = m0 + T::m_of(i, lane, wave);
+      if (m >= p.m) continue;  // p.m is a multiple of 8
+      f32x4_t* at = (f32x4_t*)(sums + (uint64_t)n * p.m + m);
+      *at = p.add ? *at + acc[i][j] : acc[i][j];
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(T::kThreads) void ce_dw_kernel(GradParams p) {
+  __shared__ alignas(1024) char lds[T::kLds];
+  uint32_t m0, n0;
+  typename T::Acc acc;
+  grad_tile<T, true, true>(p, lds, m0, n0, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+  for (int j = 0; j < T::FN; ++j) {
+    const uint32_t n = n0 + T::n_of(j, lane, wave);
+    if (n >= p.n) continue;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+      const uint32_t m = m0 + T::m_of(i, lane, wave);
+      uint2 o;
+      o.x = bf16x2_rne(__float_as_uint(acc[i][j][0]), __float_as_uint(acc[i][j][1]));
+      o.y = bf16x2_rne(__float_as_uint(acc[i][j][2]), __float_as_uint(acc[i][j][3]));
+      uint16_t* at = p.out + n * p.out_ld + m;
+      if (p.out_ld % 4 == 0) {
+        if (m < p.m) *(uint2*)at = o;
+      } else {
+        const uint32_t w[2] = {o.x, o.y};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (m + e < p.m) at[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
+      }
+    }
+  }
+}
+
+// dx from the splits' sums; a token without a target gets zeros.
+__global__ __launch_bounds__(256) void ce_dx_join_kernel(const float* sums, uint32_t splits, uint32_t tokens,
+                                                         uint32_t ld, uint32_t hidden,
+                                                         const int64_t* targets, uint32_t vocab,
+                                                         uint16_t* dx, uint64_t dx_ld) {
+  const uint32_t t = blockIdx.x;
+  const uint32_t c = (blockIdx.y * 256 + threadIdx.x) * 4;
+  if (c >= ld) return;
+  const int64_t y = targets[t];
+  f32x4_t a = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (y >= 0 && y < (int64_t)vocab)
+    for (uint32_t s = 0; s < splits; ++s) a += *(const f32x4_t*)(sums + ((uint64_t)s * tokens + t) * ld + c);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (c + e < hidden) dx[t * dx_ld + c + e] = (uint16_t)bf16x2_rne(__float_as_uint(a[e]), 0u);
+}
+
+// ---------------------------------------------------------------- copies
+
+// Rows padded with zeros to `ld`; rows of tokens without a target (`targets` not
+// null) all zero: what is in them must not reach the other rows' sums.
+__global__ __launch_bounds__(256) void ce_copy_kernel(const uint16_t* from, uint64_t from_ld, uint32_t cols,
+                                                      uint16_t* to, uint32_t ld, uint64_t rows,
+                                                      const int64_t* targets, uint32_t vocab) {
+  const uint64_t groups = ld / 8, all = rows * groups;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
+    const uint64_t r = i / groups;
+    const uint32_t c = (uint32_t)(i % groups) * 8;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    bool kept = true;
+    if (targets) {
+      const int64_t y = targets[r];
+      kept = y >= 0 && y < (int64_t)vocab;
+    }
+    if (kept) {
+      const uint16_t* p = from + r * from_ld + c;
+      if (c + 8 <= cols && from_ld % 8 == 0) {
+        v = load16(p);
+      } else {
+        uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (c + e < cols) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    store16(to + r * ld + c, v);
+  }
+}
+
+void copy_rows(const uint16_t* from, uint64_t from_ld, uint32_t cols, uint16_t* to, uint32_t ld, uint64_t rows,
+               const int64_t* targets, uint32_t vocab, hipStream_t stream) {
+  uint64_t blocks = (rows * (ld / 8) + 255) / 256;
+  if (blocks > 8192) blocks = 8192;
+  hipLaunchKernelGGL(ce_copy_kernel, dim3((uint32_t)blocks), dim3(256), 0, stream, from, from_ld, cols, to, ld,
+                     rows, targets, vocab);
+}
+
+// ---------------------------------------------------------------- shapes
+
+uint32_t up(uint32_t v, uint32_t to) { return (v + to - 1) / to * to; }
+uint32_t parts(uint64_t v, uint32_t of) { return (uint32_t)((v + of - 1) / of); }
+
+constexpr uint32_t kVocabTile = 256;
+
+// Tiles: vocabulary (or hidden) by tokens (or vocabulary), by the tokens' count.
+typedef Gemm<256, 256, 2, 4, 2, false, false> LogitsL;
+typedef Gemm<256, 128, 4, 2, 3, false, false> LogitsM;
+typedef Gemm<256, 64, 4, 1, 2, false, false> LogitsS;
+typedef Gemm<256, 256, 2, 4, 2, true, false> DxL;
+typedef Gemm<256, 128, 4, 2, 3, true, false> DxM;
+typedef Gemm<128, 64, 4, 1, 2, true, false> DxS;
+typedef Gemm<256, 256, 2, 4, 2, true, true> DwL;
+typedef Gemm<128, 128, 2, 2, 2, true, true> DwS;
+
+constexpr uint64_t kMaxStride = 1u << 20;  // a tile's byte offsets stay in 32 bits
+constexpr uint64_t kPieceBytes = 256ull << 20;  // of G
+constexpr uint64_t kPieceWeight = 128ull << 20; // of W, where the tokens are few
+
+struct Plan {
+  uint32_t ld;      // of the padded copies and of dx's sums: hidden to a multiple of 8
+  bool copy_w;
+  uint32_t piece;   // vocabulary entries a piece, a multiple of the tile
+  uint32_t splits;  // of dx's k
+  // byte offsets in the workspace
+  uint64_t w, x, part, hit, g, sums, forward, total;
+};
+
+Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
+  Plan q;
+  q.ld = up(hidden, 8);
+  q.copy_w = hidden % 8 != 0;
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) {
+    const uint64_t here = at;
+    at += (bytes + 255) & ~255ull;
+    return here;
+  };
+  q.w = take(q.copy_w ? (uint64_t)vocab * q.ld * 2 : 0);
+  q.x = take((uint64_t)tokens * q.ld * 2);
+  const uint64_t both = at;
+  q.part = take((uint64_t)tokens * parts(vocab, kVocabTile) * sizeof(float2));
+  q.hit = take((uint64_t)tokens * sizeof(float));
+  q.forward = at;
+  at = both;
+  uint64_t piece = kPieceBytes / 2 / tokens;
+  if (tokens <= 128 && piece > kPieceWeight / 2 / q.ld) piece = kPieceWeight / 2 / q.ld;
+  piece = piece / kVocabTile * kVocabTile;
+  if (piece < kVocabTile) piece = kVocabTile;
+  const uint32_t pieces = parts(vocab, (uint32_t)(piece > vocab ? up(vocab, kVocabTile) : piece));
+  q.piece = up(parts(vocab, pieces), kVocabTile);
+  // few tokens: split dx's k until there are two blocks a CU
+  const uint32_t bm = tokens <= 64 ? DxS::BM : 256, bn = tokens <= 64 ? 64 : tokens <= 128 ? 128 : 256;
+  const uint32_t tiles = parts(q.ld, bm) * parts(tokens, bn);
+  q.splits = 1;
+  while (tiles * q.splits < 256 && q.splits * 2 * 256 <= q.piece) q.splits *= 2;
+  q.g = take((uint64_t)tokens * q.piece * 2);
+  q.sums = take((uint64_t)q.splits * tokens * q.ld * 4);
+  q.total = at > q.forward ? at : q.forward;
+  return q;
+}
+
+template <typename T>
+void run_logits(LogitParams p, bool forward, hipStream_t stream) {
+  p.tiles_m = parts(p.v_end - p.v_begin, T::BM);
+  p.tiles_n = parts(p.tokens, T::BN);
+  const dim3 grid(p.tiles_m * p.tiles_n), block(T::kThreads);
+  if (forward) hipLaunchKernelGGL(ce_forward_kernel<T>, grid, block, 0, stream, p);
+  else hipLaunchKernelGGL(ce_grad_kernel<T>, grid, block, 0, stream, p);
+}
+
+void run_logits(const LogitParams& p, bool forward, hipStream_t stream) {
+  if (p.tokens <= 64) run_logits<LogitsS>(p, forward, stream);
+  else if (p.tokens <= 128) run_logits<LogitsM>(p, forward, stream);
+  else run_logits<LogitsL>(p, forward, stream);
+}
+
+template <typename T>
+void run_dx(GradParams p, uint32_t splits, hipStream_t stream) {
+  p.tiles_m = parts(p.m, T::BM);
+  p.tiles_n = parts(p.n, T::BN);
+  hipLaunchKernelGGL(ce_dx_kernel<T>, dim3(p.tiles_m * p.tiles_n, splits), dim3(T::kThreads), 0, stream, p);
+}
+
+template <typename T>
+void run_dw(GradParams p, hipStream_t stream) {
+  p.tiles_m = parts(p.m, T::BM);
+  p.tiles_n = parts(p.n, T::BN);
+  hipLaunchKernelGGL(ce_dw_kernel<T>, dim3(p.tiles_m * p.tiles_n), dim3(T::kThreads), 0, stream, p);
+}
+
+}  // namespace
+
+__global__ __launch_bounds__(256) void zero_bytes_kernel(uint16_t* p, uint64_t n) {
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (uint64_t)gridDim.x * 256) p[i] = 0;
+}
+
+hipError_t launch_zero_bytes(void* p, uint64_t bytes, hipStream_t stream) {
+  hipLaunchKernelGGL(zero_bytes_kernel, dim3(4096), dim3(256), 0, stream, (uint16_t*)p, bytes / 2);
+  return hipGetLastError();
+}
+
+uint64_t linear_ce_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
+  return plan_of(tokens, vocab, hidden).total;
+}
+
+hipError_t launch_linear_ce(const LinearCeParams& c, char* ws, hipStream_t stream) {
+  const Plan q = plan_of(c.tokens, c.vocab, c.hidden);
+  LogitParams p = {};
+  p.w = c.weight;
+  p.w_ld = c.hidden;
+  if (q.copy_w) {
+    uint16_t* w = (uint16_t*)(ws + q.w);
+    copy_rows(c.weight, c.hidden, c.hidden, w, q.ld, c.vocab, nullptr, c.vocab, stream);
+    p.w = w;
+    p.w_ld = q.ld;
+  }
+  p.x = c.x;
+  p.x_ld = c.x_stride;
+  if (c.hidden % 8 || c.x_stride % 8 || c.x_stride > kMaxStride) {
+    uint16_t* x = (uint16_t*)(ws + q.x);
+    copy_rows(c.x, c.x_stride, c.hidden, x, q.ld, c.tokens, nullptr, c.vocab, stream);
+    p.x = x;
+    p.x_ld = q.ld;
+  }
+  p.targets = c.targets;
+  p.tokens = c.tokens;
+  p.hidden = q.ld;
+  p.v_begin = 0;
+  p.v_end = p.vocab = c.vocab;
+  p.scale = c.logit_scale;
+  p.part = (float2*)(ws + q.part);
+  p.hit = (float*)(ws + q.hit);
+  run_logits(p, true, stream);
+  hipLaunchKernelGGL(ce_join_kernel, dim3(parts(c.tokens, 4)), dim3(256), 0, stream, p.part, p.hit, c.targets,
+                     c.tokens, c.vocab, parts(c.vocab, kVocabTile), c.loss, c.lse);
+  return hipGetLastError();
+}
+
+hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStream_t stream) {
+  const Plan q = plan_of(c.tokens, c.vocab, c.hidden);
+  LogitParams p = {};
+  p.w = c.weight;
+  p.w_ld = c.hidden;
+  if (q.copy_w) {
+    uint16_t* w = (uint16_t*)(ws + q.w);
+    copy_rows(c.weight, c.hidden, c.hidden, w, q.ld, c.vocab, nullptr, c.vocab, stream);
+    p.w = w;
+    p.w_ld = q.ld;
+  }
+  uint16_t* x = (uint16_t*)(ws + q.x);
+  copy_rows(c.x, c.x_stride, c.hidden, x, q.ld, c.tokens, c.targets, c.vocab, stream);
+  p.x = x;
+  p.x_ld = q.ld;
+  p.targets = c.targets;
+  p.tokens = c.tokens;
+  p.hidden = q.ld;
+  p.vocab = c.vocab;
+  p.scale = c.logit_scale;
+  p.lse = c.lse;
+  p.dloss = c.dloss;
+  p.g = (uint16_t*)(ws + q.g);
+  p.g_ld = q.piece;
+  float* sums = (float*)(ws + q.sums);
+  for (uint32_t v = 0; v < c.vocab; v += q.piece) {
+    const uint32_t n = c.vocab - v < q.piece ? c.vocab - v : q.piece;
+    p.v_begin = v;
+    p.v_end = v + n;
+    run_logits(p, false, stream);
+    GradParams d = {};
+    d.a = {p.w + (uint64_t)v * p.w_ld, p.w_ld, q.ld};
+    d.b = {p.g, q.piece, c.tokens};
+    d.m = q.ld;
+    d.n = c.tokens;
+    d.k = n;
+    d.k_split = up(parts(q.piece, q.splits), kGemmK);
+    d.sums = sums;
+    d.add = v > 0;
+    // a short last piece leaves the last splits without k: their sums stay
+    const uint32_t splits = v > 0 ? parts(n, d.k_split) : q.splits;
+    if (c.tokens <= 64) run_dx<DxS>(d, splits, stream);
+    else if (c.tokens <= 128) run_dx<DxM>(d, splits, stream);
+    else run_dx<DxL>(d, splits, stream);
+    GradParams e = {};
+    e.a = {p.x, q.ld, q.ld};
+    e.b = {p.g, q.piece, q.piece};
+    e.m = c.hidden;
+    e.n = n;
+    e.k = e.k_split = c.tokens;
+    e.out = c.dweight + (uint64_t)v * c.hidden;
+    e.out_ld = c.hidden;
+    if (c.tokens <= 128) run_dw<DwS>(e, stream);
+    else run_dw<DwL>(e, stream);
+  }
+  hipLaunchKernelGGL(ce_dx_join_kernel, dim3(c.tokens, parts(q.ld, 1024)), dim3(256), 0, stream, sums, q.splits,
+                     c.tokens, q.ld, c.hidden, c.targets, c.vocab, c.dx, c.dx_stride);
+  return hipGetLastError();
+}
+
+}  // namespace pulse

@@ -25,9 +25,11 @@ from .pulse import PulseError, _check, _f32, _p, _stream
 F32, BF16 = 3, 4  # PULSE_DTYPE_F32, PULSE_DTYPE_BF16
 NORM_RMS = 1      # PULSE_NORM_RMS
 NORM_MAX_COLS = 16384
+CE_MAX_HIDDEN = 65536
 
 EXPORTS = ("pulse_layer_norm_workspace_bytes", "pulse_layer_norm_forward",
-           "pulse_layer_norm_backward", "pulse_lowp_matmul")
+           "pulse_layer_norm_backward", "pulse_linear_ce_workspace_bytes", "pulse_linear_ce_forward",
+           "pulse_linear_ce_backward", "pulse_lowp_matmul")
 
 _lock = threading.Lock()
 _lib = None
@@ -50,6 +52,10 @@ def lib():
             L.pulse_layer_norm_backward.argtypes = [i32, vp, u64, vp, u64, i32, vp, vp, vp, vp, u64,
                                                     vp, vp, u64, u32, u32, vp, sz, vp]
             L.pulse_lowp_matmul.argtypes = [i32, vp, vp, f32, u32, u32, vp, u64, u32, i32, vp, u64, vp]
+            L.pulse_linear_ce_workspace_bytes.argtypes = [u32, u32, u32]
+            L.pulse_linear_ce_forward.argtypes = [vp, u64, vp, vp, u32, u32, u32, f32, vp, vp, vp, sz, vp]
+            L.pulse_linear_ce_backward.argtypes = [vp, u64, vp, vp, u32, u32, u32, f32, vp, vp, vp, u64,
+                                                   vp, vp, sz, vp]
             for name in EXPORTS:
                 getattr(L, name).restype = sz if name.endswith("_workspace_bytes") else i32
             _lib = L
@@ -161,8 +167,77 @@ class LayerNorm:
             sdx, _f32(dweight, "dweight", self.cols, dev),
             _f32(dbias, "dbias", self.cols, dev, optional=True), rows, self.cols,
             NORM_RMS if self.rms else 0, self.ws.data_ptr(), self.ws.numel(), _stream(stream, dev)),
-            "pulse_layer_norm_backward", "pulse_lowp_matmul")
+            "pulse_layer_norm_backward", "pulse_linear_ce_workspace_bytes", "pulse_linear_ce_forward",
+           "pulse_linear_ce_backward", "pulse_lowp_matmul")
         return dx, dweight, dbias
+
+
+class LinearCE:
+    """Softmax cross entropy of logits = logit_scale * x weight^T that are never
+    stored, per token, and its gradient.
+
+    ``weight`` is bfloat16 [vocab, hidden] and may change in place between
+    calls; the workspace serves up to ``max_tokens`` tokens a call.
+    """
+
+    def __init__(self, weight: torch.Tensor, max_tokens: int, logit_scale: float = 1.0):
+        if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+            raise PulseError("weight must be a tensor [vocab, hidden]")
+        _p(weight, "weight", dtype=torch.bfloat16, min_numel=1, optional=False)
+        self.device, (self.vocab, self.hidden) = weight.device, weight.shape
+        if self.hidden > CE_MAX_HIDDEN:
+            raise PulseError(f"hidden size {self.hidden}, 1 to {CE_MAX_HIDDEN} are handled")
+        if not 0 <= max_tokens < 1 << 31:
+            raise PulseError(f"max_tokens {max_tokens} is out of range")
+        self.weight, self.max_tokens, self.logit_scale = weight, max_tokens, float(logit_scale)
+        need = lib().pulse_linear_ce_workspace_bytes(max_tokens, self.vocab, self.hidden)
+        self.ws = torch.empty(max(int(need), 1), dtype=torch.uint8, device=self.device)
+
+    def _tokens(self, x, targets):
+        px, sx = _matrix(x, "x", self.hidden, dtype=torch.bfloat16, device=self.device)
+        n = x.shape[0]
+        if n > self.max_tokens:
+            raise PulseError(f"{n} tokens, this object was built for {self.max_tokens}")
+        return px, sx, _p(targets, "targets", dtype=torch.int64, numel=n, device=self.device,
+                          optional=False), n
+
+    def forward(self, x: torch.Tensor, targets: torch.Tensor, loss: Optional[torch.Tensor] = None,
+                lse: Optional[torch.Tensor] = None, stream=None):
+        """(loss, lse), float32 [tokens], of x [tokens, hidden] and int64 targets;
+        a target outside [0, vocab) is ignored and has loss 0."""
+        dev = self.device
+        px, sx, pt, n = self._tokens(x, targets)
+        if loss is None:
+            loss = _new((n,), torch.float32, dev, stream)
+        if lse is None:
+            lse = _new((n,), torch.float32, dev, stream)
+        _check(lib().pulse_linear_ce_forward(px, sx, self.weight.data_ptr(), pt, n, self.vocab,
+                                             self.hidden, self.logit_scale, _f32(loss, "loss", n, dev),
+                                             _f32(lse, "lse", n, dev), self.ws.data_ptr(),
+                                             self.ws.numel(), _stream(stream, dev)),
+               "pulse_linear_ce_forward")
+        return loss, lse
+
+    def backward(self, x: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
+                 dloss: torch.Tensor, dx: Optional[torch.Tensor] = None,
+                 dweight: Optional[torch.Tensor] = None, stream=None):
+        """(dx, dweight), bfloat16, for the upstream gradient dloss [tokens] of
+        each token's loss and the forward pass's lse."""
+        dev = self.device
+        px, sx, pt, n = self._tokens(x, targets)
+        if dx is None:
+            dx = _new((n, self.hidden), torch.bfloat16, dev, stream)
+        pdx, sdx = _matrix(dx, "dx", self.hidden, n, torch.bfloat16, dev)
+        if dweight is None:
+            dweight = _new((self.vocab, self.hidden), torch.bfloat16, dev, stream)
+        pdw = _p(dweight, "dweight", dtype=torch.bfloat16, numel=self.vocab * self.hidden, device=dev,
+                 optional=False)
+        _check(lib().pulse_linear_ce_backward(px, sx, self.weight.data_ptr(), pt, n, self.vocab,
+                                              self.hidden, self.logit_scale, _f32(lse, "lse", n, dev),
+                                              _f32(dloss, "dloss", n, dev), pdx, sdx, pdw,
+                                              self.ws.data_ptr(), self.ws.numel(), _stream(stream, dev)),
+               "pulse_linear_ce_backward")
+        return dx, dweight
 
 
 class LowpLinear:

@@ -1,0 +1,241 @@
+"""Cross entropy of a head's logits on the GPU against the definition in 64 bits.
+
+Tolerances.  A logit is a sum of `hidden` exact products in FP32: off by at most
+hidden * 2^-24 of the sum of their magnitudes; loss and lse add the rounding of
+log and of a few sums (1e-6 of their terms).  A gradient is a sum whose terms
+carry the BF16 rounding of G (2^-8 relative to each, and the error of the logits
+in the exponent) and is itself rounded to BF16: at most 2^-8 of the sum of the
+terms' magnitudes, plus 2^-8 of the result.
+"""
+import pytest
+import torch
+
+from paper_2602_03839_amd import head, pulse
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+def inputs(tokens, vocab, hidden, seed, ignored=0.2, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    w = (torch.randn(vocab, hidden, generator=g) * 2 / hidden ** 0.5).bfloat16()
+    y = torch.randint(vocab, (tokens,), generator=g)
+    x = (torch.randn(tokens, hidden, generator=g) + torch.rand(tokens, 1, generator=g) * w[y]).bfloat16()
+    y[torch.rand(tokens, generator=g) < ignored] = -100
+    return x, w, y, torch.randn(tokens, generator=g) / max(tokens, 1)
+
+
+def exact(x, w, y, dloss, scale):
+    """loss, lse, their error bound, G in 64 bits."""
+    x, w = x.double(), w.double()
+    z = scale * (x @ w.t())
+    size = abs(scale) * (x.abs() @ w.abs().t())
+    lse = torch.logsumexp(z, 1)
+    kept = (y >= 0) & (y < w.shape[0])
+    at = torch.where(kept, y, torch.zeros_like(y))
+    hit = z.gather(1, at[:, None])[:, 0]
+    loss = torch.where(kept, lse - hit, torch.zeros_like(lse))
+    dz = (x.shape[1] + 2) * U * size.amax(1)
+    g = torch.exp(z - lse[:, None])
+    g[torch.arange(len(y)), at] -= 1
+    g = torch.where(kept[:, None], g * dloss.double()[:, None] * scale, torch.zeros_like(g))
+    return loss, lse, 2 * dz + 1e-6 * (1 + lse.abs() + hit.abs()), g
+
+
+def check(tokens, vocab, hidden, seed=0, scale=1.0, data=None):
+    x, w, y, dl = data or inputs(tokens, vocab, hidden, seed)
+    ce = head.LinearCE(w.cuda(), max_tokens=tokens, logit_scale=scale)
+    loss, lse = ce.forward(x.cuda(), y.cuda())
+    el, es, bound, g = exact(x, w, y, dl, scale)
+    assert ((loss.cpu().double() - el).abs() <= bound).all()
+    assert ((lse.cpu().double() - es).abs() <= bound).all()
+    kept = (y >= 0) & (y < vocab)
+    assert (loss.cpu()[~kept] == 0).all()
+    dx, dw = ce.backward(x.cuda(), y.cuda(), lse, dl.cuda())
+    xk = torch.where(kept[:, None], x.double(), torch.zeros((), dtype=torch.float64))
+    # G's own relative error: its rounding, and twice the logits' error in the exponent
+    rel = 2.0 ** -8 + 2 * bound.max().item()
+    size = g.abs() + 2 * U * dl.double().abs()[:, None] * abs(scale)
+    for got, want, terms in ((dx, g @ w.double(), size @ w.double().abs()),
+                             (dw, g.t() @ xk, size.t() @ xk.abs())):
+        off = (got.cpu().double() - want).abs()
+        allowed = (rel + (vocab + tokens) * U) * terms + 2.0 ** -8 * want.abs() + 1e-38
+        assert got.shape == want.shape
+        assert (off <= allowed).all(), ((off - allowed).max(), off.max(), want.abs().max())
+    assert (dx.cpu()[~kept] == 0).all()
+    return dx, dw
+
+
+# tokens through every tile shape and its edges
+@pytest.mark.parametrize("tokens", [1, 2, 17, 63, 64, 65, 127, 128, 129, 255, 256, 257, 600])
+def test_tokens(tokens):
+    check(tokens, 1500, 192, seed=tokens)
+
+
+@pytest.mark.parametrize("vocab", [1, 2, 7, 63, 64, 255, 256, 257, 511, 1023, 5003])
+@pytest.mark.parametrize("tokens", [5, 100, 300])
+def test_vocabularies(vocab, tokens):
+    check(tokens, vocab, 128, seed=vocab)
+
+
+@pytest.mark.parametrize("hidden", [1, 3, 7, 8, 9, 56, 63, 64, 65, 72, 96, 100, 128, 203, 264, 520])
+@pytest.mark.parametrize("tokens", [3, 70, 200])
+def test_hidden_sizes(hidden, tokens):
+    check(tokens, 700, hidden, seed=hidden)
+
+
+@pytest.mark.parametrize("scale", [0.0, 0.5, 1 / 0.7, -1.0])
+def test_scales(scale):
+    check(33, 900, 64, seed=3, scale=scale)
+
+
+def test_several_pieces():
+    """More vocabulary than one piece of G holds, and a short last piece."""
+    for tokens, vocab, hidden in ((40, 40000, 2048), (2100, 66000, 64)):
+        x, w, y, dl = inputs(tokens, vocab, hidden, 8)
+        ce = head.LinearCE(w.cuda(), max_tokens=tokens)
+        _, lse = ce.forward(x.cuda(), y.cuda())
+        dx, dw = ce.backward(x.cuda(), y.cuda(), lse, dl.cuda())
+        # in FP32 on the GPU: the 64-bit definition piece by piece
+        xd, wd = x.cuda().double(), w.cuda().double()
+        z = xd @ wd.t()
+        assert (lse.double() - torch.logsumexp(z, 1)).abs().max() < 1e-4
+        g = torch.exp(z - torch.logsumexp(z, 1)[:, None])
+        kept = (y >= 0).cuda()
+        at = y.clamp(min=0).cuda()
+        g[torch.arange(tokens), at] -= 1
+        g *= torch.where(kept, dl.cuda().double(), torch.zeros((), dtype=torch.float64, device="cuda"))[:, None]
+        for got, want in ((dx, g @ wd), (dw, g.t().contiguous() @ xd)):
+            assert (got.double() - want).norm() <= 2.0 ** -8 * want.norm()
+
+
+def test_all_ignored_and_odd_targets():
+    x, w, y, dl = inputs(50, 300, 64, 1)
+    y[:] = -100
+    dx, dw = check(50, 300, 64, data=(x, w, y, dl))
+    assert (dx == 0).all() and (dw == 0).all()
+    y = torch.tensor([0, 299, 300, -1, 2 ** 40, -2 ** 40, 5, 2 ** 32 + 5] * 6 + [1, 2])
+    check(50, 300, 64, data=(x, w, y, dl))
+
+
+def test_nothing_of_an_ignored_token_gets_out():
+    """NaN and infinities in the rows and upstream gradients of ignored tokens."""
+    for tokens in (40, 300):
+        x, w, y, dl = inputs(tokens, 520, 96, 2)
+        y[::3] = -100
+        want = check(tokens, 520, 96, data=(x, w, y, dl))
+        x, dl = x.clone(), dl.clone()
+        bad = (y < 0).nonzero()[:, 0]
+        x[bad[0::2]], x[bad[1::2], 5] = float("nan"), float("inf")
+        dl[bad] = float("nan")
+        ce = head.LinearCE(w.cuda(), max_tokens=tokens)
+        loss, lse = ce.forward(x.cuda(), y.cuda())
+        assert (loss.cpu()[bad] == 0).all() and torch.isfinite(lse.cpu()[y >= 0]).all()
+        got = ce.backward(x.cuda(), y.cuda(), lse, dl.cuda())
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_large_logits():
+    """Logits of +-several hundred: no overflow, and a loss far below 1 and far
+    above it keep their relative size."""
+    x, w, y, dl = inputs(64, 400, 64, 4, ignored=0.0)
+    y[0] = (x[0].double() @ w.double().t()).argmax()
+    y[1] = (x[1].double() @ w.double().t()).argmin()
+    check(64, 400, 64, scale=60.0, data=(x, w, y, dl))
+
+
+def test_minus_infinite_logits():
+    """A weight row of infinities on one side: a probability of zero."""
+    x, w, y, dl = inputs(20, 300, 32, 5)
+    x[:, 0] = x[:, 0].abs() + 1
+    w[7, 0] = float("-inf")
+    w[7, 1:] = 0
+    y[y == 7] = 8
+    ce = head.LinearCE(w.cuda(), max_tokens=20)
+    loss, lse = ce.forward(x.cuda(), y.cuda())
+    z = x.double() @ w.double().t()
+    assert (lse.cpu().double() - torch.logsumexp(z, 1)).abs().max() < 1e-5
+    assert torch.isfinite(loss.cpu()).all()
+
+
+def test_gradient_against_differences():
+    """dx against central differences of the loss in 64 bits, for inputs that are
+    exact in BF16; the gradient's own roundings allow 2^-7 of its largest entry."""
+    x, w, y, dl = inputs(6, 40, 16, 6)
+    ce = head.LinearCE(w.cuda(), max_tokens=6, logit_scale=1.25)
+    _, lse = ce.forward(x.cuda(), y.cuda())
+    dx, dw = ce.backward(x.cuda(), y.cuda(), lse, dl.cuda())
+
+    def total(xv, wv):
+        z = 1.25 * xv @ wv.t()
+        kept = y >= 0
+        per = torch.logsumexp(z, 1) - z.gather(1, y.clamp(min=0)[:, None])[:, 0]
+        return (per[kept] * dl.double()[kept]).sum()
+
+    for which, grad in ((0, dx), (1, dw)):
+        args = [x.double(), w.double()]
+        flat, grad = args[which].view(-1), grad.cpu().double().view(-1)
+        for i in range(0, flat.numel(), 7):
+            keep, h = flat[i].item(), 1e-4
+            flat[i] = keep + h
+            up = total(*args)
+            flat[i] = keep - h
+            down = total(*args)
+            flat[i] = keep
+            assert abs((up - down) / (2 * h) - grad[i]) <= 2.0 ** -7 * grad.abs().max() + 1e-7, (which, i)
+
+
+def test_views_streams_and_same_bits():
+    tokens, vocab, hidden = 90, 1000, 128
+    x, w, y, dl = inputs(tokens, vocab, hidden, 7)
+    wide = torch.zeros(tokens, 200, dtype=torch.bfloat16, device="cuda")
+    odd = torch.zeros(tokens, 133, dtype=torch.bfloat16, device="cuda")
+    wide[:, :hidden] = x.cuda()
+    odd[:, :hidden] = x.cuda()
+    yd, dld = y.cuda(), dl.cuda()
+    ce = head.LinearCE(w.cuda(), max_tokens=200)
+    loss, lse = ce.forward(x.cuda(), yd)
+    dx, dw = ce.backward(x.cuda(), yd, lse, dld)
+    out = torch.full((tokens, 131), 7.0, dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    for view in (wide, odd):
+        l2, s2 = ce.forward(view[:, :hidden], yd, stream=s)
+        dx2, dw2 = ce.backward(view[:, :hidden], yd, s2, dld, dx=out[:, :hidden], stream=s)
+        s.synchronize()
+        assert torch.equal(loss, l2) and torch.equal(lse, s2)
+        assert torch.equal(dx, out[:, :hidden]) and torch.equal(dw, dw2)
+        assert (out[:, hidden:] == 7).all()
+
+
+def test_no_tokens():
+    _, w, _, _ = inputs(1, 64, 32, 1)
+    ce = head.LinearCE(w.cuda(), max_tokens=0)
+    x, y = torch.empty(0, 32, dtype=torch.bfloat16, device="cuda"), torch.empty(0, dtype=torch.int64, device="cuda")
+    loss, lse = ce.forward(x, y)
+    assert loss.numel() == lse.numel() == 0
+    dw = torch.ones(64, 32, dtype=torch.bfloat16, device="cuda")
+    dx, dw = ce.backward(x, y, lse, loss, dweight=dw)
+    assert dx.shape == (0, 32) and (dw == 0).all()
+
+
+def test_refusals():
+    x, w, y, dl = (t.cuda() for t in inputs(8, 64, 32, 1))
+    ce = head.LinearCE(w, max_tokens=8)
+    _, lse = ce.forward(x, y)
+    bad = [lambda: head.LinearCE(w.float(), 8), lambda: head.LinearCE(w[0], 8), lambda: head.LinearCE(w.t(), 8),
+           lambda: head.LinearCE(w.cpu(), 8), lambda: head.LinearCE(w, -1), lambda: head.LinearCE(w[:0], 8),
+           lambda: head.LinearCE(torch.zeros(1, 65537, dtype=torch.bfloat16, device="cuda"), 1),
+           lambda: ce.forward(x.float(), y), lambda: ce.forward(x[:, :16], y), lambda: ce.forward(x, y[:4]),
+           lambda: ce.forward(x, y.int()), lambda: ce.forward(x, y.cpu()), lambda: ce.forward(x, None),
+           lambda: ce.forward(torch.cat([x, x]), torch.cat([y, y])),
+           lambda: ce.forward(x, y, loss=lse[:3]), lambda: ce.forward(x, y, lse=lse.double()),
+           lambda: ce.backward(x, y, lse[:3], dl), lambda: ce.backward(x, y, lse, dl.double()),
+           lambda: ce.backward(x, y, lse, dl, dx=x[:4]), lambda: ce.backward(x, y, lse, dl, dweight=w.t()),
+           lambda: ce.backward(x, y, lse, dl, dweight=w[:8].clone()),
+           lambda: head.LinearCE(w, 8, logit_scale=float("nan")).forward(x, y)]
+    for k, call in enumerate(bad):
+        with pytest.raises(pulse.PulseError):
+            call()
+            pytest.fail(f"call {k} was not refused")
