@@ -167,8 +167,7 @@ class LayerNorm:
             sdx, _f32(dweight, "dweight", self.cols, dev),
             _f32(dbias, "dbias", self.cols, dev, optional=True), rows, self.cols,
             NORM_RMS if self.rms else 0, self.ws.data_ptr(), self.ws.numel(), _stream(stream, dev)),
-            "pulse_layer_norm_backward", "pulse_linear_ce_workspace_bytes", "pulse_linear_ce_forward",
-           "pulse_linear_ce_backward", "pulse_lowp_matmul")
+            "pulse_layer_norm_backward")
         return dx, dweight, dbias
 
 
