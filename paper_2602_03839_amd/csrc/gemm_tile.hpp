@@ -23,6 +23,7 @@
 // ds_read_b64_tr_b16 give 4 of those k each.
 #pragma once
 
+#include "device_common.hpp"
 #include "head.hpp"
 
 namespace pulse {
@@ -39,6 +40,20 @@ struct GemmOperand {
 
 namespace {
 __device__ __align__(16) uint32_t gemm_zeros[4];  // what k past the end is read from
+}
+
+// 16 bytes a lane from the buffer `rsrc` at byte offset `off` into 1,024 adjacent
+// bytes of LDS.  As an instruction of its own, since the compiler would make
+// every later transposing LDS read wait for a load that it knows of; the waits
+// are wait_and_meet's.  It writes no register and leaves m0 as it was.
+__device__ __forceinline__ void load_to_lds(char* lds, uint32_t off, u32x4_t rsrc) {
+  const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  uint32_t m0;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
+      "buffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+      : "=&s"(m0)
+      : "s"(to), "v"(off), "s"(rsrc));
 }
 
 // Waits until at most N of the wave's loads into LDS are on their way and its LDS
@@ -64,50 +79,51 @@ struct GemmTile {
   }
 
   uint32_t off[kLoads];  // byte offset from the operand's k position
-  uint32_t k_of[kLoads];
   const char* at;
   uint64_t step;
+
+  // k (of the 64) that the lane's i-th load starts at
+  static __device__ __forceinline__ int32_t k_of(int i, int wave, int lane) {
+    if constexpr (!KMAJOR) return (((lane & 7) ^ (((lane >> 4) & 3) | (((i * WAVES + wave) & 1) << 2))) * 8);
+    else return (i * WAVES + wave) * (512 / ROWS) + lane / (ROWS / 8);
+  }
 
   __device__ __forceinline__ void init(const GemmOperand& o, uint32_t k0, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const uint32_t load = i * WAVES + wave;
       if constexpr (!KMAJOR) {
-        uint32_t r = load * 8 + (lane >> 3);
-        const uint32_t c = (lane & 7) ^ ((r >> 1) & 7);
+        uint32_t r = (i * WAVES + wave) * 8 + (lane >> 3);
         if (r >= o.limit) r = o.limit - 1;
-        off[i] = (uint32_t)(r * o.ld * 2 + c * 16);
-        k_of[i] = c * 8;
+        off[i] = (uint32_t)(r * o.ld * 2 + k_of(i, wave, lane) * 2);
       } else {
-        constexpr uint32_t kGroups = ROWS / 8;
-        const uint32_t k = load * (64 / kGroups) + lane / kGroups, g = lane % kGroups;
+        const uint32_t k = k_of(i, wave, lane), g = lane % (ROWS / 8);
         uint32_t c = (((g >> 1) ^ mix(k)) << 1 | (g & 1)) * 8;
         if (c >= o.limit) c = o.limit - 8;
         off[i] = (uint32_t)(k * o.ld * 2 + c * 2);
-        k_of[i] = k;
       }
     }
     at = (const char*)o.p + (KMAJOR ? k0 * o.ld * 2 : (uint64_t)k0 * 2);
     step = KMAJOR ? kGemmK * o.ld * 2 : kGemmK * 2;
   }
 
-  // The next 64 k, of which `left` lie in the matrix, into `lds`.
-  __device__ __forceinline__ void load(char* lds, int32_t left, int wave) {
-    typedef const __attribute__((address_space(1))) void* global_t;
-    typedef __attribute__((address_space(3))) void* lds_t;
-    if (left >= kGemmK) {
+  // The i-th load of the next 64 k, all in the matrix, into `lds`; then next().
+  __device__ __forceinline__ void load(char* lds, int i, int wave) const {
+    const uint64_t base = (uint64_t)at;
+    // base, no stride, no bound (every offset is in the matrix by construction)
+    const u32x4_t rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, 0xFFFFFFFFu, 0x00027000u};
+    load_to_lds(lds + (i * WAVES + wave) * 1024, off[i], rsrc);
+  }
+  __device__ __forceinline__ void next() { at += step; }
+
+  // The same where only `left` of the 64 k may lie in the matrix.
+  __device__ __forceinline__ void load_end(char* lds, int32_t left, int wave, int lane) {
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-        __builtin_amdgcn_global_load_lds((global_t)(at + off[i]), (lds_t)(lds + (i * WAVES + wave) * 1024),
-                                         16, 0, 0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        const char* from = (int32_t)k_of[i] < left ? at + off[i] : (const char*)gemm_zeros;
-        __builtin_amdgcn_global_load_lds((global_t)from, (lds_t)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
-      }
+    for (int i = 0; i < kLoads; ++i) {
+      const char* from = k_of(i, wave, lane) < left ? at + off[i] : (const char*)gemm_zeros;
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)from,
+          (__attribute__((address_space(3))) void*)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
     }
-    at += step;
   }
 
   // The lane's fragment of the 16 rows from `first` (a multiple of 16), k = 32 ks ...
@@ -126,15 +142,16 @@ struct GemmTile {
   }
 };
 
-template <int BM_, int BN_, int WM_, int WN_, int NST_, bool AK_, bool BK_>
+template <int BM_, int BN_, int WM_, int WN_, bool AK_, bool BK_>
 struct Gemm {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NST = NST_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;  // fragments of a wave
   typedef GemmTile<BM, kWaves, AK_> A;
   typedef GemmTile<BN, kWaves, BK_> B;
   static constexpr int kStage = A::kBytes + B::kBytes;
-  static constexpr int kLds = NST * kStage;
+  static constexpr int kLds = 2 * kStage;
+  static constexpr int kLoads = A::kLoads + B::kLoads;  // of a wave and step
   typedef f32x4_t Acc[FM][FN];
 
   // acc[i][j][e] of lane (l & 15, l >> 4): m = wave's m + 16 i + 4 (l >> 4) + e,
@@ -159,42 +176,89 @@ struct Gemm {
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    const int32_t steps = (int32_t)((k1 - k0 + kGemmK - 1) / kGemmK);
-    int32_t left = (int32_t)(k1 - k0);
+    const int32_t full = (int32_t)((k1 - k0) / kGemmK), steps = (int32_t)((k1 - k0 + kGemmK - 1) / kGemmK);
+    if (steps == 0) return;
+    const int32_t rest = (int32_t)((k1 - k0) % kGemmK);
     const uint32_t m = (wave / WN) * (FM * 16), n = (wave % WN) * (FN * 16);
-    int fill = 0;
-    auto issue = [&] {
-      la.load(lds + fill * kStage, left, wave);
-      lb.load(lds + fill * kStage + A::kBytes, left, wave);
-      left -= kGemmK;
-      fill = fill + 1 == NST ? 0 : fill + 1;
+
+    struct Frags {
+      bf16x8_t a[FM], b[FN];
     };
+    auto load = [&](int32_t s, int i) {  // the i-th load of step s, which is whole
+      char* to = lds + (s & 1) * kStage;
+      if (i < A::kLoads) la.load(to, i, wave);
+      else lb.load(to + A::kBytes, i - A::kLoads, wave);
+    };
+    auto load_step = [&](int32_t s) {  // step s, any
+      char* to = lds + (s & 1) * kStage;
+      if (s < full) {
 #pragma unroll
-    for (int s = 0; s < NST - 1; ++s)
-      if (s < steps) issue();
-    int use = 0;
-    for (int32_t s = 0; s < steps; ++s) {
-      // buffer `use` has landed for every wave, and every wave is done with the
-      // one that is filled next
-      if (NST > 2 && s + NST - 1 <= steps) wait_and_meet<(NST - 2) * (A::kLoads + B::kLoads)>();
-      else wait_and_meet<0>();
-      if (s + NST - 1 < steps) issue();
-      const char* la_ = lds + use * kStage;
-      const char* lb_ = la_ + A::kBytes;
-#pragma unroll
-      for (int ks = 0; ks < 2; ++ks) {
-        bf16x8_t fb[FN];
-#pragma unroll
-        for (int j = 0; j < FN; ++j) fb[j] = B::fragment(lb_, n + j * 16, ks, lane);
-#pragma unroll
-        for (int i = 0; i < FM; ++i) {
-          const bf16x8_t fa = A::fragment(la_, m + i * 16, ks, lane);
-#pragma unroll
-          for (int j = 0; j < FN; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa, fb[j], acc[i][j], 0, 0, 0);
-        }
+        for (int i = 0; i < kLoads; ++i) load(s, i);
+      } else {
+        la.load_end(to, rest, wave, lane);
+        lb.load_end(to + A::kBytes, rest, wave, lane);
       }
-      use = use + 1 == NST ? 0 : use + 1;
+      la.next();
+      lb.next();
+    };
+    auto read = [&](Frags& f, int32_t s, int ks, int i) {  // fragment i of that half of step s
+      const char* from = lds + (s & 1) * kStage;
+      if (i < FN) f.b[i] = B::fragment(from + A::kBytes, n + i * 16, ks, lane);
+      else f.a[i - FN] = A::fragment(from, m + (i - FN) * 16, ks, lane);
+    };
+    auto multiply = [&](const Frags& f, int i) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.a[i], f.b[j], acc[i][j], 0, 0, 0);
+    };
+
+    // Half a step ahead: while the matrix cores work on one half of a buffer the
+    // other half's fragments are read.  Between the halves the next buffer has
+    // landed and this one is done with, so the step after next goes there.
+    // Loads, reads and products are issued in turn, in this order; the last
+    // turn has no reads, so that they are back when the next half starts.
+    constexpr int kTurns = FM - 1;
+    Frags f0, f1;
+    auto half = [&](Frags& to, int32_t s, int ks, const Frags& by, bool loads) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        if (loads) {
+#pragma unroll
+          for (int l = i * kLoads / FM; l < (i + 1) * kLoads / FM; ++l) load(s + 1, l);
+        }
+#pragma unroll
+        for (int r = i * (FM + FN) / kTurns; r < (i + 1) * (FM + FN) / kTurns && r < FM + FN; ++r)
+          read(to, s, ks, r);
+        multiply(by, i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+    load_step(0);
+    wait_and_meet<0>();
+    if (steps > 1) load_step(1);
+#pragma unroll
+    for (int i = 0; i < FM + FN; ++i) read(f0, 0, 0, i);
+    int32_t s = 0;
+    for (; s + 2 < full; ++s) {
+      half(f1, s, 1, f0, false);
+      wait_and_meet<0>();
+      half(f0, s + 1, 0, f1, true);
+      la.next();
+      lb.next();
+    }
+    // the last steps (and short sums), one half after the other
+    for (; s < steps; ++s) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) multiply(f0, i);
+#pragma unroll
+      for (int i = 0; i < FM + FN; ++i) read(f0, s, 1, i);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) multiply(f0, i);
+      if (s + 1 == steps) break;
+      wait_and_meet<0>();
+      if (s + 2 < steps) load_step(s + 2);
+#pragma unroll
+      for (int i = 0; i < FM + FN; ++i) read(f0, s + 1, 0, i);
     }
     __syncthreads();
   }

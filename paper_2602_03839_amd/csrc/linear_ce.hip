@@ -329,18 +329,17 @@ uint32_t parts(uint64_t v, uint32_t of) { return (uint32_t)((v + of - 1) / of); 
 constexpr uint32_t kVocabTile = 256;
 
 // Tiles: vocabulary (or hidden) by tokens (or vocabulary), by the tokens' count.
-typedef Gemm<256, 256, 2, 4, 2, false, false> LogitsL;
-typedef Gemm<256, 128, 4, 2, 3, false, false> LogitsM;
-typedef Gemm<256, 64, 4, 1, 2, false, false> LogitsS;
-typedef Gemm<256, 256, 2, 4, 2, true, false> DxL;
-typedef Gemm<256, 128, 4, 2, 3, true, false> DxM;
-typedef Gemm<128, 64, 4, 1, 2, true, false> DxS;
-typedef Gemm<256, 256, 2, 4, 2, true, true> DwL;
-typedef Gemm<128, 128, 2, 2, 2, true, true> DwS;
+typedef Gemm<256, 256, 2, 4, false, false> LogitsL;
+typedef Gemm<256, 128, 4, 2, false, false> LogitsM;
+typedef Gemm<256, 64, 4, 1, false, false> LogitsS;
+typedef Gemm<256, 256, 2, 4, true, false> DxL;
+typedef Gemm<256, 128, 4, 2, true, false> DxM;
+typedef Gemm<128, 64, 4, 1, true, false> DxS;
+typedef Gemm<256, 256, 2, 4, true, true> DwL;
+typedef Gemm<128, 128, 2, 2, true, true> DwS;
 
 constexpr uint64_t kMaxStride = 1u << 20;  // a tile's byte offsets stay in 32 bits
 constexpr uint64_t kPieceBytes = 256ull << 20;  // of G
-constexpr uint64_t kPieceWeight = 128ull << 20; // of W, where the tokens are few
 
 struct Plan {
   uint32_t ld;      // of the padded copies and of dx's sums: hidden to a multiple of 8
@@ -369,7 +368,6 @@ Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   q.forward = at;
   at = both;
   uint64_t piece = kPieceBytes / 2 / tokens;
-  if (tokens <= 128 && piece > kPieceWeight / 2 / q.ld) piece = kPieceWeight / 2 / q.ld;
   piece = piece / kVocabTile * kVocabTile;
   if (piece < kVocabTile) piece = kVocabTile;
   const uint32_t pieces = parts(vocab, (uint32_t)(piece > vocab ? up(vocab, kVocabTile) : piece));
