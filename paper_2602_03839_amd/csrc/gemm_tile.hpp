@@ -163,6 +163,36 @@ struct Gemm {
     return (wave % WN) * (FN * 16) + j * 16 + (lane & 15);
   }
 
+  // The tile as BF16 rows out[n][m], 16 bytes a lane and whole lines at a time: a
+  // lane's own four values of 16 rows would be written in pieces of 32 bytes.
+  // `value(i, j)` gives them as two packed pairs; only rows n < n_left and groups
+  // of 8 m below m_left are written.  Group c of row n lies at place c ^ (n & 15).
+  template <bool STREAM, typename F>
+  static __device__ __forceinline__ void store_rows(char* lds, uint16_t* out, uint64_t ld, uint32_t m_left,
+                                                    uint32_t n_left, F value) {
+    static_assert(BM >= 128 && BM * BN * 2 <= kLds, "the tile fits, with 16 groups a row");
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) {
+      const uint32_t n = n_of(j, lane, wave);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const uint32_t m = m_of(i, lane, wave);
+        *(uint2*)(lds + n * (BM * 2) + (((m >> 3) ^ (n & 15)) << 4) + (m & 4) * 2) = value(i, j);
+      }
+    }
+    __syncthreads();
+#pragma unroll 4
+    for (uint32_t q = threadIdx.x; q < BN * (BM / 8); q += kThreads) {
+      const uint32_t n = q / (BM / 8), c = q % (BM / 8);
+      const uint4 v = *(const uint4*)(lds + n * (BM * 2) + ((c ^ (n & 15)) << 4));
+      if (n < n_left && c * 8 < m_left) {
+        if constexpr (STREAM) store16_stream(out + n * ld + c * 8, v);
+        else store16(out + n * ld + c * 8, v);
+      }
+    }
+  }
+
   // Sums over k0 <= k < k1 (k0 a multiple of 64).  Every wave calls it; ends with
   // a barrier, after which `lds` is free.
   static __device__ __forceinline__ void run(char* lds, const GemmOperand& a, const GemmOperand& b, uint32_t k0,

@@ -124,29 +124,34 @@ __global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
   T::run(lds, a, b, 0, p.hidden, acc);
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t y[T::FN];
+  float by[T::FN], lse[T::FN];
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
     const uint32_t t = n0 + T::n_of(j, lane, wave);
-    if (t >= p.tokens) continue;
-    const int64_t y = p.targets[t];
-    const bool kept = y >= 0 && y < (int64_t)p.vocab;
-    const float by = p.dloss[t] * p.scale, lse = p.lse[t];
-#pragma unroll
-    for (int i = 0; i < T::FM; ++i) {
-      float g[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t v = m0 + T::m_of(i, lane, wave) + e;
-        const float pr = exp2_fast((acc[i][j][e] * p.scale - lse) * kLog2e);
-        const float d = (int64_t)v == y ? pr - 1.0f : pr;
-        g[e] = kept && v < p.v_end ? d * by : 0.0f;
-      }
-      uint2 o;
-      o.x = bf16x2_rne(__float_as_uint(g[0]), __float_as_uint(g[1]));
-      o.y = bf16x2_rne(__float_as_uint(g[2]), __float_as_uint(g[3]));
-      *(uint2*)(p.g + t * p.g_ld + (m0 - p.v_begin + T::m_of(i, lane, wave))) = o;
-    }
+    y[j] = t < p.tokens ? p.targets[t] : -1;
+    const bool kept = y[j] >= 0 && y[j] < (int64_t)p.vocab;
+    if (!kept) y[j] = -1;
+    by[j] = kept ? p.dloss[t] * p.scale : 0.0f;
+    lse[j] = kept ? p.lse[t] : 0.0f;
   }
+  T::template store_rows<false>(
+      lds, p.g + n0 * p.g_ld + (m0 - p.v_begin), p.g_ld, T::BM, p.tokens - n0, [&](int i, int j) {
+        float g[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t v = m0 + T::m_of(i, lane, wave) + e;
+          // z rounded as in the forward pass and the difference before the factor:
+          // exact where z is near lse, so a large logit costs a likely target no digits
+          const float pr = exp2_fast((acc[i][j][e] * p.scale - lse[j]) * kLog2e);
+          const float d = (int64_t)v == y[j] ? pr - 1.0f : pr;
+          g[e] = y[j] >= 0 && v < p.v_end ? d * by[j] : 0.0f;
+        }
+        uint2 o;
+        o.x = bf16x2_rne(__float_as_uint(g[0]), __float_as_uint(g[1]));
+        o.y = bf16x2_rne(__float_as_uint(g[2]), __float_as_uint(g[3]));
+        return o;
+      });
 }
 
 // A token's pairs joined, one wave each.
@@ -240,6 +245,16 @@ __global__ __launch_bounds__(T::kThreads) void ce_dw_kernel(GradParams p) {
   typename T::Acc acc;
   grad_tile<T, true, true>(p, lds, m0, n0, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  auto value = [&](int i, int j) {
+    uint2 o;
+    o.x = bf16x2_rne(__float_as_uint(acc[i][j][0]), __float_as_uint(acc[i][j][1]));
+    o.y = bf16x2_rne(__float_as_uint(acc[i][j][2]), __float_as_uint(acc[i][j][3]));
+    return o;
+  };
+  if (p.out_ld % 8 == 0) {
+    T::template store_rows<true>(lds, p.out + n0 * p.out_ld + m0, p.out_ld, p.m - m0, p.n - n0, value);
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
     const uint32_t n = n0 + T::n_of(j, lane, wave);
@@ -247,18 +262,11 @@ __global__ __launch_bounds__(T::kThreads) void ce_dw_kernel(GradParams p) {
 #pragma unroll
     for (int i = 0; i < T::FM; ++i) {
       const uint32_t m = m0 + T::m_of(i, lane, wave);
-      uint2 o;
-      o.x = bf16x2_rne(__float_as_uint(acc[i][j][0]), __float_as_uint(acc[i][j][1]));
-      o.y = bf16x2_rne(__float_as_uint(acc[i][j][2]), __float_as_uint(acc[i][j][3]));
-      uint16_t* at = p.out + n * p.out_ld + m;
-      if (p.out_ld % 4 == 0) {
-        if (m < p.m) *(uint2*)at = o;
-      } else {
-        const uint32_t w[2] = {o.x, o.y};
+      const uint2 o = value(i, j);
+      const uint32_t w[2] = {o.x, o.y};
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (m + e < p.m) at[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
-      }
+      for (int e = 0; e < 4; ++e)
+        if (m + e < p.m) p.out[n * p.out_ld + m + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
     }
   }
 }
