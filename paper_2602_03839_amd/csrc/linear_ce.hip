@@ -9,10 +9,12 @@
 // Backward: the vocabulary is taken in pieces.  For a piece, the logits are
 // computed again and turned into G[t][v] = g_t s (e^(z - lse) - [v = y_t]) in
 // BF16, and two products follow: dx += G W (FP32 sums, kept across pieces) and
-// dw = G^T X.  G of one piece is all that is ever stored.  It is the one
-// rounding to BF16 besides the outputs' own: the products need a BF16 operand,
-// and the rounding is relative to each entry, like the rounding of W and X
-// that the model already has.
+// dw = G^T X.  G of one piece is all that is ever stored, in BF16 since the
+// products need a BF16 operand.  A token's target entry is by far its largest, so
+// what that entry loses in the rounding (`rest`, FP32) is added back to both
+// products: rest W[y] to the token's dx, rest x to row y of dw.  The other
+// entries' roundings are relative to each and independent, and average out over
+// many tokens; for few, what they lose is kept as a second BF16 matrix for dw.
 //
 // The three products of the backward pass and the one of the forward pass are
 // bound by the matrix cores for many tokens, by reading W for few.
@@ -28,6 +30,19 @@ constexpr float kLog2e = 1.4426950408889634f;
 
 // 2^x (v_exp_f32, 1 ulp).
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// A pair (largest logit, sum of exponentials below it) as a sum below `top`.  A
+// pair without a finite logit has a sum of 0, or NaN, which stays one.
+__device__ __forceinline__ float below(float2 q, float top) {
+  return q.y * (q.x == -INFINITY ? 0.0f : exp2_fast((q.x - top) * kLog2e));
+}
+
+// Where target y lies among a lane's entries first + 16 i + e (e < 4), as 16 i + e;
+// -1 where it does not.
+__device__ __forceinline__ int32_t entry_of(int64_t y, uint32_t first, int rows) {
+  const int64_t d = y - (int64_t)first;
+  return d >= 0 && d < rows * 16 && (d & 15) < 4 ? (int32_t)d : -1;
+}
 
 // ---------------------------------------------------------------- logits
 
@@ -50,6 +65,7 @@ struct LogitParams {
   uint32_t vocab;
   uint16_t* g;  // [tokens][g_ld]
   uint64_t g_ld;
+  float* rest;  // [tokens]: what the target's entry lost in the rounding
 };
 
 template <typename T>
@@ -63,51 +79,60 @@ __global__ __launch_bounds__(T::kThreads) void ce_forward_kernel(LogitParams p) 
   const GemmOperand b = {p.x + (uint64_t)n0 * p.x_ld, p.x_ld, p.tokens - n0};
   T::run(lds, a, b, 0, p.hidden, acc);
 
+  // The work per entry is kept to a scaling, a maximum, a difference, a factor, an
+  // exponential and a sum: with a short hidden size this is a third of the time.
+  // The end of the vocabulary and the target are looked at where they occur.
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   float2(*s_part)[T::BN] = (float2(*)[T::BN])lds;  // [WM][BN]
+  const uint32_t mine = m0 + T::m_of(0, lane, wave);  // the lane's entries: + 16 i + e
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
     const uint32_t n = T::n_of(j, lane, wave), t = n0 + n;
-    const int64_t y = t < p.tokens ? p.targets[t] : -1;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] *= p.scale;
+    if (m0 + T::BM > p.v_end) {
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (mine + i * 16 + e >= p.v_end) acc[i][j][e] = -INFINITY;
+    }
+    const int32_t at = entry_of(t < p.tokens ? p.targets[t] : -1, mine, T::FM);
+    if (__builtin_amdgcn_ballot_w64(at >= 0)) {
+      float z = 0.0f;
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z = at == i * 16 + e ? acc[i][j][e] : z;
+      if (at >= 0) p.hit[t] = z;
+    }
+    // a NaN is passed over here and comes out of the sum
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t v = m0 + T::m_of(i, lane, wave) + e;
-        float z = acc[i][j][e] * p.scale;
-        if (v >= p.v_end) z = -INFINITY;
-        if ((int64_t)v == y) p.hit[t] = z;
-        acc[i][j][e] = z;
-        top = z > top || z != z ? z : top;  // a NaN stays
-      }
-#pragma unroll
-    for (int x = 16; x < 64; x *= 2) {
-      const float o = __shfl_xor(top, x);
-      top = o > top || o != o ? o : top;
-    }
+      for (int e = 0; e < 4; ++e) top = __builtin_fmaxf(top, acc[i][j][e]);
+    top = __builtin_fmaxf(top, __shfl_xor(top, 16));
+    top = __builtin_fmaxf(top, __shfl_xor(top, 32));
+    const float from = top == -INFINITY ? 0.0f : top;
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) sum += exp2_fast((acc[i][j][e] - top) * kLog2e);
+      for (int e = 0; e < 4; ++e) sum += exp2_fast((acc[i][j][e] - from) * kLog2e);
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if (lane < 16) s_part[wave / T::WN][n] = make_float2(top, top == -INFINITY ? 0.0f : sum);
+    if (lane < 16) s_part[wave / T::WN][n] = make_float2(top, sum);
   }
   __syncthreads();
   for (uint32_t n = threadIdx.x; n < T::BN; n += T::kThreads) {
     float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-    for (int w = 0; w < T::WM; ++w) {
-      const float o = s_part[w][n].x;
-      top = o > top || o != o ? o : top;
-    }
+    for (int w = 0; w < T::WM; ++w) top = __builtin_fmaxf(top, s_part[w][n].x);
 #pragma unroll
-    for (int w = 0; w < T::WM; ++w) {
-      const float2 q = s_part[w][n];
-      sum += q.x == -INFINITY ? 0.0f : q.y * exp2_fast((q.x - top) * kLog2e);
-    }
+    for (int w = 0; w < T::WM; ++w) sum += below(s_part[w][n], top);
     if (n0 + n < p.tokens) p.part[(uint64_t)(n0 + n) * p.tiles_m + tm] = make_float2(top, sum);
   }
 }
@@ -135,23 +160,66 @@ __global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
     by[j] = kept ? p.dloss[t] * p.scale : 0.0f;
     lse[j] = kept ? p.lse[t] : 0.0f;
   }
-  T::template store_rows<false>(
-      lds, p.g + n0 * p.g_ld + (m0 - p.v_begin), p.g_ld, T::BM, p.tokens - n0, [&](int i, int j) {
-        float g[4];
+  const uint32_t mine = m0 + T::m_of(0, lane, wave);  // the lane's entries: + 16 i + e
+  int32_t at[T::FN];                                  // which of them is the target
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t v = m0 + T::m_of(i, lane, wave) + e;
-          // z rounded as in the forward pass and the difference before the factor:
-          // exact where z is near lse, so a large logit costs a likely target no digits
-          const float pr = exp2_fast((acc[i][j][e] * p.scale - lse[j]) * kLog2e);
-          const float d = (int64_t)v == y[j] ? pr - 1.0f : pr;
-          g[e] = y[j] >= 0 && v < p.v_end ? d * by[j] : 0.0f;
-        }
-        uint2 o;
-        o.x = bf16x2_rne(__float_as_uint(g[0]), __float_as_uint(g[1]));
-        o.y = bf16x2_rne(__float_as_uint(g[2]), __float_as_uint(g[3]));
-        return o;
-      });
+  for (int j = 0; j < T::FN; ++j) {
+    at[j] = entry_of(y[j], mine, T::FM);
+    const bool any = __builtin_amdgcn_ballot_w64(at[j] >= 0) != 0;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        // z rounded as in the forward pass and the difference before the factor:
+        // exact where z is near lse, so a large logit costs a likely target no digits
+        acc[i][j][e] = exp2_fast((acc[i][j][e] * p.scale - lse[j]) * kLog2e);
+    if (any) {
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[i][j][e] = at[j] == i * 16 + e ? acc[i][j][e] - 1.0f : acc[i][j][e];
+    }
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[i][j][e] = y[j] >= 0 ? acc[i][j][e] * by[j] : 0.0f;
+    if (m0 + T::BM > p.v_end) {
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (mine + i * 16 + e >= p.v_end) acc[i][j][e] = 0.0f;
+    }
+    if (any) {
+      float rest = 0.0f;
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) rest = at[j] == i * 16 + e ? acc[i][j][e] : rest;
+      rest -= __uint_as_float(bf16x2_rne(__float_as_uint(rest), 0u) << 16);
+      if (at[j] >= 0) p.rest[n0 + T::n_of(j, lane, wave)] = rest;
+    }
+  }
+  auto rounded = [&](int i, int j) {
+    uint2 o;
+    o.x = bf16x2_rne(__float_as_uint(acc[i][j][0]), __float_as_uint(acc[i][j][1]));
+    o.y = bf16x2_rne(__float_as_uint(acc[i][j][2]), __float_as_uint(acc[i][j][3]));
+    return o;
+  };
+  uint16_t* const out = p.g + n0 * p.g_ld + (m0 - p.v_begin);
+  T::template store_rows<false>(lds, out, p.g_ld, T::BM, p.tokens - n0, rounded);
+  if constexpr (T::BN < 256) {  // few tokens: the rests of all entries, as rows of their own
+    __syncthreads();
+    T::template store_rows<false>(lds, out + (uint64_t)p.tokens * p.g_ld, p.g_ld, T::BM, p.tokens - n0,
+                                  [&](int i, int j) {
+                                    const uint2 o = rounded(i, j);
+                                    acc[i][j][0] -= __uint_as_float(o.x << 16);
+                                    acc[i][j][1] -= __uint_as_float(o.x & 0xFFFF0000u);
+                                    acc[i][j][2] -= __uint_as_float(o.y << 16);
+                                    acc[i][j][3] -= __uint_as_float(o.y & 0xFFFF0000u);
+                                    return rounded(i, j);
+                                  });
+  }
 }
 
 // A token's pairs joined, one wave each.
@@ -163,21 +231,11 @@ __global__ __launch_bounds__(256) void ce_join_kernel(const float2* part, const 
   if (t >= tokens) return;
   const int lane = threadIdx.x & 63;
   const float2* mine = part + (uint64_t)t * tiles;
-  float top = -INFINITY;
-  for (uint32_t i = lane; i < tiles; i += 64) {
-    const float o = mine[i].x;
-    top = o > top || o != o ? o : top;
-  }
+  float top = -INFINITY, sum = 0.0f;
+  for (uint32_t i = lane; i < tiles; i += 64) top = __builtin_fmaxf(top, mine[i].x);
 #pragma unroll
-  for (int x = 1; x < 64; x *= 2) {
-    const float o = __shfl_xor(top, x);
-    top = o > top || o != o ? o : top;
-  }
-  float sum = 0.0f;
-  for (uint32_t i = lane; i < tiles; i += 64) {
-    const float2 q = mine[i];
-    sum += q.x == -INFINITY ? 0.0f : q.y * exp2_fast((q.x - top) * kLog2e);
-  }
+  for (int x = 1; x < 64; x *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, x));
+  for (uint32_t i = lane; i < tiles; i += 64) sum += below(mine[i], top);
   sum = wave_sum(sum);
   if (lane == 0) {
     const float rest = logf(sum);
@@ -199,6 +257,9 @@ struct GradParams {
   int add;           // dx: onto what is there
   uint16_t* out;     // dw: [n][out_ld]
   uint64_t out_ld;
+  const int32_t* y;  // dw: [k] targets, -1 for none
+  uint32_t v_begin;  // the piece's first entry
+  const float* rest;
 };
 
 template <typename T, bool AK, bool BK>
@@ -238,12 +299,71 @@ __global__ __launch_bounds__(T::kThreads) void ce_dx_kernel(GradParams p) {
   }
 }
 
+// Adds rest[t] x[t] to the row of the tile that is token t's target.  The block
+// looks through the targets, collects those of its rows in LDS in a fixed order,
+// and every wave adds those that lie in its own columns of the tile.
 template <typename T>
+__device__ void add_rests(const GradParams& p, char* lds, uint32_t m0, uint32_t n0, typename T::Acc& acc) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t* s_list = (uint32_t*)lds;                       // [4 kThreads]
+  uint32_t* s_count = (uint32_t*)lds + 4 * T::kThreads;     // [kWaves]
+  const uint32_t first = T::n_of(0, 0, wave), m = m0 + T::m_of(0, lane, wave);
+  for (uint32_t base = 0; base < p.k; base += 4 * T::kThreads) {
+    uint64_t hits[4];
+    uint32_t count = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const uint32_t t = base + q * T::kThreads + threadIdx.x;
+      const uint32_t at = (t < p.k ? (uint32_t)p.y[t] : ~0u) - p.v_begin - n0;  // none: not below BN
+      hits[q] = __builtin_amdgcn_ballot_w64(at < T::BN);
+      count += (uint32_t)__popcll(hits[q]);
+    }
+    if (lane == 0) s_count[wave] = count;
+    __syncthreads();
+    uint32_t all = 0, before = 0;
+#pragma unroll
+    for (int w = 0; w < T::kWaves; ++w) {
+      if (w == wave) before = all;
+      all += s_count[w];
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (hits[q] >> lane & 1)
+        s_list[before + __popcll(hits[q] & ((1ull << lane) - 1))] = base + q * T::kThreads + threadIdx.x;
+      before += (uint32_t)__popcll(hits[q]);
+    }
+    __syncthreads();
+    for (uint32_t h = 0; h < all; ++h) {
+      const uint32_t t = __builtin_amdgcn_readfirstlane(s_list[h]);
+      const uint32_t n = (uint32_t)p.y[t] - p.v_begin - n0 - first;  // in the wave's columns, or not
+      if (n >= T::FN * 16) continue;
+      const float r = (uint32_t)(lane & 15) == (n & 15) ? p.rest[t] : 0.0f;
+      const uint16_t* x = p.a.p + t * p.a.ld;
+#pragma unroll
+      for (int j = 0; j < T::FN; ++j) {
+        if (n >> 4 != (uint32_t)j) continue;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i) {
+          const uint32_t c = m + i * 16 < p.a.limit ? m + i * 16 : 0;
+          const uint2 v = *(const uint2*)(x + c);
+          acc[i][j][0] = __builtin_fmaf(r, __uint_as_float(v.x << 16), acc[i][j][0]);
+          acc[i][j][1] = __builtin_fmaf(r, __uint_as_float(v.x & 0xFFFF0000u), acc[i][j][1]);
+          acc[i][j][2] = __builtin_fmaf(r, __uint_as_float(v.y << 16), acc[i][j][2]);
+          acc[i][j][3] = __builtin_fmaf(r, __uint_as_float(v.y & 0xFFFF0000u), acc[i][j][3]);
+        }
+      }
+    }
+    __syncthreads();  // the list and the counts are free again
+  }
+}
+
+template <typename T, bool RESTS>
 __global__ __launch_bounds__(T::kThreads) void ce_dw_kernel(GradParams p) {
   __shared__ alignas(1024) char lds[T::kLds];
   uint32_t m0, n0;
   typename T::Acc acc;
   grad_tile<T, true, true>(p, lds, m0, n0, acc);
+  if constexpr (RESTS) add_rests<T>(p, lds, m0, n0, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   auto value = [&](int i, int j) {
     uint2 o;
@@ -271,18 +391,27 @@ __global__ __launch_bounds__(T::kThreads) void ce_dw_kernel(GradParams p) {
   }
 }
 
-// dx from the splits' sums; a token without a target gets zeros.
+// dx from the splits' sums and what the target's entry lost; a token without a target gets zeros.
 __global__ __launch_bounds__(256) void ce_dx_join_kernel(const float* sums, uint32_t splits, uint32_t tokens,
                                                          uint32_t ld, uint32_t hidden,
                                                          const int64_t* targets, uint32_t vocab,
-                                                         uint16_t* dx, uint64_t dx_ld) {
+                                                         const uint16_t* w, uint64_t w_ld,
+                                                         const float* rest, uint16_t* dx,
+                                                         uint64_t dx_ld) {
   const uint32_t t = blockIdx.x;
   const uint32_t c = (blockIdx.y * 256 + threadIdx.x) * 4;
   if (c >= ld) return;
   const int64_t y = targets[t];
   f32x4_t a = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (y >= 0 && y < (int64_t)vocab)
+  if (y >= 0 && y < (int64_t)vocab) {
+    const uint2 v = *(const uint2*)(w + y * w_ld + c);
     for (uint32_t s = 0; s < splits; ++s) a += *(const f32x4_t*)(sums + ((uint64_t)s * tokens + t) * ld + c);
+    const float r = rest[t];
+    a[0] = __builtin_fmaf(r, __uint_as_float(v.x << 16), a[0]);
+    a[1] = __builtin_fmaf(r, __uint_as_float(v.x & 0xFFFF0000u), a[1]);
+    a[2] = __builtin_fmaf(r, __uint_as_float(v.y << 16), a[2]);
+    a[3] = __builtin_fmaf(r, __uint_as_float(v.y & 0xFFFF0000u), a[3]);
+  }
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (c + e < hidden) dx[t * dx_ld + c + e] = (uint16_t)bf16x2_rne(__float_as_uint(a[e]), 0u);
@@ -290,10 +419,10 @@ __global__ __launch_bounds__(256) void ce_dx_join_kernel(const float* sums, uint
 
 // ---------------------------------------------------------------- copies
 
-// Rows padded with zeros to `ld`; rows of tokens without a target (`targets` not
+// Rows padded with zeros to `ld`, `times` over; rows of tokens without a target (`targets` not
 // null) all zero: what is in them must not reach the other rows' sums.
 __global__ __launch_bounds__(256) void ce_copy_kernel(const uint16_t* from, uint64_t from_ld, uint32_t cols,
-                                                      uint16_t* to, uint32_t ld, uint64_t rows,
+                                                      uint16_t* to, uint32_t ld, uint64_t rows, uint32_t times,
                                                       const int64_t* targets, uint32_t vocab) {
   const uint64_t groups = ld / 8, all = rows * groups;
   for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
@@ -317,16 +446,25 @@ __global__ __launch_bounds__(256) void ce_copy_kernel(const uint16_t* from, uint
         v = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
-    store16(to + r * ld + c, v);
+    for (uint32_t k = 0; k < times; ++k) store16(to + (k * rows + r) * ld + c, v);
   }
 }
 
+// targets as 32-bit entries, -1 for an ignored one
+__global__ __launch_bounds__(256) void ce_targets_kernel(const int64_t* targets, uint32_t tokens, uint32_t vocab,
+                                                         int32_t* y) {
+  const uint32_t t = blockIdx.x * 256 + threadIdx.x;
+  if (t >= tokens) return;
+  const int64_t v = targets[t];
+  y[t] = v >= 0 && v < (int64_t)vocab ? (int32_t)v : -1;
+}
+
 void copy_rows(const uint16_t* from, uint64_t from_ld, uint32_t cols, uint16_t* to, uint32_t ld, uint64_t rows,
-               const int64_t* targets, uint32_t vocab, hipStream_t stream) {
+               uint32_t times, const int64_t* targets, uint32_t vocab, hipStream_t stream) {
   uint64_t blocks = (rows * (ld / 8) + 255) / 256;
   if (blocks > 8192) blocks = 8192;
   hipLaunchKernelGGL(ce_copy_kernel, dim3((uint32_t)blocks), dim3(256), 0, stream, from, from_ld, cols, to, ld,
-                     rows, targets, vocab);
+                     rows, times, targets, vocab);
 }
 
 // ---------------------------------------------------------------- shapes
@@ -335,6 +473,7 @@ uint32_t up(uint32_t v, uint32_t to) { return (v + to - 1) / to * to; }
 uint32_t parts(uint64_t v, uint32_t of) { return (uint32_t)((v + of - 1) / of); }
 
 constexpr uint32_t kVocabTile = 256;
+constexpr uint32_t kFewTokens = 128;  // up to here G's rests are kept for all entries
 
 // Tiles: vocabulary (or hidden) by tokens (or vocabulary), by the tokens' count.
 typedef Gemm<256, 256, 2, 4, false, false> LogitsL;
@@ -355,7 +494,7 @@ struct Plan {
   uint32_t piece;   // vocabulary entries a piece, a multiple of the tile
   uint32_t splits;  // of dx's k
   // byte offsets in the workspace
-  uint64_t w, x, part, hit, g, sums, forward, total;
+  uint64_t w, x, part, hit, g, y, rest, sums, forward, total;
 };
 
 Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
@@ -369,7 +508,8 @@ Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
     return here;
   };
   q.w = take(q.copy_w ? (uint64_t)vocab * q.ld * 2 : 0);
-  q.x = take((uint64_t)tokens * q.ld * 2);
+  const uint32_t times = tokens <= kFewTokens ? 2 : 1;
+  q.x = take((uint64_t)times * tokens * q.ld * 2);
   const uint64_t both = at;
   q.part = take((uint64_t)tokens * parts(vocab, kVocabTile) * sizeof(float2));
   q.hit = take((uint64_t)tokens * sizeof(float));
@@ -385,7 +525,9 @@ Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   const uint32_t tiles = parts(q.ld, bm) * parts(tokens, bn);
   q.splits = 1;
   while (tiles * q.splits < 256 && q.splits * 2 * 256 <= q.piece) q.splits *= 2;
-  q.g = take((uint64_t)tokens * q.piece * 2);
+  q.g = take((uint64_t)times * tokens * q.piece * 2);
+  q.y = take((uint64_t)tokens * sizeof(int32_t));
+  q.rest = take((uint64_t)tokens * sizeof(float));
   q.sums = take((uint64_t)q.splits * tokens * q.ld * 4);
   q.total = at > q.forward ? at : q.forward;
   return q;
@@ -413,11 +555,11 @@ void run_dx(GradParams p, uint32_t splits, hipStream_t stream) {
   hipLaunchKernelGGL(ce_dx_kernel<T>, dim3(p.tiles_m * p.tiles_n, splits), dim3(T::kThreads), 0, stream, p);
 }
 
-template <typename T>
+template <typename T, bool RESTS>
 void run_dw(GradParams p, hipStream_t stream) {
   p.tiles_m = parts(p.m, T::BM);
   p.tiles_n = parts(p.n, T::BN);
-  hipLaunchKernelGGL(ce_dw_kernel<T>, dim3(p.tiles_m * p.tiles_n), dim3(T::kThreads), 0, stream, p);
+  hipLaunchKernelGGL((ce_dw_kernel<T, RESTS>), dim3(p.tiles_m * p.tiles_n), dim3(T::kThreads), 0, stream, p);
 }
 
 }  // namespace
@@ -442,7 +584,7 @@ hipError_t launch_linear_ce(const LinearCeParams& c, char* ws, hipStream_t strea
   p.w_ld = c.hidden;
   if (q.copy_w) {
     uint16_t* w = (uint16_t*)(ws + q.w);
-    copy_rows(c.weight, c.hidden, c.hidden, w, q.ld, c.vocab, nullptr, c.vocab, stream);
+    copy_rows(c.weight, c.hidden, c.hidden, w, q.ld, c.vocab, 1, nullptr, c.vocab, stream);
     p.w = w;
     p.w_ld = q.ld;
   }
@@ -450,7 +592,7 @@ hipError_t launch_linear_ce(const LinearCeParams& c, char* ws, hipStream_t strea
   p.x_ld = c.x_stride;
   if (c.hidden % 8 || c.x_stride % 8 || c.x_stride > kMaxStride) {
     uint16_t* x = (uint16_t*)(ws + q.x);
-    copy_rows(c.x, c.x_stride, c.hidden, x, q.ld, c.tokens, nullptr, c.vocab, stream);
+    copy_rows(c.x, c.x_stride, c.hidden, x, q.ld, c.tokens, 1, nullptr, c.vocab, stream);
     p.x = x;
     p.x_ld = q.ld;
   }
@@ -475,12 +617,15 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
   p.w_ld = c.hidden;
   if (q.copy_w) {
     uint16_t* w = (uint16_t*)(ws + q.w);
-    copy_rows(c.weight, c.hidden, c.hidden, w, q.ld, c.vocab, nullptr, c.vocab, stream);
+    copy_rows(c.weight, c.hidden, c.hidden, w, q.ld, c.vocab, 1, nullptr, c.vocab, stream);
     p.w = w;
     p.w_ld = q.ld;
   }
+  // few tokens: G's rests are 128 more rows at most of k for dw, which then meet x
+  // again; more tokens add the targets' rests alone
+  const bool few = c.tokens <= kFewTokens;
   uint16_t* x = (uint16_t*)(ws + q.x);
-  copy_rows(c.x, c.x_stride, c.hidden, x, q.ld, c.tokens, c.targets, c.vocab, stream);
+  copy_rows(c.x, c.x_stride, c.hidden, x, q.ld, c.tokens, few ? 2 : 1, c.targets, c.vocab, stream);
   p.x = x;
   p.x_ld = q.ld;
   p.targets = c.targets;
@@ -492,6 +637,10 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
   p.dloss = c.dloss;
   p.g = (uint16_t*)(ws + q.g);
   p.g_ld = q.piece;
+  p.rest = (float*)(ws + q.rest);
+  int32_t* y = (int32_t*)(ws + q.y);
+  hipLaunchKernelGGL(ce_targets_kernel, dim3(parts(c.tokens, 256)), dim3(256), 0, stream, c.targets, c.tokens,
+                     c.vocab, y);
   float* sums = (float*)(ws + q.sums);
   for (uint32_t v = 0; v < c.vocab; v += q.piece) {
     const uint32_t n = c.vocab - v < q.piece ? c.vocab - v : q.piece;
@@ -517,14 +666,17 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
     e.b = {p.g, q.piece, q.piece};
     e.m = c.hidden;
     e.n = n;
-    e.k = e.k_split = c.tokens;
+    e.k = e.k_split = few ? 2 * c.tokens : c.tokens;
+    e.y = y;
+    e.rest = p.rest;
+    e.v_begin = v;
     e.out = c.dweight + (uint64_t)v * c.hidden;
     e.out_ld = c.hidden;
-    if (c.tokens <= 128) run_dw<DwS>(e, stream);
-    else run_dw<DwL>(e, stream);
+    if (few) run_dw<DwS, false>(e, stream);
+    else run_dw<DwL, true>(e, stream);
   }
   hipLaunchKernelGGL(ce_dx_join_kernel, dim3(c.tokens, parts(q.ld, 1024)), dim3(256), 0, stream, sums, q.splits,
-                     c.tokens, q.ld, c.hidden, c.targets, c.vocab, c.dx, c.dx_stride);
+                     c.tokens, q.ld, c.hidden, c.targets, c.vocab, p.w, p.w_ld, p.rest, c.dx, c.dx_stride);
   return hipGetLastError();
 }
 
