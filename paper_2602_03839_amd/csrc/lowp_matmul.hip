@@ -253,6 +253,201 @@ __global__ __launch_bounds__(1024) void lowp_matmul_kernel(LowpMatmulParams p, u
   }
 }
 
+// The sum of a tile's parts and its rows' results: lane (token r16, group g) has
+// the rows row0 + 4 g + i.
+__device__ __forceinline__ void store_result(const LowpMatmulParams& p, bool mx, f32x4_t v, uint32_t t,
+                                             uint64_t row) {
+  if (t >= p.tokens) return;
+  if (!mx) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] /= p.inv_scale;
+  }
+  const uint64_t at = t * p.y_stride + row;
+  if (p.y_bf16) {
+    uint16_t* y = (uint16_t*)p.y + at;
+    const uint2 o = make_uint2(bf16x2_rne(__float_as_uint(v[0]), __float_as_uint(v[1])),
+                               bf16x2_rne(__float_as_uint(v[2]), __float_as_uint(v[3])));
+    if (at % 4 == 0 && row + 4 <= p.rows) {
+      *(uint2*)y = o;
+    } else {
+      const uint32_t w[2] = {o.x, o.y};
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (row + i < p.rows) y[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    }
+  } else {
+    float* y = (float*)p.y + at;
+    if (at % 4 == 0 && row + 4 <= p.rows) {
+      *(f32x4_t*)y = v;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (row + i < p.rows) y[i] = v[i];
+    }
+  }
+}
+
+struct __attribute__((packed)) Bytes4 {
+  uint32_t w;
+};
+
+// A tile's parts added by one wave; the waves take turns.  `part` is free again
+// after the next tile's barrier, so callers alternate between two.
+__device__ __forceinline__ void join_parts(const LowpMatmulParams& p, bool mx, f32x4_t* part, f32x4_t acc,
+                                           uint32_t turn, uint32_t t, uint32_t tile) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  part[wave * 64 + lane] = acc;
+  __syncthreads();
+  if ((int)(turn % waves) != wave) return;
+  f32x4_t v = part[lane];
+  for (int w = 1; w < waves; ++w) v += part[w * 64 + lane];
+  store_result(p, mx, v, t, (uint64_t)tile * 16 + 4 * (lane >> 4));
+}
+
+// A lane's codes of one chunk of row `row`: its unit, and its scale byte.
+template <bool MX>
+struct ChunkCodes {
+  uint4 c;
+  uint32_t scale;
+};
+
+template <bool MX>
+__device__ __forceinline__ void load_codes(const LowpMatmulParams& p, uint64_t row, uint32_t units, uint32_t u,
+                                           bool in, ChunkCodes<MX>& q) {
+  if (row >= p.rows) row = p.rows - 1;
+  const uint64_t unit = row * units + (in ? u : 0);
+  q.c = load16_any(p.codes + unit * 16);
+  if constexpr (MX) q.scale = p.scales[unit];
+  if (!in) {  // past the row's end: zeros
+    q.c = make_uint4(0, 0, 0, 0);
+    q.scale = 127;
+  }
+}
+
+template <bool MX>
+__device__ __forceinline__ f32x4_t multiply_codes(const ChunkCodes<MX>& q, const uint4 (&x)[Unit<MX>::kFrags],
+                                                  f32x4_t acc) {
+  const float scale = MX ? __uint_as_float(q.scale << 23) : 1.0f;
+#pragma unroll
+  for (uint32_t f = 0; f < Unit<MX>::kFrags; ++f)
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<MX>(q.c, f, scale), __builtin_bit_cast(bf16x8_t, x[f]),
+                                                  acc, 0, 0, 0);
+  return acc;
+}
+
+// Up to 16 tokens whose values fit LDS.  The block's waves share the chunks of a row
+// tile; each wave has the codes of its next kAheadChunks chunks on their way, over
+// the ends of tiles, and reads the tokens' values of a chunk when it gets there.
+constexpr int kAheadChunks = 8;
+
+template <bool MX>
+__global__ __launch_bounds__(1024) void lowp_lds_kernel(LowpMatmulParams p, uint32_t tiles, uint32_t chunks) {
+  typedef Unit<MX> U;
+  extern __shared__ f32x4_t s_part[];  // [2][waves][64], then the tokens' rows
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int r16 = lane & 15, g = lane >> 4;
+  const uint32_t units = p.cols / U::kValues;
+  const uint32_t ld = p.cols * 2 + 16;  // bytes; the 16 move each row to other banks
+  char* const s_x = (char*)(s_part + 2 * waves * 64);
+
+  // where the wave's loads are: `ahead` chunks before its products
+  uint32_t load_tile = blockIdx.x, load_chunk = wave;
+  ChunkCodes<MX> q[kAheadChunks];
+  auto fetch = [&](ChunkCodes<MX>& to) {
+    if (load_tile >= tiles) return;
+    const uint32_t u = load_chunk * kLpGroups + g;
+    load_codes<MX>(p, (uint64_t)load_tile * 16 + r16, units, u, u < units, to);
+    load_chunk += waves;
+    if (load_chunk >= chunks) {
+      load_chunk = wave;
+      load_tile += gridDim.x;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < kAheadChunks; ++i) fetch(q[i]);
+
+  const uint32_t pieces = p.cols / 8;  // of 16 bytes, in a row
+  for (uint32_t i = threadIdx.x; i < p.tokens * pieces; i += blockDim.x) {
+    const uint32_t t = i / pieces, c = i % pieces;
+    *(uint4*)(s_x + t * ld + c * 16) = load16_any(p.x + t * p.x_stride + c * 8);
+  }
+  __syncthreads();
+  const char* const mine = s_x + (r16 < (int)p.tokens ? r16 : p.tokens - 1) * ld;
+
+  uint32_t tile = blockIdx.x, chunk = wave, turn = 0;
+  f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  while (tile < tiles) {
+#pragma unroll
+    for (int i = 0; i < kAheadChunks; ++i) {
+      if (tile >= tiles) break;
+      const uint32_t u = chunk * kLpGroups + g;
+      uint4 x[U::kFrags];
+#pragma unroll
+      for (uint32_t f = 0; f < U::kFrags; ++f)
+        x[f] = u < units ? *(const uint4*)(mine + u * (U::kValues * 2) + f * 16) : make_uint4(0, 0, 0, 0);
+      acc = multiply_codes<MX>(q[i], x, acc);
+      fetch(q[i]);
+      chunk += waves;
+      if (chunk >= chunks) {
+        join_parts(p, MX, s_part + (turn & 1) * waves * 64, acc, turn, r16, tile);
+        acc = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        chunk = wave;
+        tile += gridDim.x;
+        ++turn;
+      }
+    }
+  }
+}
+
+// Up to 16 tokens, in registers: wave w of a block owns the chunks w S ... w S + S - 1
+// of k for as long as it runs, and the block goes through row tiles, the next two
+// tiles' codes on their way.  The waves of a block together read whole rows, 16 of
+// them adjacent; nothing but codes and scales is loaded in the loop.
+template <bool MX, int S, int AHEAD>
+__global__ __launch_bounds__(768) void lowp_sweep_kernel(LowpMatmulParams p, uint32_t tiles) {
+  typedef Unit<MX> U;
+  extern __shared__ f32x4_t s_part[];  // [2][waves][64]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int r16 = lane & 15, g = lane >> 4;
+  const uint32_t units = p.cols / U::kValues;  // of a row
+  const uint32_t t = blockIdx.y * 16 + r16;
+  const uint16_t* const xrow = p.x + (uint64_t)(t < p.tokens ? t : p.tokens - 1) * p.x_stride;
+
+  uint4 x[S][U::kFrags];
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    const uint32_t u = (wave * S + s) * kLpGroups + g;
+#pragma unroll
+    for (uint32_t f = 0; f < U::kFrags; ++f)
+      x[s][f] = u < units ? load16_any(xrow + (uint64_t)u * U::kValues + 8 * f) : make_uint4(0, 0, 0, 0);
+  }
+  ChunkCodes<MX> q[AHEAD + 1][S];
+  auto fetch = [&](ChunkCodes<MX> (&to)[S], uint32_t tile) {
+    if (tile >= tiles) return;
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const uint32_t u = (wave * S + s) * kLpGroups + g;
+      load_codes<MX>(p, (uint64_t)tile * 16 + r16, units, u, u < units, to[s]);
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) fetch(q[i], blockIdx.x + i * gridDim.x);
+  uint32_t tile = blockIdx.x, turn = 0;
+  while (tile < tiles) {
+#pragma unroll
+    for (int i = 0; i < AHEAD + 1; ++i) {
+      if (tile >= tiles) break;
+      fetch(q[(i + AHEAD) % (AHEAD + 1)], tile + AHEAD * gridDim.x);
+      f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int s = 0; s < S; ++s) acc = multiply_codes<MX>(q[i][s], x[s], acc);
+      join_parts(p, MX, s_part + (turn & 1) * waves * 64, acc, turn, t, tile);
+      ++turn;
+      tile += gridDim.x;
+    }
+  }
+}
+
 template <bool MX, int RT, int NT, bool SHIFT>
 void launch_shape(const LowpMatmulParams& p, hipStream_t stream) {
   typedef Unit<MX> U;
@@ -269,11 +464,39 @@ void launch_shape(const LowpMatmulParams& p, hipStream_t stream) {
                      dim3(64 * waves), lds, stream, p, classes);
 }
 
+constexpr uint32_t kLpCus = 256;
+
+// Whether 16 tokens or fewer fit LDS beside the parts of 16 waves.
+bool tokens_fit(const LowpMatmulParams& p) {
+  return p.tokens <= 16 && (uint64_t)p.tokens * (p.cols * 2ull + 16) <= 128 * 1024;
+}
+
+template <bool MX>
+void launch_lds(const LowpMatmulParams& p, uint32_t chunks, hipStream_t stream) {
+  const uint32_t tiles = (p.rows + 15) / 16, waves = chunks < 16 ? chunks : 16;
+  const size_t lds = (size_t)2 * waves * 64 * sizeof(f32x4_t) + (size_t)p.tokens * (p.cols * 2 + 16);
+  hipLaunchKernelGGL(lowp_lds_kernel<MX>, dim3(tiles < kLpCus ? tiles : kLpCus), dim3(64 * waves), lds, stream, p,
+                     tiles, chunks);
+}
+
+template <bool MX, int S, int AHEAD>
+void launch_sweep(const LowpMatmulParams& p, uint32_t chunks, hipStream_t stream) {
+  const uint32_t tiles = (p.rows + 15) / 16, waves = (chunks + S - 1) / S;
+  hipLaunchKernelGGL((lowp_sweep_kernel<MX, S, AHEAD>), dim3(tiles < kLpCus ? tiles : kLpCus, (p.tokens + 15) / 16),
+                     dim3(64 * waves), (size_t)2 * waves * 64 * sizeof(f32x4_t), stream, p, tiles);
+}
+
 template <bool MX>
 void launch_type(const LowpMatmulParams& p, hipStream_t stream) {
-  if (p.cols % Unit<MX>::kValues) launch_shape<MX, 1, 1, true>(p, stream);
-  else if (p.rows >= 65536) launch_shape<MX, 2, 1, false>(p, stream);
-  else launch_shape<MX, 1, 1, false>(p, stream);
+  typedef Unit<MX> U;
+  if (p.cols % U::kValues) return launch_shape<MX, 1, 1, true>(p, stream);
+  const uint32_t chunks = (p.cols + U::kChunk - 1) / U::kChunk;
+  if (tokens_fit(p)) return launch_lds<MX>(p, chunks, stream);
+  constexpr int kS = MX ? 4 : 8;
+  if (p.tokens <= 16 && chunks <= 12 * kS) return launch_sweep<MX, kS, MX ? 2 : 1>(p, chunks, stream);
+  if (p.tokens <= 16) launch_shape<MX, 1, 1, false>(p, stream);
+  else if (p.tokens <= 32) launch_shape<MX, 2, 2, false>(p, stream);
+  else launch_shape<MX, 2, 4, false>(p, stream);
 }
 
 }  // namespace
