@@ -300,6 +300,7 @@ __device__ __forceinline__ void join_parts(const LowpMatmulParams& p, bool mx, f
   __syncthreads();
   if ((int)(turn % waves) != wave) return;
   f32x4_t v = part[lane];
+#pragma unroll 5
   for (int w = 1; w < waves; ++w) v += part[w * 64 + lane];
   store_result(p, mx, v, t, (uint64_t)tile * 16 + 4 * (lane >> 4));
 }
@@ -311,16 +312,19 @@ struct ChunkCodes {
   uint32_t scale;
 };
 
+// Always a load, so that nothing branches on the way: a row past the last is the
+// last, and a unit past the row's end its last unit, with a finite scale; the
+// tokens' values there are zeros.
 template <bool MX>
-__device__ __forceinline__ void load_codes(const LowpMatmulParams& p, uint64_t row, uint32_t units, uint32_t u,
-                                           bool in, ChunkCodes<MX>& q) {
+__device__ __forceinline__ void load_codes(const LowpMatmulParams& p, uint32_t row, uint32_t units, uint32_t u,
+                                           ChunkCodes<MX>& q) {
   if (row >= p.rows) row = p.rows - 1;
-  const uint64_t unit = row * units + (in ? u : 0);
+  const bool in = u < units;
+  const uint64_t unit = (uint64_t)row * units + (in ? u : units - 1);
   q.c = load16_any(p.codes + unit * 16);
-  if constexpr (MX) q.scale = p.scales[unit];
-  if (!in) {  // past the row's end: zeros
-    q.c = make_uint4(0, 0, 0, 0);
-    q.scale = 127;
+  if constexpr (MX) {
+    const uint32_t scale = p.scales[unit];
+    q.scale = in ? scale : 127u;
   }
 }
 
@@ -335,65 +339,71 @@ __device__ __forceinline__ f32x4_t multiply_codes(const ChunkCodes<MX>& q, const
   return acc;
 }
 
-// Up to 16 tokens whose values fit LDS.  The block's waves share the chunks of a row
-// tile; each wave has the codes of its next kAheadChunks chunks on their way, over
-// the ends of tiles, and reads the tokens' values of a chunk when it gets there.
-constexpr int kAheadChunks = 8;
+// Up to 16 tokens whose values fit LDS.  The block's waves share a row tile: they take
+// pairs of chunks in turn (a pair is 128 bytes of each row, a whole line).  Each wave
+// has the codes of its next kAheadPairs pairs on their way, over the ends of tiles,
+// and reads the tokens' values of a chunk when it gets there.
+constexpr int kAheadPairs = 4;
 
 template <bool MX>
-__global__ __launch_bounds__(1024) void lowp_lds_kernel(LowpMatmulParams p, uint32_t tiles, uint32_t chunks) {
+__global__ __launch_bounds__(1024) void lowp_lds_kernel(LowpMatmulParams p, uint32_t tiles, uint32_t pairs) {
   typedef Unit<MX> U;
   extern __shared__ f32x4_t s_part[];  // [2][waves][64], then the tokens' rows
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int r16 = lane & 15, g = lane >> 4;
   const uint32_t units = p.cols / U::kValues;
-  const uint32_t ld = p.cols * 2 + 16;  // bytes; the 16 move each row to other banks
+  // bytes of a token's row, zeros from its end to the pair's; the 16 move each
+  // row to other banks
+  const uint32_t ld = pairs * U::kChunk * 4 + 16;
   char* const s_x = (char*)(s_part + 2 * waves * 64);
 
-  // where the wave's loads are: `ahead` chunks before its products
-  uint32_t load_tile = blockIdx.x, load_chunk = wave;
-  ChunkCodes<MX> q[kAheadChunks];
-  auto fetch = [&](ChunkCodes<MX>& to) {
+  // where the wave's loads are, ahead of its products
+  uint32_t load_tile = blockIdx.x, load_pair = wave;
+  ChunkCodes<MX> q[kAheadPairs][2];
+  auto fetch = [&](ChunkCodes<MX> (&to)[2]) {
     if (load_tile >= tiles) return;
-    const uint32_t u = load_chunk * kLpGroups + g;
-    load_codes<MX>(p, (uint64_t)load_tile * 16 + r16, units, u, u < units, to);
-    load_chunk += waves;
-    if (load_chunk >= chunks) {
-      load_chunk = wave;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      load_codes<MX>(p, load_tile * 16 + r16, units, (load_pair * 2 + h) * kLpGroups + g, to[h]);
+    load_pair += waves;
+    if (load_pair >= pairs) {
+      load_pair = wave;
       load_tile += gridDim.x;
     }
   };
 #pragma unroll
-  for (int i = 0; i < kAheadChunks; ++i) fetch(q[i]);
+  for (int i = 0; i < kAheadPairs; ++i) fetch(q[i]);
 
-  const uint32_t pieces = p.cols / 8;  // of 16 bytes, in a row
+  const uint32_t pieces = pairs * U::kChunk / 4, filled = p.cols / 8;  // of 16 bytes, in a row
   for (uint32_t i = threadIdx.x; i < p.tokens * pieces; i += blockDim.x) {
     const uint32_t t = i / pieces, c = i % pieces;
-    *(uint4*)(s_x + t * ld + c * 16) = load16_any(p.x + t * p.x_stride + c * 8);
+    *(uint4*)(s_x + t * ld + c * 16) = c < filled ? load16_any(p.x + t * p.x_stride + c * 8) : make_uint4(0, 0, 0, 0);
   }
   __syncthreads();
-  const char* const mine = s_x + (r16 < (int)p.tokens ? r16 : p.tokens - 1) * ld;
+  const char* const mine = s_x + (r16 < (int)p.tokens ? r16 : p.tokens - 1) * ld + g * (U::kValues * 2);
 
-  uint32_t tile = blockIdx.x, chunk = wave, turn = 0;
+  uint32_t tile = blockIdx.x, pair = wave, turn = 0;
   f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  while (tile < tiles) {
+  for (;;) {
 #pragma unroll
-    for (int i = 0; i < kAheadChunks; ++i) {
-      if (tile >= tiles) break;
-      const uint32_t u = chunk * kLpGroups + g;
-      uint4 x[U::kFrags];
+    for (int i = 0; i < kAheadPairs; ++i) {
 #pragma unroll
-      for (uint32_t f = 0; f < U::kFrags; ++f)
-        x[f] = u < units ? *(const uint4*)(mine + u * (U::kValues * 2) + f * 16) : make_uint4(0, 0, 0, 0);
-      acc = multiply_codes<MX>(q[i], x, acc);
+      for (int h = 0; h < 2; ++h) {
+        uint4 x[U::kFrags];
+#pragma unroll
+        for (uint32_t f = 0; f < U::kFrags; ++f)
+          x[f] = *(const uint4*)(mine + (pair * 2 + h) * (U::kChunk * 2) + f * 16);
+        acc = multiply_codes<MX>(q[i][h], x, acc);
+      }
       fetch(q[i]);
-      chunk += waves;
-      if (chunk >= chunks) {
+      pair += waves;
+      if (pair >= pairs) {
         join_parts(p, MX, s_part + (turn & 1) * waves * 64, acc, turn, r16, tile);
         acc = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        chunk = wave;
+        pair = wave;
         tile += gridDim.x;
         ++turn;
+        if (tile >= tiles) return;
       }
     }
   }
@@ -422,13 +432,11 @@ __global__ __launch_bounds__(768) void lowp_sweep_kernel(LowpMatmulParams p, uin
       x[s][f] = u < units ? load16_any(xrow + (uint64_t)u * U::kValues + 8 * f) : make_uint4(0, 0, 0, 0);
   }
   ChunkCodes<MX> q[AHEAD + 1][S];
+  uint32_t last = blockIdx.x;
   auto fetch = [&](ChunkCodes<MX> (&to)[S], uint32_t tile) {
-    if (tile >= tiles) return;
+    if (tile < tiles) last = tile;  // past the last tile: the same again, unused
 #pragma unroll
-    for (int s = 0; s < S; ++s) {
-      const uint32_t u = (wave * S + s) * kLpGroups + g;
-      load_codes<MX>(p, (uint64_t)tile * 16 + r16, units, u, u < units, to[s]);
-    }
+    for (int s = 0; s < S; ++s) load_codes<MX>(p, last * 16 + r16, units, (wave * S + s) * kLpGroups + g, to[s]);
   };
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) fetch(q[i], blockIdx.x + i * gridDim.x);
@@ -467,16 +475,18 @@ void launch_shape(const LowpMatmulParams& p, hipStream_t stream) {
 constexpr uint32_t kLpCus = 256;
 
 // Whether 16 tokens or fewer fit LDS beside the parts of 16 waves.
-bool tokens_fit(const LowpMatmulParams& p) {
-  return p.tokens <= 16 && (uint64_t)p.tokens * (p.cols * 2ull + 16) <= 128 * 1024;
+bool tokens_fit(const LowpMatmulParams& p, uint64_t row_bytes) {
+  return p.tokens <= 16 && p.tokens * (row_bytes + 16) <= 128 * 1024;
 }
 
 template <bool MX>
 void launch_lds(const LowpMatmulParams& p, uint32_t chunks, hipStream_t stream) {
-  const uint32_t tiles = (p.rows + 15) / 16, waves = chunks < 16 ? chunks : 16;
-  const size_t lds = (size_t)2 * waves * 64 * sizeof(f32x4_t) + (size_t)p.tokens * (p.cols * 2 + 16);
-  hipLaunchKernelGGL(lowp_lds_kernel<MX>, dim3(tiles < kLpCus ? tiles : kLpCus), dim3(64 * waves), lds, stream, p,
-                     tiles, chunks);
+  const uint32_t tiles = (p.rows + 15) / 16, pairs = (chunks + 1) / 2;
+  // as many waves as give each the same number of pairs, and blocks the same of tiles
+  const uint32_t each = (pairs + 15) / 16, waves = (pairs + each - 1) / each;
+  const uint32_t rounds = (tiles + 2 * kLpCus - 1) / (2 * kLpCus), blocks = (tiles + rounds - 1) / rounds;
+  const size_t lds = (size_t)2 * waves * 64 * sizeof(f32x4_t) + (size_t)p.tokens * (pairs * Unit<MX>::kChunk * 4 + 16);
+  hipLaunchKernelGGL(lowp_lds_kernel<MX>, dim3(blocks), dim3(64 * waves), lds, stream, p, tiles, pairs);
 }
 
 template <bool MX, int S, int AHEAD>
@@ -491,7 +501,7 @@ void launch_type(const LowpMatmulParams& p, hipStream_t stream) {
   typedef Unit<MX> U;
   if (p.cols % U::kValues) return launch_shape<MX, 1, 1, true>(p, stream);
   const uint32_t chunks = (p.cols + U::kChunk - 1) / U::kChunk;
-  if (tokens_fit(p)) return launch_lds<MX>(p, chunks, stream);
+  if (tokens_fit(p, (uint64_t)(chunks + 1) / 2 * U::kChunk * 4)) return launch_lds<MX>(p, chunks, stream);
   constexpr int kS = MX ? 4 : 8;
   if (p.tokens <= 16 && chunks <= 12 * kS) return launch_sweep<MX, kS, MX ? 2 : 1>(p, chunks, stream);
   if (p.tokens <= 16) launch_shape<MX, 1, 1, false>(p, stream);
