@@ -25,6 +25,7 @@
 
 #include "device_common.hpp"
 #include "head.hpp"
+#include "lds_load.hpp"
 
 namespace pulse {
 
@@ -40,20 +41,6 @@ struct GemmOperand {
 
 namespace {
 __device__ __align__(16) uint32_t gemm_zeros[4];  // what k past the end is read from
-}
-
-// 16 bytes a lane from the buffer `rsrc` at byte offset `off` into 1,024 adjacent
-// bytes of LDS.  As an instruction of its own, since the compiler would make
-// every later transposing LDS read wait for a load that it knows of; the waits
-// are wait_and_meet's.  It writes no register and leaves m0 as it was.
-__device__ __forceinline__ void load_to_lds(char* lds, uint32_t off, u32x4_t rsrc) {
-  const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
-  uint32_t m0;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\t"
-      "buffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
-      : "=&s"(m0)
-      : "s"(to), "v"(off), "s"(rsrc));
 }
 
 // Waits until at most N of the wave's loads into LDS are on their way and its LDS
@@ -108,10 +95,7 @@ struct GemmTile {
 
   // The i-th load of the next 64 k, all in the matrix, into `lds`; then next().
   __device__ __forceinline__ void load(char* lds, int i, int wave) const {
-    const uint64_t base = (uint64_t)at;
-    // base, no stride, no bound (every offset is in the matrix by construction)
-    const u32x4_t rsrc = {(uint32_t)base, (uint32_t)(base >> 32) & 0xFFFFu, 0xFFFFFFFFu, 0x00027000u};
-    load_to_lds(lds + (i * WAVES + wave) * 1024, off[i], rsrc);
+    load_to_lds<false>(lds + (i * WAVES + wave) * 1024, off[i], buffer_at(at));
   }
   __device__ __forceinline__ void next() { at += step; }
 

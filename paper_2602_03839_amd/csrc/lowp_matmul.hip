@@ -22,6 +22,7 @@
 // masked.
 #include "device_common.hpp"
 #include "head.hpp"
+#include "lds_load.hpp"
 
 namespace pulse {
 
@@ -291,168 +292,169 @@ struct __attribute__((packed)) Bytes4 {
   uint32_t w;
 };
 
-// A tile's parts added by one wave; the waves take turns.  `part` is free again
-// after the next tile's barrier, so callers alternate between two.
-__device__ __forceinline__ void join_parts(const LowpMatmulParams& p, bool mx, f32x4_t* part, f32x4_t acc,
-                                           uint32_t turn, uint32_t t, uint32_t tile) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  part[wave * 64 + lane] = acc;
-  __syncthreads();
-  if ((int)(turn % waves) != wave) return;
-  f32x4_t v = part[lane];
-#pragma unroll 5
-  for (int w = 1; w < waves; ++w) v += part[w * 64 + lane];
-  store_result(p, mx, v, t, (uint64_t)tile * 16 + 4 * (lane >> 4));
-}
+// ---------------------------------------------------------------- up to 16 tokens
+//
+// Codes through LDS.  A lane of the matrix instruction has its own row, so loading
+// codes where they are used reads 16 rows, 64 bytes of each, at a time: 4.4 to
+// 5.4 TB/s here.  Read as pieces of 256 bytes and marked as read once, the same
+// weight streams at 6.8 to 6.9.  So a wave loads a slab, 16 rows by 256 bytes,
+// into LDS of its own and reads it back by rows.  No barrier is needed for that:
+// each wave waits for its own loads and has up to `depth` slabs on their way, over
+// the ends of tiles.
+//
+// In a slab, unit 4 g + s of a row (16 bytes of codes) belongs to lane group g,
+// so that a lane's four scales are adjacent too.  Unit u of row r lies at place
+// u ^ r: the 16 rows that are read at one u are then in different banks.
+constexpr uint32_t kSlabUnits = 16;
+constexpr uint32_t kSlabBytes = 16 * kSlabUnits * 16 + 256;  // codes, then scales
 
-// A lane's codes of one chunk of row `row`: its unit, and its scale byte.
-template <bool MX>
-struct ChunkCodes {
-  uint4 c;
-  uint32_t scale;
+struct SlabShape {
+  uint32_t tiles, slabs;   // of 16 rows; of a row
+  uint32_t wk, wr, depth;  // waves side by side in k, in rows; slabs ahead
+  uint32_t run;            // groups of wr tiles that a block takes in a row
 };
 
-// Always a load, so that nothing branches on the way: a row past the last is the
-// last, and a unit past the row's end its last unit, with a finite scale; the
-// tokens' values there are zeros.
 template <bool MX>
-__device__ __forceinline__ void load_codes(const LowpMatmulParams& p, uint32_t row, uint32_t units, uint32_t u,
-                                           ChunkCodes<MX>& q) {
-  if (row >= p.rows) row = p.rows - 1;
-  const bool in = u < units;
-  const uint64_t unit = (uint64_t)row * units + (in ? u : units - 1);
-  q.c = load16_any(p.codes + unit * 16);
-  if constexpr (MX) {
-    const uint32_t scale = p.scales[unit];
-    q.scale = in ? scale : 127u;
+struct SlabStream {
+  const LowpMatmulParams& p;
+  const SlabShape& z;
+  char* ring;
+  uint32_t units, kw, rw, lane;
+  uint32_t group, slab, slot = 0;  // of the next load
+  int flying = 0;
+
+  // The block's next group of tiles: `run` adjacent ones, so that their results'
+  // lines are completed in one L2, then the next blocks' runs are passed over.
+  __device__ __forceinline__ uint32_t after(uint32_t at) const {
+    return (at + 1) % z.run ? at + 1 : at + 1 + (gridDim.x - 1) * z.run;
   }
-}
 
-template <bool MX>
-__device__ __forceinline__ f32x4_t multiply_codes(const ChunkCodes<MX>& q, const uint4 (&x)[Unit<MX>::kFrags],
-                                                  f32x4_t acc) {
-  const float scale = MX ? __uint_as_float(q.scale << 23) : 1.0f;
+  __device__ __forceinline__ void load() {
+    const uint32_t tile = group * z.wr + rw < z.tiles ? group * z.wr + rw : z.tiles - 1;
+    const uint32_t row0 = tile * 16, u0 = slab * kSlabUnits;
+    const uint32_t rows = p.rows - row0 < 16 ? p.rows - row0 : 16;
+    const uint32_t left = units - u0 < kSlabUnits ? units - u0 : kSlabUnits;
+    const uint64_t first = (uint64_t)row0 * units + u0;
+    char* const to = ring + slot * kSlabBytes;
+    const u32x4_t codes = buffer_at(p.codes + first * 16);
 #pragma unroll
-  for (uint32_t f = 0; f < Unit<MX>::kFrags; ++f)
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<MX>(q.c, f, scale), __builtin_bit_cast(bf16x8_t, x[f]),
-                                                  acc, 0, 0, 0);
-  return acc;
-}
+    for (int i = 0; i < 4; ++i) {
+      // what lies past the last row or the row's end is read from before it
+      uint32_t r = i * 4 + (lane >> 4), u = (lane & 15) ^ r;
+      r = r < rows ? r : rows - 1;
+      u = u < left ? u : left - 1;
+      load_to_lds<true>(to + i * 1024, (r * units + u) * 16, codes);
+    }
+    if constexpr (MX) {
+      uint32_t r = lane >> 2, u = (lane & 3) * 4;
+      r = r < rows ? r : rows - 1;
+      u = u < left ? u : left - 4;
+      load4_to_lds(to + 4096, r * units + u, buffer_at(p.scales + first));
+    }
+    slot = slot + 1 == z.depth ? 0 : slot + 1;
+    ++flying;
+    slab += z.wk;
+    if (slab >= z.slabs) {
+      slab = kw;
+      group = after(group);
+    }
+  }
+  __device__ __forceinline__ bool more() const { return group * z.wr < z.tiles; }
 
-// Up to 16 tokens whose values fit LDS.  The block's waves share a row tile: they take
-// pairs of chunks in turn (a pair is 128 bytes of each row, a whole line).  Each wave
-// has the codes of its next kAheadPairs pairs on their way, over the ends of tiles,
-// and reads the tokens' values of a chunk when it gets there.
-constexpr int kAheadPairs = 4;
+  // Waits until the oldest slab has landed.
+  __device__ __forceinline__ void wait() {
+    constexpr int kLoads = MX ? 5 : 4;
+    if (flying >= 4) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * kLoads) : "memory");
+    else if (flying == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
+    else if (flying == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    --flying;
+  }
+};
 
-template <bool MX>
-__global__ __launch_bounds__(1024) void lowp_lds_kernel(LowpMatmulParams p, uint32_t tiles, uint32_t pairs) {
+// XREG: each wave has one slab of k for good (slabs <= wk) and the tokens' values of
+// it in registers; otherwise all tokens' values lie in LDS.
+template <bool MX, bool XREG>
+__global__ __launch_bounds__(XREG ? 768 : 1024) void lowp_slab_kernel(LowpMatmulParams p, SlabShape z) {
   typedef Unit<MX> U;
-  extern __shared__ f32x4_t s_part[];  // [2][waves][64], then the tokens' rows
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int r16 = lane & 15, g = lane >> 4;
+  extern __shared__ char s_lds[];  // waves' slabs, [2][waves][64] parts, the tokens' rows
+  const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t waves = z.wk * z.wr, kw = wave % z.wk, rw = wave / z.wk;
+  const uint32_t r16 = lane & 15, g = lane >> 4;
   const uint32_t units = p.cols / U::kValues;
-  // bytes of a token's row, zeros from its end to the pair's; the 16 move each
-  // row to other banks
-  const uint32_t ld = pairs * U::kChunk * 4 + 16;
+  const uint32_t t = r16 < p.tokens ? r16 : p.tokens - 1;
+  f32x4_t* const s_part = (f32x4_t*)(s_lds + waves * z.depth * kSlabBytes);
   char* const s_x = (char*)(s_part + 2 * waves * 64);
+  // bytes of a token's row in LDS, zeros from its end to the slab's; the 16 move each
+  // row to other banks
+  const uint32_t ld = z.slabs * kSlabUnits * U::kValues * 2 + 16;
 
-  // where the wave's loads are, ahead of its products
-  uint32_t load_tile = blockIdx.x, load_pair = wave;
-  ChunkCodes<MX> q[kAheadPairs][2];
-  auto fetch = [&](ChunkCodes<MX> (&to)[2]) {
-    if (load_tile >= tiles) return;
+  uint4 x[4][U::kFrags];
+  if constexpr (XREG) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      load_codes<MX>(p, load_tile * 16 + r16, units, (load_pair * 2 + h) * kLpGroups + g, to[h]);
-    load_pair += waves;
-    if (load_pair >= pairs) {
-      load_pair = wave;
-      load_tile += gridDim.x;
+    for (int s = 0; s < 4; ++s) {
+      const uint32_t u = kw * kSlabUnits + g * 4 + s;
+#pragma unroll
+      for (uint32_t f = 0; f < U::kFrags; ++f)
+        x[s][f] = u < units ? load16_any(p.x + t * p.x_stride + (uint64_t)u * U::kValues + 8 * f)
+                            : make_uint4(0, 0, 0, 0);
     }
-  };
-#pragma unroll
-  for (int i = 0; i < kAheadPairs; ++i) fetch(q[i]);
-
-  const uint32_t pieces = pairs * U::kChunk / 4, filled = p.cols / 8;  // of 16 bytes, in a row
-  for (uint32_t i = threadIdx.x; i < p.tokens * pieces; i += blockDim.x) {
-    const uint32_t t = i / pieces, c = i % pieces;
-    *(uint4*)(s_x + t * ld + c * 16) = c < filled ? load16_any(p.x + t * p.x_stride + c * 8) : make_uint4(0, 0, 0, 0);
   }
-  __syncthreads();
-  const char* const mine = s_x + (r16 < (int)p.tokens ? r16 : p.tokens - 1) * ld + g * (U::kValues * 2);
+  SlabStream<MX> in = {p, z, s_lds + wave * z.depth * kSlabBytes, units, kw, rw, lane, blockIdx.x * z.run, kw};
+  for (uint32_t i = 0; i < z.depth && in.more(); ++i) in.load();
+  if constexpr (!XREG) {
+    const uint32_t pieces = (ld - 16) / 16, filled = p.cols / 8;  // of 16 bytes, in a row
+    for (uint32_t i = threadIdx.x; i < p.tokens * pieces; i += blockDim.x) {
+      const uint32_t row = i / pieces, c = i % pieces;
+      *(uint4*)(s_x + row * ld + c * 16) =
+          c < filled ? load16_any(p.x + row * p.x_stride + c * 8) : make_uint4(0, 0, 0, 0);
+    }
+    __syncthreads();
+  }
 
-  uint32_t tile = blockIdx.x, pair = wave, turn = 0;
-  f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (;;) {
+  uint32_t slot = 0, turn = 0;
+  for (uint32_t group = blockIdx.x * z.run; group * z.wr < z.tiles; group = in.after(group), ++turn) {
+    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t slab = kw; slab < z.slabs; slab += z.wk) {
+      in.wait();
+      const char* const from = in.ring + slot * kSlabBytes;
+      slot = slot + 1 == z.depth ? 0 : slot + 1;
+      uint4 c[4];
 #pragma unroll
-    for (int i = 0; i < kAheadPairs; ++i) {
+      for (int s = 0; s < 4; ++s) c[s] = *(const uint4*)(from + r16 * 256 + (((g * 4 + s) ^ r16) << 4));
+      uint32_t scales = 0;
+      if constexpr (MX) scales = *(const uint32_t*)(from + 4096 + (r16 * 4 + g) * 4);
+      // the slab is in registers: its place is free for the next load
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      if (in.more()) in.load();
+      // past the row's end the tokens are zeros; the scale has to be finite there
+      if (slab * kSlabUnits + g * 4 >= units) scales = 0x7F7F7F7Fu;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint4 x[U::kFrags];
+      for (int s = 0; s < 4; ++s) {
+        const float scale = MX ? __uint_as_float((scales >> (8 * s) & 255u) << 23) : 1.0f;
 #pragma unroll
-        for (uint32_t f = 0; f < U::kFrags; ++f)
-          x[f] = *(const uint4*)(mine + (pair * 2 + h) * (U::kChunk * 2) + f * 16);
-        acc = multiply_codes<MX>(q[i][h], x, acc);
+        for (uint32_t f = 0; f < U::kFrags; ++f) {
+          uint4 v;
+          if constexpr (XREG) v = x[s][f];
+          else v = *(const uint4*)(s_x + t * ld + (slab * kSlabUnits + g * 4 + s) * (U::kValues * 2) + f * 16);
+          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<MX>(c[s], f, scale), __builtin_bit_cast(bf16x8_t, v),
+                                                        acc, 0, 0, 0);
+        }
       }
-      fetch(q[i]);
-      pair += waves;
-      if (pair >= pairs) {
-        join_parts(p, MX, s_part + (turn & 1) * waves * 64, acc, turn, r16, tile);
-        acc = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        pair = wave;
-        tile += gridDim.x;
-        ++turn;
-        if (tile >= tiles) return;
-      }
     }
-  }
-}
-
-// Up to 16 tokens, in registers: wave w of a block owns the chunks w S ... w S + S - 1
-// of k for as long as it runs, and the block goes through row tiles, the next two
-// tiles' codes on their way.  The waves of a block together read whole rows, 16 of
-// them adjacent; nothing but codes and scales is loaded in the loop.
-template <bool MX, int S, int AHEAD>
-__global__ __launch_bounds__(768) void lowp_sweep_kernel(LowpMatmulParams p, uint32_t tiles) {
-  typedef Unit<MX> U;
-  extern __shared__ f32x4_t s_part[];  // [2][waves][64]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int r16 = lane & 15, g = lane >> 4;
-  const uint32_t units = p.cols / U::kValues;  // of a row
-  const uint32_t t = blockIdx.y * 16 + r16;
-  const uint16_t* const xrow = p.x + (uint64_t)(t < p.tokens ? t : p.tokens - 1) * p.x_stride;
-
-  uint4 x[S][U::kFrags];
-#pragma unroll
-  for (int s = 0; s < S; ++s) {
-    const uint32_t u = (wave * S + s) * kLpGroups + g;
-#pragma unroll
-    for (uint32_t f = 0; f < U::kFrags; ++f)
-      x[s][f] = u < units ? load16_any(xrow + (uint64_t)u * U::kValues + 8 * f) : make_uint4(0, 0, 0, 0);
-  }
-  ChunkCodes<MX> q[AHEAD + 1][S];
-  uint32_t last = blockIdx.x;
-  auto fetch = [&](ChunkCodes<MX> (&to)[S], uint32_t tile) {
-    if (tile < tiles) last = tile;  // past the last tile: the same again, unused
-#pragma unroll
-    for (int s = 0; s < S; ++s) load_codes<MX>(p, last * 16 + r16, units, (wave * S + s) * kLpGroups + g, to[s]);
-  };
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i) fetch(q[i], blockIdx.x + i * gridDim.x);
-  uint32_t tile = blockIdx.x, turn = 0;
-  while (tile < tiles) {
-#pragma unroll
-    for (int i = 0; i < AHEAD + 1; ++i) {
-      if (tile >= tiles) break;
-      fetch(q[(i + AHEAD) % (AHEAD + 1)], tile + AHEAD * gridDim.x);
-      f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int s = 0; s < S; ++s) acc = multiply_codes<MX>(q[i][s], x[s], acc);
-      join_parts(p, MX, s_part + (turn & 1) * waves * 64, acc, turn, t, tile);
-      ++turn;
-      tile += gridDim.x;
+    const uint32_t tile = group * z.wr + rw;
+    if (z.wk > 1) {
+      // the parts of a tile are added by one of its waves, in turn; they are free again
+      // after the next barrier but one
+      f32x4_t* const part = s_part + (turn & 1) * waves * 64;
+      part[wave * 64 + lane] = acc;
+      __syncthreads();
+      if (turn % z.wk != kw) continue;
+      acc = part[rw * z.wk * 64 + lane];
+#pragma unroll 5
+      for (uint32_t w = 1; w < z.wk; ++w) acc += part[(rw * z.wk + w) * 64 + lane];
     }
+    if (tile < z.tiles) store_result(p, MX, acc, r16, (uint64_t)tile * 16 + 4 * g);
   }
 }
 
@@ -473,40 +475,53 @@ void launch_shape(const LowpMatmulParams& p, hipStream_t stream) {
 }
 
 constexpr uint32_t kLpCus = 256;
+constexpr uint32_t kLpLds = 160 * 1024;
 
-// Whether 16 tokens or fewer fit LDS beside the parts of 16 waves.
-bool tokens_fit(const LowpMatmulParams& p, uint64_t row_bytes) {
-  return p.tokens <= 16 && p.tokens * (row_bytes + 16) <= 128 * 1024;
-}
-
+// Up to 16 tokens by slabs; false where that does not fit: rows that are not whole
+// groups of four units, other alignment, or too many values of the tokens.
 template <bool MX>
-void launch_lds(const LowpMatmulParams& p, uint32_t chunks, hipStream_t stream) {
-  const uint32_t tiles = (p.rows + 15) / 16, pairs = (chunks + 1) / 2;
-  // as many waves as give each the same number of pairs, and blocks the same of tiles
-  const uint32_t each = (pairs + 15) / 16, waves = (pairs + each - 1) / each;
-  const uint32_t rounds = (tiles + 2 * kLpCus - 1) / (2 * kLpCus), blocks = (tiles + rounds - 1) / rounds;
-  const size_t lds = (size_t)2 * waves * 64 * sizeof(f32x4_t) + (size_t)p.tokens * (pairs * Unit<MX>::kChunk * 4 + 16);
-  hipLaunchKernelGGL(lowp_lds_kernel<MX>, dim3(blocks), dim3(64 * waves), lds, stream, p, tiles, pairs);
-}
-
-template <bool MX, int S, int AHEAD>
-void launch_sweep(const LowpMatmulParams& p, uint32_t chunks, hipStream_t stream) {
-  const uint32_t tiles = (p.rows + 15) / 16, waves = (chunks + S - 1) / S;
-  hipLaunchKernelGGL((lowp_sweep_kernel<MX, S, AHEAD>), dim3(tiles < kLpCus ? tiles : kLpCus, (p.tokens + 15) / 16),
-                     dim3(64 * waves), (size_t)2 * waves * 64 * sizeof(f32x4_t), stream, p, tiles);
+bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
+  typedef Unit<MX> U;
+  if (p.tokens > 16 || p.cols % U::kChunk || ((uintptr_t)p.codes & 15) || (MX && ((uintptr_t)p.scales & 3)))
+    return false;
+  SlabShape z;
+  z.tiles = (p.rows + 15) / 16;
+  z.slabs = (p.cols / U::kValues + kSlabUnits - 1) / kSlabUnits;
+  const uint64_t x_bytes = p.tokens * ((uint64_t)z.slabs * kSlabUnits * U::kValues * 2 + 16);
+  // the tokens in registers where a block's waves cover k; then as many rows of waves
+  // as make twelve
+  const bool xreg = z.slabs <= 12;
+  if (xreg) {
+    z.wk = z.slabs;
+    z.wr = 12 / z.wk;
+    while (z.wr > 1 && z.wr * kLpCus > z.tiles) --z.wr;
+  } else {
+    // as many waves as give each the same number of slabs
+    const uint32_t each = (z.slabs + 11) / 12;
+    z.wk = (z.slabs + each - 1) / each;
+    z.wr = 1;
+  }
+  const uint32_t waves = z.wk * z.wr;
+  const uint64_t rest = (uint64_t)2 * waves * 64 * sizeof(f32x4_t) + (xreg ? 0 : x_bytes);
+  if (rest + waves * kSlabBytes > kLpLds) return false;
+  z.depth = (uint32_t)((kLpLds - rest) / (waves * kSlabBytes));
+  if (z.depth > 4) z.depth = 4;
+  const uint32_t groups = (z.tiles + z.wr - 1) / z.wr;
+  z.run = groups >= 16 * kLpCus ? 2 : 1;
+  const dim3 grid(groups < kLpCus ? groups : kLpCus), block(64 * waves);
+  const size_t lds = (size_t)(rest + (uint64_t)z.depth * waves * kSlabBytes);
+  if (xreg) hipLaunchKernelGGL((lowp_slab_kernel<MX, true>), grid, block, lds, stream, p, z);
+  else hipLaunchKernelGGL((lowp_slab_kernel<MX, false>), grid, block, lds, stream, p, z);
+  return true;
 }
 
 template <bool MX>
 void launch_type(const LowpMatmulParams& p, hipStream_t stream) {
   typedef Unit<MX> U;
   if (p.cols % U::kValues) return launch_shape<MX, 1, 1, true>(p, stream);
-  const uint32_t chunks = (p.cols + U::kChunk - 1) / U::kChunk;
-  if (tokens_fit(p, (uint64_t)(chunks + 1) / 2 * U::kChunk * 4)) return launch_lds<MX>(p, chunks, stream);
-  constexpr int kS = MX ? 4 : 8;
-  if (p.tokens <= 16 && chunks <= 12 * kS) return launch_sweep<MX, kS, MX ? 2 : 1>(p, chunks, stream);
+  if (launch_slabs<MX>(p, stream)) return;
   if (p.tokens <= 16) launch_shape<MX, 1, 1, false>(p, stream);
-  else if (p.tokens <= 32) launch_shape<MX, 2, 2, false>(p, stream);
-  else launch_shape<MX, 2, 4, false>(p, stream);
+  else launch_shape<MX, 2, 2, false>(p, stream);
 }
 
 }  // namespace
