@@ -25,9 +25,20 @@ constexpr bool kIsBf16 = std::is_same<T, uint16_t>::value;
 __device__ __forceinline__ float from_bits(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 __device__ __forceinline__ float from_bits(float v) { return v; }
 
-__device__ __forceinline__ void load8(const uint16_t* p, float* v) {
-  const uint4 a = load16(p);
-  const uint32_t w[4] = {a.x, a.y, a.z, a.w};
+// 8 elements as they lie in memory, and as FP32.
+template <typename T>
+struct Raw8 {
+  uint4 v[sizeof(T) / 2];
+};
+
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, Raw8<T>& r) {
+#pragma unroll
+  for (size_t i = 0; i < sizeof(T) / 2; ++i) r.v[i] = load16(p + 16 / sizeof(T) * i);
+}
+
+__device__ __forceinline__ void unpack8(const Raw8<uint16_t>& r, float* v) {
+  const uint32_t w[4] = {r.v[0].x, r.v[0].y, r.v[0].z, r.v[0].w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     v[2 * i] = __uint_as_float(w[i] << 16);
@@ -35,11 +46,9 @@ __device__ __forceinline__ void load8(const uint16_t* p, float* v) {
   }
 }
 
-__device__ __forceinline__ void load8(const float* p, float* v) {
-  const uint4 a = load16(p), b = load16(p + 4);
-  const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+__device__ __forceinline__ void unpack8(const Raw8<float>& r, float* v) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+  for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(get_u32(r.v[i / 4], i & 3));
 }
 
 __device__ __forceinline__ void store8(uint16_t* p, const float* v) {
@@ -70,19 +79,39 @@ struct Row {
   static constexpr int kStep = VEC ? 8 : 1;
   static __device__ __forceinline__ uint32_t at(int j, uint32_t t) { return (uint32_t)(j * G + t) * kStep; }
 
+  // a row's elements as they lie in memory, zeros past its end
   template <typename T>
-  static __device__ __forceinline__ void load(const T* p, uint32_t cols, uint32_t t, float (&v)[E]) {
+  struct Raw {
+    typename std::conditional<VEC, Raw8<T>, T>::type v[E / kStep];
+  };
+  template <typename T>
+  static __device__ __forceinline__ void load(const T* p, uint32_t cols, uint32_t t, Raw<T>& r) {
 #pragma unroll
     for (int j = 0; j < E / kStep; ++j) {
       const uint32_t c = at(j, t);
-      if (c < cols) {
-        if constexpr (VEC) load8(p + c, v + 8 * j);
-        else v[j] = from_bits(p[c]);
-      } else {
+      if constexpr (VEC) {
+        if (c < cols) load8(p + c, r.v[j]);
+        else
 #pragma unroll
-        for (int i = 0; i < kStep; ++i) v[kStep * j + i] = 0.0f;
+          for (size_t i = 0; i < sizeof(T) / 2; ++i) r.v[j].v[i] = make_uint4(0, 0, 0, 0);
+      } else {
+        r.v[j] = c < cols ? p[c] : (T)0;
       }
     }
+  }
+  template <typename T>
+  static __device__ __forceinline__ void unpack(const Raw<T>& r, float (&v)[E]) {
+#pragma unroll
+    for (int j = 0; j < E / kStep; ++j) {
+      if constexpr (VEC) unpack8(r.v[j], v + 8 * j);
+      else v[j] = from_bits(r.v[j]);
+    }
+  }
+  template <typename T>
+  static __device__ __forceinline__ void load(const T* p, uint32_t cols, uint32_t t, float (&v)[E]) {
+    Raw<T> r;
+    load(p, cols, t, r);
+    unpack(r, v);
   }
   template <typename T>
   static __device__ __forceinline__ void store(T* p, uint32_t cols, uint32_t t, const float (&v)[E]) {
@@ -163,45 +192,154 @@ __global__ __launch_bounds__(block_of(G)) void norm_kernel(NormParams p) {
   }
 }
 
-template <typename T, int E, int G, bool VEC>
-__global__ __launch_bounds__(block_of(G)) void norm_grad_kernel(NormGradParams p) {
-  typedef Row<E, G, VEC> R;
-  constexpr int kRows = block_of(G) / G;
-  __shared__ float s[2][2][16];
-  const uint32_t t = threadIdx.x % G;
-  const uint64_t first = (uint64_t)blockIdx.x * kRows + threadIdx.x / G;
-  const float inv_n = 1.0f / (float)p.cols;
-  float w[E], dw[E], db[E];
-  R::params(p.weight, p.param_bf16, p.cols, t, w);
+// The G lanes' sums of two values, with one barrier (none for a wave); as for
+// group_sum, callers alternate between two `s`.
+template <int G>
+__device__ __forceinline__ float2 group_sum2(float a, float b, float2* s) {
+  a = wave_sum(a);
+  b = wave_sum(b);
+  if constexpr (G == 64) return make_float2(a, b);
+  const int wave = threadIdx.x >> 6, first = wave & ~(G / 64 - 1);
+  if (lane_id() == 0) s[wave] = make_float2(a, b);
+  __syncthreads();
+  float2 r = make_float2(0.0f, 0.0f);
 #pragma unroll
-  for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.0f;
-  int turn = 0;
-  for (uint64_t row = first; row < p.rows; row += (uint64_t)gridDim.x * kRows, turn ^= 1) {
+  for (int i = 0; i < G / 64; ++i) {
+    r.x += s[first + i].x;
+    r.y += s[first + i].y;
+  }
+  return r;
+}
+
+constexpr int grad_block_of(int g) { return g == 64 ? 256 : g == 256 ? 512 : 1024; }
+
+// Each block has several groups of G lanes and each group a row at a time, the next
+// one's x and dy on their way: a row alone is too little in flight to
+// cover the way to HBM and the sums in between (16,384 x 3,584 in BF16: 119 us
+// without, 67 with).  SUMS: the columns' sums are kept as well.
+template <typename T, int E, int G, bool VEC, bool SUMS>
+__device__ __forceinline__ void grad_rows(const NormGradParams& p, uint64_t first, uint64_t step,
+                                          float (&dw)[E], float (&db)[E]) {
+  typedef Row<E, G, VEC> R;
+  __shared__ float2 s[2][16];
+  const uint32_t t = threadIdx.x % G;
+  const float inv_n = 1.0f / (float)p.cols;
+  float w[E];
+  R::params(p.weight, p.param_bf16, p.cols, t, w);
+  // every group of the block makes the same number of turns: there are barriers
+  const uint64_t turns = first - threadIdx.x / G < p.rows ? (p.rows - (first - threadIdx.x / G) + step - 1) / step : 0;
+  typename R::template Raw<T> nx, ndy;
+  float nrstd = 0.0f, nmean = 0.0f;
+  auto fetch = [&](uint64_t row) {
+    if (row >= p.rows) row = p.rows - 1;
+    R::load((const T*)p.x + row * p.x_stride, p.cols, t, nx);
+    R::load((const T*)p.dy + row * p.dy_stride, p.cols, t, ndy);
+    nrstd = p.rstd[row];
+    nmean = p.mean ? p.mean[row] : 0.0f;
+  };
+  if (turns) fetch(first);
+  for (uint64_t k = 0; k < turns; ++k) {
+    const uint64_t row = first + k * step;
+    const bool valid = row < p.rows;
     float x[E], dy[E];
-    R::load((const T*)p.x + row * p.x_stride, p.cols, t, x);
-    R::load((const T*)p.dy + row * p.dy_stride, p.cols, t, dy);
-    const float rstd = p.rstd[row], mean = p.mean ? p.mean[row] : 0.0f;
+    R::unpack(nx, x);
+    R::unpack(ndy, dy);
+    const float rstd = nrstd, mean = nmean;
+    if (k + 1 < turns) fetch(row + step);
     float sa = 0.0f, sax = 0.0f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      x[e] = (x[e] - mean) * rstd;  // past the row: meets dy = w = 0
-      dw[e] = __builtin_fmaf(dy[e], x[e], dw[e]);
-      db[e] += dy[e];
+      x[e] = (x[e] - mean) * rstd;  // past the row: meets dy = 0
+      if (SUMS && valid) {
+        dw[e] = __builtin_fmaf(dy[e], x[e], dw[e]);
+        db[e] += dy[e];
+      }
       dy[e] *= w[e];
       sa += dy[e];
       sax = __builtin_fmaf(dy[e], x[e], sax);
     }
-    sax = group_sum<G>(sax, s[turn][0]) * inv_n;
-    sa = p.mean ? group_sum<G>(sa, s[turn][1]) * inv_n : 0.0f;
+    const float2 sum = group_sum2<G>(sa, sax, s[k & 1]);
+    sa = p.mean ? sum.x * inv_n : 0.0f;
+    sax = sum.y * inv_n;
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = (dy[e] - sa - x[e] * sax) * rstd;
-    R::store((T*)p.dx + row * p.dx_stride, p.cols, t, x);
+    if (valid) R::store((T*)p.dx + row * p.dx_stride, p.cols, t, x);
   }
-  // one row of sums for each group of lanes
-  const uint64_t mine = first, all = (uint64_t)gridDim.x * kRows;
-  float* out = p.partial + mine * p.cols;
+}
+
+template <typename T, int E, int G, bool VEC>
+__global__ __launch_bounds__(grad_block_of(G)) void norm_grad_kernel(NormGradParams p) {
+  typedef Row<E, G, VEC> R;
+  constexpr int kGroups = grad_block_of(G) / G;
+  __shared__ float s_sum[kGroups > 1 ? G * E : 1];
+  const uint32_t t = threadIdx.x % G, group = threadIdx.x / G;
+  float dw[E], db[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.0f;
+  grad_rows<T, E, G, VEC, true>(p, (uint64_t)blockIdx.x * kGroups + group, (uint64_t)gridDim.x * kGroups, dw, db);
+  // the groups' sums one after the other, then one row of sums for the block
+  if constexpr (kGroups > 1) {
+    for (int what = 0; what < (p.dbias ? 2 : 1); ++what)
+      for (uint32_t k = 1; k < kGroups; ++k) {
+        __syncthreads();
+        if (group == k) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) s_sum[e * G + t] = what ? db[e] : dw[e];
+        }
+        __syncthreads();
+        if (group == 0) {
+#pragma unroll
+          for (int e = 0; e < E; ++e) (what ? db[e] : dw[e]) += s_sum[e * G + t];
+        }
+      }
+  }
+  if (group != 0) return;
+  float* out = p.partial + (uint64_t)blockIdx.x * p.cols;
   R::store(out, p.cols, t, dw);
-  if (p.dbias) R::store(out + all * p.cols, p.cols, t, db);
+  if (p.dbias) R::store(out + (uint64_t)gridDim.x * p.cols, p.cols, t, db);
+}
+
+// Few rows: one launch, whose blocks past the first `row_blocks` sum kStrip columns
+// each over all rows, a wave 8 rows at a time.  mean and rstd are given, so these
+// sums need nothing of the other blocks; x and dy are read twice, the second time
+// from a cache.
+constexpr int kStrip = 8;
+
+constexpr int few_block_of(int g) { return g == 1024 ? 1024 : 512; }
+
+template <typename T, int E, int G, bool VEC>
+__global__ __launch_bounds__(few_block_of(G)) void norm_grad_few_kernel(NormGradParams p, uint32_t row_blocks) {
+  constexpr int kBlock = few_block_of(G), kGroups = kBlock / G;
+  if (blockIdx.x < row_blocks) {
+    float none[E];
+    grad_rows<T, E, G, VEC, false>(p, (uint64_t)blockIdx.x * kGroups + threadIdx.x / G,
+                                   (uint64_t)row_blocks * kGroups, none, none);
+    return;
+  }
+  constexpr uint32_t kRows = kBlock / kStrip;
+  __shared__ float s[2][kBlock];
+  const uint32_t c = (blockIdx.x - row_blocks) * kStrip + threadIdx.x % kStrip, r0 = threadIdx.x / kStrip;
+  float dw = 0.0f, db = 0.0f;
+  if (c < p.cols) {
+#pragma unroll 8
+    for (uint32_t r = r0; r < (uint32_t)p.rows; r += kRows) {
+      const float dy = from_bits(((const T*)p.dy)[r * p.dy_stride + c]);
+      const float x = from_bits(((const T*)p.x)[r * p.x_stride + c]);
+      dw = __builtin_fmaf(dy, (x - (p.mean ? p.mean[r] : 0.0f)) * p.rstd[r], dw);
+      db += dy;
+    }
+  }
+  s[0][threadIdx.x] = dw;
+  s[1][threadIdx.x] = db;
+  __syncthreads();
+  if (threadIdx.x >= 2 * kStrip) return;
+  const uint32_t what = threadIdx.x / kStrip, lane = threadIdx.x % kStrip;
+  const uint32_t col = (blockIdx.x - row_blocks) * kStrip + lane;
+  if (col >= p.cols || (what && !p.dbias)) return;
+  float a = 0.0f;
+#pragma unroll 8
+  for (uint32_t k = 0; k < kRows; ++k) a += s[what][k * kStrip + lane];
+  (what ? p.dbias : p.dweight)[col] = a;
 }
 
 // The sums of the n partial rows: 64 columns a block, its 16 waves a slice of
@@ -227,6 +365,8 @@ __global__ __launch_bounds__(1024) void norm_columns_kernel(const float* partial
     (blockIdx.y ? dbias : dweight)[c] = a;
   }
 }
+
+constexpr uint64_t kNormFewRows = 1280;
 
 template <typename F>
 void by_shape(uint32_t cols, F f) {
@@ -263,24 +403,31 @@ hipError_t launch_layer_norm(bool bf16, const NormParams& p, hipStream_t stream)
 
 hipError_t launch_layer_norm_grad(bool bf16, const NormGradParams& p, hipStream_t stream) {
   const bool vec = p.cols % 8 == 0 && p.x_stride % 8 == 0 && p.dy_stride % 8 == 0 && p.dx_stride % 8 == 0;
+  // one launch for few rows: the second one costs its 3 us on the host and as much
+  // again on the GPU, a strip of columns 0.5 us for every 128 rows
+  const bool few = p.rows > 0 && p.rows <= kNormFewRows;
   uint32_t sums = 0;
   by_shape(p.cols, [&](auto e, auto g) {
     constexpr int E = decltype(e)::value, G = decltype(g)::value;
-    constexpr uint32_t kRows = block_of(G) / G;
-    uint64_t blocks = (p.rows + kRows - 1) / kRows;
-    if (blocks > kNormBlocks / kRows) blocks = kNormBlocks / kRows;
-    sums = (uint32_t)blocks * kRows;
+    const uint32_t size = few ? few_block_of(G) : grad_block_of(G), groups = size / G;
+    uint64_t blocks = (p.rows + groups - 1) / groups;
+    if (blocks > kNormBlocks) blocks = kNormBlocks;
+    sums = (uint32_t)blocks;
     if (blocks == 0) return;
-    const dim3 block(block_of(G)), grid((uint32_t)blocks);
-    if (bf16) {
-      if (vec) hipLaunchKernelGGL((norm_grad_kernel<uint16_t, E, G, true>), grid, block, 0, stream, p);
-      else hipLaunchKernelGGL((norm_grad_kernel<uint16_t, E, G, false>), grid, block, 0, stream, p);
-    } else {
-      if (vec) hipLaunchKernelGGL((norm_grad_kernel<float, E, G, true>), grid, block, 0, stream, p);
-      else hipLaunchKernelGGL((norm_grad_kernel<float, E, G, false>), grid, block, 0, stream, p);
-    }
+    const dim3 block(size), grid((uint32_t)blocks + (few ? (p.cols + kStrip - 1) / kStrip : 0));
+    auto run = [&](auto type, auto v) {
+      typedef decltype(type) T;
+      constexpr bool V = decltype(v)::value;
+      if (few) hipLaunchKernelGGL((norm_grad_few_kernel<T, E, G, V>), grid, block, 0, stream, p, (uint32_t)blocks);
+      else hipLaunchKernelGGL((norm_grad_kernel<T, E, G, V>), grid, block, 0, stream, p);
+    };
+    if (bf16 && vec) run(uint16_t{}, std::true_type{});
+    else if (bf16) run(uint16_t{}, std::false_type{});
+    else if (vec) run(float{}, std::true_type{});
+    else run(float{}, std::false_type{});
   });
   if (hipError_t e = hipGetLastError()) return e;
+  if (few) return hipSuccess;
   hipLaunchKernelGGL(norm_columns_kernel, dim3((p.cols + 63) / 64, p.dbias ? 2 : 1), dim3(1024), 0,
                      stream, p.partial, sums, p.cols, p.dweight, p.dbias);
   return hipGetLastError();

@@ -74,6 +74,15 @@ def _dtype(t: torch.Tensor, name: str) -> int:
 
 def _matrix(t: torch.Tensor, name: str, cols: int, rows: Optional[int] = None, dtype=None, device=None):
     """(pointer, row stride) of a device matrix whose rows are adjacent elements."""
+    # one chain of cheap tests, as in pulse._p; a failing one is named below
+    if isinstance(t, torch.Tensor) and t.dim() == 2 and t.is_cuda:
+        r, c = t.shape
+        if (c == cols and (rows is None or r == rows) and (dtype is None or t.dtype is dtype)
+                and (device is None or t.device == device)):
+            if t.is_contiguous():
+                return t.data_ptr(), cols
+            if t.stride(1) == 1 and t.stride(0) >= cols:
+                return t.data_ptr(), t.stride(0)
     if not isinstance(t, torch.Tensor):
         raise PulseError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
     if not t.is_cuda:
@@ -85,11 +94,8 @@ def _matrix(t: torch.Tensor, name: str, cols: int, rows: Optional[int] = None, d
         raise PulseError(f"{name} must be {dtype}, got {t.dtype}")
     if device is not None and t.device != device:
         raise PulseError(f"{name} is on {t.device}, the call's other tensors on {device}")
-    stride = t.stride(0) if t.shape[0] > 1 else cols
-    if (cols > 1 and t.stride(1) != 1) or stride < cols:
-        raise PulseError(f"{name} must have rows of adjacent elements that do not overlap "
-                         f"(strides {t.stride()})")
-    return t.data_ptr(), stride
+    raise PulseError(f"{name} must have rows of adjacent elements that do not overlap "
+                     f"(strides {t.stride()})")
 
 
 def _new(shape, dtype, device, stream):
@@ -98,6 +104,22 @@ def _new(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _out(t, name, cols, rows, dtype, device, stream):
+    """A matrix to write: the caller's, checked, or a new one; with pointer and row stride."""
+    if t is None:
+        t = _new((rows, cols), dtype, device, stream)
+        return t, t.data_ptr(), cols
+    return (t, *_matrix(t, name, cols, rows, dtype, device))
+
+
+def _vec(t, name, n, device, stream):
+    """A float32 vector to write: the caller's, checked, or a new one; with its pointer."""
+    if t is None:
+        t = _new((n,), torch.float32, device, stream)
+        return t, t.data_ptr()
+    return t, _f32(t, name, n, device)
 
 
 class LayerNorm:
@@ -111,35 +133,29 @@ class LayerNorm:
                  eps: float = 1e-6, rms: bool = False):
         self._dt = _dtype(weight, "weight")
         self.device, self.cols = weight.device, weight.numel()
-        _p(weight, "weight", optional=False)
-        _p(bias, "bias", dtype=weight.dtype, numel=self.cols, device=self.device)
+        self._pw = _p(weight, "weight", optional=False)
+        self._pb = _p(bias, "bias", dtype=weight.dtype, numel=self.cols, device=self.device)
         if not 1 <= self.cols <= NORM_MAX_COLS:
             raise PulseError(f"weight has {self.cols} elements, 1 to {NORM_MAX_COLS} are handled")
         self.weight, self.bias, self.eps, self.rms = weight, bias, float(eps), bool(rms)
-        self.ws = torch.empty(int(lib().pulse_layer_norm_workspace_bytes(self.cols)),
-                              dtype=torch.uint8, device=self.device)
+        self._flags, self._lib = NORM_RMS if rms else 0, lib()
+        self._nws = int(self._lib.pulse_layer_norm_workspace_bytes(self.cols))
+        self.ws = torch.empty(self._nws, dtype=torch.uint8, device=self.device)
+        self._pws = self.ws.data_ptr()
 
     def __call__(self, x: torch.Tensor, y: Optional[torch.Tensor] = None,
                  mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None):
         """(y, mean, rstd) of x [rows, cols]; mean is None for the RMS form."""
-        dev, dt = self.device, _dtype(x, "x")
-        px, sx = _matrix(x, "x", self.cols, device=dev)
+        dev, cols, dt = self.device, self.cols, _dtype(x, "x")
+        px, sx = _matrix(x, "x", cols, device=dev)
         rows = x.shape[0]
-        if y is None:
-            y = _new((rows, self.cols), x.dtype, dev, stream)
-        py, sy = _matrix(y, "y", self.cols, rows, x.dtype, dev)
-        if self.rms:
-            mean = None
-        elif mean is None:
-            mean = _new((rows,), torch.float32, dev, stream)
-        if rstd is None:
-            rstd = _new((rows,), torch.float32, dev, stream)
-        _check(lib().pulse_layer_norm_forward(
-            dt, px, sx, self._dt, self.weight.data_ptr(),
-            None if self.bias is None else self.bias.data_ptr(), py, sy,
-            _f32(mean, "mean", rows, dev, optional=True), _f32(rstd, "rstd", rows, dev), rows,
-            self.cols, self.eps, NORM_RMS if self.rms else 0, _stream(stream, dev)),
-            "pulse_layer_norm_forward")
+        y, py, sy = _out(y, "y", cols, rows, x.dtype, dev, stream)
+        mean, pm = (None, None) if self.rms else _vec(mean, "mean", rows, dev, stream)
+        rstd, pr = _vec(rstd, "rstd", rows, dev, stream)
+        rc = self._lib.pulse_layer_norm_forward(dt, px, sx, self._dt, self._pw, self._pb, py, sy, pm, pr,
+                                                rows, cols, self.eps, self._flags, _stream(stream, dev))
+        if rc:
+            _check(rc, "pulse_layer_norm_forward")
         return y, mean, rstd
 
     def backward(self, dy: torch.Tensor, x: torch.Tensor, mean: Optional[torch.Tensor],
@@ -148,26 +164,20 @@ class LayerNorm:
                  stream=None):
         """(dx, dweight, dbias) for the upstream gradient dy and the forward
         pass's x, mean and rstd; dbias is None where there is no bias."""
-        dev, dt = self.device, _dtype(x, "x")
-        px, sx = _matrix(x, "x", self.cols, device=dev)
+        dev, cols, dt = self.device, self.cols, _dtype(x, "x")
+        px, sx = _matrix(x, "x", cols, device=dev)
         rows = x.shape[0]
-        pdy, sdy = _matrix(dy, "dy", self.cols, rows, x.dtype, dev)
-        if dx is None:
-            dx = _new((rows, self.cols), x.dtype, dev, stream)
-        pdx, sdx = _matrix(dx, "dx", self.cols, rows, x.dtype, dev)
-        if dweight is None:
-            dweight = _new((self.cols,), torch.float32, dev, stream)
-        if self.bias is None:
-            dbias = None
-        elif dbias is None:
-            dbias = _new((self.cols,), torch.float32, dev, stream)
-        _check(lib().pulse_layer_norm_backward(
-            dt, pdy, sdy, px, sx, self._dt, self.weight.data_ptr(),
-            None if self.rms else _f32(mean, "mean", rows, dev), _f32(rstd, "rstd", rows, dev), pdx,
-            sdx, _f32(dweight, "dweight", self.cols, dev),
-            _f32(dbias, "dbias", self.cols, dev, optional=True), rows, self.cols,
-            NORM_RMS if self.rms else 0, self.ws.data_ptr(), self.ws.numel(), _stream(stream, dev)),
-            "pulse_layer_norm_backward")
+        pdy, sdy = _matrix(dy, "dy", cols, rows, x.dtype, dev)
+        pm = None if self.rms else _f32(mean, "mean", rows, dev)
+        pr = _f32(rstd, "rstd", rows, dev)
+        dx, pdx, sdx = _out(dx, "dx", cols, rows, x.dtype, dev, stream)
+        dweight, pdw = _vec(dweight, "dweight", cols, dev, stream)
+        dbias, pdb = (None, None) if self.bias is None else _vec(dbias, "dbias", cols, dev, stream)
+        rc = self._lib.pulse_layer_norm_backward(dt, pdy, sdy, px, sx, self._dt, self._pw, pm, pr, pdx, sdx,
+                                                 pdw, pdb, rows, cols, self._flags, self._pws, self._nws,
+                                                 _stream(stream, dev))
+        if rc:
+            _check(rc, "pulse_layer_norm_backward")
         return dx, dweight, dbias
 
 
@@ -189,8 +199,11 @@ class LinearCE:
         if not 0 <= max_tokens < 1 << 31:
             raise PulseError(f"max_tokens {max_tokens} is out of range")
         self.weight, self.max_tokens, self.logit_scale = weight, max_tokens, float(logit_scale)
-        need = lib().pulse_linear_ce_workspace_bytes(max_tokens, self.vocab, self.hidden)
-        self.ws = torch.empty(max(int(need), 1), dtype=torch.uint8, device=self.device)
+        self._lib, self._pw = lib(), weight.data_ptr()
+        need = int(self._lib.pulse_linear_ce_workspace_bytes(max_tokens, self.vocab, self.hidden))
+        self._nws = max(need, 1)
+        self.ws = torch.empty(self._nws, dtype=torch.uint8, device=self.device)
+        self._pws = self.ws.data_ptr()
 
     def _tokens(self, x, targets):
         px, sx = _matrix(x, "x", self.hidden, dtype=torch.bfloat16, device=self.device)
@@ -206,15 +219,13 @@ class LinearCE:
         a target outside [0, vocab) is ignored and has loss 0."""
         dev = self.device
         px, sx, pt, n = self._tokens(x, targets)
-        if loss is None:
-            loss = _new((n,), torch.float32, dev, stream)
-        if lse is None:
-            lse = _new((n,), torch.float32, dev, stream)
-        _check(lib().pulse_linear_ce_forward(px, sx, self.weight.data_ptr(), pt, n, self.vocab,
-                                             self.hidden, self.logit_scale, _f32(loss, "loss", n, dev),
-                                             _f32(lse, "lse", n, dev), self.ws.data_ptr(),
-                                             self.ws.numel(), _stream(stream, dev)),
-               "pulse_linear_ce_forward")
+        loss, pl = _vec(loss, "loss", n, dev, stream)
+        lse, ps = _vec(lse, "lse", n, dev, stream)
+        rc = self._lib.pulse_linear_ce_forward(px, sx, self._pw, pt, n, self.vocab, self.hidden,
+                                               self.logit_scale, pl, ps, self._pws, self._nws,
+                                               _stream(stream, dev))
+        if rc:
+            _check(rc, "pulse_linear_ce_forward")
         return loss, lse
 
     def backward(self, x: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor,
@@ -224,18 +235,17 @@ class LinearCE:
         each token's loss and the forward pass's lse."""
         dev = self.device
         px, sx, pt, n = self._tokens(x, targets)
-        if dx is None:
-            dx = _new((n, self.hidden), torch.bfloat16, dev, stream)
-        pdx, sdx = _matrix(dx, "dx", self.hidden, n, torch.bfloat16, dev)
+        ps, pd = _f32(lse, "lse", n, dev), _f32(dloss, "dloss", n, dev)
+        dx, pdx, sdx = _out(dx, "dx", self.hidden, n, torch.bfloat16, dev, stream)
         if dweight is None:
             dweight = _new((self.vocab, self.hidden), torch.bfloat16, dev, stream)
         pdw = _p(dweight, "dweight", dtype=torch.bfloat16, numel=self.vocab * self.hidden, device=dev,
                  optional=False)
-        _check(lib().pulse_linear_ce_backward(px, sx, self.weight.data_ptr(), pt, n, self.vocab,
-                                              self.hidden, self.logit_scale, _f32(lse, "lse", n, dev),
-                                              _f32(dloss, "dloss", n, dev), pdx, sdx, pdw,
-                                              self.ws.data_ptr(), self.ws.numel(), _stream(stream, dev)),
-               "pulse_linear_ce_backward")
+        rc = self._lib.pulse_linear_ce_backward(px, sx, self._pw, pt, n, self.vocab, self.hidden,
+                                                self.logit_scale, ps, pd, pdx, sdx, pdw, self._pws,
+                                                self._nws, _stream(stream, dev))
+        if rc:
+            _check(rc, "pulse_linear_ce_backward")
         return dx, dweight
 
 
@@ -251,18 +261,25 @@ class LowpLinear:
         self._scales = _p(scales, "scales", esize=1, min_numel=ns, device=self.device,
                           optional=dtype != pulse.MXFP4)
         self.dtype, self.rows, self.cols, self.inv_scale = dtype, rows, cols, float(inv_scale)
-        self.keep = (codes, scales)
+        self.keep, self._lib = (codes, scales), lib()
 
     def __call__(self, x: torch.Tensor, out: Optional[torch.Tensor] = None,
                  out_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
         """x W^T for BF16 x [tokens, cols]: [tokens, rows], float32 or bfloat16."""
         dev = self.device
         px, sx = _matrix(x, "x", self.cols, dtype=torch.bfloat16, device=dev)
+        n = x.shape[0]
         if out is None:
-            out = _new((x.shape[0], self.rows), out_dtype, dev, stream)
-        dt = _dtype(out, "out")
-        py, sy = _matrix(out, "out", self.rows, x.shape[0], device=dev)
-        _check(lib().pulse_lowp_matmul(self.dtype, self._codes, self._scales, self.inv_scale, self.rows,
-                                       self.cols, px, sx, x.shape[0], dt, py, sy,
-                                       _stream(stream, dev)), "pulse_lowp_matmul")
+            dt = _DTYPES.get(out_dtype)
+            if dt is None:
+                raise PulseError(f"out_dtype must be float32 or bfloat16, got {out_dtype}")
+            out = _new((n, self.rows), out_dtype, dev, stream)
+            py, sy = out.data_ptr(), self.rows
+        else:
+            dt = _dtype(out, "out")
+            py, sy = _matrix(out, "out", self.rows, n, device=dev)
+        rc = self._lib.pulse_lowp_matmul(self.dtype, self._codes, self._scales, self.inv_scale, self.rows,
+                                         self.cols, px, sx, n, dt, py, sy, _stream(stream, dev))
+        if rc:
+            _check(rc, "pulse_lowp_matmul")
         return out
