@@ -94,8 +94,9 @@ struct GemmTile {
   }
 
   // The i-th load of the next 64 k, all in the matrix, into `lds`; then next().
+  template <bool STREAM>
   __device__ __forceinline__ void load(char* lds, int i, int wave) const {
-    load_to_lds<false>(lds + (i * WAVES + wave) * 1024, off[i], buffer_at(at));
+    load_to_lds<STREAM>(lds + (i * WAVES + wave) * 1024, off[i], buffer_at(at));
   }
   __device__ __forceinline__ void next() { at += step; }
 
@@ -126,7 +127,7 @@ struct GemmTile {
   }
 };
 
-template <int BM_, int BN_, int WM_, int WN_, bool AK_, bool BK_>
+template <int BM_, int BN_, int WM_, int WN_, bool AK_, bool BK_, bool STREAM_ = false>
 struct Gemm {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
   static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
@@ -200,8 +201,8 @@ struct Gemm {
     };
     auto load = [&](int32_t s, int i) {  // the i-th load of step s, which is whole
       char* to = lds + (s & 1) * kStage;
-      if (i < A::kLoads) la.load(to, i, wave);
-      else lb.load(to + A::kBytes, i - A::kLoads, wave);
+      if (i < A::kLoads) la.template load<STREAM_>(to, i, wave);
+      else lb.template load<false>(to + A::kBytes, i - A::kLoads, wave);
     };
     auto load_step = [&](int32_t s) {  // step s, any
       char* to = lds + (s & 1) * kStage;

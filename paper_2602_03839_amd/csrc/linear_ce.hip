@@ -478,10 +478,10 @@ constexpr uint32_t kFewTokens = 128;  // up to here G's rests are kept for all e
 // Tiles: vocabulary (or hidden) by tokens (or vocabulary), by the tokens' count.
 typedef Gemm<256, 256, 2, 4, false, false> LogitsL;
 typedef Gemm<256, 128, 4, 2, false, false> LogitsM;
-typedef Gemm<256, 64, 4, 1, false, false> LogitsS;
+typedef Gemm<256, 64, 4, 1, false, false, true> LogitsS;
 typedef Gemm<256, 256, 2, 4, true, false> DxL;
 typedef Gemm<256, 128, 4, 2, true, false> DxM;
-typedef Gemm<128, 64, 4, 1, true, false> DxS;
+typedef Gemm<128, 64, 4, 1, true, false, true> DxS;
 typedef Gemm<256, 256, 2, 4, true, true> DwL;
 typedef Gemm<128, 128, 2, 2, true, true> DwS;
 
