@@ -280,16 +280,16 @@ struct Gemm {
 };
 
 // Tile (m, n) of block `id`: each of the 8 XCDs, to which blocks go in turn, gets
-// a run of adjacent tiles, 8 in m by as many in n as are in flight, so that its
-// L2 serves each operand row several times.
-__device__ __forceinline__ void gemm_tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t& m,
-                                             uint32_t& n) {
+// a run of adjacent tiles, `band` of them in m, then on in n, so that its L2 serves
+// each operand row several times.
+__device__ __forceinline__ void gemm_tile_of(uint32_t id, uint32_t tiles_m, uint32_t tiles_n, uint32_t band,
+                                             uint32_t& m, uint32_t& n) {
   const uint32_t all = tiles_m * tiles_n, per = all / 8, rest = all % 8;
   const uint32_t x = id % 8, at = id / 8;
   const uint32_t t = x * per + (x < rest ? x : rest) + at;
-  const uint32_t band = t / (8 * tiles_n), in = t % (8 * tiles_n);
-  const uint32_t high = tiles_m - band * 8 < 8 ? tiles_m - band * 8 : 8;
-  m = band * 8 + in % high;
+  const uint32_t b = t / (band * tiles_n), in = t % (band * tiles_n);
+  const uint32_t high = tiles_m - b * band < band ? tiles_m - b * band : band;
+  m = b * band + in % high;
   n = in / high;
 }
 

@@ -26,6 +26,7 @@ namespace pulse {
 
 namespace {
 
+constexpr uint32_t kBand = 8;  // tiles in m of a band: 32 CUs then work on 8 by 4
 constexpr float kLog2e = 1.4426950408889634f;
 
 // 2^x (v_exp_f32, 1 ulp).
@@ -72,7 +73,7 @@ template <typename T>
 __global__ __launch_bounds__(T::kThreads) void ce_forward_kernel(LogitParams p) {
   __shared__ alignas(1024) char lds[T::kLds];
   uint32_t tm, tn;
-  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, kBand, tm, tn);
   const uint32_t m0 = p.v_begin + tm * T::BM, n0 = tn * T::BN;
   typename T::Acc acc;
   const GemmOperand a = {p.w + (uint64_t)m0 * p.w_ld, p.w_ld, p.v_end - m0};
@@ -141,7 +142,7 @@ template <typename T>
 __global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
   __shared__ alignas(1024) char lds[T::kLds];
   uint32_t tm, tn;
-  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, kBand, tm, tn);
   const uint32_t m0 = p.v_begin + tm * T::BM, n0 = tn * T::BN;
   typename T::Acc acc;
   const GemmOperand a = {p.w + (uint64_t)m0 * p.w_ld, p.w_ld, p.v_end - m0};
@@ -251,7 +252,7 @@ __global__ __launch_bounds__(256) void ce_join_kernel(const float2* part, const 
 struct GradParams {
   GemmOperand a, b;  // at the first tile
   uint32_t m, n, k;  // sizes
-  uint32_t tiles_m, tiles_n;
+  uint32_t tiles_m, tiles_n, band;
   uint32_t k_split;  // k per blockIdx.y, a multiple of 64
   float* sums;       // dx: [splits][n][m]
   int add;           // dx: onto what is there
@@ -266,7 +267,7 @@ template <typename T, bool AK, bool BK>
 __device__ __forceinline__ void grad_tile(const GradParams& p, char* lds, uint32_t& m0, uint32_t& n0,
                                           typename T::Acc& acc) {
   uint32_t tm, tn;
-  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, tm, tn);
+  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.band, tm, tn);
   m0 = tm * T::BM;
   n0 = tn * T::BN;
   const GemmOperand a = {p.a.p + (AK ? (uint64_t)m0 : m0 * p.a.ld), p.a.ld, p.a.limit - m0};
@@ -520,11 +521,13 @@ Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   if (piece < kVocabTile) piece = kVocabTile;
   const uint32_t pieces = parts(vocab, (uint32_t)(piece > vocab ? up(vocab, kVocabTile) : piece));
   q.piece = up(parts(vocab, pieces), kVocabTile);
-  // few tokens: split dx's k until there are two blocks a CU
+  // few tokens: split dx's k until the blocks fill the chip
   const uint32_t bm = tokens <= 64 ? DxS::BM : 256, bn = tokens <= 64 ? 64 : tokens <= 128 ? 128 : 256;
   const uint32_t tiles = parts(q.ld, bm) * parts(tokens, bn);
-  q.splits = 1;
-  while (tiles * q.splits < 256 && q.splits * 2 * 256 <= q.piece) q.splits *= 2;
+  // (three of the small tiles fit a CU, one of the others)
+  const uint32_t wanted = tokens <= 64 ? 768 : 192;
+  q.splits = tiles < wanted ? wanted / tiles : 1;
+  if (q.splits > q.piece / 256) q.splits = q.piece / 256;
   q.g = take((uint64_t)times * tokens * q.piece * 2);
   q.y = take((uint64_t)tokens * sizeof(int32_t));
   q.rest = take((uint64_t)tokens * sizeof(float));
@@ -552,6 +555,7 @@ template <typename T>
 void run_dx(GradParams p, uint32_t splits, hipStream_t stream) {
   p.tiles_m = parts(p.m, T::BM);
   p.tiles_n = parts(p.n, T::BN);
+  p.band = kBand;
   hipLaunchKernelGGL(ce_dx_kernel<T>, dim3(p.tiles_m * p.tiles_n, splits), dim3(T::kThreads), 0, stream, p);
 }
 
@@ -559,6 +563,8 @@ template <typename T, bool RESTS>
 void run_dw(GradParams p, hipStream_t stream) {
   p.tiles_m = parts(p.m, T::BM);
   p.tiles_n = parts(p.n, T::BN);
+  // few tokens: bound by writing dw, so whole rows of it at a time
+  p.band = RESTS ? kBand : p.tiles_m;
   hipLaunchKernelGGL((ce_dw_kernel<T, RESTS>), dim3(p.tiles_m * p.tiles_n), dim3(T::kThreads), 0, stream, p);
 }
 
