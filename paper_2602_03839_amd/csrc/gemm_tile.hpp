@@ -249,8 +249,12 @@ struct Gemm {
       }
     };
     load_step(0);
-    wait_and_meet<0>();
-    if (steps > 1) load_step(1);
+    if (steps > 1) {
+      load_step(1);
+      wait_and_meet<kLoads>();  // step 0 has landed
+    } else {
+      wait_and_meet<0>();
+    }
 #pragma unroll
     for (int i = 0; i < FM + FN; ++i) read(f0, 0, 0, i);
     int32_t s = 0;
