@@ -264,28 +264,29 @@ struct GradParams {
 };
 
 template <typename T, bool AK, bool BK>
-__device__ __forceinline__ void grad_tile(const GradParams& p, char* lds, uint32_t& m0, uint32_t& n0,
-                                          typename T::Acc& acc) {
+__device__ __forceinline__ void grad_tile(const GradParams& p, char* lds, uint32_t id, uint32_t split,
+                                          uint32_t& m0, uint32_t& n0, typename T::Acc& acc) {
   uint32_t tm, tn;
-  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, p.band, tm, tn);
+  gemm_tile_of(id, p.tiles_m, p.tiles_n, p.band, tm, tn);
   m0 = tm * T::BM;
   n0 = tn * T::BN;
   const GemmOperand a = {p.a.p + (AK ? (uint64_t)m0 : m0 * p.a.ld), p.a.ld, p.a.limit - m0};
   const GemmOperand b = {p.b.p + (BK ? (uint64_t)n0 : n0 * p.b.ld), p.b.ld, p.b.limit - n0};
-  const uint32_t k0 = blockIdx.y * p.k_split;
+  const uint32_t k0 = split * p.k_split;
   // a split past the end has no k and gives zeros
   const uint32_t k1 = k0 >= p.k ? k0 : p.k - k0 < p.k_split ? p.k : k0 + p.k_split;
   T::run(lds, a, b, k0, k1, acc);
 }
 
+// Block `id` of dx: its split's part of a tile of the sums.
 template <typename T>
-__global__ __launch_bounds__(T::kThreads) void ce_dx_kernel(GradParams p) {
-  __shared__ alignas(1024) char lds[T::kLds];
+__device__ void dx_block(const GradParams& p, char* lds, uint32_t id) {
+  const uint32_t tiles = p.tiles_m * p.tiles_n, split = id / tiles;
   uint32_t m0, n0;
   typename T::Acc acc;
-  grad_tile<T, true, false>(p, lds, m0, n0, acc);
+  grad_tile<T, true, false>(p, lds, id % tiles, split, m0, n0, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  float* sums = p.sums + (uint64_t)blockIdx.y * p.n * p.m;
+  float* sums = p.sums + (uint64_t)split * p.n * p.m;
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
     const uint32_t n = n0 + T::n_of(j, lane, wave);
@@ -359,11 +360,10 @@ __device__ void add_rests(const GradParams& p, char* lds, uint32_t m0, uint32_t 
 }
 
 template <typename T, bool RESTS>
-__global__ __launch_bounds__(T::kThreads) void ce_dw_kernel(GradParams p) {
-  __shared__ alignas(1024) char lds[T::kLds];
+__device__ void dw_block(const GradParams& p, char* lds, uint32_t id) {
   uint32_t m0, n0;
   typename T::Acc acc;
-  grad_tile<T, true, true>(p, lds, m0, n0, acc);
+  grad_tile<T, true, true>(p, lds, id, 0, m0, n0, acc);
   if constexpr (RESTS) add_rests<T>(p, lds, m0, n0, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   auto value = [&](int i, int j) {
@@ -392,6 +392,27 @@ __global__ __launch_bounds__(T::kThreads) void ce_dw_kernel(GradParams p) {
   }
 }
 
+template <typename T>
+__global__ __launch_bounds__(T::kThreads) void ce_dx_kernel(GradParams p) {
+  __shared__ alignas(1024) char lds[T::kLds];
+  dx_block<T>(p, lds, blockIdx.x);
+}
+
+template <typename T, bool RESTS>
+__global__ __launch_bounds__(T::kThreads) void ce_dw_kernel(GradParams p) {
+  __shared__ alignas(1024) char lds[T::kLds];
+  dw_block<T, RESTS>(p, lds, blockIdx.x);
+}
+
+// Both products in one launch: dx's blocks first, whose sums are the longer ones.
+template <typename TX, typename TW, bool RESTS>
+__global__ __launch_bounds__(TX::kThreads) void ce_both_kernel(GradParams x, GradParams w, uint32_t dx_blocks) {
+  static_assert(TX::kThreads == TW::kThreads, "blocks of one size");
+  __shared__ alignas(1024) char lds[TX::kLds > TW::kLds ? TX::kLds : TW::kLds];
+  if (blockIdx.x < dx_blocks) dx_block<TX>(x, lds, blockIdx.x);
+  else dw_block<TW, RESTS>(w, lds, blockIdx.x - dx_blocks);
+}
+
 // dx from the splits' sums and what the target's entry lost; a token without a target gets zeros.
 __global__ __launch_bounds__(256) void ce_dx_join_kernel(const float* sums, uint32_t splits, uint32_t tokens,
                                                          uint32_t ld, uint32_t hidden,
@@ -406,6 +427,7 @@ __global__ __launch_bounds__(256) void ce_dx_join_kernel(const float* sums, uint
   f32x4_t a = {0.0f, 0.0f, 0.0f, 0.0f};
   if (y >= 0 && y < (int64_t)vocab) {
     const uint2 v = *(const uint2*)(w + y * w_ld + c);
+#pragma unroll 8
     for (uint32_t s = 0; s < splits; ++s) a += *(const f32x4_t*)(sums + ((uint64_t)s * tokens + t) * ld + c);
     const float r = rest[t];
     a[0] = __builtin_fmaf(r, __uint_as_float(v.x << 16), a[0]);
@@ -420,52 +442,67 @@ __global__ __launch_bounds__(256) void ce_dx_join_kernel(const float* sums, uint
 
 // ---------------------------------------------------------------- copies
 
-// Rows padded with zeros to `ld`, `times` over; rows of tokens without a target (`targets` not
-// null) all zero: what is in them must not reach the other rows' sums.
-__global__ __launch_bounds__(256) void ce_copy_kernel(const uint16_t* from, uint64_t from_ld, uint32_t cols,
-                                                      uint16_t* to, uint32_t ld, uint64_t rows, uint32_t times,
-                                                      const int64_t* targets, uint32_t vocab) {
-  const uint64_t groups = ld / 8, all = rows * groups;
+// Rows to be padded with zeros to `ld`, `times` over.
+struct CopyJob {
+  const uint16_t* from;  // null: no such job
+  uint64_t from_ld;
+  uint16_t* to;
+  uint64_t rows;
+  uint32_t times;
+};
+
+struct PrepareParams {
+  CopyJob w, x;
+  uint32_t cols, ld;
+  const int64_t* targets;  // null, or: rows of x without a target become zeros, as
+  uint32_t vocab;          // what is in them must not reach the other rows' sums;
+  int32_t* y;              // and the targets as 32 bits, -1 for none
+};
+
+__device__ __forceinline__ void copy_group(const CopyJob& j, uint32_t cols, uint32_t ld, uint64_t r, uint32_t c,
+                                           bool kept) {
+  uint4 v = make_uint4(0, 0, 0, 0);
+  if (kept) {
+    const uint16_t* p = j.from + r * j.from_ld + c;
+    if (c + 8 <= cols && j.from_ld % 8 == 0) {
+      v = load16(p);
+    } else {
+      uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (c + e < cols) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+      v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+  for (uint32_t k = 0; k < j.times; ++k) store16(j.to + (k * j.rows + r) * ld + c, v);
+}
+
+__global__ __launch_bounds__(256) void ce_prepare_kernel(PrepareParams p) {
+  const uint64_t groups = p.ld / 8;  // of 8 elements, in a row
+  const uint64_t nx = p.x.from ? p.x.rows * groups : 0, all = nx + (p.w.from ? p.w.rows * groups : 0);
   for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
+    if (i >= nx) {
+      copy_group(p.w, p.cols, p.ld, (i - nx) / groups, (uint32_t)((i - nx) % groups) * 8, true);
+      continue;
+    }
     const uint64_t r = i / groups;
     const uint32_t c = (uint32_t)(i % groups) * 8;
-    uint4 v = make_uint4(0, 0, 0, 0);
     bool kept = true;
-    if (targets) {
-      const int64_t y = targets[r];
-      kept = y >= 0 && y < (int64_t)vocab;
+    if (p.targets) {
+      const int64_t y = p.targets[r];
+      kept = y >= 0 && y < (int64_t)p.vocab;
+      if (c == 0) p.y[r] = kept ? (int32_t)y : -1;
     }
-    if (kept) {
-      const uint16_t* p = from + r * from_ld + c;
-      if (c + 8 <= cols && from_ld % 8 == 0) {
-        v = load16(p);
-      } else {
-        uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (c + e < cols) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
-        v = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
-    for (uint32_t k = 0; k < times; ++k) store16(to + (k * rows + r) * ld + c, v);
+    copy_group(p.x, p.cols, p.ld, r, c, kept);
   }
 }
 
-// targets as 32-bit entries, -1 for an ignored one
-__global__ __launch_bounds__(256) void ce_targets_kernel(const int64_t* targets, uint32_t tokens, uint32_t vocab,
-                                                         int32_t* y) {
-  const uint32_t t = blockIdx.x * 256 + threadIdx.x;
-  if (t >= tokens) return;
-  const int64_t v = targets[t];
-  y[t] = v >= 0 && v < (int64_t)vocab ? (int32_t)v : -1;
-}
-
-void copy_rows(const uint16_t* from, uint64_t from_ld, uint32_t cols, uint16_t* to, uint32_t ld, uint64_t rows,
-               uint32_t times, const int64_t* targets, uint32_t vocab, hipStream_t stream) {
-  uint64_t blocks = (rows * (ld / 8) + 255) / 256;
+void prepare(const PrepareParams& p, hipStream_t stream) {
+  const uint64_t rows = (p.x.from ? p.x.rows : 0) + (p.w.from ? p.w.rows : 0);
+  if (rows == 0) return;
+  uint64_t blocks = (rows * (p.ld / 8) + 255) / 256;
   if (blocks > 8192) blocks = 8192;
-  hipLaunchKernelGGL(ce_copy_kernel, dim3((uint32_t)blocks), dim3(256), 0, stream, from, from_ld, cols, to, ld,
-                     rows, times, targets, vocab);
+  hipLaunchKernelGGL(ce_prepare_kernel, dim3((uint32_t)blocks), dim3(256), 0, stream, p);
 }
 
 // ---------------------------------------------------------------- shapes
@@ -474,6 +511,7 @@ uint32_t up(uint32_t v, uint32_t to) { return (v + to - 1) / to * to; }
 uint32_t parts(uint64_t v, uint32_t of) { return (uint32_t)((v + of - 1) / of); }
 
 constexpr uint32_t kVocabTile = 256;
+constexpr uint32_t kBothBlocks = 512;
 constexpr uint32_t kFewTokens = 128;  // up to here G's rests are kept for all entries
 
 // Tiles: vocabulary (or hidden) by tokens (or vocabulary), by the tokens' count.
@@ -485,6 +523,7 @@ typedef Gemm<256, 128, 4, 2, true, false> DxM;
 typedef Gemm<128, 64, 4, 1, true, false, true> DxS;
 typedef Gemm<256, 256, 2, 4, true, true> DwL;
 typedef Gemm<128, 128, 2, 2, true, true> DwS;
+typedef Gemm<128, 128, 4, 2, true, true> DwM;
 
 constexpr uint64_t kMaxStride = 1u << 20;  // a tile's byte offsets stay in 32 bits
 constexpr uint64_t kPieceBytes = 256ull << 20;  // of G
@@ -551,21 +590,25 @@ void run_logits(const LogitParams& p, bool forward, hipStream_t stream) {
   else run_logits<LogitsL>(p, forward, stream);
 }
 
-template <typename T>
-void run_dx(GradParams p, uint32_t splits, hipStream_t stream) {
-  p.tiles_m = parts(p.m, T::BM);
-  p.tiles_n = parts(p.n, T::BN);
-  p.band = kBand;
-  hipLaunchKernelGGL(ce_dx_kernel<T>, dim3(p.tiles_m * p.tiles_n, splits), dim3(T::kThreads), 0, stream, p);
-}
-
-template <typename T, bool RESTS>
-void run_dw(GradParams p, hipStream_t stream) {
-  p.tiles_m = parts(p.m, T::BM);
-  p.tiles_n = parts(p.n, T::BN);
+// dx's and dw's products of a piece.  One launch where both fit the chip at once
+// (each launch costs 3 us on the host and 2 to 4 of latency on the GPU); for more blocks
+// each product keeps the registers and LDS, hence the occupancy, of its own kernel.
+template <typename TX, typename TW, bool RESTS>
+void run_products(GradParams x, uint32_t splits, GradParams w, hipStream_t stream) {
+  x.tiles_m = parts(x.m, TX::BM);
+  x.tiles_n = parts(x.n, TX::BN);
+  x.band = kBand;
+  w.tiles_m = parts(w.m, TW::BM);
+  w.tiles_n = parts(w.n, TW::BN);
   // few tokens: bound by writing dw, so whole rows of it at a time
-  p.band = RESTS ? kBand : p.tiles_m;
-  hipLaunchKernelGGL((ce_dw_kernel<T, RESTS>), dim3(p.tiles_m * p.tiles_n), dim3(T::kThreads), 0, stream, p);
+  w.band = RESTS ? kBand : w.tiles_m;
+  const uint32_t nx = x.tiles_m * x.tiles_n * splits, nw = w.tiles_m * w.tiles_n;
+  if (nx + nw <= kBothBlocks) {
+    hipLaunchKernelGGL((ce_both_kernel<TX, TW, RESTS>), dim3(nx + nw), dim3(TX::kThreads), 0, stream, x, w, nx);
+    return;
+  }
+  hipLaunchKernelGGL(ce_dx_kernel<TX>, dim3(nx), dim3(TX::kThreads), 0, stream, x);
+  hipLaunchKernelGGL((ce_dw_kernel<TW, RESTS>), dim3(nw), dim3(TW::kThreads), 0, stream, w);
 }
 
 }  // namespace
@@ -586,22 +629,24 @@ uint64_t linear_ce_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
 hipError_t launch_linear_ce(const LinearCeParams& c, char* ws, hipStream_t stream) {
   const Plan q = plan_of(c.tokens, c.vocab, c.hidden);
   LogitParams p = {};
+  PrepareParams r = {};
+  r.cols = c.hidden;
+  r.ld = q.ld;
   p.w = c.weight;
   p.w_ld = c.hidden;
   if (q.copy_w) {
-    uint16_t* w = (uint16_t*)(ws + q.w);
-    copy_rows(c.weight, c.hidden, c.hidden, w, q.ld, c.vocab, 1, nullptr, c.vocab, stream);
-    p.w = w;
+    r.w = {c.weight, c.hidden, (uint16_t*)(ws + q.w), c.vocab, 1};
+    p.w = r.w.to;
     p.w_ld = q.ld;
   }
   p.x = c.x;
   p.x_ld = c.x_stride;
   if (c.hidden % 8 || c.x_stride % 8 || c.x_stride > kMaxStride) {
-    uint16_t* x = (uint16_t*)(ws + q.x);
-    copy_rows(c.x, c.x_stride, c.hidden, x, q.ld, c.tokens, 1, nullptr, c.vocab, stream);
-    p.x = x;
+    r.x = {c.x, c.x_stride, (uint16_t*)(ws + q.x), c.tokens, 1};
+    p.x = r.x.to;
     p.x_ld = q.ld;
   }
+  prepare(r, stream);
   p.targets = c.targets;
   p.tokens = c.tokens;
   p.hidden = q.ld;
@@ -619,20 +664,26 @@ hipError_t launch_linear_ce(const LinearCeParams& c, char* ws, hipStream_t strea
 hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStream_t stream) {
   const Plan q = plan_of(c.tokens, c.vocab, c.hidden);
   LogitParams p = {};
+  PrepareParams r = {};
+  r.cols = c.hidden;
+  r.ld = q.ld;
   p.w = c.weight;
   p.w_ld = c.hidden;
   if (q.copy_w) {
-    uint16_t* w = (uint16_t*)(ws + q.w);
-    copy_rows(c.weight, c.hidden, c.hidden, w, q.ld, c.vocab, 1, nullptr, c.vocab, stream);
-    p.w = w;
+    r.w = {c.weight, c.hidden, (uint16_t*)(ws + q.w), c.vocab, 1};
+    p.w = r.w.to;
     p.w_ld = q.ld;
   }
   // few tokens: G's rests are 128 more rows at most of k for dw, which then meet x
   // again; more tokens add the targets' rests alone
   const bool few = c.tokens <= kFewTokens;
-  uint16_t* x = (uint16_t*)(ws + q.x);
-  copy_rows(c.x, c.x_stride, c.hidden, x, q.ld, c.tokens, few ? 2 : 1, c.targets, c.vocab, stream);
-  p.x = x;
+  int32_t* y = (int32_t*)(ws + q.y);
+  r.x = {c.x, c.x_stride, (uint16_t*)(ws + q.x), c.tokens, few ? 2u : 1u};
+  r.targets = c.targets;
+  r.vocab = c.vocab;
+  r.y = y;
+  prepare(r, stream);
+  p.x = r.x.to;
   p.x_ld = q.ld;
   p.targets = c.targets;
   p.tokens = c.tokens;
@@ -644,9 +695,6 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
   p.g = (uint16_t*)(ws + q.g);
   p.g_ld = q.piece;
   p.rest = (float*)(ws + q.rest);
-  int32_t* y = (int32_t*)(ws + q.y);
-  hipLaunchKernelGGL(ce_targets_kernel, dim3(parts(c.tokens, 256)), dim3(256), 0, stream, c.targets, c.tokens,
-                     c.vocab, y);
   float* sums = (float*)(ws + q.sums);
   for (uint32_t v = 0; v < c.vocab; v += q.piece) {
     const uint32_t n = c.vocab - v < q.piece ? c.vocab - v : q.piece;
@@ -664,9 +712,6 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
     d.add = v > 0;
     // a short last piece leaves the last splits without k: their sums stay
     const uint32_t splits = v > 0 ? parts(n, d.k_split) : q.splits;
-    if (c.tokens <= 64) run_dx<DxS>(d, splits, stream);
-    else if (c.tokens <= 128) run_dx<DxM>(d, splits, stream);
-    else run_dx<DxL>(d, splits, stream);
     GradParams e = {};
     e.a = {p.x, q.ld, q.ld};
     e.b = {p.g, q.piece, q.piece};
@@ -678,8 +723,9 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
     e.v_begin = v;
     e.out = c.dweight + (uint64_t)v * c.hidden;
     e.out_ld = c.hidden;
-    if (few) run_dw<DwS, false>(e, stream);
-    else run_dw<DwL, true>(e, stream);
+    if (c.tokens <= 64) run_products<DxS, DwS, false>(d, splits, e, stream);
+    else if (few) run_products<DxM, DwM, false>(d, splits, e, stream);
+    else run_products<DxL, DwL, true>(d, splits, e, stream);
   }
   hipLaunchKernelGGL(ce_dx_join_kernel, dim3(c.tokens, parts(q.ld, 1024)), dim3(256), 0, stream, sums, q.splits,
                      c.tokens, q.ld, c.hidden, c.targets, c.vocab, p.w, p.w_ld, p.rest, c.dx, c.dx_stride);
