@@ -149,7 +149,11 @@ class LayerNorm:
         dev, cols, dt = self.device, self.cols, _dtype(x, "x")
         px, sx = _matrix(x, "x", cols, device=dev)
         rows = x.shape[0]
-        y, py, sy = _out(y, "y", cols, rows, x.dtype, dev, stream)
+        if y is None and stream is None and sx == cols:
+            y = torch.empty_like(x)
+            py, sy = y.data_ptr(), cols
+        else:
+            y, py, sy = _out(y, "y", cols, rows, x.dtype, dev, stream)
         mean, pm = (None, None) if self.rms else _vec(mean, "mean", rows, dev, stream)
         rstd, pr = _vec(rstd, "rstd", rows, dev, stream)
         rc = self._lib.pulse_layer_norm_forward(dt, px, sx, self._dt, self._pw, self._pb, py, sy, pm, pr,
@@ -170,7 +174,11 @@ class LayerNorm:
         pdy, sdy = _matrix(dy, "dy", cols, rows, x.dtype, dev)
         pm = None if self.rms else _f32(mean, "mean", rows, dev)
         pr = _f32(rstd, "rstd", rows, dev)
-        dx, pdx, sdx = _out(dx, "dx", cols, rows, x.dtype, dev, stream)
+        if dx is None and stream is None and sx == cols:
+            dx = torch.empty_like(x)
+            pdx, sdx = dx.data_ptr(), cols
+        else:
+            dx, pdx, sdx = _out(dx, "dx", cols, rows, x.dtype, dev, stream)
         dweight, pdw = _vec(dweight, "dweight", cols, dev, stream)
         dbias, pdb = (None, None) if self.bias is None else _vec(dbias, "dbias", cols, dev, stream)
         rc = self._lib.pulse_layer_norm_backward(dt, pdy, sdy, px, sx, self._dt, self._pw, pm, pr, pdx, sdx,
