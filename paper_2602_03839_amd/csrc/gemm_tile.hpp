@@ -111,6 +111,27 @@ struct GemmTile {
     }
   }
 
+  // k-major: rows of the operand picked by `row(k)` (negative: zeros) as the 64 k.
+  template <typename F>
+  static __device__ __forceinline__ void gather(const GemmOperand& o, char* lds, int wave, int lane, F row) {
+    static_assert(KMAJOR, "");
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t k = k_of(i, wave, lane), g = lane % (ROWS / 8);
+      uint32_t c = (((g >> 1) ^ mix(k)) << 1 | (g & 1)) * 8;
+      if (c >= o.limit) c = o.limit - 8;
+      const int32_t r = row(k);
+      const uint16_t* from = r >= 0 ? o.p + (uint64_t)(uint32_t)r * o.ld + c : (const uint16_t*)gemm_zeros;
+      __builtin_amdgcn_global_load_lds(
+          (const __attribute__((address_space(1))) void*)from,
+          (__attribute__((address_space(3))) void*)(lds + (i * WAVES + wave) * 1024), 16, 0, 0);
+    }
+  }
+  // k-major: where element (k, row) lies.
+  static __device__ __forceinline__ uint32_t place(uint32_t k, uint32_t row) {
+    return k * (ROWS * 2) + (((row >> 4) ^ mix(k)) << 5) + (row & 15) * 2;
+  }
+
   // The lane's fragment of the 16 rows from `first` (a multiple of 16), k = 32 ks ...
   static __device__ __forceinline__ bf16x8_t fragment(const char* lds, uint32_t first, int ks, int lane) {
     const uint32_t r = lane & 15, g = lane >> 4;
@@ -150,9 +171,10 @@ struct Gemm {
 
   // The tile as BF16 rows out[n][m], 16 bytes a lane and whole lines at a time: a
   // lane's own four values of 16 rows would be written in pieces of 32 bytes.
-  // `value(i, j)` gives them as two packed pairs; only rows n < n_left and groups
-  // of 8 m below m_left are written.  Group c of row n lies at place c ^ (n & 15).
-  template <bool STREAM, typename F>
+  // `value(i, j)` gives them as two packed pairs; only n < n_left and m < m_left are
+  // written.  Group c of row n lies at place c ^ (n & 15).  ALIGNED: rows start at 16
+  // bytes and m_left is a multiple of 8.  STREAM: written past the caches.
+  template <bool STREAM, bool ALIGNED, typename F>
   static __device__ __forceinline__ void store_rows(char* lds, uint16_t* out, uint64_t ld, uint32_t m_left,
                                                     uint32_t n_left, F value) {
     static_assert(BM >= 128 && BM * BN * 2 <= kLds, "the tile fits, with 16 groups a row");
@@ -171,9 +193,39 @@ struct Gemm {
     for (uint32_t q = threadIdx.x; q < BN * (BM / 8); q += kThreads) {
       const uint32_t n = q / (BM / 8), c = q % (BM / 8);
       const uint4 v = *(const uint4*)(lds + n * (BM * 2) + ((c ^ (n & 15)) << 4));
-      if (n < n_left && c * 8 < m_left) {
-        if constexpr (STREAM) store16_stream(out + n * ld + c * 8, v);
-        else store16(out + n * ld + c * 8, v);
+      uint16_t* const to = out + n * ld + c * 8;
+      if (n >= n_left || c * 8 >= m_left) continue;
+      if constexpr (!ALIGNED) {
+        if (c * 8 + 8 <= m_left) {
+          store16_any(to, v);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (c * 8 + e < m_left) to[e] = (uint16_t)(get_u32(v, e >> 1) >> (16 * (e & 1)));
+        }
+      } else if constexpr (STREAM) {
+        store16_stream(to, v);
+      } else {
+        store16(to, v);
+      }
+    }
+  }
+
+  // One more step of up to 64 k on `lds` (a step's two tiles, landed for every wave).
+  static __device__ __forceinline__ void add_step(const char* lds, Acc& acc) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t m = (wave / WN) * (FM * 16), n = (wave % WN) * (FN * 16);
+#pragma unroll 1
+    for (int ks = 0; ks < 2; ++ks) {
+      bf16x8_t b[FN];
+#pragma unroll
+      for (int j = 0; j < FN; ++j) b[j] = B::fragment(lds + A::kBytes, n + j * 16, ks, lane);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const bf16x8_t a = A::fragment(lds, m + i * 16, ks, lane);
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[j], acc[i][j], 0, 0, 0);
       }
     }
   }

@@ -122,4 +122,18 @@ __device__ __forceinline__ float wave_sum(float v) {
   return (row(0) + row(16)) + (row(32) + row(48));
 }
 
+// 16 bytes at any address of a 2-byte type (such an access is one instruction here).
+struct __attribute__((packed, aligned(2))) Unaligned16 {
+  uint32_t w[4];
+};
+
+__device__ __forceinline__ uint4 load16_any(const void* p) {
+  const Unaligned16 u = *reinterpret_cast<const Unaligned16*>(p);
+  return make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]);
+}
+
+__device__ __forceinline__ void store16_any(void* p, uint4 v) {
+  *reinterpret_cast<Unaligned16*>(p) = Unaligned16{{v.x, v.y, v.z, v.w}};
+}
+
 }  // namespace pulse

@@ -67,6 +67,7 @@ struct LogitParams {
   uint16_t* g;  // [tokens][g_ld]
   uint64_t g_ld;
   float* rest;  // [tokens]: what the target's entry lost in the rounding
+  bool rest_rows;  // what every entry lost follows G, as as many rows again
 };
 
 template <typename T>
@@ -208,10 +209,10 @@ __global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
     return o;
   };
   uint16_t* const out = p.g + n0 * p.g_ld + (m0 - p.v_begin);
-  T::template store_rows<false>(lds, out, p.g_ld, T::BM, p.tokens - n0, rounded);
-  if constexpr (T::BN < 256) {  // few tokens: the rests of all entries, as rows of their own
+  T::template store_rows<false, true>(lds, out, p.g_ld, T::BM, p.tokens - n0, rounded);
+  if (p.rest_rows) {  // few tokens: the rests of all entries, as rows of their own
     __syncthreads();
-    T::template store_rows<false>(lds, out + (uint64_t)p.tokens * p.g_ld, p.g_ld, T::BM, p.tokens - n0,
+    T::template store_rows<false, true>(lds, out + (uint64_t)p.tokens * p.g_ld, p.g_ld, T::BM, p.tokens - n0,
                                   [&](int i, int j) {
                                     const uint2 o = rounded(i, j);
                                     acc[i][j][0] -= __uint_as_float(o.x << 16);
@@ -301,16 +302,25 @@ __device__ void dx_block(const GradParams& p, char* lds, uint32_t id) {
   }
 }
 
-// Adds rest[t] x[t] to the row of the tile that is token t's target.  The block
-// looks through the targets, collects those of its rows in LDS in a fixed order,
-// and every wave adds those that lie in its own columns of the tile.
+// Adds rest[t] x[t] to the row of the tile that is token t's target: more steps of the
+// product, of 64 such tokens each.  The block looks through the targets and collects
+// those of its rows in LDS in a fixed order; their rows of x are one operand, and
+// the other is zeros but for each token's rest (BF16 of a number that is itself
+// what BF16 dropped) in the column of its target.
 template <typename T>
 __device__ void add_rests(const GradParams& p, char* lds, uint32_t m0, uint32_t n0, typename T::Acc& acc) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t* s_list = (uint32_t*)lds;                       // [4 kThreads]
-  uint32_t* s_count = (uint32_t*)lds + 4 * T::kThreads;     // [kWaves]
-  const uint32_t first = T::n_of(0, 0, wave), m = m0 + T::m_of(0, lane, wave);
-  for (uint32_t base = 0; base < p.k; base += 4 * T::kThreads) {
+  int lane = threadIdx.x & 63;
+  // opaque, so that no address below is worked out before the product and kept
+  // in registers through it
+  asm volatile("" : "+v"(lane));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr uint32_t kSeen = 4 * T::kThreads;                // tokens looked at at a time
+  uint32_t* const s_list = (uint32_t*)(lds + T::kStage);      // [kSeen], past the first step's tiles
+  uint32_t* const s_count = s_list + kSeen;                  // [kWaves]
+  static_assert(T::kStage >= 4 * kSeen + 4 * T::kWaves, "the list fits the second buffer");
+  char* const tile_b = lds + T::A::kBytes;
+  const GemmOperand a = {p.a.p + m0, p.a.ld, p.a.limit - m0};
+  for (uint32_t base = 0; base < p.k; base += kSeen) {
     uint64_t hits[4];
     uint32_t count = 0;
 #pragma unroll
@@ -335,28 +345,23 @@ __device__ void add_rests(const GradParams& p, char* lds, uint32_t m0, uint32_t 
       before += (uint32_t)__popcll(hits[q]);
     }
     __syncthreads();
-    for (uint32_t h = 0; h < all; ++h) {
-      const uint32_t t = __builtin_amdgcn_readfirstlane(s_list[h]);
-      const uint32_t n = (uint32_t)p.y[t] - p.v_begin - n0 - first;  // in the wave's columns, or not
-      if (n >= T::FN * 16) continue;
-      const float r = (uint32_t)(lane & 15) == (n & 15) ? p.rest[t] : 0.0f;
-      const uint16_t* x = p.a.p + t * p.a.ld;
-#pragma unroll
-      for (int j = 0; j < T::FN; ++j) {
-        if (n >> 4 != (uint32_t)j) continue;
-#pragma unroll
-        for (int i = 0; i < T::FM; ++i) {
-          const uint32_t c = m + i * 16 < p.a.limit ? m + i * 16 : 0;
-          const uint2 v = *(const uint2*)(x + c);
-          acc[i][j][0] = __builtin_fmaf(r, __uint_as_float(v.x << 16), acc[i][j][0]);
-          acc[i][j][1] = __builtin_fmaf(r, __uint_as_float(v.x & 0xFFFF0000u), acc[i][j][1]);
-          acc[i][j][2] = __builtin_fmaf(r, __uint_as_float(v.y << 16), acc[i][j][2]);
-          acc[i][j][3] = __builtin_fmaf(r, __uint_as_float(v.y & 0xFFFF0000u), acc[i][j][3]);
-        }
+    for (uint32_t h = 0; h < all; h += kGemmK) {
+      const uint32_t left = all - h;
+      T::A::gather(a, lds, wave, lane, [&](uint32_t k) { return k < left ? (int32_t)s_list[h + k] : -1; });
+      for (uint32_t i = threadIdx.x; i < T::B::kBytes / 16; i += T::kThreads)
+        *(uint4*)(tile_b + i * 16) = make_uint4(0, 0, 0, 0);
+      __syncthreads();
+      if (threadIdx.x < kGemmK && threadIdx.x < left) {
+        const uint32_t t = s_list[h + threadIdx.x];
+        *(uint16_t*)(tile_b + T::B::place(threadIdx.x, (uint32_t)p.y[t] - p.v_begin - n0)) =
+            (uint16_t)bf16x2_rne(__float_as_uint(p.rest[t]), 0u);
       }
+      wait_and_meet<0>();
+      T::add_step(lds, acc);
+      __syncthreads();  // the tiles are free again
     }
-    __syncthreads();  // the list and the counts are free again
   }
+  __syncthreads();
 }
 
 template <typename T, bool RESTS>
@@ -365,31 +370,15 @@ __device__ void dw_block(const GradParams& p, char* lds, uint32_t id) {
   typename T::Acc acc;
   grad_tile<T, true, true>(p, lds, id, 0, m0, n0, acc);
   if constexpr (RESTS) add_rests<T>(p, lds, m0, n0, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   auto value = [&](int i, int j) {
     uint2 o;
     o.x = bf16x2_rne(__float_as_uint(acc[i][j][0]), __float_as_uint(acc[i][j][1]));
     o.y = bf16x2_rne(__float_as_uint(acc[i][j][2]), __float_as_uint(acc[i][j][3]));
     return o;
   };
-  if (p.out_ld % 8 == 0) {
-    T::template store_rows<true>(lds, p.out + n0 * p.out_ld + m0, p.out_ld, p.m - m0, p.n - n0, value);
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < T::FN; ++j) {
-    const uint32_t n = n0 + T::n_of(j, lane, wave);
-    if (n >= p.n) continue;
-#pragma unroll
-    for (int i = 0; i < T::FM; ++i) {
-      const uint32_t m = m0 + T::m_of(i, lane, wave);
-      const uint2 o = value(i, j);
-      const uint32_t w[2] = {o.x, o.y};
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (m + e < p.m) p.out[n * p.out_ld + m + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
-    }
-  }
+  uint16_t* const out = p.out + n0 * p.out_ld + m0;
+  if (p.out_ld % 8 == 0) T::template store_rows<true, true>(lds, out, p.out_ld, p.m - m0, p.n - n0, value);
+  else T::template store_rows<false, false>(lds, out, p.out_ld, p.m - m0, p.n - n0, value);
 }
 
 template <typename T>
@@ -464,8 +453,8 @@ __device__ __forceinline__ void copy_group(const CopyJob& j, uint32_t cols, uint
   uint4 v = make_uint4(0, 0, 0, 0);
   if (kept) {
     const uint16_t* p = j.from + r * j.from_ld + c;
-    if (c + 8 <= cols && j.from_ld % 8 == 0) {
-      v = load16(p);
+    if (c + 8 <= cols) {
+      v = load16_any(p);
     } else {
       uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -514,17 +503,21 @@ constexpr uint32_t kVocabTile = 256;
 constexpr uint32_t kBothBlocks = 512;
 constexpr uint32_t kFewTokens = 128;  // up to here G's rests are kept for all entries
 
-// Tiles: vocabulary (or hidden) by tokens (or vocabulary), by the tokens' count.
+// Tiles: vocabulary (or hidden) by tokens (or vocabulary).  The large ones reach the
+// matrix cores' rate where there are tiles enough for all CUs; the smaller ones fill
+// the chip with fewer and overlap one block's epilogue with another's loads.
 typedef Gemm<256, 256, 2, 4, false, false> LogitsL;
 typedef Gemm<256, 128, 4, 2, false, false> LogitsM;
-typedef Gemm<256, 64, 4, 1, false, false, true> LogitsS;
+typedef Gemm<256, 64, 4, 1, false, false> LogitsS;
+typedef Gemm<256, 64, 4, 1, false, false, true> LogitsW;  // past the caches, for a weight larger than they are
 typedef Gemm<256, 256, 2, 4, true, false> DxL;
 typedef Gemm<256, 128, 4, 2, true, false> DxM;
 typedef Gemm<128, 64, 4, 1, true, false, true> DxS;
 typedef Gemm<256, 256, 2, 4, true, true> DwL;
-typedef Gemm<128, 128, 2, 2, true, true> DwS;
 typedef Gemm<128, 128, 4, 2, true, true> DwM;
+typedef Gemm<128, 128, 2, 2, true, true> DwS;
 
+constexpr uint64_t kCacheBytes = 256ull << 20;  // of the last level
 constexpr uint64_t kMaxStride = 1u << 20;  // a tile's byte offsets stay in 32 bits
 constexpr uint64_t kPieceBytes = 256ull << 20;  // of G
 
@@ -533,6 +526,7 @@ struct Plan {
   bool copy_w;
   uint32_t piece;   // vocabulary entries a piece, a multiple of the tile
   uint32_t splits;  // of dx's k
+  bool small;       // the products in the smaller tiles
   // byte offsets in the workspace
   uint64_t w, x, part, hit, g, y, rest, sums, forward, total;
 };
@@ -561,7 +555,8 @@ Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   const uint32_t pieces = parts(vocab, (uint32_t)(piece > vocab ? up(vocab, kVocabTile) : piece));
   q.piece = up(parts(vocab, pieces), kVocabTile);
   // few tokens: split dx's k until the blocks fill the chip
-  const uint32_t bm = tokens <= 64 ? DxS::BM : 256, bn = tokens <= 64 ? 64 : tokens <= 128 ? 128 : 256;
+  q.small = tokens <= kFewTokens || parts(q.ld, 256) * parts(q.piece, 256) < 256;
+  const uint32_t bm = tokens <= 64 ? DxS::BM : 256, bn = tokens <= 64 ? 64 : q.small ? 128 : 256;
   const uint32_t tiles = parts(q.ld, bm) * parts(tokens, bn);
   // (three of the small tiles fit a CU, one of the others)
   const uint32_t wanted = tokens <= 64 ? 768 : 192;
@@ -584,10 +579,31 @@ void run_logits(LogitParams p, bool forward, hipStream_t stream) {
   else hipLaunchKernelGGL(ce_grad_kernel<T>, grid, block, 0, stream, p);
 }
 
+// A block's time in thousands of cycles, for the choice of a tile: a fixed part (the first
+// loads and the epilogue) and one per step of 64 k, as measured alone on a CU.
+struct TileCost {
+  uint32_t bn, slots;  // blocks that are on the chip at once
+  float fixed, step;
+};
+
+float cost_of(const TileCost& c, uint32_t tiles_m, uint32_t tokens, uint32_t k) {
+  const uint32_t blocks = tiles_m * parts(tokens, c.bn);
+  return (float)parts(blocks, c.slots) * (c.fixed + c.step * (float)parts(k, kGemmK));
+}
+
 void run_logits(const LogitParams& p, bool forward, hipStream_t stream) {
-  if (p.tokens <= 64) run_logits<LogitsS>(p, forward, stream);
-  else if (p.tokens <= 128) run_logits<LogitsM>(p, forward, stream);
-  else run_logits<LogitsL>(p, forward, stream);
+  if (p.tokens <= 64) {
+    if ((uint64_t)p.vocab * p.w_ld * 2 > kCacheBytes) run_logits<LogitsW>(p, forward, stream);
+    else run_logits<LogitsS>(p, forward, stream);
+    return;
+  }
+  const uint32_t tiles_m = parts(p.v_end - p.v_begin, kVocabTile);
+  const float l = cost_of({256, 256, 18.0f, 2.2f}, tiles_m, p.tokens, p.hidden);
+  const float m = cost_of({128, 256, 11.0f, 1.3f}, tiles_m, p.tokens, p.hidden);
+  const float s = cost_of({64, 512, 12.0f, 1.5f}, tiles_m, p.tokens, p.hidden);
+  if (l <= m && l <= s) run_logits<LogitsL>(p, forward, stream);
+  else if (m <= s) run_logits<LogitsM>(p, forward, stream);
+  else run_logits<LogitsS>(p, forward, stream);
 }
 
 // dx's and dw's products of a piece.  One launch where both fit the chip at once
@@ -695,6 +711,7 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
   p.g = (uint16_t*)(ws + q.g);
   p.g_ld = q.piece;
   p.rest = (float*)(ws + q.rest);
+  p.rest_rows = few;
   float* sums = (float*)(ws + q.sums);
   for (uint32_t v = 0; v < c.vocab; v += q.piece) {
     const uint32_t n = c.vocab - v < q.piece ? c.vocab - v : q.piece;
@@ -725,6 +742,7 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
     e.out_ld = c.hidden;
     if (c.tokens <= 64) run_products<DxS, DwS, false>(d, splits, e, stream);
     else if (few) run_products<DxM, DwM, false>(d, splits, e, stream);
+    else if (q.small) run_products<DxM, DwM, true>(d, splits, e, stream);
     else run_products<DxL, DwL, true>(d, splits, e, stream);
   }
   hipLaunchKernelGGL(ce_dx_join_kernel, dim3(c.tokens, parts(q.ld, 1024)), dim3(256), 0, stream, sums, q.splits,

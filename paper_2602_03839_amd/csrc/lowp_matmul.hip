@@ -37,15 +37,6 @@ struct Unit {
   static constexpr uint32_t kChunk = kValues * kLpGroups;
 };
 
-struct __attribute__((packed, aligned(2))) Unaligned16 {
-  uint32_t w[4];
-};
-
-__device__ __forceinline__ uint4 load16_any(const void* p) {
-  const Unaligned16 u = *reinterpret_cast<const Unaligned16*>(p);
-  return make_uint4(u.w[0], u.w[1], u.w[2], u.w[3]);
-}
-
 template <bool MX>
 __device__ __forceinline__ bf16x8_t decode8(const uint4& c, int f, float scale) {
   typedef __bf16 pair_t __attribute__((ext_vector_type(2)));

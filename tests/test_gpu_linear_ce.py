@@ -4,8 +4,8 @@ Tolerances.  A logit is a sum of `hidden` exact products in FP32: off by at most
 hidden * 2^-24 of the sum of their magnitudes; loss and lse add the rounding of
 log and of a few sums (1e-6 of their terms).  A gradient is a sum whose terms
 carry the BF16 rounding of G (2^-8 relative to each, and the error of the logits
-in the exponent) and is itself rounded to BF16: at most 2^-8 of the sum of the
-terms' magnitudes, plus 2^-8 of the result.
+and of lse in the exponent, which is relative to p) and is itself rounded to BF16:
+at most 2^-8 of the sum of the terms' magnitudes, plus 2^-8 of the result.
 """
 import pytest
 import torch
@@ -57,6 +57,9 @@ def check(tokens, vocab, hidden, seed=0, scale=1.0, data=None):
     # G's own relative error: its rounding, and twice the logits' error in the exponent
     rel = 2.0 ** -8 + 2 * bound.max().item()
     size = g.abs() + 2 * U * dl.double().abs()[:, None] * abs(scale)
+    # at the target p's error is relative to p, up to 1, and not to p - 1
+    at = torch.where(kept, y, torch.zeros_like(y))
+    size[torch.arange(tokens), at] += 2 * bound / rel * dl.double().abs() * abs(scale)
     for got, want, terms in ((dx, g @ w.double(), size @ w.double().abs()),
                              (dw, g.t() @ xk, size.t() @ xk.abs())):
         off = (got.cpu().double() - want).abs()
@@ -92,7 +95,7 @@ def test_scales(scale):
 
 def test_several_pieces():
     """More vocabulary than one piece of G holds, and a short last piece."""
-    for tokens, vocab, hidden in ((40, 40000, 2048), (2100, 66000, 64)):
+    for tokens, vocab, hidden in ((40, 40000, 2048), (2100, 66000, 64), (2500, 70000, 520)):
         x, w, y, dl = inputs(tokens, vocab, hidden, 8)
         ce = head.LinearCE(w.cuda(), max_tokens=tokens)
         _, lse = ce.forward(x.cuda(), y.cuda())
@@ -108,6 +111,28 @@ def test_several_pieces():
         g *= torch.where(kept, dl.cuda().double(), torch.zeros((), dtype=torch.float64, device="cuda"))[:, None]
         for got, want in ((dx, g @ wd), (dw, g.t().contiguous() @ xd)):
             assert (got.double() - want).norm() <= 2.0 ** -8 * want.norm()
+
+
+@pytest.mark.parametrize("tokens,vocab,hidden", [(300, 40, 72), (1000, 300, 203), (700, 3, 64)])
+def test_many_tokens_share_a_target(tokens, vocab, hidden):
+    """Far more tokens than entries, and half of them with the same target."""
+    x, w, y, dl = inputs(tokens, vocab, hidden, 11)
+    y[::2] = vocab - 1
+    check(tokens, vocab, hidden, data=(x, w, y, dl))
+
+
+def test_precision_of_few_and_many_tokens():
+    """Every gradient is as exact as its own rounding to BF16: what G's rounding
+    takes from the targets' entries is added back (a relative error, in the
+    2-norm, of 0.0017 for the output's rounding alone; 0.0024 with G's)."""
+    for tokens in (1, 5, 64, 65, 128, 129, 400):
+        x, w, y, dl = inputs(tokens, 3000, 256, tokens, ignored=0.0)
+        ce = head.LinearCE(w.cuda(), max_tokens=tokens)
+        _, lse = ce.forward(x.cuda(), y.cuda())
+        dx, dw = ce.backward(x.cuda(), y.cuda(), lse, dl.cuda())
+        g = exact(x, w, y, dl, 1.0)[3]
+        for got, want in ((dx, g @ w.double()), (dw, g.t() @ x.double())):
+            assert (got.cpu().double() - want).norm() <= 0.002 * want.norm(), tokens
 
 
 def test_all_ignored_and_odd_targets():
