@@ -132,17 +132,25 @@ struct GemmTile {
     return k * (ROWS * 2) + (((row >> 4) ^ mix(k)) << 5) + (row & 15) * 2;
   }
 
-  // The lane's fragment of the 16 rows from `first` (a multiple of 16), k = 32 ks ...
-  static __device__ __forceinline__ bf16x8_t fragment(const char* lds, uint32_t first, int ks, int lane) {
+  // The lane's part of a fragment's place, for the rows from `first` (the wave's; a
+  // multiple of 16 fragments' rows): fragment i and half ks of the step are told by
+  // constants, so one register serves all of a wave's reads.
+  static __device__ __forceinline__ uint32_t lane_place(uint32_t first, int lane) {
     const uint32_t r = lane & 15, g = lane >> 4;
+    if constexpr (!KMAJOR) return (first + r) * 128 + ((g ^ ((r >> 1) & 7)) << 4);
+    const uint32_t k = g * 8 + (r >> 2);
+    return k * (ROWS * 2) + ((first * 2) ^ (mix(k) << 5)) + (r & 3) * 8;
+  }
+
+  // The lane's fragment of rows 16 i ..., k = 32 ks ..., `at`: its place and the tile's.
+  static __device__ __forceinline__ bf16x8_t fragment(uint32_t at, int i, int ks) {
     if constexpr (!KMAJOR) {
-      return *(const bf16x8_t*)(lds + (first + r) * 128 + (((ks * 4 + g) ^ ((r >> 1) & 7)) << 4));
+      return *(const __attribute__((address_space(3))) bf16x8_t*)((at ^ (ks << 6)) + i * 2048);
     } else {
-      const uint32_t k = ks * 32 + g * 8 + (r >> 2);
-      const uint32_t at = k * (ROWS * 2) + (((first >> 4) ^ mix(k)) << 5) + (r & 3) * 8;
+      const uint32_t to = (at ^ (i << 5)) + ks * 32 * ROWS * 2;
       s16x4_t v[2];
-      v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(lds + at));
-      v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(lds + at + 4 * ROWS * 2));
+      v[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)to);
+      v[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(to + 4 * ROWS * 2));
       return __builtin_bit_cast(bf16x8_t, *(const uint4*)v);
     }
   }
@@ -214,15 +222,16 @@ struct Gemm {
   // One more step of up to 64 k on `lds` (a step's two tiles, landed for every wave).
   static __device__ __forceinline__ void add_step(const char* lds, Acc& acc) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t m = (wave / WN) * (FM * 16), n = (wave % WN) * (FN * 16);
-#pragma unroll 1
+    const uint32_t at_a = lds_address(lds) + A::lane_place((wave / WN) * (FM * 16), lane);
+    const uint32_t at_b = lds_address(lds) + A::kBytes + B::lane_place((wave % WN) * (FN * 16), lane);
+#pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
       bf16x8_t b[FN];
 #pragma unroll
-      for (int j = 0; j < FN; ++j) b[j] = B::fragment(lds + A::kBytes, n + j * 16, ks, lane);
+      for (int j = 0; j < FN; ++j) b[j] = B::fragment(at_b, j, ks);
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
-        const bf16x8_t a = A::fragment(lds, m + i * 16, ks, lane);
+        const bf16x8_t a = A::fragment(at_a, i, ks);
 #pragma unroll
         for (int j = 0; j < FN; ++j)
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b[j], acc[i][j], 0, 0, 0);
@@ -246,7 +255,8 @@ struct Gemm {
     const int32_t full = (int32_t)((k1 - k0) / kGemmK), steps = (int32_t)((k1 - k0 + kGemmK - 1) / kGemmK);
     if (steps == 0) return;
     const int32_t rest = (int32_t)((k1 - k0) % kGemmK);
-    const uint32_t m = (wave / WN) * (FM * 16), n = (wave % WN) * (FN * 16);
+    const uint32_t at_a = lds_address(lds) + A::lane_place((wave / WN) * (FM * 16), lane);
+    const uint32_t at_b = lds_address(lds) + A::kBytes + B::lane_place((wave % WN) * (FN * 16), lane);
 
     struct Frags {
       bf16x8_t a[FM], b[FN];
@@ -269,9 +279,9 @@ struct Gemm {
       lb.next();
     };
     auto read = [&](Frags& f, int32_t s, int ks, int i) {  // fragment i of that half of step s
-      const char* from = lds + (s & 1) * kStage;
-      if (i < FN) f.b[i] = B::fragment(from + A::kBytes, n + i * 16, ks, lane);
-      else f.a[i - FN] = A::fragment(from, m + (i - FN) * 16, ks, lane);
+      const uint32_t from = (s & 1) * kStage;
+      if (i < FN) f.b[i] = B::fragment(from + at_b, i, ks);
+      else f.a[i - FN] = A::fragment(from + at_a, i - FN, ks);
     };
     auto multiply = [&](const Frags& f, int i) {
 #pragma unroll
