@@ -5,7 +5,9 @@
 // (row k holds adjacent m or n), so that no operand has to be transposed in
 // memory first.  64 k at a time go straight from global memory to LDS
 // (16 bytes a lane, no registers), into one of NST buffers, while the matrix
-// cores work on an earlier one.
+// cores work on an earlier one: with one step ahead a step takes at least the way to
+// memory (some 2,000 cycles), which the 256 by 256 tile's products fill; smaller
+// tiles have more steps ahead, or several blocks on a CU.
 //
 // LDS layout.  Such a load writes a wave's 64 groups of 16 bytes side by side, so
 // any permutation has to be made on the global side: which lane loads
@@ -156,15 +158,15 @@ struct GemmTile {
   }
 };
 
-template <int BM_, int BN_, int WM_, int WN_, bool AK_, bool BK_, bool STREAM_ = false>
+template <int BM_, int BN_, int WM_, int WN_, int NST_, bool AK_, bool BK_, bool STREAM_ = false>
 struct Gemm {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NST = NST_;
   static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;  // fragments of a wave
   typedef GemmTile<BM, kWaves, AK_> A;
   typedef GemmTile<BN, kWaves, BK_> B;
   static constexpr int kStage = A::kBytes + B::kBytes;
-  static constexpr int kLds = 2 * kStage;
+  static constexpr int kLds = NST * kStage;
   static constexpr int kLoads = A::kLoads + B::kLoads;  // of a wave and step
   typedef f32x4_t Acc[FM][FN];
 
@@ -261,16 +263,22 @@ struct Gemm {
     struct Frags {
       bf16x8_t a[FM], b[FN];
     };
-    auto load = [&](int32_t s, int i) {  // the i-th load of step s, which is whole
-      char* to = lds + (s & 1) * kStage;
+    // the buffers of the step that is worked on and of the one after it
+    uint32_t here = 0, after = kStage;
+    auto advance = [&] {
+      here = after;
+      after = after + kStage == kLds ? 0 : after + kStage;
+    };
+    auto load = [&](uint32_t buffer, int i) {  // the i-th load of the next step, which is whole
+      char* to = lds + buffer;
       if (i < A::kLoads) la.template load<STREAM_>(to, i, wave);
       else lb.template load<false>(to + A::kBytes, i - A::kLoads, wave);
     };
-    auto load_step = [&](int32_t s) {  // step s, any
-      char* to = lds + (s & 1) * kStage;
+    auto load_step = [&](uint32_t buffer, int32_t s) {  // step s, any
+      char* to = lds + buffer;
       if (s < full) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) load(s, i);
+        for (int i = 0; i < kLoads; ++i) load(buffer, i);
       } else {
         la.load_end(to, rest, wave, lane);
         lb.load_end(to + A::kBytes, rest, wave, lane);
@@ -278,8 +286,7 @@ struct Gemm {
       la.next();
       lb.next();
     };
-    auto read = [&](Frags& f, int32_t s, int ks, int i) {  // fragment i of that half of step s
-      const uint32_t from = (s & 1) * kStage;
+    auto read = [&](Frags& f, uint32_t from, int ks, int i) {  // fragment i of that half of a buffer
       if (i < FN) f.b[i] = B::fragment(from + at_b, i, ks);
       else f.a[i - FN] = A::fragment(from + at_a, i - FN, ks);
     };
@@ -291,55 +298,56 @@ struct Gemm {
 
     // Half a step ahead: while the matrix cores work on one half of a buffer the
     // other half's fragments are read.  Between the halves the next buffer has
-    // landed and this one is done with, so the step after next goes there.
+    // landed and this one is done with, so the step NST ahead goes there.
     // Loads, reads and products are issued in turn, in this order; the last
     // turn has no reads, so that they are back when the next half starts.
     constexpr int kTurns = FM - 1;
     Frags f0, f1;
-    auto half = [&](Frags& to, int32_t s, int ks, const Frags& by, bool loads) {
+    auto half = [&](Frags& to, uint32_t from, int ks, const Frags& by, bool loads, uint32_t buffer) {
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
         if (loads) {
 #pragma unroll
-          for (int l = i * kLoads / FM; l < (i + 1) * kLoads / FM; ++l) load(s + 1, l);
+          for (int l = i * kLoads / FM; l < (i + 1) * kLoads / FM; ++l) load(buffer, l);
         }
 #pragma unroll
         for (int r = i * (FM + FN) / kTurns; r < (i + 1) * (FM + FN) / kTurns && r < FM + FN; ++r)
-          read(to, s, ks, r);
+          read(to, from, ks, r);
         multiply(by, i);
         __builtin_amdgcn_sched_barrier(0);
       }
     };
-    load_step(0);
-    if (steps > 1) {
-      load_step(1);
-      wait_and_meet<kLoads>();  // step 0 has landed
-    } else {
-      wait_and_meet<0>();
-    }
+#pragma unroll
+    for (int i = 0; i < NST; ++i)
+      if (i < steps) load_step(i * kStage, i);
+    // step 0 has landed, where NST are on their way
+    if (steps >= NST) wait_and_meet<(NST - 1) * kLoads>();
+    else wait_and_meet<0>();
 #pragma unroll
     for (int i = 0; i < FM + FN; ++i) read(f0, 0, 0, i);
     int32_t s = 0;
-    for (; s + 2 < full; ++s) {
-      half(f1, s, 1, f0, false);
-      wait_and_meet<0>();
-      half(f0, s + 1, 0, f1, true);
+    for (; s + NST < full; ++s) {
+      half(f1, here, 1, f0, false, 0);
+      wait_and_meet<(NST - 2) * kLoads>();
+      half(f0, after, 0, f1, true, here);
       la.next();
       lb.next();
+      advance();
     }
     // the last steps (and short sums), one half after the other
     for (; s < steps; ++s) {
 #pragma unroll
       for (int i = 0; i < FM; ++i) multiply(f0, i);
 #pragma unroll
-      for (int i = 0; i < FM + FN; ++i) read(f0, s, 1, i);
+      for (int i = 0; i < FM + FN; ++i) read(f0, here, 1, i);
 #pragma unroll
       for (int i = 0; i < FM; ++i) multiply(f0, i);
       if (s + 1 == steps) break;
       wait_and_meet<0>();
-      if (s + 2 < steps) load_step(s + 2);
+      if (s + NST < steps) load_step(here, s + NST);
 #pragma unroll
-      for (int i = 0; i < FM + FN; ++i) read(f0, s + 1, 0, i);
+      for (int i = 0; i < FM + FN; ++i) read(f0, after, 0, i);
+      advance();
     }
     __syncthreads();
   }

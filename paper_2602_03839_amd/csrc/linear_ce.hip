@@ -506,16 +506,16 @@ constexpr uint32_t kFewTokens = 128;  // up to here G's rests are kept for all e
 // Tiles: vocabulary (or hidden) by tokens (or vocabulary).  The large ones reach the
 // matrix cores' rate where there are tiles enough for all CUs; the smaller ones fill
 // the chip with fewer and overlap one block's epilogue with another's loads.
-typedef Gemm<256, 256, 2, 4, false, false> LogitsL;
-typedef Gemm<256, 128, 4, 2, false, false> LogitsM;
-typedef Gemm<256, 64, 4, 1, false, false> LogitsS;
-typedef Gemm<256, 64, 4, 1, false, false, true> LogitsW;  // past the caches, for a weight larger than they are
-typedef Gemm<256, 256, 2, 4, true, false> DxL;
-typedef Gemm<256, 128, 4, 2, true, false> DxM;
-typedef Gemm<128, 64, 4, 1, true, false, true> DxS;
-typedef Gemm<256, 256, 2, 4, true, true> DwL;
-typedef Gemm<128, 128, 4, 2, true, true> DwM;
-typedef Gemm<128, 128, 2, 2, true, true> DwS;
+typedef Gemm<256, 256, 2, 4, 2, false, false> LogitsL;
+typedef Gemm<256, 128, 4, 2, 3, false, false> LogitsM;
+typedef Gemm<256, 64, 4, 1, 4, false, false> LogitsS;
+typedef Gemm<256, 64, 4, 1, 4, false, false, true> LogitsW;  // past the caches, for a weight larger than they are
+typedef Gemm<256, 256, 2, 4, 2, true, false> DxL;
+typedef Gemm<256, 128, 4, 2, 3, true, false> DxM;
+typedef Gemm<128, 64, 4, 1, 2, true, false, true> DxS;
+typedef Gemm<256, 256, 2, 4, 2, true, true> DwL;
+typedef Gemm<128, 128, 4, 2, 2, true, true> DwM;
+typedef Gemm<128, 128, 2, 2, 2, true, true> DwS;
 
 constexpr uint64_t kCacheBytes = 256ull << 20;  // of the last level
 constexpr uint64_t kMaxStride = 1u << 20;  // a tile's byte offsets stay in 32 bits
@@ -555,7 +555,7 @@ Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   const uint32_t pieces = parts(vocab, (uint32_t)(piece > vocab ? up(vocab, kVocabTile) : piece));
   q.piece = up(parts(vocab, pieces), kVocabTile);
   // few tokens: split dx's k until the blocks fill the chip
-  q.small = tokens <= kFewTokens || parts(q.ld, 256) * parts(q.piece, 256) < 256;
+  q.small = tokens <= 512 || parts(q.ld, 256) * parts(q.piece, 256) < 256;
   const uint32_t bm = tokens <= 64 ? DxS::BM : 256, bn = tokens <= 64 ? 64 : q.small ? 128 : 256;
   const uint32_t tiles = parts(q.ld, bm) * parts(tokens, bn);
   // (three of the small tiles fit a CU, one of the others)
