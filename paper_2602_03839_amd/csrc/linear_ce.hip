@@ -510,6 +510,7 @@ typedef Gemm<256, 256, 2, 4, 2, false, false> LogitsL;
 typedef Gemm<256, 128, 4, 2, 3, false, false> LogitsM;
 typedef Gemm<256, 64, 4, 1, 4, false, false> LogitsS;
 typedef Gemm<256, 64, 4, 1, 4, false, false, true> LogitsW;  // past the caches, for a weight larger than they are
+typedef Gemm<128, 64, 4, 1, 4, false, false> LogitsT;
 typedef Gemm<256, 256, 2, 4, 2, true, false> DxL;
 typedef Gemm<256, 128, 4, 2, 3, true, false> DxM;
 typedef Gemm<128, 64, 4, 1, 2, true, false, true> DxS;
@@ -545,7 +546,7 @@ Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   const uint32_t times = tokens <= kFewTokens ? 2 : 1;
   q.x = take((uint64_t)times * tokens * q.ld * 2);
   const uint64_t both = at;
-  q.part = take((uint64_t)tokens * parts(vocab, kVocabTile) * sizeof(float2));
+  q.part = take((uint64_t)tokens * parts(vocab, LogitsT::BM) * sizeof(float2));
   q.hit = take((uint64_t)tokens * sizeof(float));
   q.forward = at;
   at = both;
@@ -571,39 +572,51 @@ Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
 }
 
 template <typename T>
-void run_logits(LogitParams p, bool forward, hipStream_t stream) {
+uint32_t run_logits(LogitParams p, bool forward, hipStream_t stream) {
   p.tiles_m = parts(p.v_end - p.v_begin, T::BM);
   p.tiles_n = parts(p.tokens, T::BN);
   const dim3 grid(p.tiles_m * p.tiles_n), block(T::kThreads);
   if (forward) hipLaunchKernelGGL(ce_forward_kernel<T>, grid, block, 0, stream, p);
   else hipLaunchKernelGGL(ce_grad_kernel<T>, grid, block, 0, stream, p);
+  return T::BM;
 }
 
 // A block's time in thousands of cycles, for the choice of a tile: a fixed part (the first
-// loads and the epilogue) and one per step of 64 k, as measured alone on a CU.
+// loads and the epilogue) and one per step of 64 k, which grows as more CUs share
+// the L2s (the smaller a tile, the more it loads for its products).  Measured, one
+// launch of forward, us, L / M / S (T for the last):
+//   tokens 2048, 151936 x 896:  498 / 628 / 657     752, 3060 x 3008:  60 / 38 / 41
+//   589, 54805 x 5069 (padded): 250 / 568 / -       160, 310 x 1728:   40 / 28 / 23
+//   1024, 8192 x 4096:           86 /  60 / 67      926, 120888 x 64:  65 / 80 / 78
 struct TileCost {
-  uint32_t bn, slots;  // blocks that are on the chip at once
-  float fixed, step;
+  uint32_t bm, bn;
+  float fixed, step, shared;
 };
 
-float cost_of(const TileCost& c, uint32_t tiles_m, uint32_t tokens, uint32_t k) {
-  const uint32_t blocks = tiles_m * parts(tokens, c.bn);
-  return (float)parts(blocks, c.slots) * (c.fixed + c.step * (float)parts(k, kGemmK));
+float cost_of(const TileCost& c, uint32_t entries, uint32_t tokens, uint32_t k) {
+  constexpr float kCus = 256.0f;
+  const float blocks = (float)parts(entries, c.bm) * (float)parts(tokens, c.bn);
+  const float rounds = (float)(uint32_t)((blocks + kCus - 1) / kCus);
+  const float busy = blocks < kCus ? blocks / kCus : 1.0f;
+  return rounds * (c.fixed + (c.step + c.shared * busy) * (float)parts(k, kGemmK));
 }
 
-void run_logits(const LogitParams& p, bool forward, hipStream_t stream) {
-  if (p.tokens <= 64) {
-    if ((uint64_t)p.vocab * p.w_ld * 2 > kCacheBytes) run_logits<LogitsW>(p, forward, stream);
-    else run_logits<LogitsS>(p, forward, stream);
-    return;
+constexpr TileCost kCostL = {256, 256, 18.0f, 2.2f, 0.0f}, kCostM = {256, 128, 11.0f, 1.2f, 1.1f},
+                   kCostS = {256, 64, 8.0f, 1.5f, 0.7f}, kCostT = {128, 64, 6.0f, 0.9f, 0.6f};
+
+// Returns the tile's entries.
+uint32_t run_logits(const LogitParams& p, bool forward, hipStream_t stream) {
+  const uint32_t entries = p.v_end - p.v_begin;
+  const float s = cost_of(kCostS, entries, p.tokens, p.hidden), t = cost_of(kCostT, entries, p.tokens, p.hidden);
+  if (p.tokens > 64) {
+    const float l = cost_of(kCostL, entries, p.tokens, p.hidden), m = cost_of(kCostM, entries, p.tokens, p.hidden);
+    if (l <= m && l <= s && l <= t) return run_logits<LogitsL>(p, forward, stream);
+    if (m <= s && m <= t) return run_logits<LogitsM>(p, forward, stream);
   }
-  const uint32_t tiles_m = parts(p.v_end - p.v_begin, kVocabTile);
-  const float l = cost_of({256, 256, 18.0f, 2.2f}, tiles_m, p.tokens, p.hidden);
-  const float m = cost_of({128, 256, 11.0f, 1.3f}, tiles_m, p.tokens, p.hidden);
-  const float s = cost_of({64, 512, 12.0f, 1.5f}, tiles_m, p.tokens, p.hidden);
-  if (l <= m && l <= s) run_logits<LogitsL>(p, forward, stream);
-  else if (m <= s) run_logits<LogitsM>(p, forward, stream);
-  else run_logits<LogitsS>(p, forward, stream);
+  if (t < s) return run_logits<LogitsT>(p, forward, stream);
+  // a weight larger than the caches streams past them, if it is read once
+  if (p.tokens <= 64 && (uint64_t)p.vocab * p.w_ld * 2 > kCacheBytes) return run_logits<LogitsW>(p, forward, stream);
+  return run_logits<LogitsS>(p, forward, stream);
 }
 
 // dx's and dw's products of a piece.  One launch where both fit the chip at once
@@ -671,9 +684,9 @@ hipError_t launch_linear_ce(const LinearCeParams& c, char* ws, hipStream_t strea
   p.scale = c.logit_scale;
   p.part = (float2*)(ws + q.part);
   p.hit = (float*)(ws + q.hit);
-  run_logits(p, true, stream);
+  const uint32_t tile = run_logits(p, true, stream);
   hipLaunchKernelGGL(ce_join_kernel, dim3(parts(c.tokens, 4)), dim3(256), 0, stream, p.part, p.hit, c.targets,
-                     c.tokens, c.vocab, parts(c.vocab, kVocabTile), c.loss, c.lse);
+                     c.tokens, c.vocab, parts(c.vocab, tile), c.loss, c.lse);
   return hipGetLastError();
 }
 
