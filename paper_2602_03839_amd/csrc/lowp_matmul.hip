@@ -283,7 +283,7 @@ struct __attribute__((packed)) Bytes4 {
   uint32_t w;
 };
 
-// ---------------------------------------------------------------- up to 16 tokens
+// ---------------------------------------------------------------- slabs
 //
 // Codes through LDS.  A lane of the matrix instruction has its own row, so loading
 // codes where they are used reads 16 rows, 64 bytes of each, at a time: 4.4 to
@@ -373,7 +373,8 @@ __global__ __launch_bounds__(XREG ? 768 : 1024) void lowp_slab_kernel(LowpMatmul
   const uint32_t waves = z.wk * z.wr, kw = wave % z.wk, rw = wave / z.wk;
   const uint32_t r16 = lane & 15, g = lane >> 4;
   const uint32_t units = p.cols / U::kValues;
-  const uint32_t t = r16 < p.tokens ? r16 : p.tokens - 1;
+  const uint32_t t0 = blockIdx.y * 16, tokens = p.tokens - t0 < 16 ? p.tokens - t0 : 16;
+  const uint32_t t = r16 < tokens ? r16 : tokens - 1;
   f32x4_t* const s_part = (f32x4_t*)(s_lds + waves * z.depth * kSlabBytes);
   char* const s_x = (char*)(s_part + 2 * waves * 64);
   // bytes of a token's row in LDS, zeros from its end to the slab's; the 16 move each
@@ -387,7 +388,7 @@ __global__ __launch_bounds__(XREG ? 768 : 1024) void lowp_slab_kernel(LowpMatmul
       const uint32_t u = kw * kSlabUnits + g * 4 + s;
 #pragma unroll
       for (uint32_t f = 0; f < U::kFrags; ++f)
-        x[s][f] = u < units ? load16_any(p.x + t * p.x_stride + (uint64_t)u * U::kValues + 8 * f)
+        x[s][f] = u < units ? load16_any(p.x + (t0 + t) * p.x_stride + (uint64_t)u * U::kValues + 8 * f)
                             : make_uint4(0, 0, 0, 0);
     }
   }
@@ -395,10 +396,10 @@ __global__ __launch_bounds__(XREG ? 768 : 1024) void lowp_slab_kernel(LowpMatmul
   for (uint32_t i = 0; i < z.depth && in.more(); ++i) in.load();
   if constexpr (!XREG) {
     const uint32_t pieces = (ld - 16) / 16, filled = p.cols / 8;  // of 16 bytes, in a row
-    for (uint32_t i = threadIdx.x; i < p.tokens * pieces; i += blockDim.x) {
+    for (uint32_t i = threadIdx.x; i < tokens * pieces; i += blockDim.x) {
       const uint32_t row = i / pieces, c = i % pieces;
       *(uint4*)(s_x + row * ld + c * 16) =
-          c < filled ? load16_any(p.x + row * p.x_stride + c * 8) : make_uint4(0, 0, 0, 0);
+          c < filled ? load16_any(p.x + (t0 + row) * p.x_stride + c * 8) : make_uint4(0, 0, 0, 0);
     }
     __syncthreads();
   }
@@ -445,7 +446,7 @@ __global__ __launch_bounds__(XREG ? 768 : 1024) void lowp_slab_kernel(LowpMatmul
 #pragma unroll 5
       for (uint32_t w = 1; w < z.wk; ++w) acc += part[(rw * z.wk + w) * 64 + lane];
     }
-    if (tile < z.tiles) store_result(p, MX, acc, r16, (uint64_t)tile * 16 + 4 * g);
+    if (tile < z.tiles) store_result(p, MX, acc, t0 + r16, (uint64_t)tile * 16 + 4 * g);
   }
 }
 
@@ -468,17 +469,18 @@ void launch_shape(const LowpMatmulParams& p, hipStream_t stream) {
 constexpr uint32_t kLpCus = 256;
 constexpr uint32_t kLpLds = 160 * 1024;
 
-// Up to 16 tokens by slabs; false where that does not fit: rows that are not whole
+// Up to 64 tokens by slabs, 16 at a time (the weight is then read again, from the last
+// level cache if it fits there); false where that does not fit: rows that are not whole
 // groups of four units, other alignment, or too many values of the tokens.
 template <bool MX>
 bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
   typedef Unit<MX> U;
-  if (p.tokens > 16 || p.cols % U::kChunk || ((uintptr_t)p.codes & 15) || (MX && ((uintptr_t)p.scales & 3)))
+  if (p.tokens > 64 || p.cols % U::kChunk || ((uintptr_t)p.codes & 15) || (MX && ((uintptr_t)p.scales & 3)))
     return false;
   SlabShape z;
   z.tiles = (p.rows + 15) / 16;
   z.slabs = (p.cols / U::kValues + kSlabUnits - 1) / kSlabUnits;
-  const uint64_t x_bytes = p.tokens * ((uint64_t)z.slabs * kSlabUnits * U::kValues * 2 + 16);
+  const uint64_t x_bytes = (p.tokens < 16 ? p.tokens : 16) * ((uint64_t)z.slabs * kSlabUnits * U::kValues * 2 + 16);
   // the tokens in registers where a block's waves cover k; then as many rows of waves
   // as make twelve
   const bool xreg = z.slabs <= 12;
@@ -499,7 +501,7 @@ bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
   if (z.depth > 4) z.depth = 4;
   const uint32_t groups = (z.tiles + z.wr - 1) / z.wr;
   z.run = groups >= 16 * kLpCus ? 2 : 1;
-  const dim3 grid(groups < kLpCus ? groups : kLpCus), block(64 * waves);
+  const dim3 grid(groups < kLpCus ? groups : kLpCus, (p.tokens + 15) / 16), block(64 * waves);
   const size_t lds = (size_t)(rest + (uint64_t)z.depth * waves * kSlabBytes);
   if (xreg) hipLaunchKernelGGL((lowp_slab_kernel<MX, true>), grid, block, lds, stream, p, z);
   else hipLaunchKernelGGL((lowp_slab_kernel<MX, false>), grid, block, lds, stream, p, z);
