@@ -363,11 +363,12 @@ struct SlabStream {
   }
 };
 
-// XREG: each wave has one slab of k for good (slabs <= wk) and the tokens' values of
-// it in registers; otherwise all tokens' values lie in LDS.
-template <bool MX, bool XREG>
-__global__ __launch_bounds__(XREG ? 768 : 1024) void lowp_slab_kernel(LowpMatmulParams p, SlabShape z) {
+// NS > 0: each wave has up to NS slabs of k for good (slabs <= NS wk) and the tokens'
+// values of them in registers; otherwise all tokens' values lie in LDS.
+template <bool MX, int NS>
+__global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulParams p, SlabShape z) {
   typedef Unit<MX> U;
+  constexpr bool XREG = NS > 0;
   extern __shared__ char s_lds[];  // waves' slabs, [2][waves][64] parts, the tokens' rows
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t waves = z.wk * z.wr, kw = wave % z.wk, rw = wave / z.wk;
@@ -381,11 +382,11 @@ __global__ __launch_bounds__(XREG ? 768 : 1024) void lowp_slab_kernel(LowpMatmul
   // row to other banks
   const uint32_t ld = z.slabs * kSlabUnits * U::kValues * 2 + 16;
 
-  uint4 x[4][U::kFrags];
+  uint4 x[XREG ? 4 * NS : 1][U::kFrags];
   if constexpr (XREG) {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      const uint32_t u = kw * kSlabUnits + g * 4 + s;
+    for (int s = 0; s < 4 * NS; ++s) {
+      const uint32_t u = (kw + s / 4 * z.wk) * kSlabUnits + g * 4 + s % 4;
 #pragma unroll
       for (uint32_t f = 0; f < U::kFrags; ++f)
         x[s][f] = u < units ? load16_any(p.x + (t0 + t) * p.x_stride + (uint64_t)u * U::kValues + 8 * f)
@@ -407,7 +408,7 @@ __global__ __launch_bounds__(XREG ? 768 : 1024) void lowp_slab_kernel(LowpMatmul
   uint32_t slot = 0, turn = 0;
   for (uint32_t group = blockIdx.x * z.run; group * z.wr < z.tiles; group = in.after(group), ++turn) {
     f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (uint32_t slab = kw; slab < z.slabs; slab += z.wk) {
+    auto take = [&](uint32_t slab, int n) {
       in.wait();
       const char* const from = in.ring + slot * kSlabBytes;
       slot = slot + 1 == z.depth ? 0 : slot + 1;
@@ -427,12 +428,19 @@ __global__ __launch_bounds__(XREG ? 768 : 1024) void lowp_slab_kernel(LowpMatmul
 #pragma unroll
         for (uint32_t f = 0; f < U::kFrags; ++f) {
           uint4 v;
-          if constexpr (XREG) v = x[s][f];
+          if constexpr (XREG) v = x[n * 4 + s][f];
           else v = *(const uint4*)(s_x + t * ld + (slab * kSlabUnits + g * 4 + s) * (U::kValues * 2) + f * 16);
           acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<MX>(c[s], f, scale), __builtin_bit_cast(bf16x8_t, v),
                                                         acc, 0, 0, 0);
         }
       }
+    };
+    if constexpr (XREG) {
+#pragma unroll
+      for (int n = 0; n < NS; ++n)
+        if (kw + n * z.wk < z.slabs) take(kw + n * z.wk, n);
+    } else {
+      for (uint32_t slab = kw; slab < z.slabs; slab += z.wk) take(slab, 0);
     }
     const uint32_t tile = group * z.wr + rw;
     if (z.wk > 1) {
@@ -483,9 +491,10 @@ bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
   const uint64_t x_bytes = (p.tokens < 16 ? p.tokens : 16) * ((uint64_t)z.slabs * kSlabUnits * U::kValues * 2 + 16);
   // the tokens in registers where a block's waves cover k; then as many rows of waves
   // as make twelve
-  const bool xreg = z.slabs <= 12;
+  constexpr uint32_t kEach = MX ? 1 : 2;  // 64 registers of them
+  const bool xreg = z.slabs <= 12 * kEach;
   if (xreg) {
-    z.wk = z.slabs;
+    z.wk = z.slabs <= 12 ? z.slabs : (z.slabs + 1) / 2;
     z.wr = 12 / z.wk;
     while (z.wr > 1 && z.wr * kLpCus > z.tiles) --z.wr;
   } else {
@@ -503,8 +512,9 @@ bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
   z.run = groups >= 16 * kLpCus ? 2 : 1;
   const dim3 grid(groups < kLpCus ? groups : kLpCus, (p.tokens + 15) / 16), block(64 * waves);
   const size_t lds = (size_t)(rest + (uint64_t)z.depth * waves * kSlabBytes);
-  if (xreg) hipLaunchKernelGGL((lowp_slab_kernel<MX, true>), grid, block, lds, stream, p, z);
-  else hipLaunchKernelGGL((lowp_slab_kernel<MX, false>), grid, block, lds, stream, p, z);
+  if (xreg && z.slabs <= z.wk) hipLaunchKernelGGL((lowp_slab_kernel<MX, 1>), grid, block, lds, stream, p, z);
+  else if (xreg) hipLaunchKernelGGL((lowp_slab_kernel<MX, kEach>), grid, block, lds, stream, p, z);
+  else hipLaunchKernelGGL((lowp_slab_kernel<MX, 0>), grid, block, lds, stream, p, z);
   return true;
 }
 
