@@ -98,6 +98,8 @@ struct LinearCeGradParams {
 };
 
 hipError_t launch_zero_bytes(void* p, uint64_t bytes, hipStream_t stream);  // an even number of them
+uint64_t linear_ce_needs(uint32_t tokens, uint32_t vocab, uint32_t hidden);  // one call's workspace
+// a workspace for any call of up to `tokens` tokens
 uint64_t linear_ce_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden);
 hipError_t launch_linear_ce(const LinearCeParams& p, char* ws, hipStream_t stream);
 hipError_t launch_linear_ce_grad(const LinearCeGradParams& p, char* ws, hipStream_t stream);

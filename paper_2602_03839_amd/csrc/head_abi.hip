@@ -64,7 +64,7 @@ int check_ce(const char* who, const void* x, uint64_t x_stride, const void* weig
   if (!weight || !targets) return fail(PULSE_EINVAL, "%s: weight or targets is NULL", who);
   if (!aligned16(weight)) return fail(PULSE_EALIGN, "%s: weight not 16-byte aligned", who);
   if (!aligned(targets, 8)) return fail(PULSE_EALIGN, "%s: targets not 8-byte aligned", who);
-  return check_space(who, ws, ws_bytes, pulse::linear_ce_bytes(tokens, vocab, hidden));
+  return check_space(who, ws, ws_bytes, pulse::linear_ce_needs(tokens, vocab, hidden));
 }
 
 }  // namespace

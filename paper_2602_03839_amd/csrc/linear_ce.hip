@@ -501,6 +501,8 @@ uint32_t parts(uint64_t v, uint32_t of) { return (uint32_t)((v + of - 1) / of); 
 
 constexpr uint32_t kVocabTile = 256;
 constexpr uint32_t kBothBlocks = 512;
+constexpr uint32_t kSmallTokens = 512;  // up to here the gradient's products take the smaller tiles
+constexpr uint32_t kWantedTiles = 192;
 constexpr uint32_t kFewTokens = 128;  // up to here G's rests are kept for all entries
 
 // Tiles: vocabulary (or hidden) by tokens (or vocabulary).  The large ones reach the
@@ -556,11 +558,11 @@ Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   const uint32_t pieces = parts(vocab, (uint32_t)(piece > vocab ? up(vocab, kVocabTile) : piece));
   q.piece = up(parts(vocab, pieces), kVocabTile);
   // few tokens: split dx's k until the blocks fill the chip
-  q.small = tokens <= 512 || parts(q.ld, 256) * parts(q.piece, 256) < 256;
+  q.small = tokens <= kSmallTokens || parts(q.ld, 256) * parts(q.piece, 256) < 256;
   const uint32_t bm = tokens <= 64 ? DxS::BM : 256, bn = tokens <= 64 ? 64 : q.small ? 128 : 256;
   const uint32_t tiles = parts(q.ld, bm) * parts(tokens, bn);
   // (three of the small tiles fit a CU, one of the others)
-  const uint32_t wanted = tokens <= 64 ? 768 : 192;
+  const uint32_t wanted = tokens <= 64 ? 768 : kWantedTiles;
   q.splits = tiles < wanted ? wanted / tiles : 1;
   if (q.splits > q.piece / 256) q.splits = q.piece / 256;
   q.g = take((uint64_t)times * tokens * q.piece * 2);
@@ -651,8 +653,28 @@ hipError_t launch_zero_bytes(void* p, uint64_t bytes, hipStream_t stream) {
   return hipGetLastError();
 }
 
-uint64_t linear_ce_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
+uint64_t linear_ce_needs(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   return plan_of(tokens, vocab, hidden).total;
+}
+
+// What a plan needs does not grow with the tokens alone (its tiles, splits and
+// pieces change with them), so: the largest of every plan up to 512 tokens, and past
+// those a bound on each part.
+uint64_t linear_ce_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
+  uint64_t most = 0;
+  for (uint32_t t = 1; t <= tokens && t <= kSmallTokens; ++t) {
+    const uint64_t total = plan_of(t, vocab, hidden).total;
+    if (total > most) most = total;
+  }
+  if (tokens <= kSmallTokens) return most;
+  const uint64_t t = tokens, ld = up(hidden, 8), entries = up(vocab, kVocabTile);
+  const uint64_t g = t * entries * 2 < kPieceBytes ? t * entries * 2 : kPieceBytes + t * kVocabTile * 2;
+  // splits * tokens is at most the tokens, or the tiles wanted times a tile's tokens
+  const uint64_t sums = (t + (uint64_t)kWantedTiles * 256 / parts(ld, 256)) * ld * 4;
+  const uint64_t both = (hidden % 8 ? (uint64_t)vocab * ld * 2 : 0) + t * ld * 2;
+  const uint64_t forward = t * parts(vocab, LogitsT::BM) * sizeof(float2) + t * sizeof(float);
+  const uint64_t bound = both + (g + t * 8 + sums > forward ? g + t * 8 + sums : forward) + 16 * 256;
+  return bound > most ? bound : most;
 }
 
 hipError_t launch_linear_ce(const LinearCeParams& c, char* ws, hipStream_t stream) {

@@ -234,6 +234,20 @@ def test_views_streams_and_same_bits():
         assert (out[:, hidden:] == 7).all()
 
 
+@pytest.mark.parametrize("most", [65, 129, 513, 3000])
+def test_fewer_tokens_than_built_for(most):
+    """One object's workspace serves every smaller call."""
+    _, w, _, _ = inputs(1, 9000, 136, 1)
+    ce = head.LinearCE(w.cuda(), max_tokens=most)
+    for tokens in (1, 64, 65, 128, 129, 512, 513, most):
+        if tokens > most:
+            continue
+        x, _, y, dl = inputs(tokens, 9000, 136, tokens)
+        _, lse = ce.forward(x.cuda(), y.cuda())
+        ce.backward(x.cuda(), y.cuda(), lse, dl.cuda())
+    torch.cuda.synchronize()
+
+
 def test_no_tokens():
     _, w, _, _ = inputs(1, 64, 32, 1)
     ce = head.LinearCE(w.cuda(), max_tokens=0)

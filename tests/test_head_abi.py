@@ -111,6 +111,19 @@ def test_linear_ce_validation(L):
         refused(bwd(**k), status, L, word)
 
 
+def test_linear_ce_workspace_serves_fewer_tokens(L):
+    """The size for n tokens covers every call of fewer: each such call gets past the
+    workspace check (and stops at the missing loss, before any launch)."""
+    for vocab, hidden in ((1000, 64), (152064, 3584), (5003, 203), (40, 5120), (3_000_000, 128)):
+        for most in (1, 64, 100, 128, 129, 300, 513, 2000, 5000, 40000):
+            size = L.pulse_linear_ce_workspace_bytes(most, vocab, hidden)
+            for n in {1, 2, 33, 64, 65, 127, 128, 129, 200, 511, 512, 513, 700, 1023, 1999, 3333, 4097, 20011, most}:
+                if n > most:
+                    continue
+                rc = L.pulse_linear_ce_forward(A, hidden, A, A, n, vocab, hidden, 1.0, None, A, A, size, None)
+                refused(rc, EINVAL, L, b"loss")
+
+
 def test_lowp_matmul_validation(L):
     good = dict(dtype=MX, codes=A, scales=A, inv=1.0, rows=16, cols=64, x=A, xs=64, tokens=2, yd=F32, y=A, ys=16,
                 stream=None)
