@@ -1,14 +1,17 @@
 // lowp_matmul.hip -- y = x W^T for a few BF16 tokens x and a weight W that a
 // receiver holds as MXFP4 or FP8 codes.
 //
-// The codes are read once from HBM, which bounds the kernel: half a byte and a
+// The codes are read once from HBM, which bounds the kernels: half a byte and a
 // thirty-second of a byte of scale a value (MXFP4), or a byte (FP8).  A wave
-// takes 16 rows (times RT) and converts 16 bytes of each lane's codes to BF16
-// in registers: exact, since a code has at most 3 (FP8: 4) significant bits and
-// a power-of-two scale moves only the exponent.  v_mfma_f32_16x16x32_bf16
-// multiplies them with 16 tokens (times NT); its columns past the last token
-// are computed and dropped, which costs nothing here.  Products are exact in
-// FP32 and summed in FP32.
+// takes 16 rows and converts 16 bytes of each lane's codes to BF16 in registers:
+// exact, since a code has at most 3 (FP8: 4) significant bits and a power-of-two
+// scale moves only the exponent.  v_mfma_f32_16x16x32_bf16 multiplies them with 16
+// tokens; its columns past the last token are computed and dropped, which costs
+// nothing here.  Products are exact in FP32 and summed in FP32.
+//
+// Two kernels: the slab kernel below for rows of whole chunks, up to 64 tokens, whose
+// values fit LDS or registers (152,064 x 5,120 MXFP4, 1 and 16 tokens: 65 and 79 us,
+// 6.4 and 5.3 TB/s); and lowp_matmul_kernel for every other call.
 //
 // Any order of k serves a dot product as long as both operands use the same:
 // lane (row r, group g) holds one block of 32 values (FP8: 16) with one scale,
