@@ -31,10 +31,11 @@ struct Raw8 {
   uint4 v[sizeof(T) / 2];
 };
 
-template <typename T>
+template <bool STREAM, typename T>
 __device__ __forceinline__ void load8(const T* p, Raw8<T>& r) {
 #pragma unroll
-  for (size_t i = 0; i < sizeof(T) / 2; ++i) r.v[i] = load16(p + 16 / sizeof(T) * i);
+  for (size_t i = 0; i < sizeof(T) / 2; ++i)
+    r.v[i] = STREAM ? load16_stream(p + 16 / sizeof(T) * i) : load16(p + 16 / sizeof(T) * i);
 }
 
 __device__ __forceinline__ void unpack8(const Raw8<uint16_t>& r, float* v) {
@@ -84,13 +85,13 @@ struct Row {
   struct Raw {
     typename std::conditional<VEC, Raw8<T>, T>::type v[E / kStep];
   };
-  template <typename T>
+  template <bool STREAM, typename T>
   static __device__ __forceinline__ void load(const T* p, uint32_t cols, uint32_t t, Raw<T>& r) {
 #pragma unroll
     for (int j = 0; j < E / kStep; ++j) {
       const uint32_t c = at(j, t);
       if constexpr (VEC) {
-        if (c < cols) load8(p + c, r.v[j]);
+        if (c < cols) load8<STREAM>(p + c, r.v[j]);
         else
 #pragma unroll
           for (size_t i = 0; i < sizeof(T) / 2; ++i) r.v[j].v[i] = make_uint4(0, 0, 0, 0);
@@ -107,10 +108,10 @@ struct Row {
       else v[j] = from_bits(r.v[j]);
     }
   }
-  template <typename T>
+  template <bool STREAM, typename T>
   static __device__ __forceinline__ void load(const T* p, uint32_t cols, uint32_t t, float (&v)[E]) {
     Raw<T> r;
-    load(p, cols, t, r);
+    load<STREAM>(p, cols, t, r);
     unpack(r, v);
   }
   template <typename T>
@@ -129,8 +130,8 @@ struct Row {
   }
   static __device__ __forceinline__ void params(const void* p, int bf16, uint32_t cols, uint32_t t,
                                                 float (&v)[E]) {
-    if (bf16) load((const uint16_t*)p, cols, t, v);
-    else load((const float*)p, cols, t, v);
+    if (bf16) load<false>((const uint16_t*)p, cols, t, v);
+    else load<false>((const float*)p, cols, t, v);
   }
 };
 
@@ -164,7 +165,7 @@ __global__ __launch_bounds__(block_of(G)) void norm_kernel(NormParams p) {
   if (row >= p.rows) return;  // whole waves: G is 64 where a block has several rows
   const float inv_n = 1.0f / (float)p.cols;
   float v[E];
-  R::load((const T*)p.x + row * p.x_stride, p.cols, t, v);
+  R::template load<true>((const T*)p.x + row * p.x_stride, p.cols, t, v);
   float mean = 0.0f;
   if (p.mean) {
     float a = 0.0f;
@@ -234,8 +235,8 @@ __device__ __forceinline__ void grad_rows(const NormGradParams& p, uint64_t firs
   float nrstd = 0.0f, nmean = 0.0f;
   auto fetch = [&](uint64_t row) {
     if (row >= p.rows) row = p.rows - 1;
-    R::load((const T*)p.x + row * p.x_stride, p.cols, t, nx);
-    R::load((const T*)p.dy + row * p.dy_stride, p.cols, t, ndy);
+    R::template load<SUMS>((const T*)p.x + row * p.x_stride, p.cols, t, nx);
+    R::template load<SUMS>((const T*)p.dy + row * p.dy_stride, p.cols, t, ndy);
     nrstd = p.rstd[row];
     nmean = p.mean ? p.mean[row] : 0.0f;
   };
