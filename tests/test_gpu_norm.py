@@ -105,6 +105,21 @@ def test_row_counts(rows):
         near(db, edb, 1e-5, "dbias")
 
 
+@pytest.mark.parametrize("rows", [16383, 16385, 4097, 2049])
+def test_many_rows_forward(rows):
+    """Two rows a group of lanes, and an odd last one."""
+    for cols in (24, 700, 2000, 2500):
+        if rows * cols > 40_000_000:
+            continue
+        x = rows_of(rows, cols, torch.bfloat16, rows)
+        w, b = params(cols, torch.float32, 5, True)
+        y, mean, rstd = head.LayerNorm(w.cuda(), b.cuda())(x.cuda())
+        ey, em, er = exact_forward(x, w, b, 1e-6, False)
+        near(y, ey, TOL[torch.bfloat16], "y")
+        near(mean, em, 1e-5, "mean")
+        near(rstd, er, 1e-5, "rstd")
+
+
 def test_gradient_against_differences():
     """The formula's gradient against central differences of a 64-bit loss
     sum(dy * y): second order, so a step of 1e-4 leaves about 1e-7."""
