@@ -404,6 +404,115 @@ __global__ __launch_bounds__(TX::kThreads) void ce_both_kernel(GradParams x, Gra
   else dw_block<TW, RESTS>(w, lds, blockIdx.x - dx_blocks);
 }
 
+// dw for up to 64 tokens, where writing it bounds the time: a block keeps its 256
+// hidden columns of x in registers, for all k (the tokens twice, for G and its rests),
+// and runs on over the vocabulary, 64 entries at a time: the next tiles of G are on
+// their way while one is multiplied, turned into rows in LDS and stored.
+// 61 tokens, 152,064 x 5,120: NOW us (NOW TB/s of writes); 406 with a block a tile.
+constexpr int kRunN = 64, kRunRing = 4;
+
+__global__ __launch_bounds__(512) void ce_dw_run_kernel(GradParams p, uint32_t runs) {
+  typedef GemmTile<256, 8, true> A;  // of 64 k each
+  typedef GemmTile<kRunN, 8, true> B;
+  constexpr int kSlot = 2 * B::kBytes, kRowBytes = 256 * 2;
+  constexpr int kLoads = 2, kStores = kRunN * kRowBytes / 16 / 512;  // of a thread and tile
+  static_assert(B::kLoads == 1 && 2 * A::kBytes <= kRunRing * kSlot, "x passes through the ring");
+  __shared__ alignas(1024) char ring[kRunRing * kSlot];
+  __shared__ alignas(1024) char rows[kRunN * kRowBytes];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t tm, run;  // every column tile of a run side by side: whole rows of dw at a time
+  gemm_tile_of(blockIdx.x, p.tiles_m, runs, p.tiles_m, tm, run);
+  const uint32_t m0 = tm * 256, m_left = p.m - m0;
+  const uint32_t tiles = (p.n + kRunN - 1) / kRunN, each = (tiles + runs - 1) / runs;
+  const uint32_t first = run * each, count = first >= tiles ? 0 : tiles - first < each ? tiles - first : each;
+  if (count == 0) return;
+
+  // the wave's 32 columns of x: fragments of all four halves of k
+  bf16x8_t fa[4][2];
+  {
+    const GemmOperand x = {p.a.p + m0, p.a.ld, p.a.limit - m0};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int32_t left = (int32_t)p.k - 64 * h;
+      A::gather(x, ring + h * A::kBytes, wave, lane, [&](uint32_t k) { return (int32_t)k < left ? (int32_t)(64 * h + k) : -1; });
+    }
+    wait_and_meet<0>();
+    const uint32_t at = lds_address(ring) + A::lane_place(wave * 32, lane);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) fa[2 * h + ks][i] = A::fragment(at + h * A::kBytes, i, ks);
+    __syncthreads();
+  }
+
+  // rows of G past the last token meet zeros of x: any row will do
+  uint32_t off[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const uint32_t k = B::k_of(0, wave, lane), g = lane % (kRunN / 8);
+    const uint32_t row = 64 * h + k < p.k ? 64 * h + k : p.k - 1;
+    off[h] = (uint32_t)(row * p.b.ld * 2 + ((((g >> 1) ^ B::mix(k)) << 1 | (g & 1)) * 16));
+  }
+  auto load = [&](uint32_t tile) {  // the run's tile
+    char* const to = ring + tile % kRunRing * kSlot + wave * 1024;
+    const u32x4_t from = buffer_at(p.b.p + (uint64_t)(first + tile) * kRunN);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) load_to_lds<false>(to + h * B::kBytes, off[h], from);
+  };
+  for (uint32_t i = 0; i < kRunRing - 1 && i < count; ++i) load(i);
+  const uint32_t at_b = lds_address(ring) + B::lane_place(0, lane);
+  for (uint32_t i = 0; i < count; ++i) {
+    // tile i has landed.  After its loads came the stores of three tiles and the loads
+    // of two; near the ends there were fewer, so everything is waited for
+    if (i >= kRunRing - 1 && i + kRunRing - 1 < count) wait_and_meet<(kRunRing - 1) * kStores + (kRunRing - 2) * kLoads>();
+    else wait_and_meet<0>();
+    if (i + kRunRing - 1 < count) load(i + kRunRing - 1);  // where tile i - 1 was
+    f32x4_t acc[2][4];
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[m][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    const uint32_t at = at_b + i % kRunRing * kSlot;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (q * 32 >= (int)p.k) break;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const bf16x8_t b = B::fragment(at + q / 2 * B::kBytes, j, q % 2);
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+          acc[m][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[q][m], b, acc[m][j], 0, 0, 0);
+      }
+    }
+    // group c of row n lies at place c ^ (n & 15)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t n = j * 16 + (lane & 15);
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        const uint32_t c = wave * 32 + m * 16 + (lane >> 4) * 4;
+        uint2 o;
+        o.x = bf16x2_rne(__float_as_uint(acc[m][j][0]), __float_as_uint(acc[m][j][1]));
+        o.y = bf16x2_rne(__float_as_uint(acc[m][j][2]), __float_as_uint(acc[m][j][3]));
+        *(uint2*)(rows + n * kRowBytes + (((c >> 3) ^ (n & 15)) << 4) + (c & 4) * 2) = o;
+      }
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    const uint32_t n0 = (first + i) * kRunN;
+    uint16_t* const out = p.out + (uint64_t)n0 * p.out_ld + m0;
+#pragma unroll
+    for (int r = 0; r < kStores; ++r) {
+      const uint32_t q = threadIdx.x + r * 512, n = q / 32, c = q % 32;
+      const uint4 v = *(const uint4*)(rows + n * kRowBytes + ((c ^ (n & 15)) << 4));
+      // a wave always has a lane that stores, but for the vocabulary's last tile, after
+      // which nothing is counted
+      if (n0 + n < p.n && c * 8 < m_left) store16_stream(out + n * p.out_ld + c * 8, v);
+    }
+  }
+}
+
 // dx from the splits' sums and what the target's entry lost; a token without a target gets zeros.
 __global__ __launch_bounds__(256) void ce_dx_join_kernel(const float* sums, uint32_t splits, uint32_t tokens,
                                                          uint32_t ld, uint32_t hidden,
@@ -503,6 +612,7 @@ uint32_t parts(uint64_t v, uint32_t of) { return (uint32_t)((v + of - 1) / of); 
 
 constexpr uint32_t kVocabTile = 256;
 constexpr uint32_t kBothBlocks = 512;
+constexpr uint64_t kRunElements = 1ull << 26;  // of dw: 16 tiles of 64 entries for every CU
 constexpr uint32_t kSmallTokens = 512;  // up to here the gradient's products take the smaller tiles
 constexpr uint32_t kWantedTiles = 192;
 constexpr uint32_t kFewTokens = 128;  // up to here G's rests are kept for all entries
@@ -636,6 +746,13 @@ void run_products(GradParams x, uint32_t splits, GradParams w, hipStream_t strea
   // few tokens: bound by writing dw, so whole rows of it at a time
   w.band = RESTS ? kBand : w.tiles_m;
   const uint32_t nx = x.tiles_m * x.tiles_n * splits, nw = w.tiles_m * w.tiles_n;
+  if (w.k <= 128 && w.out_ld % 8 == 0 && (uint64_t)w.m * w.n >= kRunElements) {
+    w.tiles_m = parts(w.m, 256);
+    const uint32_t runs = w.tiles_m < 256 ? 256 / w.tiles_m : 1;
+    hipLaunchKernelGGL(ce_dx_kernel<TX>, dim3(nx), dim3(TX::kThreads), 0, stream, x);
+    hipLaunchKernelGGL(ce_dw_run_kernel, dim3(w.tiles_m * runs), dim3(512), 0, stream, w, runs);
+    return;
+  }
   if (nx + nw <= kBothBlocks) {
     hipLaunchKernelGGL((ce_both_kernel<TX, TW, RESTS>), dim3(nx + nw), dim3(TX::kThreads), 0, stream, x, w, nx);
     return;

@@ -95,7 +95,8 @@ def test_scales(scale):
 
 def test_several_pieces():
     """More vocabulary than one piece of G holds, and a short last piece."""
-    for tokens, vocab, hidden in ((40, 40000, 2048), (2100, 66000, 64), (2500, 70000, 520)):
+    for tokens, vocab, hidden in ((40, 40000, 2048), (2100, 66000, 64), (2500, 70000, 520),
+                                  (1, 90001, 776), (17, 66003, 1032), (64, 70000, 1024), (33, 300000, 264)):
         x, w, y, dl = inputs(tokens, vocab, hidden, 8)
         ce = head.LinearCE(w.cuda(), max_tokens=tokens)
         _, lse = ce.forward(x.cuda(), y.cuda())
