@@ -19,7 +19,7 @@
 // The three products of the backward pass and the one of the forward pass are
 // bound by the matrix cores for many tokens (4,096 at 152,064 x 3,584, 4.46 TFLOP
 // each: forward 3.5 ms, G 3.7, dx 3.6, dw 3.9), by the weight's bytes for few (61 at
-// 152,064 x 5,120, 1.56 GB: 297, 310 and 285 us to read it, 406 to write dw).
+// 152,064 x 5,120, 1.56 GB: 297, 310 and 285 us to read it, 303 to write dw).
 #include "device_common.hpp"
 #include "gemm_tile.hpp"
 #include "head.hpp"
@@ -408,7 +408,9 @@ __global__ __launch_bounds__(TX::kThreads) void ce_both_kernel(GradParams x, Gra
 // hidden columns of x in registers, for all k (the tokens twice, for G and its rests),
 // and runs on over the vocabulary, 64 entries at a time: the next tiles of G are on
 // their way while one is multiplied, turned into rows in LDS and stored.
-// 61 tokens, 152,064 x 5,120: NOW us (NOW TB/s of writes); 406 with a block a tile.
+// 61 tokens, 152,064 x 5,120: 303 us (5.1 TB/s of writes); 406 with a block a tile.
+// With a ring of 3 and two blocks a CU, forward and backward together took 1,181 us
+// to 1,154.
 constexpr int kRunN = 64, kRunRing = 4;
 
 __global__ __launch_bounds__(512) void ce_dw_run_kernel(GradParams p, uint32_t runs) {
