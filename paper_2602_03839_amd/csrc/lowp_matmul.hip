@@ -308,7 +308,14 @@ struct SlabShape {
   uint32_t run;            // groups of wr tiles that a block takes in a row
 };
 
-template <bool MX>
+// TIGHT: places are computed where they are used, since no registers are left to keep them in.
+template <bool TIGHT>
+__device__ __forceinline__ uint32_t afresh(uint32_t lane) {
+  if constexpr (TIGHT) asm volatile("" : "+v"(lane));
+  return lane;
+}
+
+template <bool MX, bool TIGHT>
 struct SlabStream {
   const LowpMatmulParams& p;
   const SlabShape& z;
@@ -331,6 +338,7 @@ struct SlabStream {
     const uint64_t first = (uint64_t)row0 * units + u0;
     char* const to = ring + slot * kSlabBytes;
     const u32x4_t codes = buffer_at(p.codes + first * 16);
+    const uint32_t lane = afresh<TIGHT>(this->lane);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       // what lies past the last row or the row's end is read from before it
@@ -367,36 +375,44 @@ struct SlabStream {
 };
 
 // NS > 0: each wave has up to NS slabs of k for good (slabs <= NS wk) and the tokens'
-// values of them in registers; otherwise all tokens' values lie in LDS.
-template <bool MX, int NS>
+// values of them in registers; otherwise all tokens' values lie in LDS.  A block
+// takes NT tiles of 16 tokens.
+template <bool MX, int NS, int NT>
 __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulParams p, SlabShape z) {
   typedef Unit<MX> U;
   constexpr bool XREG = NS > 0;
-  extern __shared__ char s_lds[];  // waves' slabs, [2][waves][64] parts, the tokens' rows
+  // units of a lane's codes, and parts of a sum, in registers at once
+  constexpr int kAtOnce = NT == 1 ? 4 : 2, kAdds = NT == 1 ? 5 : 2;
+  static_assert(XREG || NT == 1, "LDS holds one tile of tokens");
+  extern __shared__ char s_lds[];  // waves' slabs, [2][waves][NT][64] parts, the tokens' rows
   const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint32_t waves = z.wk * z.wr, kw = wave % z.wk, rw = wave / z.wk;
   const uint32_t r16 = lane & 15, g = lane >> 4;
   const uint32_t units = p.cols / U::kValues;
-  const uint32_t t0 = blockIdx.y * 16, tokens = p.tokens - t0 < 16 ? p.tokens - t0 : 16;
-  const uint32_t t = r16 < tokens ? r16 : tokens - 1;
+  const uint32_t t0 = blockIdx.y * 16 * NT, tokens = p.tokens - t0 < 16 * NT ? p.tokens - t0 : 16 * NT;
   f32x4_t* const s_part = (f32x4_t*)(s_lds + waves * z.depth * kSlabBytes);
-  char* const s_x = (char*)(s_part + 2 * waves * 64);
+  char* const s_x = (char*)(s_part + 2 * waves * NT * 64);
   // bytes of a token's row in LDS, zeros from its end to the slab's; the 16 move each
   // row to other banks
   const uint32_t ld = z.slabs * kSlabUnits * U::kValues * 2 + 16;
 
-  uint4 x[XREG ? 4 * NS : 1][U::kFrags];
-  if constexpr (XREG) {
+  uint4 x[NT][XREG ? 4 * NS : 1][U::kFrags];
+  uint32_t t[NT];  // the lane's token of each tile, or some other: its sums are dropped
 #pragma unroll
-    for (int s = 0; s < 4 * NS; ++s) {
-      const uint32_t u = (kw + s / 4 * z.wk) * kSlabUnits + g * 4 + s % 4;
+  for (int n = 0; n < NT; ++n) {
+    t[n] = n * 16 + r16 < tokens ? n * 16 + r16 : tokens - 1;
+    if constexpr (XREG) {
 #pragma unroll
-      for (uint32_t f = 0; f < U::kFrags; ++f)
-        x[s][f] = u < units ? load16_any(p.x + (t0 + t) * p.x_stride + (uint64_t)u * U::kValues + 8 * f)
-                            : make_uint4(0, 0, 0, 0);
+      for (int s = 0; s < 4 * NS; ++s) {
+        const uint32_t u = (kw + s / 4 * z.wk) * kSlabUnits + g * 4 + s % 4;
+#pragma unroll
+        for (uint32_t f = 0; f < U::kFrags; ++f)
+          x[n][s][f] = u < units ? load16_any(p.x + (t0 + t[n]) * p.x_stride + (uint64_t)u * U::kValues + 8 * f)
+                                 : make_uint4(0, 0, 0, 0);
+      }
     }
   }
-  SlabStream<MX> in = {p, z, s_lds + wave * z.depth * kSlabBytes, units, kw, rw, lane, blockIdx.x * z.run, kw};
+  SlabStream<MX, (NT > 1)> in = {p, z, s_lds + wave * z.depth * kSlabBytes, units, kw, rw, lane, blockIdx.x * z.run, kw};
   for (uint32_t i = 0; i < z.depth && in.more(); ++i) in.load();
   if constexpr (!XREG) {
     const uint32_t pieces = (ld - 16) / 16, filled = p.cols / 8;  // of 16 bytes, in a row
@@ -410,31 +426,41 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
 
   uint32_t slot = 0, turn = 0;
   for (uint32_t group = blockIdx.x * z.run; group * z.wr < z.tiles; group = in.after(group), ++turn) {
-    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto take = [&](uint32_t slab, int n) {
+    f32x4_t acc[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) acc[n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    auto take = [&](uint32_t slab, int own) {
       in.wait();
       const char* const from = in.ring + slot * kSlabBytes;
+      const uint32_t now = afresh<(NT > 1)>(lane), r16 = now & 15, g = now >> 4;
       slot = slot + 1 == z.depth ? 0 : slot + 1;
-      uint4 c[4];
-#pragma unroll
-      for (int s = 0; s < 4; ++s) c[s] = *(const uint4*)(from + r16 * 256 + (((g * 4 + s) ^ r16) << 4));
       uint32_t scales = 0;
       if constexpr (MX) scales = *(const uint32_t*)(from + 4096 + (r16 * 4 + g) * 4);
-      // the slab is in registers: its place is free for the next load
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-      if (in.more()) in.load();
       // past the row's end the tokens are zeros; the scale has to be finite there
       if (slab * kSlabUnits + g * 4 >= units) scales = 0x7F7F7F7Fu;
+      uint4 c[kAtOnce];
 #pragma unroll
       for (int s = 0; s < 4; ++s) {
+        if (s % kAtOnce == 0) {
+#pragma unroll
+          for (int i = 0; i < kAtOnce; ++i) c[i] = *(const uint4*)(from + r16 * 256 + (((g * 4 + s + i) ^ r16) << 4));
+          if (s + kAtOnce == 4) {
+            // the slab is in registers: its place is free for the next load
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            if (in.more()) in.load();
+          }
+        }
         const float scale = MX ? __uint_as_float((scales >> (8 * s) & 255u) << 23) : 1.0f;
 #pragma unroll
         for (uint32_t f = 0; f < U::kFrags; ++f) {
-          uint4 v;
-          if constexpr (XREG) v = x[n * 4 + s][f];
-          else v = *(const uint4*)(s_x + t * ld + (slab * kSlabUnits + g * 4 + s) * (U::kValues * 2) + f * 16);
-          acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(decode8<MX>(c[s], f, scale), __builtin_bit_cast(bf16x8_t, v),
-                                                        acc, 0, 0, 0);
+          const bf16x8_t a = decode8<MX>(c[s % kAtOnce], f, scale);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            uint4 v;
+            if constexpr (XREG) v = x[n][own * 4 + s][f];
+            else v = *(const uint4*)(s_x + t[n] * ld + (slab * kSlabUnits + g * 4 + s) * (U::kValues * 2) + f * 16);
+            acc[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, __builtin_bit_cast(bf16x8_t, v), acc[n], 0, 0, 0);
+          }
         }
       }
     };
@@ -446,18 +472,27 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
       for (uint32_t slab = kw; slab < z.slabs; slab += z.wk) take(slab, 0);
     }
     const uint32_t tile = group * z.wr + rw;
+    const uint32_t lane = afresh<(NT > 1)>(threadIdx.x & 63), r16 = lane & 15, g = lane >> 4;
     if (z.wk > 1) {
       // the parts of a tile are added by one of its waves, in turn; they are free again
       // after the next barrier but one
-      f32x4_t* const part = s_part + (turn & 1) * waves * 64;
-      part[wave * 64 + lane] = acc;
+      f32x4_t* const part = s_part + (turn & 1) * waves * NT * 64;
+#pragma unroll
+      for (int n = 0; n < NT; ++n) part[(wave * NT + n) * 64 + lane] = acc[n];
       __syncthreads();
-      if (turn % z.wk != kw) continue;
-      acc = part[rw * z.wk * 64 + lane];
-#pragma unroll 5
-      for (uint32_t w = 1; w < z.wk; ++w) acc += part[(rw * z.wk + w) * 64 + lane];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        if ((turn * NT + n) % z.wk != kw) continue;
+        acc[n] = part[(rw * z.wk * NT + n) * 64 + lane];
+#pragma unroll kAdds
+        for (uint32_t w = 1; w < z.wk; ++w) acc[n] += part[((rw * z.wk + w) * NT + n) * 64 + lane];
+        if (tile < z.tiles) store_result(p, MX, acc[n], t0 + n * 16 + r16, (uint64_t)tile * 16 + 4 * g);
+      }
+    } else if (tile < z.tiles) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+        store_result(p, MX, acc[n], t0 + n * 16 + r16, (uint64_t)tile * 16 + 4 * g);
     }
-    if (tile < z.tiles) store_result(p, MX, acc, t0 + r16, (uint64_t)tile * 16 + 4 * g);
   }
 }
 
@@ -480,7 +515,7 @@ void launch_shape(const LowpMatmulParams& p, hipStream_t stream) {
 constexpr uint32_t kLpCus = 256;
 constexpr uint32_t kLpLds = 160 * 1024;
 
-// Up to 64 tokens by slabs, 16 at a time (the weight is then read again, from the last
+// Up to 64 tokens by slabs, 16 or 32 at a time (the weight is then read again, from the last
 // level cache if it fits there); false where that does not fit: rows that are not whole
 // groups of four units, other alignment, or too many values of the tokens.
 template <bool MX>
@@ -507,17 +542,21 @@ bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
     z.wr = 1;
   }
   const uint32_t waves = z.wk * z.wr;
-  const uint64_t rest = (uint64_t)2 * waves * 64 * sizeof(f32x4_t) + (xreg ? 0 : x_bytes);
+  // two tiles of tokens where one would leave blocks waiting for a CU: 64 tokens, MXFP4,
+  // 152,064 x 5,120: 182 us (311 with one); 512 x 3,584, 128 blocks: 10 (7 with one)
+  const uint32_t groups = (z.tiles + z.wr - 1) / z.wr;
+  const uint32_t nt = xreg && p.tokens > 16 && groups * ((p.tokens + 15) / 16) > kLpCus ? 2 : 1;
+  const uint64_t rest = (uint64_t)2 * waves * nt * 64 * sizeof(f32x4_t) + (xreg ? 0 : x_bytes);
   if (rest + waves * kSlabBytes > kLpLds) return false;
   z.depth = (uint32_t)((kLpLds - rest) / (waves * kSlabBytes));
   if (z.depth > 4) z.depth = 4;
-  const uint32_t groups = (z.tiles + z.wr - 1) / z.wr;
   z.run = groups >= 16 * kLpCus ? 2 : 1;
-  const dim3 grid(groups < kLpCus ? groups : kLpCus, (p.tokens + 15) / 16), block(64 * waves);
+  const dim3 grid(groups < kLpCus ? groups : kLpCus, (p.tokens + 16 * nt - 1) / (16 * nt)), block(64 * waves);
   const size_t lds = (size_t)(rest + (uint64_t)z.depth * waves * kSlabBytes);
-  if (xreg && z.slabs <= z.wk) hipLaunchKernelGGL((lowp_slab_kernel<MX, 1>), grid, block, lds, stream, p, z);
-  else if (xreg) hipLaunchKernelGGL((lowp_slab_kernel<MX, kEach>), grid, block, lds, stream, p, z);
-  else hipLaunchKernelGGL((lowp_slab_kernel<MX, 0>), grid, block, lds, stream, p, z);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, lds, stream, p, z); };
+  if (!xreg) launch(lowp_slab_kernel<MX, 0, 1>);
+  else if (z.slabs <= z.wk) launch(nt == 1 ? lowp_slab_kernel<MX, 1, 1> : lowp_slab_kernel<MX, 1, 2>);
+  else launch(nt == 1 ? lowp_slab_kernel<MX, kEach, 1> : lowp_slab_kernel<MX, kEach, 2>);
   return true;
 }
 
@@ -526,7 +565,14 @@ void launch_type(const LowpMatmulParams& p, hipStream_t stream) {
   typedef Unit<MX> U;
   if (p.cols % U::kValues) return launch_shape<MX, 1, 1, true>(p, stream);
   if (launch_slabs<MX>(p, stream)) return;
-  if (p.tokens <= 16) launch_shape<MX, 1, 1, false>(p, stream);
+  // Each group of row tiles reads all tokens' values again, and a round of blocks takes as
+  // long as its last: as few groups as fit one round; of many rounds, two tiles each.  16
+  // tokens, MXFP4, in us with 1, 2 and 4 tiles: 5,120 x 27,648 (320 tiles) 75 and 51;
+  // 12,288 x 16,384 (768) 61 with 2, 47 with 4; one token, 40,000 x 5,056 (2,500) 33, 28, 33.
+  const uint32_t tiles = (p.rows + 15) / 16;
+  if (p.tokens <= 16 && tiles <= kLpCus) launch_shape<MX, 1, 1, false>(p, stream);
+  else if (p.tokens <= 16 && tiles > 2 * kLpCus && tiles <= 4 * kLpCus) launch_shape<MX, 4, 1, false>(p, stream);
+  else if (p.tokens <= 16) launch_shape<MX, 2, 1, false>(p, stream);
   else launch_shape<MX, 2, 2, false>(p, stream);
 }
 

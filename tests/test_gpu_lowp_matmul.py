@@ -79,6 +79,20 @@ def test_many_rows(dtype):
     check(dtype, 70001, 160, 33, torch.bfloat16, seed=4)
 
 
+@pytest.mark.parametrize("dtype", [MX, FP8])
+@pytest.mark.parametrize("rows,cols", [(4103, 128), (3001, 1152), (2500, 4224)])
+@pytest.mark.parametrize("tokens", [17, 32, 33, 47, 64])
+def test_more_tiles_than_cus_for_two_tiles_of_tokens(dtype, rows, cols, tokens):
+    check(dtype, rows, cols, tokens, seed=tokens)
+
+
+@pytest.mark.parametrize("dtype,cols", [(MX, 160), (MX, 224), (FP8, 80), (FP8, 208)])
+@pytest.mark.parametrize("rows", [4096, 4097, 5000, 8192, 8193, 9001, 16384, 16385])
+def test_tiles_of_a_block(dtype, cols, rows):
+    check(dtype, rows, cols, 5, seed=rows)
+    check(dtype, rows, cols, 16, torch.bfloat16, seed=rows + 1)
+
+
 @pytest.mark.parametrize("inv_scale", [1.0, 3.5, 1 / 3, 3584.0])
 def test_fp8_scale(inv_scale):
     check(FP8, 48, 256, 4, seed=9, inv_scale=inv_scale)
