@@ -9,7 +9,7 @@
 // tokens; its columns past the last token are computed and dropped, which costs
 // nothing here.  Products are exact in FP32 and summed in FP32.
 //
-// Two kernels: the slab kernel below for rows of whole chunks, up to 64 tokens, whose
+// Two kernels: the slab kernel below for rows of whole chunks (FP8: units), up to 64 tokens, whose
 // values fit LDS or registers (152,064 x 5,120 MXFP4, 1 and 16 tokens: 65 and 79 us,
 // 6.4 and 5.3 TB/s); and lowp_matmul_kernel for every other call.
 //
@@ -517,14 +517,22 @@ constexpr uint32_t kLpLds = 160 * 1024;
 
 // Up to 64 tokens by slabs, 16 or 32 at a time (the weight is then read again, from the last
 // level cache if it fits there); false where that does not fit: rows that are not whole
-// groups of four units, other alignment, or too many values of the tokens.
+// units (MXFP4, whose scales are loaded by fours: groups of four), other alignment, or too
+// many values of the tokens.  FP8 rows of whole units, 27,648 x 5,136, 1 and 64 tokens: 25
+// and 84 us (30 and 96 by the other kernel).
 template <bool MX>
 bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
   typedef Unit<MX> U;
-  if (p.tokens > 64 || p.cols % U::kChunk || ((uintptr_t)p.codes & 15) || (MX && ((uintptr_t)p.scales & 3)))
+  if (p.tokens > 64 || p.cols % (MX ? U::kChunk : U::kValues) || ((uintptr_t)p.codes & 15) ||
+      (MX && ((uintptr_t)p.scales & 3)))
     return false;
   SlabShape z;
   z.tiles = (p.rows + 15) / 16;
+  // a block with one tile or two loads its tokens for little: the other kernel's blocks,
+  // which take two tiles of each at once, are one round up to kLpCus tiles.  64 tokens,
+  // MXFP4, us by slabs and by the other: 2,048 x 3,584 11 and 12, 4,096 x 3,584 21 and 12.5,
+  // 8,192 x 3,584 25 and 21, 12,288 x 5,120 both 44
+  if (p.tokens > 32 && z.tiles > kLpCus / 2 && z.tiles <= 2 * kLpCus) return false;
   z.slabs = (p.cols / U::kValues + kSlabUnits - 1) / kSlabUnits;
   const uint64_t x_bytes = (p.tokens < 16 ? p.tokens : 16) * ((uint64_t)z.slabs * kSlabUnits * U::kValues * 2 + 16);
   // the tokens in registers where a block's waves cover k; then as many rows of waves

@@ -86,6 +86,13 @@ def test_more_tiles_than_cus_for_two_tiles_of_tokens(dtype, rows, cols, tokens):
     check(dtype, rows, cols, tokens, seed=tokens)
 
 
+@pytest.mark.parametrize("dtype", [MX, FP8])
+@pytest.mark.parametrize("rows,cols", [(2003, 1152), (2003, 4224), (8300, 640)])
+@pytest.mark.parametrize("tokens", [33, 47, 64])
+def test_two_groups_of_two_tiles_of_tokens(dtype, rows, cols, tokens):
+    check(dtype, rows, cols, tokens, seed=tokens)
+
+
 @pytest.mark.parametrize("dtype,cols", [(MX, 160), (MX, 224), (FP8, 80), (FP8, 208)])
 @pytest.mark.parametrize("rows", [4096, 4097, 5000, 8192, 8193, 9001, 16384, 16385])
 def test_tiles_of_a_block(dtype, cols, rows):
@@ -138,6 +145,16 @@ def test_nan_stays_with_its_row_and_token(dtype, cols):
     bad[:, rows_nan] = True
     bad[[3, 18]] = True
     assert np.array_equal(~torch.isfinite(got).numpy(), bad)
+
+
+@pytest.mark.parametrize("cols", [16, 80, 272])
+@pytest.mark.parametrize("tokens", [1, 20])
+def test_fp8_nan_at_the_end_of_a_row(cols, tokens):
+    codes, scales = weight(FP8, 70, cols, 3)
+    codes[34 * cols - 1] = 0x7F
+    x = torch.randn(tokens, cols, generator=torch.Generator().manual_seed(2)).bfloat16()
+    got = head.LowpLinear(FP8, codes, scales, 70, cols)(x.cuda()).cpu()
+    assert torch.isnan(got[:, 33]).all() and torch.isnan(got).sum() == tokens
 
 
 def test_views_and_streams():
