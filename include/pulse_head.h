@@ -16,8 +16,8 @@
  *   - outputs do not overlap inputs;
  *   - a workspace is 256-byte aligned, needs no initialisation, holds nothing
  *     between calls, and serves any calls ordered on one stream;
- *   - results are the same bits for the same inputs: no atomics, a fixed order
- *     of every sum.
+ *   - results are the same bits for the same inputs: every sum has a fixed
+ *     order.
  * Sums, statistics and products are accumulated in FP32.
  */
 #ifndef PULSE_HEAD_H
@@ -115,7 +115,11 @@ int pulse_linear_ce_forward(const uint16_t *x, uint64_t x_stride, const uint16_t
  * again and G[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - [v == targets[t]]) is
  * rounded to BF16 for the two products
  *   dx = logit_scale * G weight,   dweight = logit_scale * G^T x,
- * which are summed in FP32 and rounded once to BF16.
+ * which are summed in FP32 and rounded once to BF16.  What the rounding of G takes
+ * is added back: to dx from large entries one by one and from the others through a
+ * mean row of the weight, so that a direction which the weight's rows share cancels as
+ * in the exact sum; to dweight from the targets' entries, and up to 128 tokens from
+ * all.
  *   dx       BF16 [tokens, hidden], rows dx_stride apart.
  *   dweight  BF16 [vocab, hidden].
  */

@@ -10,11 +10,19 @@
 // computed again and turned into G[t][v] = g_t s (e^(z - lse) - [v = y_t]) in
 // BF16, and two products follow: dx += G W (FP32 sums, kept across pieces) and
 // dw = G^T X.  G of one piece is all that is ever stored, in BF16 since the
-// products need a BF16 operand.  A token's target entry is by far its largest, so
-// what that entry loses in the rounding (`rest`, FP32) is added back to both
-// products: rest W[y] to the token's dx, rest x to row y of dw.  The other
-// entries' roundings are relative to each and independent, and average out over
-// many tokens; for few, what they lose is kept as a second BF16 matrix for dw.
+// products need a BF16 operand.  What the rounding takes is added back:
+//   to dx, what the target's entry lost (`rest`, FP32) times W[y]; the same for every
+//     other entry that lost kLargeLoss of the token's dloss or more (at most 16, which
+//     have a sixteenth of the probability or more each); and what the others lost
+//     together times the mean of 64 rows of W.  The exact row of G sums to zero, so
+//     a direction that the rows of W share cancels in dx, but the rounded row does
+//     not: with rows 10 times as long as what they differ by and half the probability on
+//     one entry beside the target, dx was 0.009 off in the 2-norm, a token's 0.026
+//     (0.0017 and 0.0020 now, which is the rounding of dx itself);
+//   to dw, rest x in row y.  The other entries' roundings are relative to each and
+//     independent, and average out over many tokens; for few, what they lose is kept
+//     as a second BF16 matrix.  A row that one token's entry dominates, not its
+//     target, is left with the rounding of that entry beside its own (0.0024).
 //
 // The three products of the backward pass and the one of the forward pass are
 // bound by the matrix cores for many tokens (4,096 at 152,064 x 3,584, 4.46 TFLOP
@@ -30,6 +38,19 @@ namespace {
 
 constexpr uint32_t kBand = 8;  // tiles in m of a band: 32 CUs then work on 8 by 4
 constexpr float kLog2e = 1.4426950408889634f;
+
+// An entry of G that loses this share of |dloss| or more in the rounding is kept by itself:
+// BF16 takes at most 2^-8 of a value, so it has p >= 1/16, and a token has 16 at most.
+constexpr float kLargeLoss = 0x1p-12f;
+constexpr uint32_t kLargeLosses = 16;
+constexpr uint32_t kMeanRows = 64;  // of W, evenly spread, for the mean row: an eighth of a row off
+constexpr uint32_t kLostTile = 128;  // entries to a sum of losses: the smallest tile's
+
+// An entry of a token that is not its target, and what it lost in the rounding.
+struct LargeLoss {
+  int32_t v;
+  float lost;
+};
 
 // 2^x (v_exp_f32, 1 ulp).
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -69,6 +90,11 @@ struct LogitParams {
   uint16_t* g;  // [tokens][g_ld]
   uint64_t g_ld;
   float* rest;  // [tokens]: what the target's entry lost in the rounding
+  float* lost;  // [tokens][lost_ld]: what the other entries lost, by kLostTile of the vocabulary
+  uint32_t lost_ld;
+  uint32_t* large_count;  // [tokens]: of `large`, zero before the first piece; above
+                          // kLargeLosses, with an lse that is not the forward's, none count
+  LargeLoss* large;       // [tokens][kLargeLosses], in any order
   bool rest_rows;  // what every entry lost follows G, as as many rows again
 };
 
@@ -143,7 +169,9 @@ __global__ __launch_bounds__(T::kThreads) void ce_forward_kernel(LogitParams p) 
 
 template <typename T>
 __global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
-  __shared__ alignas(1024) char lds[T::kLds];
+  constexpr int kRows = T::BM * T::BN * 2, kSums = T::WM * T::BN * 4;  // of the results' way out
+  __shared__ alignas(1024) char lds[T::kLds > kRows + kSums ? T::kLds : kRows + kSums];
+  float(*const s_lost)[T::BN] = (float(*)[T::BN])(lds + kRows);  // [WM][BN]
   uint32_t tm, tn;
   gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, kBand, tm, tn);
   const uint32_t m0 = p.v_begin + tm * T::BM, n0 = tn * T::BN;
@@ -166,6 +194,17 @@ __global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
   }
   const uint32_t mine = m0 + T::m_of(0, lane, wave);  // the lane's entries: + 16 i + e
   int32_t at[T::FN];                                  // which of them is the target
+  auto rounded = [&](int i, int j) {
+    uint2 o;
+    o.x = bf16x2_rne(__float_as_uint(acc[i][j][0]), __float_as_uint(acc[i][j][1]));
+    o.y = bf16x2_rne(__float_as_uint(acc[i][j][2]), __float_as_uint(acc[i][j][3]));
+    return o;
+  };
+  auto losses = [&](int i, int j) {  // exact
+    const uint2 o = rounded(i, j);
+    return acc[i][j] - f32x4_t{__uint_as_float(o.x << 16), __uint_as_float(o.x & 0xFFFF0000u),
+                               __uint_as_float(o.y << 16), __uint_as_float(o.y & 0xFFFF0000u)};
+  };
 #pragma unroll
   for (int j = 0; j < T::FN; ++j) {
     at[j] = entry_of(y[j], mine, T::FM);
@@ -194,6 +233,17 @@ __global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
         for (int e = 0; e < 4; ++e)
           if (mine + i * 16 + e >= p.v_end) acc[i][j][e] = 0.0f;
     }
+    const uint32_t n = T::n_of(j, lane, wave);
+    float lost = 0.0f, most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < T::FM; ++i) {
+      const f32x4_t r = losses(i, j);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        lost += r[e];
+        most = __builtin_fmaxf(most, __builtin_fabsf(r[e]));
+      }
+    }
     if (any) {
       float rest = 0.0f;
 #pragma unroll
@@ -201,26 +251,57 @@ __global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) rest = at[j] == i * 16 + e ? acc[i][j][e] : rest;
       rest -= __uint_as_float(bf16x2_rne(__float_as_uint(rest), 0u) << 16);
-      if (at[j] >= 0) p.rest[n0 + T::n_of(j, lane, wave)] = rest;
+      if (at[j] >= 0) {
+        p.rest[n0 + n] = rest;
+        lost -= rest;
+      }
     }
+    const float large = kLargeLoss * __builtin_fabsf(by[j]);
+    if (__builtin_amdgcn_ballot_w64(most >= large && most > 0.0f)) {
+      uint32_t which = 0;
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i) {
+        const f32x4_t r = losses(i, j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float size = __builtin_fabsf(r[e]);
+          which |= (uint32_t)(size >= large && size > 0.0f && at[j] != i * 16 + e) << (i * 4 + e);
+        }
+      }
+      uint32_t slot = which ? atomicAdd(p.large_count + n0 + n, (uint32_t)__builtin_popcount(which)) : 0;
+      for (; which && slot < kLargeLosses; ++slot) {
+        const int k = __builtin_ctz(which);
+        which &= which - 1;
+        float r = 0.0f;
+#pragma unroll
+        for (int i = 0; i < T::FM; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) r = k == i * 4 + e ? acc[i][j][e] : r;
+        r -= __uint_as_float(bf16x2_rne(__float_as_uint(r), 0u) << 16);
+        p.large[(uint64_t)(n0 + n) * kLargeLosses + slot] = {(int32_t)(mine + (k >> 2) * 16 + (k & 3)), r};
+      }
+    }
+    lost += __shfl_xor(lost, 16);
+    lost += __shfl_xor(lost, 32);
+    if (lane < 16) s_lost[wave / T::WN][n] = lost;
   }
-  auto rounded = [&](int i, int j) {
-    uint2 o;
-    o.x = bf16x2_rne(__float_as_uint(acc[i][j][0]), __float_as_uint(acc[i][j][1]));
-    o.y = bf16x2_rne(__float_as_uint(acc[i][j][2]), __float_as_uint(acc[i][j][3]));
-    return o;
-  };
   uint16_t* const out = p.g + n0 * p.g_ld + (m0 - p.v_begin);
-  T::template store_rows<false, true>(lds, out, p.g_ld, T::BM, p.tokens - n0, rounded);
+  T::template store_rows<false, true>(lds, out, p.g_ld, T::BM, p.tokens - n0, rounded);  // meets between
+  for (uint32_t n = threadIdx.x; n < T::BN; n += T::kThreads) {
+    float lost = 0.0f;
+#pragma unroll
+    for (int w = 0; w < T::WM; ++w) lost += s_lost[w][n];
+    if (n0 + n >= p.tokens) continue;
+    const uint32_t slot = m0 / kLostTile;
+    float* const to = p.lost + (uint64_t)(n0 + n) * p.lost_ld + slot;
+    to[0] = lost;
+    if (T::BM > kLostTile && slot + 1 < p.lost_ld) to[1] = 0.0f;  // the tile's other half
+  }
   if (p.rest_rows) {  // few tokens: the rests of all entries, as rows of their own
     __syncthreads();
     T::template store_rows<false, true>(lds, out + (uint64_t)p.tokens * p.g_ld, p.g_ld, T::BM, p.tokens - n0,
                                   [&](int i, int j) {
-                                    const uint2 o = rounded(i, j);
-                                    acc[i][j][0] -= __uint_as_float(o.x << 16);
-                                    acc[i][j][1] -= __uint_as_float(o.x & 0xFFFF0000u);
-                                    acc[i][j][2] -= __uint_as_float(o.y << 16);
-                                    acc[i][j][3] -= __uint_as_float(o.y & 0xFFFF0000u);
+                                    acc[i][j] = losses(i, j);
                                     return rounded(i, j);
                                   });
   }
@@ -515,31 +596,71 @@ __global__ __launch_bounds__(512) void ce_dw_run_kernel(GradParams p, uint32_t r
   }
 }
 
-// dx from the splits' sums and what the target's entry lost; a token without a target gets zeros.
-__global__ __launch_bounds__(256) void ce_dx_join_kernel(const float* sums, uint32_t splits, uint32_t tokens,
-                                                         uint32_t ld, uint32_t hidden,
-                                                         const int64_t* targets, uint32_t vocab,
-                                                         const uint16_t* w, uint64_t w_ld,
-                                                         const float* rest, uint16_t* dx,
-                                                         uint64_t dx_ld) {
+struct DxJoinParams {
+  const float* sums;  // [splits][tokens][ld]
+  uint32_t splits, tokens, ld, hidden;
+  const int64_t* targets;
+  uint32_t vocab;
+  const uint16_t* w;
+  uint64_t w_ld;
+  const float* rest;
+  const float* lost;
+  uint32_t lost_ld;
+  const uint32_t* large_count;
+  const LargeLoss* large;
+  const float* mean;  // [ld]: W's mean row
+  uint16_t* dx;
+  uint64_t dx_ld;
+};
+
+// dx from the splits' sums and what G's rounding took; a token without a target gets zeros.
+__global__ __launch_bounds__(256) void ce_dx_join_kernel(DxJoinParams p) {
+  __shared__ float s_lost[4];
+  __shared__ LargeLoss s_large[kLargeLosses];
   const uint32_t t = blockIdx.x;
   const uint32_t c = (blockIdx.y * 256 + threadIdx.x) * 4;
-  if (c >= ld) return;
-  const int64_t y = targets[t];
+  const int64_t y = p.targets[t];
   f32x4_t a = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (y >= 0 && y < (int64_t)vocab) {
-    const uint2 v = *(const uint2*)(w + y * w_ld + c);
+  if (y >= 0 && y < (int64_t)p.vocab) {  // the whole block
+    float lost = 0.0f;
+    for (uint32_t i = threadIdx.x; i < p.lost_ld; i += 256) lost += p.lost[(uint64_t)t * p.lost_ld + i];
+    lost = wave_sum(lost);
+    if ((threadIdx.x & 63) == 0) s_lost[threadIdx.x >> 6] = lost;
+    const uint32_t listed = p.large_count[t], count = listed > kLargeLosses ? 0 : listed;
+    if (threadIdx.x < 64) {  // in the order of the vocabulary, whatever order they were written in
+      const LargeLoss mine = threadIdx.x < count ? p.large[(uint64_t)t * kLargeLosses + threadIdx.x]
+                                                 : LargeLoss{0x7FFFFFFF, 0.0f};
+      uint32_t place = 0;
+#pragma unroll
+      for (uint32_t i = 0; i < kLargeLosses; ++i) place += __builtin_amdgcn_readlane(mine.v, i) < mine.v;
+      if (threadIdx.x < count) s_large[place] = mine;
+    }
+    __syncthreads();
+    lost = (s_lost[0] + s_lost[1]) + (s_lost[2] + s_lost[3]);
+    if (c >= p.ld) return;
+    auto add = [&](float by, const uint16_t* row) {
+      const uint2 v = *(const uint2*)(row + c);
+      a[0] = __builtin_fmaf(by, __uint_as_float(v.x << 16), a[0]);
+      a[1] = __builtin_fmaf(by, __uint_as_float(v.x & 0xFFFF0000u), a[1]);
+      a[2] = __builtin_fmaf(by, __uint_as_float(v.y << 16), a[2]);
+      a[3] = __builtin_fmaf(by, __uint_as_float(v.y & 0xFFFF0000u), a[3]);
+    };
 #pragma unroll 8
-    for (uint32_t s = 0; s < splits; ++s) a += *(const f32x4_t*)(sums + ((uint64_t)s * tokens + t) * ld + c);
-    const float r = rest[t];
-    a[0] = __builtin_fmaf(r, __uint_as_float(v.x << 16), a[0]);
-    a[1] = __builtin_fmaf(r, __uint_as_float(v.x & 0xFFFF0000u), a[1]);
-    a[2] = __builtin_fmaf(r, __uint_as_float(v.y << 16), a[2]);
-    a[3] = __builtin_fmaf(r, __uint_as_float(v.y & 0xFFFF0000u), a[3]);
+    for (uint32_t s = 0; s < p.splits; ++s)
+      a += *(const f32x4_t*)(p.sums + ((uint64_t)s * p.tokens + t) * p.ld + c);
+    add(p.rest[t], p.w + y * p.w_ld);
+#pragma unroll 4
+    for (uint32_t k = 0; k < count; ++k) {
+      lost -= s_large[k].lost;
+      add(s_large[k].lost, p.w + (uint64_t)s_large[k].v * p.w_ld);
+    }
+    const f32x4_t mean = *(const f32x4_t*)(p.mean + c);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a[e] = __builtin_fmaf(lost, mean[e], a[e]);
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (c + e < hidden) dx[t * dx_ld + c + e] = (uint16_t)bf16x2_rne(__float_as_uint(a[e]), 0u);
+    if (c + e < p.hidden) p.dx[t * p.dx_ld + c + e] = (uint16_t)bf16x2_rne(__float_as_uint(a[e]), 0u);
 }
 
 // ---------------------------------------------------------------- copies
@@ -559,30 +680,67 @@ struct PrepareParams {
   const int64_t* targets;  // null, or: rows of x without a target become zeros, as
   uint32_t vocab;          // what is in them must not reach the other rows' sums;
   int32_t* y;              // and the targets as 32 bits, -1 for none
+  uint32_t* zero;          // with targets: [rows of x], set to zero
+  float* mean;             // null, or: [ld] to take the mean row of `mean_of`
+  const uint16_t* mean_of;  // [vocab] rows, mean_ld apart
+  uint64_t mean_ld;
+  uint32_t mean_blocks;  // the first ones: 64 columns each
 };
+
+// 8 elements of a row from its column c on, zeros past its end.
+__device__ __forceinline__ uint4 load_group(const uint16_t* row, uint32_t c, uint32_t cols) {
+  if (c + 8 <= cols) return load16_any(row + c);
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (c + e < cols) w[e >> 1] |= (uint32_t)row[c + e] << (16 * (e & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The mean of kMeanRows rows (all, if there are fewer), 64 columns a block; zero in a
+// column where it is not finite.
+__device__ __forceinline__ void mean_row(const PrepareParams& p) {
+  __shared__ float s[32][64];
+  const uint32_t group = threadIdx.x & 7, first = threadIdx.x >> 3, c = blockIdx.x * 64 + group * 8;
+  const uint32_t rows = p.vocab < kMeanRows ? p.vocab : kMeanRows;
+  float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+  for (uint32_t i = 0; i < kMeanRows / 32; ++i) {
+    const uint32_t r = first + i * 32;
+    const uint64_t row = rows < kMeanRows ? r : (uint64_t)r * p.vocab / kMeanRows;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (r < rows) v = load_group(p.mean_of + row * p.mean_ld, c, p.cols);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sum[2 * e] += __uint_as_float(get_u32(v, e) << 16);
+      sum[2 * e + 1] += __uint_as_float(get_u32(v, e) & 0xFFFF0000u);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s[first][group * 8 + e] = sum[e];
+  __syncthreads();
+  const uint32_t at = blockIdx.x * 64 + threadIdx.x;
+  if (threadIdx.x >= 64 || at >= p.ld) return;
+  float mean = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 32; ++i) mean += s[i][threadIdx.x];
+  mean /= (float)rows;
+  p.mean[at] = mean - mean == 0.0f ? mean : 0.0f;
+}
 
 __device__ __forceinline__ void copy_group(const CopyJob& j, uint32_t cols, uint32_t ld, uint64_t r, uint32_t c,
                                            bool kept) {
   uint4 v = make_uint4(0, 0, 0, 0);
-  if (kept) {
-    const uint16_t* p = j.from + r * j.from_ld + c;
-    if (c + 8 <= cols) {
-      v = load16_any(p);
-    } else {
-      uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (c + e < cols) w[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
-      v = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-  }
+  if (kept) v = load_group(j.from + r * j.from_ld, c, cols);
   for (uint32_t k = 0; k < j.times; ++k) store16(j.to + (k * j.rows + r) * ld + c, v);
 }
 
 __global__ __launch_bounds__(256) void ce_prepare_kernel(PrepareParams p) {
+  if (blockIdx.x < p.mean_blocks) return mean_row(p);
+  const uint32_t block = blockIdx.x - p.mean_blocks, blocks = gridDim.x - p.mean_blocks;
   const uint64_t groups = p.ld / 8;  // of 8 elements, in a row
   const uint64_t nx = p.x.from ? p.x.rows * groups : 0, all = nx + (p.w.from ? p.w.rows * groups : 0);
-  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
+  for (uint64_t i = (uint64_t)block * 256 + threadIdx.x; i < all; i += (uint64_t)blocks * 256) {
     if (i >= nx) {
       copy_group(p.w, p.cols, p.ld, (i - nx) / groups, (uint32_t)((i - nx) % groups) * 8, true);
       continue;
@@ -593,18 +751,22 @@ __global__ __launch_bounds__(256) void ce_prepare_kernel(PrepareParams p) {
     if (p.targets) {
       const int64_t y = p.targets[r];
       kept = y >= 0 && y < (int64_t)p.vocab;
-      if (c == 0) p.y[r] = kept ? (int32_t)y : -1;
+      if (c == 0) {
+        p.y[r] = kept ? (int32_t)y : -1;
+        p.zero[r] = 0;
+      }
     }
     copy_group(p.x, p.cols, p.ld, r, c, kept);
   }
 }
 
-void prepare(const PrepareParams& p, hipStream_t stream) {
+void prepare(PrepareParams p, hipStream_t stream) {
   const uint64_t rows = (p.x.from ? p.x.rows : 0) + (p.w.from ? p.w.rows : 0);
   if (rows == 0) return;
   uint64_t blocks = (rows * (p.ld / 8) + 255) / 256;
   if (blocks > 8192) blocks = 8192;
-  hipLaunchKernelGGL(ce_prepare_kernel, dim3((uint32_t)blocks), dim3(256), 0, stream, p);
+  p.mean_blocks = p.mean ? (p.ld + 63) / 64 : 0;
+  hipLaunchKernelGGL(ce_prepare_kernel, dim3((uint32_t)blocks + p.mean_blocks), dim3(256), 0, stream, p);
 }
 
 // ---------------------------------------------------------------- shapes
@@ -645,7 +807,7 @@ struct Plan {
   uint32_t splits;  // of dx's k
   bool small;       // the products in the smaller tiles
   // byte offsets in the workspace
-  uint64_t w, x, part, hit, g, y, rest, sums, forward, total;
+  uint64_t w, x, part, hit, g, y, rest, sums, lost, large_count, large, mean, forward, total;
 };
 
 Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
@@ -683,6 +845,10 @@ Plan plan_of(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   q.y = take((uint64_t)tokens * sizeof(int32_t));
   q.rest = take((uint64_t)tokens * sizeof(float));
   q.sums = take((uint64_t)q.splits * tokens * q.ld * 4);
+  q.lost = take((uint64_t)tokens * parts(vocab, kLostTile) * sizeof(float));
+  q.large_count = take((uint64_t)tokens * sizeof(uint32_t));
+  q.large = take((uint64_t)tokens * kLargeLosses * sizeof(LargeLoss));
+  q.mean = take((uint64_t)q.ld * sizeof(float));
   q.total = at > q.forward ? at : q.forward;
   return q;
 }
@@ -794,7 +960,9 @@ uint64_t linear_ce_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   const uint64_t sums = (t + (uint64_t)kWantedTiles * 256 / parts(ld, 256)) * ld * 4;
   const uint64_t both = (hidden % 8 ? (uint64_t)vocab * ld * 2 : 0) + t * ld * 2;
   const uint64_t forward = t * parts(vocab, LogitsT::BM) * sizeof(float2) + t * sizeof(float);
-  const uint64_t bound = both + (g + t * 8 + sums > forward ? g + t * 8 + sums : forward) + 16 * 256;
+  const uint64_t lost = t * (parts(vocab, kLostTile) * sizeof(float) + 4 + kLargeLosses * sizeof(LargeLoss)) + ld * 4;
+  const uint64_t backward = g + t * 8 + sums + lost;
+  const uint64_t bound = both + (backward > forward ? backward : forward) + 16 * 256;
   return bound > most ? bound : most;
 }
 
@@ -854,6 +1022,10 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
   r.targets = c.targets;
   r.vocab = c.vocab;
   r.y = y;
+  r.zero = (uint32_t*)(ws + q.large_count);
+  r.mean = (float*)(ws + q.mean);
+  r.mean_of = c.weight;
+  r.mean_ld = c.hidden;
   prepare(r, stream);
   p.x = r.x.to;
   p.x_ld = q.ld;
@@ -867,6 +1039,10 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
   p.g = (uint16_t*)(ws + q.g);
   p.g_ld = q.piece;
   p.rest = (float*)(ws + q.rest);
+  p.lost = (float*)(ws + q.lost);
+  p.lost_ld = parts(c.vocab, kLostTile);
+  p.large_count = r.zero;
+  p.large = (LargeLoss*)(ws + q.large);
   p.rest_rows = few;
   float* sums = (float*)(ws + q.sums);
   for (uint32_t v = 0; v < c.vocab; v += q.piece) {
@@ -901,8 +1077,9 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
     else if (q.small) run_products<DxM, DwM, true>(d, splits, e, stream);
     else run_products<DxL, DwL, true>(d, splits, e, stream);
   }
-  hipLaunchKernelGGL(ce_dx_join_kernel, dim3(c.tokens, parts(q.ld, 1024)), dim3(256), 0, stream, sums, q.splits,
-                     c.tokens, q.ld, c.hidden, c.targets, c.vocab, p.w, p.w_ld, p.rest, c.dx, c.dx_stride);
+  const DxJoinParams j = {sums, q.splits, c.tokens, q.ld, c.hidden, c.targets, c.vocab, p.w, p.w_ld, p.rest, p.lost,
+                          p.lost_ld, p.large_count, p.large, r.mean, c.dx, c.dx_stride};
+  hipLaunchKernelGGL(ce_dx_join_kernel, dim3(c.tokens, parts(q.ld, 1024)), dim3(256), 0, stream, j);
   return hipGetLastError();
 }
 

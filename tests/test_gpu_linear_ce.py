@@ -136,6 +136,60 @@ def test_precision_of_few_and_many_tokens():
             assert (got.cpu().double() - want).norm() <= 0.002 * want.norm(), tokens
 
 
+@pytest.mark.parametrize("tokens,vocab,hidden", [(40, 20000, 256), (100, 5003, 203), (200, 20000, 256), (600, 9001, 320),
+                                                 (2100, 9000, 256)])
+@pytest.mark.parametrize("shared", [0, 3, 10])
+@pytest.mark.parametrize("sure", [0, 3])
+def test_precision_where_rows_share_a_direction(tokens, vocab, hidden, shared, sure):
+    """Rows of the head that share a direction, several times as long as what they
+    differ by, as trained ones do, and (`sure`) most of the probability on one
+    entry that is not the target.  A row of G sums to zero, so the shared direction cancels in
+    dx: what G's rounding loses must not bring it back.
+
+    dx's own rounding to BF16 is off by up to 2^-8 of each value, 0.0017 in the
+    2-norm and 0.0020 for a token's row.  What may be left of G's: entries that lose at most
+    2^-12 of the token's dloss, so are at most an eighth of it, with uniform errors:
+    in the 2-norm 2^-8 sqrt(1/8 / 3) = 0.0008 of a row's unshared part.  Together
+    0.0019 over all, 0.0022 for a token."""
+    g = torch.Generator().manual_seed(tokens + shared + sure)
+    w = torch.randn(vocab, hidden, generator=g) * 2 / hidden ** 0.5
+    d = torch.randn(hidden, generator=g)
+    d /= d.norm()
+    w = (w + 2 * shared * d).bfloat16()
+    y, other = torch.randint(vocab, (tokens,), generator=g), torch.randint(vocab, (tokens,), generator=g)
+    x = torch.randn(tokens, hidden, generator=g)
+    x += 2 * torch.rand(tokens, 1, generator=g) * w[y] + sure * w[other]
+    x = (x - (x @ d)[:, None] * d).bfloat16()  # along d it would only move the token's lse
+    dl = torch.randn(tokens, generator=g) / tokens
+    ce = head.LinearCE(w.cuda(), max_tokens=tokens)
+    _, lse = ce.forward(x.cuda(), y.cuda())
+    dx, _ = ce.backward(x.cuda(), y.cuda(), lse, dl.cuda())
+    want = exact(x, w, y, dl, 1.0)[3] @ w.double()
+    assert torch.equal(dx, ce.backward(x.cuda(), y.cuda(), lse, dl.cuda())[0])
+    off = dx.cpu().double() - want
+    each = off.norm(dim=1) / want.norm(dim=1)
+    print(f"off by {(off.norm() / want.norm()).item():.5f}, a token by {each.max().item():.5f}")
+    assert off.norm() <= 0.002 * want.norm() and each.max() <= 0.0025
+
+
+@pytest.mark.parametrize("tokens", [20, 300])
+def test_gradient_for_a_smaller_lse(tokens):
+    """With an lse below the forward's the entries of G are no probabilities: any
+    number of a token's may be large.  The definition holds, and the bits repeat."""
+    x, w, y, dl = inputs(tokens, 900, 64, tokens, ignored=0.0)
+    ce = head.LinearCE(w.cuda(), max_tokens=tokens)
+    lse = ce.forward(x.cuda(), y.cuda())[1] - 5
+    dx, dw = ce.backward(x.cuda(), y.cuda(), lse, dl.cuda())
+    for again, first in zip(ce.backward(x.cuda(), y.cuda(), lse, dl.cuda()), (dx, dw)):
+        assert torch.equal(again, first)
+    g = torch.exp(x.double() @ w.double().t() - lse.cpu().double()[:, None])
+    g[torch.arange(tokens), y] -= 1
+    g *= dl.double()[:, None]
+    # G's and the result's roundings, each at most 2^-8; the exponents' errors are below 2^-16
+    for got, want, size in ((dx, g @ w.double(), g.abs() @ w.double().abs()), (dw, g.t() @ x.double(), g.abs().t() @ x.double().abs())):
+        assert ((got.cpu().double() - want).abs() <= (2.0 ** -8 + 2.0 ** -15) * size + 2.0 ** -8 * want.abs()).all()
+
+
 def test_all_ignored_and_odd_targets():
     x, w, y, dl = inputs(50, 300, 64, 1)
     y[:] = -100
