@@ -99,7 +99,8 @@ int pulse_layer_norm_backward(int dtype, const void *dy, uint64_t dy_stride, con
  */
 #define PULSE_CE_MAX_HIDDEN 65536
 
-/* A workspace for calls of any number of tokens up to `tokens`, both directions. */
+/* A workspace for calls of any number of tokens up to `tokens`, both directions; 0 for
+ * sizes that no call handles. */
 size_t pulse_linear_ce_workspace_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden);
 
 /* loss and lse: FP32 [tokens]. */

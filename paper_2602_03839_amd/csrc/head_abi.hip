@@ -51,6 +51,10 @@ int check_matrix(const char* who, const char* name, const void* p, uint64_t stri
   return PULSE_OK;
 }
 
+bool ce_handles(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
+  return tokens <= 0x7FFFFFFFu && vocab != 0 && vocab <= 0x7FFFFFFFu && hidden != 0 && hidden <= PULSE_CE_MAX_HIDDEN;
+}
+
 int check_ce(const char* who, const void* x, uint64_t x_stride, const void* weight, const void* targets,
              uint32_t tokens, uint32_t vocab, uint32_t hidden, float logit_scale, const void* ws,
              size_t ws_bytes) {
@@ -116,7 +120,7 @@ int pulse_layer_norm_backward(int dtype, const void* dy, uint64_t dy_stride, con
 }
 
 size_t pulse_linear_ce_workspace_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
-  return tokens && vocab && hidden ? pulse::linear_ce_bytes(tokens, vocab, hidden) : 0;
+  return tokens && ce_handles(tokens, vocab, hidden) ? pulse::linear_ce_bytes(tokens, vocab, hidden) : 0;
 }
 
 int pulse_linear_ce_forward(const uint16_t* x, uint64_t x_stride, const uint16_t* weight,

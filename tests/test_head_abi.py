@@ -111,6 +111,16 @@ def test_linear_ce_validation(L):
         refused(bwd(**k), status, L, word)
 
 
+def test_linear_ce_workspace_of_sizes_out_of_range(L):
+    """Sizes that every call refuses have no workspace; the largest handled ones have."""
+    top = (1 << 31) - 1
+    for sizes in ((1, 100, 0), (1, 100, 65537), (1, 100, 0xFFFFFFF9), (1, 100, 0xFFFFFFFF), (1, 0, 64), (1, 1 << 31, 64),
+                  (1, 0xFFFFFFFF, 64), (1 << 31, 100, 64), (0xFFFFFFFF, 100, 64), (0xFFFFFFFF,) * 3):
+        assert L.pulse_linear_ce_workspace_bytes(*sizes) == 0, sizes
+    for sizes in ((1, top, 1), (top, 1, 1), (1, 1, 65536), (top, top, 65536)):
+        assert L.pulse_linear_ce_workspace_bytes(*sizes) > 0, sizes
+
+
 def test_linear_ce_workspace_serves_fewer_tokens(L):
     """The size for n tokens covers every call of fewer: each such call gets past the
     workspace check (and stops at the missing loss, before any launch)."""
