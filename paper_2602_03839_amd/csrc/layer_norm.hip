@@ -399,7 +399,9 @@ void by_shape(uint32_t cols, F f) {
 
 }  // namespace
 
-hipError_t launch_layer_norm(bool bf16, const NormParams& p, hipStream_t stream) {
+namespace {
+
+void run_layer_norm(bool bf16, const NormParams& p, hipStream_t stream) {
   const bool vec = p.cols % 8 == 0 && p.x_stride % 8 == 0 && p.y_stride % 8 == 0;
   by_shape(p.cols, [&](auto e, auto g) {
     constexpr int E = decltype(e)::value, G = decltype(g)::value;
@@ -419,6 +421,24 @@ hipError_t launch_layer_norm(bool bf16, const NormParams& p, hipStream_t stream)
     else if (vec) run(float{}, std::true_type{});
     else run(float{}, std::false_type{});
   });
+}
+
+// A launch has fewer than 2^32 threads; the widest form takes 512 for a row.
+constexpr uint64_t kNormRowsAtOnce = 1u << 22;
+
+}  // namespace
+
+hipError_t launch_layer_norm(bool bf16, const NormParams& p, hipStream_t stream) {
+  const uint64_t size = bf16 ? 2 : 4;
+  for (uint64_t first = 0; first < p.rows; first += kNormRowsAtOnce) {
+    NormParams q = p;
+    q.rows = p.rows - first < kNormRowsAtOnce ? p.rows - first : kNormRowsAtOnce;
+    q.x = (const char*)p.x + first * p.x_stride * size;
+    q.y = (char*)p.y + first * p.y_stride * size;
+    if (p.mean) q.mean = p.mean + first;
+    q.rstd = p.rstd + first;
+    run_layer_norm(bf16, q, stream);
+  }
   return hipGetLastError();
 }
 

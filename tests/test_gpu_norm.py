@@ -120,6 +120,26 @@ def test_many_rows_forward(rows):
         near(rstd, er, 1e-5, "rstd")
 
 
+@pytest.mark.parametrize("cols,dtype,rms", [(2, torch.bfloat16, True), (1, torch.float32, False)])
+def test_more_rows_than_one_launch_has_threads(cols, dtype, rms):
+    """2^27 rows and a few: with 32 threads a row, 2^32 threads and more."""
+    rows = (1 << 27) + 5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(rows, cols, dtype=dtype, device="cuda").normal_(generator=g)
+    w, b = params(cols, torch.float32, 2, bias=not rms)
+    y = torch.full((rows, cols), 77.0, dtype=dtype, device="cuda")
+    y, mean, rstd = head.LayerNorm(w.cuda(), None if b is None else b.cuda(), eps=1e-3, rms=rms)(x, y=y)
+    for first in (0, (1 << 22) - 3, (1 << 26) - 2, (1 << 27) - 4, rows - (1 << 20)):
+        part = slice(first, first + (1 << 20))
+        ey, em, er = exact_forward(x[part].cpu(), w, b, 1e-3, rms)
+        near(y[part], ey, TOL[dtype], "y")
+        near(rstd[part], er, 1e-5, "rstd")
+        if not rms:
+            near(mean[part], em, 1e-5, "mean")
+    step = 1 << 24
+    assert all((y[k:k + step] != 77.0).all() and torch.isfinite(rstd[k:k + step]).all() for k in range(0, rows, step))
+
+
 def test_gradient_against_differences():
     """The formula's gradient against central differences of a 64-bit loss
     sum(dy * y): second order, so a step of 1e-4 leaves about 1e-7."""
