@@ -79,6 +79,7 @@ struct LogitParams {
   uint32_t tokens, hidden;
   uint32_t v_begin, v_end;  // the piece; forward: the whole vocabulary
   uint32_t tiles_m, tiles_n;
+  uint32_t first_tile;  // of this launch
   float scale;
   // forward
   float2* part;  // [tokens][tiles_m]: largest logit, sum of exponentials below it
@@ -102,7 +103,7 @@ template <typename T>
 __global__ __launch_bounds__(T::kThreads) void ce_forward_kernel(LogitParams p) {
   __shared__ alignas(1024) char lds[T::kLds];
   uint32_t tm, tn;
-  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, kBand, tm, tn);
+  gemm_tile_of(p.first_tile + blockIdx.x, p.tiles_m, p.tiles_n, kBand, tm, tn);
   const uint32_t m0 = p.v_begin + tm * T::BM, n0 = tn * T::BN;
   typename T::Acc acc;
   const GemmOperand a = {p.w + (uint64_t)m0 * p.w_ld, p.w_ld, p.v_end - m0};
@@ -173,7 +174,7 @@ __global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
   __shared__ alignas(1024) char lds[T::kLds > kRows + kSums ? T::kLds : kRows + kSums];
   float(*const s_lost)[T::BN] = (float(*)[T::BN])(lds + kRows);  // [WM][BN]
   uint32_t tm, tn;
-  gemm_tile_of(blockIdx.x, p.tiles_m, p.tiles_n, kBand, tm, tn);
+  gemm_tile_of(p.first_tile + blockIdx.x, p.tiles_m, p.tiles_n, kBand, tm, tn);
   const uint32_t m0 = p.v_begin + tm * T::BM, n0 = tn * T::BN;
   typename T::Acc acc;
   const GemmOperand a = {p.w + (uint64_t)m0 * p.w_ld, p.w_ld, p.v_end - m0};
@@ -307,12 +308,12 @@ __global__ __launch_bounds__(T::kThreads) void ce_grad_kernel(LogitParams p) {
   }
 }
 
-// A token's pairs joined, one wave each.
+// A token's pairs joined, one wave each, from token `first` on.
 __global__ __launch_bounds__(256) void ce_join_kernel(const float2* part, const float* hit,
-                                                      const int64_t* targets, uint32_t tokens,
-                                                      uint32_t vocab, uint32_t tiles, float* loss,
-                                                      float* lse) {
-  const uint32_t t = blockIdx.x * 4 + (threadIdx.x >> 6);
+                                                      const int64_t* targets, uint32_t first,
+                                                      uint32_t tokens, uint32_t vocab, uint32_t tiles,
+                                                      float* loss, float* lse) {
+  const uint32_t t = first + blockIdx.x * 4 + (threadIdx.x >> 6);
   if (t >= tokens) return;
   const int lane = threadIdx.x & 63;
   const float2* mine = part + (uint64_t)t * tiles;
@@ -597,6 +598,7 @@ __global__ __launch_bounds__(512) void ce_dw_run_kernel(GradParams p, uint32_t r
 }
 
 struct DxJoinParams {
+  uint32_t first;     // token of this launch
   const float* sums;  // [splits][tokens][ld]
   uint32_t splits, tokens, ld, hidden;
   const int64_t* targets;
@@ -617,7 +619,7 @@ struct DxJoinParams {
 __global__ __launch_bounds__(256) void ce_dx_join_kernel(DxJoinParams p) {
   __shared__ float s_lost[4];
   __shared__ LargeLoss s_large[kLargeLosses];
-  const uint32_t t = blockIdx.x;
+  const uint32_t t = p.first + blockIdx.x;
   const uint32_t c = (blockIdx.y * 256 + threadIdx.x) * 4;
   const int64_t y = p.targets[t];
   f32x4_t a = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -776,6 +778,9 @@ uint32_t parts(uint64_t v, uint32_t of) { return (uint32_t)((v + of - 1) / of); 
 
 constexpr uint32_t kVocabTile = 256;
 constexpr uint32_t kBothBlocks = 512;
+// A launch has fewer than 2^32 threads: more tiles or tokens than these take several.
+constexpr uint32_t kTilesAtOnce = 1u << 22;  // of up to 512 threads; a multiple of 8, the XCDs
+constexpr uint32_t kTokensAtOnce = 1u << 22;  // of up to 256 threads in x
 constexpr uint64_t kRunElements = 1ull << 26;  // of dw: 16 tiles of 64 entries for every CU
 constexpr uint32_t kSmallTokens = 512;  // up to here the gradient's products take the smaller tiles
 constexpr uint32_t kWantedTiles = 192;
@@ -857,9 +862,14 @@ template <typename T>
 uint32_t run_logits(LogitParams p, bool forward, hipStream_t stream) {
   p.tiles_m = parts(p.v_end - p.v_begin, T::BM);
   p.tiles_n = parts(p.tokens, T::BN);
-  const dim3 grid(p.tiles_m * p.tiles_n), block(T::kThreads);
-  if (forward) hipLaunchKernelGGL(ce_forward_kernel<T>, grid, block, 0, stream, p);
-  else hipLaunchKernelGGL(ce_grad_kernel<T>, grid, block, 0, stream, p);
+  const uint32_t tiles = p.tiles_m * p.tiles_n;
+  for (p.first_tile = 0; p.first_tile < tiles; p.first_tile += kTilesAtOnce) {
+    const uint32_t left = tiles - p.first_tile;
+    const dim3 grid(left < kTilesAtOnce ? left : kTilesAtOnce), block(T::kThreads);
+    if (forward) hipLaunchKernelGGL(ce_forward_kernel<T>, grid, block, 0, stream, p);
+    else hipLaunchKernelGGL(ce_grad_kernel<T>, grid, block, 0, stream, p);
+    if (left <= kTilesAtOnce) break;
+  }
   return T::BM;
 }
 
@@ -996,8 +1006,11 @@ hipError_t launch_linear_ce(const LinearCeParams& c, char* ws, hipStream_t strea
   p.part = (float2*)(ws + q.part);
   p.hit = (float*)(ws + q.hit);
   const uint32_t tile = run_logits(p, true, stream);
-  hipLaunchKernelGGL(ce_join_kernel, dim3(parts(c.tokens, 4)), dim3(256), 0, stream, p.part, p.hit, c.targets,
-                     c.tokens, c.vocab, parts(c.vocab, tile), c.loss, c.lse);
+  for (uint32_t first = 0; first < c.tokens; first += kTokensAtOnce) {
+    const uint32_t left = c.tokens - first, now = left < kTokensAtOnce ? left : kTokensAtOnce;
+    hipLaunchKernelGGL(ce_join_kernel, dim3(parts(now, 4)), dim3(256), 0, stream, p.part, p.hit, c.targets, first,
+                       c.tokens, c.vocab, parts(c.vocab, tile), c.loss, c.lse);
+  }
   return hipGetLastError();
 }
 
@@ -1077,9 +1090,13 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& c, char* ws, hipStrea
     else if (q.small) run_products<DxM, DwM, true>(d, splits, e, stream);
     else run_products<DxL, DwL, true>(d, splits, e, stream);
   }
-  const DxJoinParams j = {sums, q.splits, c.tokens, q.ld, c.hidden, c.targets, c.vocab, p.w, p.w_ld, p.rest, p.lost,
+  DxJoinParams j = {0, sums, q.splits, c.tokens, q.ld, c.hidden, c.targets, c.vocab, p.w, p.w_ld, p.rest, p.lost,
                           p.lost_ld, p.large_count, p.large, r.mean, c.dx, c.dx_stride};
-  hipLaunchKernelGGL(ce_dx_join_kernel, dim3(c.tokens, parts(q.ld, 1024)), dim3(256), 0, stream, j);
+  for (; j.first < c.tokens; j.first += kTokensAtOnce) {
+    const uint32_t left = c.tokens - j.first;
+    hipLaunchKernelGGL(ce_dx_join_kernel, dim3(left < kTokensAtOnce ? left : kTokensAtOnce, parts(q.ld, 1024)), dim3(256), 0,
+                       stream, j);
+  }
   return hipGetLastError();
 }
 

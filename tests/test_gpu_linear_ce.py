@@ -303,6 +303,62 @@ def test_fewer_tokens_than_built_for(most):
     torch.cuda.synchronize()
 
 
+def test_more_tokens_than_one_launch_has_threads():
+    """2^26 tokens and a few forward (64 threads a token in the join) and 2^24 backward
+    (256), most of them without a target."""
+    hidden, vocab = 8, 100
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.randn(vocab, hidden, generator=g, device="cuda").bfloat16()
+    for tokens, backward in (((1 << 26) + 5, False), ((1 << 24) + 5, True)):
+        x = torch.empty(tokens, hidden, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+        y = torch.full((tokens,), -100, device="cuda")
+        kept = torch.cat([torch.arange(300), (1 << 22) - 5 + torch.arange(10), tokens - 300 + torch.arange(300)]).cuda()
+        y[kept] = torch.randint(vocab, (len(kept),), generator=g, device="cuda")
+        ce = head.LinearCE(w, max_tokens=tokens)
+        out = [torch.full((tokens,), 77.0, device="cuda") for _ in range(2)]
+        loss, lse = ce.forward(x, y, *out)
+        wd, step = w.double(), 1 << 22
+        for k in range(0, tokens, step):
+            z = x[k:k + step].double() @ wd.t()
+            want = torch.logsumexp(z, 1)
+            assert ((lse[k:k + step].double() - want).abs() < 1e-5).all(), k
+            yk = y[k:k + step]
+            want = torch.where(yk >= 0, want - z.gather(1, yk.clamp(min=0)[:, None])[:, 0], 0.0)
+            assert ((loss[k:k + step].double() - want).abs() < 1e-5).all(), k
+        if not backward:
+            continue
+        dl = torch.randn(tokens, generator=g, device="cuda")
+        dx = torch.full_like(x, 77.0)
+        dx, dw = ce.backward(x, y, lse, dl, dx=dx)
+        p = torch.exp(x[kept].double() @ wd.t() - lse[kept].double()[:, None])
+        p[torch.arange(len(kept)), y[kept]] -= 1
+        p *= dl[kept].double()[:, None]
+        xk = x[kept].double()
+        for got, want, size in ((dx[kept], p @ wd, p.abs() @ wd.abs()), (dw, p.t() @ xk, p.abs().t() @ xk.abs())):
+            assert ((got.double() - want).abs() <= 2.0 ** -8 * (want.abs() + size) + 1e-6).all()
+        dx[kept] = 0
+        assert (dx == 0).all()
+
+
+def test_more_tiles_than_one_launch_has_threads():
+    """2^23 tiles of 512 threads and more, in the forward pass."""
+    tokens, vocab, hidden = 1_050_000, 524_500, 8
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w = torch.randn(vocab, hidden, generator=g, device="cuda").bfloat16()
+    x = torch.randn(tokens, hidden, generator=g, device="cuda").bfloat16()
+    y = torch.randint(vocab, (tokens,), generator=g, device="cuda")
+    ce = head.LinearCE(w, max_tokens=tokens)
+    loss, lse = ce.forward(x, y, *[torch.full((tokens,), 77.0, device="cuda") for _ in range(2)])
+    assert torch.isfinite(lse).all() and (lse != 77).all() and (loss != 77).all()
+    for first in (0, 255, 400_000, 524_200, 800_000, tokens - 500):
+        part = slice(first, first + 500)
+        z = x[part].double() @ w.double().t()
+        want = torch.logsumexp(z, 1)
+        assert ((lse[part].double() - want).abs() < 1e-4).all()
+        hit = z[torch.arange(500), y[part]]
+        assert ((loss[part].double() - (want - hit)).abs() < 1e-4).all()
+
+
 def test_no_tokens():
     _, w, _, _ = inputs(1, 64, 32, 1)
     ce = head.LinearCE(w.cuda(), max_tokens=0)
