@@ -163,18 +163,19 @@ __device__ __forceinline__ void multiply_chunk(const Held<MX, RT, NT>& h, f32x4_
   }
 }
 
-// grid.x: groups of RT row tiles; grid.y: groups of NT token tiles.  The
+// grid.x: groups of RT row tiles from `first` on; grid.y: groups of NT token tiles.  The
 // block's waves share the chunks of one group and add their sums at the end.
 template <bool MX, int RT, int NT, bool SHIFT>
-__global__ __launch_bounds__(1024) void lowp_matmul_kernel(LowpMatmulParams p, uint32_t classes) {
+__global__ __launch_bounds__(1024) void lowp_matmul_kernel(LowpMatmulParams p, uint32_t classes, uint32_t first) {
   typedef Unit<MX> U;
   extern __shared__ f32x4_t s_part[];  // [waves - 1][RT * NT][64]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int r16 = lane & 15, g = lane >> 4;
   // tile t of class c holds the rows c + classes * (16 t + i): one class and
   // adjacent rows where every row starts a unit
-  const uint32_t cls = SHIFT ? blockIdx.x % classes : 0;
-  const uint32_t group = SHIFT ? blockIdx.x / classes : blockIdx.x;
+  const uint32_t block = first + blockIdx.x;
+  const uint32_t cls = SHIFT ? block % classes : 0;
+  const uint32_t group = SHIFT ? block / classes : block;
   if (cls >= p.rows) return;  // fewer rows than classes: the whole block
   const uint32_t shift = SHIFT ? (uint32_t)(((uint64_t)cls * p.cols) % U::kValues) : 0;
   auto row_of = [&](int r, uint32_t i) -> uint64_t {
@@ -496,6 +497,10 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
   }
 }
 
+// A launch has fewer than 2^32 threads (2^21 groups of up to 1,024) and groups in y.
+constexpr uint32_t kGroupsAtOnce = 1u << 21;
+constexpr uint32_t kTokensAtOnce = 1u << 15;
+
 template <bool MX, int RT, int NT, bool SHIFT>
 void launch_shape(const LowpMatmulParams& p, hipStream_t stream) {
   typedef Unit<MX> U;
@@ -508,8 +513,12 @@ void launch_shape(const LowpMatmulParams& p, hipStream_t stream) {
   uint32_t waves = 1;
   while (waves < 16 && 2 * waves <= chunks && groups * tgroups * waves < 4096) waves *= 2;
   const size_t lds = (size_t)(waves - 1) * RT * NT * 64 * sizeof(f32x4_t);
-  hipLaunchKernelGGL((lowp_matmul_kernel<MX, RT, NT, SHIFT>), dim3((uint32_t)groups, tgroups),
-                     dim3(64 * waves), lds, stream, p, classes);
+  for (uint64_t first = 0; first < groups; first += kGroupsAtOnce) {
+    const uint64_t left = groups - first;
+    hipLaunchKernelGGL((lowp_matmul_kernel<MX, RT, NT, SHIFT>),
+                       dim3(left < kGroupsAtOnce ? (uint32_t)left : kGroupsAtOnce, tgroups), dim3(64 * waves), lds,
+                       stream, p, classes, (uint32_t)first);
+  }
 }
 
 constexpr uint32_t kLpCus = 256;
@@ -587,8 +596,14 @@ void launch_type(const LowpMatmulParams& p, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_lowp_matmul(bool mxfp4, const LowpMatmulParams& p, hipStream_t stream) {
-  if (mxfp4) launch_type<true>(p, stream);
-  else launch_type<false>(p, stream);
+  for (uint32_t first = 0; first < p.tokens; first += kTokensAtOnce) {
+    LowpMatmulParams q = p;
+    q.x = p.x + first * p.x_stride;
+    q.y = (char*)p.y + first * p.y_stride * (p.y_bf16 ? 2 : 4);
+    q.tokens = p.tokens - first < kTokensAtOnce ? p.tokens - first : kTokensAtOnce;
+    if (mxfp4) launch_type<true>(q, stream);
+    else launch_type<false>(q, stream);
+  }
   return hipGetLastError();
 }
 

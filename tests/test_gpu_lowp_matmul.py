@@ -189,6 +189,43 @@ def test_offsets_past_32_bits():
     assert y[0, -1].item() == 2 * cols and (y[0, :-1] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", [MX, FP8])
+def test_more_rows_than_one_launch_has_threads(dtype):
+    """2^30 rows of one value: with 4 threads a row, 2^32 threads and more.  A product
+    of one term is exact."""
+    rows = (1 << 30) + 77
+    w = torch.empty(rows, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    codes, scales = pulse.cast_lowp(dtype, w)
+    del w
+    y = torch.full((1, rows), 77.0, device="cuda")
+    head.LowpLinear(dtype, codes, scales, rows, 1)(torch.full((1, 1), 1.5, dtype=torch.bfloat16, device="cuda"), out=y)
+    mags = torch.tensor(MAGS + [-m for m in MAGS], device="cuda")
+    step = 1 << 24
+    for k in range(0, rows, step):
+        n = min(step, rows - k)
+        if dtype == FP8:
+            want = codes[k:k + n].view(torch.float8_e4m3fn).float()
+        else:
+            pair = codes[k // 2:(k + n + 1) // 2]
+            want = mags[torch.stack((pair & 15, pair >> 4), 1).flatten().int()].view(-1)[:n]
+            want = want * torch.exp2(scales[k // 32:(k + n + 31) // 32].float() - 127).repeat_interleave(32)[:n]
+        assert torch.equal(y[0, k:k + n], 1.5 * want), k
+
+
+@pytest.mark.parametrize("dtype", [MX, FP8])
+@pytest.mark.parametrize("rows,cols", [(2, 3), (16, 128)])
+def test_most_tokens(dtype, rows, cols):
+    """2^20 tokens, for rows that start inside a block and for rows that do not."""
+    tokens = 1 << 20
+    codes, scales = weight(dtype, rows, cols, 4)
+    x = torch.empty(tokens, cols, dtype=torch.bfloat16, device="cuda").normal_(generator=torch.Generator(device="cuda").manual_seed(1))
+    y = torch.full((tokens, rows), float("nan"), device="cuda")
+    head.LowpLinear(dtype, codes, scales, rows, cols)(x, out=y)
+    w = torch.from_numpy(values(dtype, codes, scales, rows * cols).reshape(rows, cols)).cuda()
+    off = (y.double() - x.double() @ w.t()).abs()
+    assert (off <= (cols + 2) * 2.0 ** -24 * (x.double().abs() @ w.abs().t())).all()
+
+
 def test_refusals():
     codes, scales = weight(MX, 16, 64, 1)
     c8, _ = weight(FP8, 16, 64, 1)
