@@ -55,10 +55,11 @@ struct LargeLoss {
 // 2^x (v_exp_f32, 1 ulp).
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A pair (largest logit, sum of exponentials below it) as a sum below `top`.  A
-// pair without a finite logit has a sum of 0, or NaN, which stays one.
+// A pair (largest logit, sum of exponentials below it) as a sum below `top`.  Where the
+// largest is infinite the exponentials are taken as they are: the sum is 0 or
+// infinite.  A NaN stays one.
 __device__ __forceinline__ float below(float2 q, float top) {
-  return q.y * (q.x == -INFINITY ? 0.0f : exp2_fast((q.x - top) * kLog2e));
+  return q.y * (q.x == top ? 1.0f : exp2_fast((q.x - top) * kLog2e));
 }
 
 // Where target y lies among a lane's entries first + 16 i + e (e < 4), as 16 i + e;
@@ -147,7 +148,7 @@ __global__ __launch_bounds__(T::kThreads) void ce_forward_kernel(LogitParams p) 
       for (int e = 0; e < 4; ++e) top = __builtin_fmaxf(top, acc[i][j][e]);
     top = __builtin_fmaxf(top, __shfl_xor(top, 16));
     top = __builtin_fmaxf(top, __shfl_xor(top, 32));
-    const float from = top == -INFINITY ? 0.0f : top;
+    const float from = __builtin_fabsf(top) == INFINITY ? 0.0f : top;
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < T::FM; ++i)

@@ -239,6 +239,28 @@ def test_minus_infinite_logits():
     assert torch.isfinite(loss.cpu()).all()
 
 
+@pytest.mark.parametrize("tokens,vocab", [(20, 300), (100, 1300), (600, 5000)])
+def test_infinite_logits(tokens, vocab):
+    """lse is infinite with a logit, and the loss then infinite but at that very
+    target, where it is undefined; minus infinite if every logit is."""
+    x, w, y, _ = inputs(tokens, vocab, 32, 6, ignored=0.0)
+    x[:, 0] = x[:, 0].abs() + 1
+    x[1::2, 0] = 0  # zero times infinity: NaN
+    w[vocab - 2, 0] = float("inf")
+    w[5, 0] = float("-inf")
+    y[y == 5] = 6
+    y[0] = vocab - 2
+    ce = head.LinearCE(w.cuda(), max_tokens=tokens)
+    loss, lse = (t.cpu() for t in ce.forward(x.cuda(), y.cuda()))
+    assert (lse[0::2] == float("inf")).all() and torch.isnan(lse[1::2]).all()
+    there = y == vocab - 2
+    assert torch.isnan(loss[there]).all() and (loss[0::2][~there[0::2]] == float("inf")).all()
+    w[:, 0] = float("-inf")
+    ce = head.LinearCE(w.cuda(), max_tokens=tokens)
+    _, lse = ce.forward(x.cuda(), y.cuda())
+    assert (lse.cpu()[0::2] == float("-inf")).all() and torch.isnan(lse.cpu()[1::2]).all()
+
+
 def test_gradient_against_differences():
     """dx against central differences of the loss in 64 bits, for inputs that are
     exact in BF16; the gradient's own roundings allow 2^-7 of its largest entry."""
