@@ -263,7 +263,8 @@ __device__ __forceinline__ void grad_rows(const NormGradParams& p, uint64_t firs
     float sa = 0.0f, sax = 0.0f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      x[e] = (x[e] - mean) * rstd;  // past the row: meets dy = 0
+      // past the row a zero, which meets dy = 0: mean * rstd may be out of range
+      x[e] = (x[e] - (R::in(e, p.cols, t) ? mean : 0.0f)) * rstd;
       if (SUMS && valid) {
         dw[e] = __builtin_fmaf(dy[e], x[e], dw[e]);
         db[e] += dy[e];

@@ -220,6 +220,23 @@ def test_constant_rows_and_large_offsets():
     near(y, ey, 2.0 ** -12 * er[1].item() + 1e-5, "y")
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [300, 700, 896, 1500, 3584, 5120, 12000])
+@pytest.mark.parametrize("rows", [3, 1300])
+def test_mean_times_rstd_past_the_range(rows, cols, dtype):
+    """Constant rows of 2^120 and an rstd of 1,024: their product has no FP32 value,
+    but no element is that far from its mean."""
+    x = torch.full((rows, cols), 2.0 ** 120, dtype=dtype)
+    dy = rows_of(rows, cols, dtype, 1, 0.0)
+    w, b = params(cols, torch.float32, 2, True)
+    mean, rstd = torch.full((rows,), 2.0 ** 120), torch.full((rows,), 1024.0)
+    dx, dw, db = head.LayerNorm(w.cuda(), b.cuda()).backward(dy.cuda(), x.cuda(), mean.cuda(), rstd.cuda())
+    edx, edw, edb = exact_backward(dy, x, w, mean, rstd, False)
+    near(dx, edx, TOL[dtype], "dx")
+    near(db, edb, 1e-5, "dbias")
+    assert (dw == 0).all() and (edw == 0).all()
+
+
 def test_same_bits_and_other_stream():
     x, dy = rows_of(1500, 1000, torch.bfloat16, 1).cuda(), rows_of(1500, 1000, torch.bfloat16, 2).cuda()
     w, b = params(1000, torch.float32, 1, True)
