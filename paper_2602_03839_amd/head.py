@@ -26,6 +26,7 @@ F32, BF16 = 3, 4  # PULSE_DTYPE_F32, PULSE_DTYPE_BF16
 NORM_RMS = 1      # PULSE_NORM_RMS
 NORM_MAX_COLS = 16384
 CE_MAX_HIDDEN = 65536
+MAX_SIZE = (1 << 31) - 1  # of a vocabulary, a weight's rows or columns, tokens
 
 EXPORTS = ("pulse_layer_norm_workspace_bytes", "pulse_layer_norm_forward",
            "pulse_layer_norm_backward", "pulse_linear_ce_workspace_bytes", "pulse_linear_ce_forward",
@@ -200,11 +201,13 @@ class LinearCE:
     def __init__(self, weight: torch.Tensor, max_tokens: int, logit_scale: float = 1.0):
         if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
             raise PulseError("weight must be a tensor [vocab, hidden]")
-        _p(weight, "weight", dtype=torch.bfloat16, min_numel=1, optional=False)
         self.device, (self.vocab, self.hidden) = weight.device, weight.shape
-        if self.hidden > CE_MAX_HIDDEN:
+        if not 1 <= self.vocab <= MAX_SIZE:
+            raise PulseError(f"vocabulary of {self.vocab}, 1 to {MAX_SIZE} are handled")
+        if not 1 <= self.hidden <= CE_MAX_HIDDEN:
             raise PulseError(f"hidden size {self.hidden}, 1 to {CE_MAX_HIDDEN} are handled")
-        if not 0 <= max_tokens < 1 << 31:
+        _p(weight, "weight", dtype=torch.bfloat16, optional=False)
+        if not 0 <= max_tokens <= MAX_SIZE:
             raise PulseError(f"max_tokens {max_tokens} is out of range")
         self.weight, self.max_tokens, self.logit_scale = weight, max_tokens, float(logit_scale)
         self._lib, self._pw = lib(), weight.data_ptr()
@@ -263,6 +266,8 @@ class LowpLinear:
 
     def __init__(self, dtype: int, codes: torch.Tensor, scales: Optional[torch.Tensor], rows: int,
                  cols: int, inv_scale: float = 1.0):
+        if not (1 <= rows <= MAX_SIZE and 1 <= cols <= MAX_SIZE):
+            raise PulseError(f"a weight of {rows} x {cols}, 1 to {MAX_SIZE} of each are handled")
         nc, ns = pulse.lowp_sizes(dtype, rows * cols)
         self.device = codes.device
         self._codes = _p(codes, "codes", esize=1, min_numel=nc, optional=False)

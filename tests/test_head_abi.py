@@ -160,3 +160,19 @@ def test_binding_rejects_host_tensors(L):
                  lambda: head.LowpLinear(MX, torch.zeros(16, dtype=torch.uint8), torch.zeros(1, dtype=torch.uint8), 4, 8)):
         with pytest.raises(pulse.PulseError, match="device tensor"):
             call()
+
+
+def test_binding_rejects_sizes_past_32_bits():
+    """Sizes that the C calls take as 32 bits: no call computes with what is left of a
+    larger one.  The sizes are looked at before the tensors are."""
+    byte = torch.zeros(1, dtype=torch.uint8)
+    for dtype in (MX, FP8):
+        for rows, cols in (((1 << 32) + 16, 1), (1, (1 << 32) + 16), (1 << 31, 1), (1, 1 << 31), (0, 64), (64, 0), (-4, -8)):
+            with pytest.raises(pulse.PulseError, match="weight of"):
+                head.LowpLinear(dtype, byte, byte, rows, cols)
+    for shape in (((1 << 32) + 1, 1), (1 << 31, 8), (0, 8)):
+        with pytest.raises(pulse.PulseError, match="vocabulary"):
+            head.LinearCE(torch.empty(shape, dtype=torch.bfloat16, device="meta"), 4)
+    for shape in ((8, 1 << 32), (8, 65537), (8, 0)):
+        with pytest.raises(pulse.PulseError, match="hidden size"):
+            head.LinearCE(torch.empty(shape, dtype=torch.bfloat16, device="meta"), 4)
