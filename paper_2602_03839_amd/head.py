@@ -269,8 +269,8 @@ class LowpLinear:
         if not (1 <= rows <= MAX_SIZE and 1 <= cols <= MAX_SIZE):
             raise PulseError(f"a weight of {rows} x {cols}, 1 to {MAX_SIZE} of each are handled")
         nc, ns = pulse.lowp_sizes(dtype, rows * cols)
-        self.device = codes.device
         self._codes = _p(codes, "codes", esize=1, min_numel=nc, optional=False)
+        self.device = codes.device
         self._scales = _p(scales, "scales", esize=1, min_numel=ns, device=self.device,
                           optional=dtype != pulse.MXFP4)
         self.dtype, self.rows, self.cols, self.inv_scale = dtype, rows, cols, float(inv_scale)

@@ -176,3 +176,11 @@ def test_binding_rejects_sizes_past_32_bits():
     for shape in ((8, 1 << 32), (8, 65537), (8, 0)):
         with pytest.raises(pulse.PulseError, match="hidden size"):
             head.LinearCE(torch.empty(shape, dtype=torch.bfloat16, device="meta"), 4)
+
+
+def test_binding_rejects_what_is_no_tensor():
+    one = torch.zeros(16, dtype=torch.uint8)
+    for call in (lambda: head.LowpLinear(MX, None, one, 4, 8), lambda: head.LowpLinear(FP8, [1] * 32, None, 4, 8),
+                 lambda: head.LayerNorm(None), lambda: head.LinearCE(None, 4)):
+        with pytest.raises(pulse.PulseError):
+            call()
