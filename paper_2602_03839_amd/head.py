@@ -141,8 +141,7 @@ class LayerNorm:
         self.weight, self.bias, self.eps, self.rms = weight, bias, float(eps), bool(rms)
         self._flags, self._lib = NORM_RMS if rms else 0, lib()
         self._nws = int(self._lib.pulse_layer_norm_workspace_bytes(self.cols))
-        self.ws = torch.empty(self._nws, dtype=torch.uint8, device=self.device)
-        self._pws = self.ws.data_ptr()
+        self.ws = None  # of the gradient: allocated by the first call that asks for one
 
     def __call__(self, x: torch.Tensor, y: Optional[torch.Tensor] = None,
                  mean: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, stream=None):
@@ -180,10 +179,12 @@ class LayerNorm:
             pdx, sdx = dx.data_ptr(), cols
         else:
             dx, pdx, sdx = _out(dx, "dx", cols, rows, x.dtype, dev, stream)
+        if self.ws is None:
+            self.ws = _new((self._nws,), torch.uint8, dev, stream)
         dweight, pdw = _vec(dweight, "dweight", cols, dev, stream)
         dbias, pdb = (None, None) if self.bias is None else _vec(dbias, "dbias", cols, dev, stream)
         rc = self._lib.pulse_layer_norm_backward(dt, pdy, sdy, px, sx, self._dt, self._pw, pm, pr, pdx, sdx,
-                                                 pdw, pdb, rows, cols, self._flags, self._pws, self._nws,
+                                                 pdw, pdb, rows, cols, self._flags, self.ws.data_ptr(), self._nws,
                                                  _stream(stream, dev))
         if rc:
             _check(rc, "pulse_layer_norm_backward")

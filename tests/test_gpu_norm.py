@@ -252,6 +252,26 @@ def test_same_bits_and_other_stream():
         assert torch.equal(a, c)
 
 
+def test_forward_takes_no_workspace():
+    """The gradient's partial sums (67 MB at this width) are allocated when a gradient
+    is asked for: a model that answers has a norm or two a layer and no gradient."""
+    w = torch.ones(16384, device="cuda")
+    x = torch.randn(3, 16384, device="cuda")
+    before = torch.cuda.memory_allocated()
+    norms = [head.LayerNorm(w, rms=True) for _ in range(8)]
+    for n in norms:
+        _, _, rstd = n(x)
+    assert torch.cuda.memory_allocated() - before < 1 << 20
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    dx, dw, _ = norms[0].backward(x, x, None, rstd, stream=s)
+    s.synchronize()
+    edx, edw, _ = exact_backward(x.cpu(), x.cpu(), w.cpu(), None, rstd.cpu(), True)
+    # dy = x: dx cancels to its share of eps, so it is held to its terms' size
+    assert (dx.cpu().double() - edx).abs().max() <= 1e-5 * (x * rstd[:, None]).abs().max().item()
+    near(dw, edw, 1e-5, "dweight")
+
+
 def test_refusals():
     w, b = params(64, torch.float32, 1, True)
     w, b = w.cuda(), b.cuda()
