@@ -189,6 +189,67 @@ def test_offsets_past_32_bits():
     assert y[0, -1].item() == 2 * cols and (y[0, :-1] == 0).all()
 
 
+def values_on_gpu(dtype, codes, scales, n, inv_scale=1.0):
+    """``values`` on the GPU, for weights that take numpy seconds (without NaN)."""
+    if dtype == FP8:
+        c = torch.arange(256, dtype=torch.uint8)
+        return torch.from_numpy(values(FP8, c, None, 256)).cuda()[codes[:n].int()] / inv_scale
+    mags = torch.tensor(MAGS + [-m for m in MAGS], dtype=torch.float64, device="cuda")
+    v = mags[torch.stack((codes & 15, codes >> 4), 1).flatten().int()]
+    v = torch.cat([v, v.new_zeros(-v.numel() % 32)]).view(-1, 32) * torch.exp2(scales.double() - 127)[:, None]
+    return v.flatten()[:n]
+
+
+def check_on_gpu(dtype, rows, cols, tokens, out_dtype=torch.float32, seed=0, offset=0):
+    """``check`` into an output of NaN; codes `offset` bytes into their buffer."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    w = torch.empty(rows * cols, device="cuda").normal_(generator=g)
+    w *= torch.exp2(torch.randint(-6, 7, (rows * cols,), generator=g, device="cuda"))
+    codes, scales = pulse.cast_lowp(dtype, w)
+    del w
+    flat = torch.zeros(codes.numel() + 16, dtype=torch.uint8, device="cuda")
+    flat[offset:offset + codes.numel()] = codes
+    x = torch.randn(tokens, cols, generator=g, device="cuda").bfloat16()
+    y = torch.full((tokens, rows + 3), float("nan"), dtype=out_dtype, device="cuda")
+    head.LowpLinear(dtype, flat[offset:offset + codes.numel()], scales, rows, cols)(x, out=y[:, :rows])
+    assert torch.isnan(y[:, rows:]).all()
+    step = max(1, (1 << 27) // cols // 32 * 32)  # rows: whole blocks of 32 values
+    for r in range(0, rows, step):
+        n = min(step, rows - r)
+        k = r * cols
+        wd = values_on_gpu(dtype, codes[k // 2 if dtype == MX else k:], None if dtype == FP8 else scales[k // 32:], n * cols).view(n, cols)
+        want, size = x.double() @ wd.t(), x.double().abs() @ wd.abs().t()
+        bound = (cols + 2) * 2.0 ** -24 * size + (2.0 ** -8 * want.abs() if out_dtype == torch.bfloat16 else 0)
+        assert ((y[:, r:r + n].double() - want).abs() <= bound).all(), (r, n)
+
+
+# more values a row than the registers of a block's waves take: the tokens in LDS, or,
+# for too many of them, the kernel without slabs
+@pytest.mark.parametrize("dtype,cols", [(MX, 6272), (MX, 6656), (MX, 18944), (FP8, 6160), (FP8, 7008), (FP8, 7000), (FP8, 18944)])
+@pytest.mark.parametrize("rows", [17, 2003, 4103])
+def test_wide_rows(dtype, cols, rows):
+    for tokens in (1, 2, 5, 11, 16, 17, 33, 64):
+        check_on_gpu(dtype, rows, cols, tokens, torch.bfloat16 if tokens == 11 else torch.float32, seed=rows + tokens)
+
+
+# a block's runs of two groups of tiles: the waves of a tile in k, and in rows
+@pytest.mark.parametrize("dtype,rows,cols", [(MX, 65551, 5120), (MX, 131099, 3584), (MX, 800003, 128), (MX, 70001, 1152),
+                                             (FP8, 65551, 5120), (FP8, 800003, 208), (FP8, 70001, 1152)])
+@pytest.mark.parametrize("tokens", [1, 5, 17, 33])
+def test_long_weights(dtype, rows, cols, tokens):
+    check_on_gpu(dtype, rows, cols, tokens, seed=tokens)
+
+
+# the other kernel for rows that start a unit, with one, two and four tiles a block:
+# codes that are not 16-byte aligned, or several tokens of very wide rows
+@pytest.mark.parametrize("rows", [17, 2003, 4096, 4100, 8192, 8300, 16384, 17001])
+def test_fp8_without_slabs(rows):
+    for tokens in (1, 5, 16, 17, 40, 64):
+        check_on_gpu(FP8, rows, 208, tokens, seed=rows + tokens, offset=8)
+        check_on_gpu(MX, rows, 256, tokens, seed=rows + tokens, offset=4)
+    check_on_gpu(FP8, min(rows, 9000), 27648, 16, seed=rows)
+
+
 @pytest.mark.parametrize("dtype", [MX, FP8])
 def test_more_rows_than_one_launch_has_threads(dtype):
     """2^30 rows of one value: with 4 threads a row, 2^32 threads and more.  A product
