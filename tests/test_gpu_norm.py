@@ -105,6 +105,47 @@ def test_row_counts(rows):
         near(db, edb, 1e-5, "dbias")
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rms", [False, True])
+@pytest.mark.parametrize("cols", [7, 40, 700, 1000, 1025, 2000, 3584, 5120, 8199, 16384])
+@pytest.mark.parametrize("rows", [1281, 3001])
+def test_many_rows_backward(rows, cols, rms, dtype):
+    """The kernel for more than 1,280 rows, whose blocks keep the columns' sums of their
+    rows, in every form; into outputs of NaN."""
+    x, dy = rows_of(rows, cols, dtype, cols).cuda(), rows_of(rows, cols, dtype, cols + 1, 0.1).cuda()
+    w, b = params(cols, torch.float32, cols + 2, bias=not rms)
+    w, b = w.cuda(), None if b is None else b.cuda()
+    xd = x.double()
+    mean = None if rms else xd.mean(1).float()
+    rstd = (1 / torch.sqrt((xd if rms else xd - mean.double()[:, None]).square().mean(1) + 1e-5)).float()
+    none = [torch.full((rows, cols), float("nan"), dtype=dtype, device="cuda")]
+    none += [torch.full((cols,), float("nan"), device="cuda") for _ in range(1 if rms else 2)]
+    dx, dw, db = head.LayerNorm(w, b, eps=1e-5, rms=rms).backward(dy, x, mean, rstd, *none)
+    edx, edw, edb = exact_backward(dy, x, w, mean, rstd, rms)
+    near(dx, edx.cpu(), TOL[dtype], "dx")
+    # a column's sum has 3,001 terms of either sign: 1e-5 of the largest of their magnitudes
+    xh = (xd if rms else xd - mean.double()[:, None]) * rstd.double()[:, None]
+    assert (dw.double() - edw).abs().max() <= 1e-5 * (dy.double() * xh).abs().sum(0).max()
+    assert (db is None) == rms
+    if not rms:
+        assert (db.double() - edb).abs().max() <= 1e-5 * dy.double().abs().sum(0).max()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("cols", [7, 700, 896, 1500, 2500, 5120, 8200, 16383])
+def test_two_rows_a_group(cols, dtype):
+    """The forward kernel that takes two rows at a time, in every form, with an odd last row."""
+    rows = 16387 if cols <= 1024 else 4099
+    x = rows_of(rows, cols, dtype, cols).cuda()
+    w, b = params(cols, torch.float32, 5, True)
+    w, b = w.cuda(), b.cuda()
+    y, mean, rstd = head.LayerNorm(w, b)(x, y=torch.full_like(x, float("nan")))
+    ey, em, er = exact_forward(x, w, b, 1e-6, False)
+    near(y, ey.cpu(), TOL[dtype], "y")
+    near(mean, em.cpu(), 1e-5, "mean")
+    near(rstd, er.cpu(), 1e-5, "rstd")
+
+
 @pytest.mark.parametrize("rows", [16383, 16385, 4097, 2049])
 def test_many_rows_forward(rows):
     """Two rows a group of lanes, and an odd last one."""
