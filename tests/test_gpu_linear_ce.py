@@ -114,6 +114,78 @@ def test_several_pieces():
             assert (got.double() - want).norm() <= 2.0 ** -8 * want.norm()
 
 
+def check_on_gpu(tokens, vocab, hidden, seed=8, ignored=0.1):
+    """``check`` in 64 bits on the GPU, into outputs of NaN and row by row: a row of dw
+    is off by at most 2^-8 of each token's term (G's rounding) and 2^-8 of itself, a
+    row of dx by the same over the entries; FP32 sums add (terms) * 2^-24 of the terms, and
+    the logits in G's exponents 2 * (hidden + 2) * 2^-24 of their magnitudes."""
+    x, w, y, dl = (t.cuda() for t in inputs(tokens, vocab, hidden, seed, ignored))
+    nan = float("nan")
+    ce = head.LinearCE(w, max_tokens=tokens)
+    loss, lse = ce.forward(x, y, *[torch.full((tokens,), nan, device="cuda") for _ in range(2)])
+    dx, dw = ce.backward(x, y, lse, dl, torch.full_like(x, nan), torch.full_like(w, nan))
+    xd, wd, kept = x.double(), w.double(), y >= 0
+    z, size = xd @ wd.t(), (xd.abs() @ wd.abs().t()).amax(1)
+    want = torch.logsumexp(z, 1)
+    dz = (hidden + 2) * U * size
+    bound = 2 * dz + 1e-6 * (1 + want.abs() + z.abs().amax(1))
+    hit = z.gather(1, y.clamp(min=0)[:, None])[:, 0]
+    assert ((lse.double() - want).abs() <= bound).all()
+    assert ((loss.double() - torch.where(kept, want - hit, 0.0)).abs() <= bound).all()
+    p = torch.exp(z - want[:, None])
+    by = torch.where(kept, dl.double(), 0.0)[:, None]
+    g, terms = p * by, p * by.abs()
+    rows = torch.arange(tokens, device="cuda")
+    g[rows, y.clamp(min=0)] -= by[:, 0]
+    # G's error: of its rounding, and of p through its exponent (relative to p, not to p - 1)
+    err = g.abs() * 2.0 ** -8 + terms * 2 * bound[:, None] + (g.abs() + terms) * (vocab + tokens) * U
+    xd = torch.where(kept[:, None], xd, 0.0)
+    for got, want, allowed in ((dw, g.t() @ xd, err.t() @ xd.norm(dim=1)), (dx, g @ wd, err @ wd.norm(dim=1))):
+        off = (got.double() - want).norm(dim=1)
+        assert (off <= allowed + 2.0 ** -8 * want.norm(dim=1) + 1e-30).all(), (off - allowed).max()
+    return g, (dx, g @ wd), (dw, g.t() @ xd)
+
+
+# pieces, the running dw kernel, all tile shapes, a weight past the caches (61 x 40,003 x 4,096),
+# odd hidden sizes, with ragged last tiles everywhere
+@pytest.mark.parametrize("tokens,vocab,hidden", [(1, 90001, 776), (17, 66003, 1032), (33, 300000, 264), (40, 40000, 2048),
+                                                 (61, 40003, 4096), (64, 70000, 1024), (64, 66003, 1032), (100, 66003, 1032),
+                                                 (128, 20001, 1032), (129, 30011, 520), (500, 40003, 203), (600, 90001, 264),
+                                                 (2100, 66000, 64), (2500, 70000, 520), (2500, 70001, 521)])
+def test_rows_of_large_gradients(tokens, vocab, hidden):
+    _, of_x, of_w = check_on_gpu(tokens, vocab, hidden, ignored=0.0 if tokens == 1 else 0.1)
+    for got, want in (of_x, of_w):  # as exact as their own rounding
+        assert (got.double() - want).norm() <= 0.002 * want.norm()
+
+
+@pytest.mark.parametrize("most", [65, 129, 513, 3000])
+def test_one_workspace_for_fewer_tokens(most):
+    """Calls of fewer tokens than a workspace was sized for give the bits that an object of
+    that number gives, and write nothing past its end."""
+    vocab, hidden = 9000, 136
+    w = inputs(1, vocab, hidden, 1)[1].cuda()
+    L, size = head.lib(), head.lib().pulse_linear_ce_workspace_bytes(most, vocab, hidden)
+    ws = torch.full((size + 65536,), 0xA5, dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    for tokens in (1, 64, 65, 128, 129, 512, 513, most):
+        if tokens > most:
+            continue
+        x, _, y, dl = (t.cuda() for t in inputs(tokens, vocab, hidden, tokens))
+        ce = head.LinearCE(w, max_tokens=tokens)
+        loss, lse = ce.forward(x, y)
+        dx, dw = ce.backward(x, y, lse, dl)
+        got = [torch.full_like(t, float("nan")) for t in (loss, lse, dx, dw)]
+        ws[:size] = 0xA5
+        assert L.pulse_linear_ce_forward(x.data_ptr(), hidden, w.data_ptr(), y.data_ptr(), tokens, vocab, hidden, 1.0,
+                                         got[0].data_ptr(), got[1].data_ptr(), ws.data_ptr(), size, stream) == 0
+        assert L.pulse_linear_ce_backward(x.data_ptr(), hidden, w.data_ptr(), y.data_ptr(), tokens, vocab, hidden, 1.0,
+                                          lse.data_ptr(), dl.data_ptr(), got[2].data_ptr(), hidden, got[3].data_ptr(),
+                                          ws.data_ptr(), size, stream) == 0
+        for a, b in zip(got, (loss, lse, dx, dw)):
+            assert torch.equal(a, b), tokens
+        assert (ws[size:] == 0xA5).all(), tokens
+
+
 @pytest.mark.parametrize("tokens,vocab,hidden", [(300, 40, 72), (1000, 300, 203), (700, 3, 64)])
 def test_many_tokens_share_a_target(tokens, vocab, hidden):
     """Far more tokens than entries, and half of them with the same target."""
