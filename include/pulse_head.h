@@ -139,7 +139,7 @@ int pulse_linear_ce_backward(const uint16_t *x, uint64_t x_stride, const uint16_
  *   W = code * 2^(scale - 127)  (MXFP4; a block with scale 0xFF is NaN),
  *   W = code / inv_scale        (FP8 E4M3, inv_scale as it was cast with).
  * Meant for the few tokens of a decoding step: the weight is read once for
- * every 64 tokens.  Products are exact, summed in FP32, rounded once to y.
+ * every 16 or 32 tokens.  Products are exact, summed in FP32, rounded once to y.
  *   dtype    PULSE_DTYPE_MXFP4 (codes 4-byte aligned) or PULSE_DTYPE_FP8_E4M3
  *            (codes 8-byte aligned; scales unused).
  *   x        BF16 [tokens, cols]; y [tokens, rows] of `y_dtype` (F32 or BF16).

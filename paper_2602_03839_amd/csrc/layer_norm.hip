@@ -3,7 +3,10 @@
 // A row lies in the registers of G lanes, E elements each, so that x (and dy)
 // are read once: the mean, then the sum of squares about it, then the result.
 // Both passes are bound by HBM: forward x in, y out; backward x and dy in, dx
-// out.
+// out.  Two forms fall short of that: the gradient of few rows reads x and dy a second
+// time, from a cache (below), and that of rows of more than 8,192 elements keeps 31 (BF16)
+// to 104 (FP32, element by element) of a lane's values in scratch memory, since 1,024
+// threads have 128 registers each.
 //
 // The gradients of weight and bias are sums down the columns.  A lane owns the
 // same columns of every row that its block takes, so it keeps their sums in

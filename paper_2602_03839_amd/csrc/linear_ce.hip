@@ -1,7 +1,7 @@
 // linear_ce.hip -- softmax cross entropy of z = s x W^T over a large vocabulary,
 // forward and backward, with the logits in registers only.
 //
-// Forward: a block computes a tile of 256 vocabulary entries by its tokens
+// Forward: a block computes a tile of 256 (128 for few) vocabulary entries by its tokens
 // (gemm_tile.hpp), reduces it per token to the largest logit and the sum of
 // exponentials below it, and writes those two numbers; a second kernel joins a
 // token's pairs.  The logit of the target is written by the lane that has it.
@@ -449,6 +449,8 @@ __device__ void add_rests(const GradParams& p, char* lds, uint32_t m0, uint32_t 
   __syncthreads();
 }
 
+// (The 256 by 256 tile's rests and way out keep 60 registers in scratch memory; the
+// product's loop does not.)
 template <typename T, bool RESTS>
 __device__ void dw_block(const GradParams& p, char* lds, uint32_t id) {
   uint32_t m0, n0;

@@ -1,8 +1,10 @@
 // lowp_matmul.hip -- y = x W^T for a few BF16 tokens x and a weight W that a
 // receiver holds as MXFP4 or FP8 codes.
 //
-// The codes are read once from HBM, which bounds the kernels: half a byte and a
-// thirty-second of a byte of scale a value (MXFP4), or a byte (FP8).  A wave
+// The codes' way from HBM bounds the kernels: half a byte and a thirty-second of a byte
+// of scale a value (MXFP4), or a byte (FP8).  They are read once for every 32 tokens, or
+// 16 (rows that start inside a unit, tokens in LDS, fewer blocks than CUs), after the
+// first time from the last level cache if they fit there.  A wave
 // takes 16 rows and converts 16 bytes of each lane's codes to BF16 in registers:
 // exact, since a code has at most 3 (FP8: 4) significant bits and a power-of-two
 // scale moves only the exponent.  v_mfma_f32_16x16x32_bf16 multiplies them with 16
@@ -539,8 +541,10 @@ bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
   z.tiles = (p.rows + 15) / 16;
   // a block with one tile or two loads its tokens for little: the other kernel's blocks,
   // which take two tiles of each at once, are one round up to kLpCus tiles.  64 tokens,
-  // MXFP4, us by slabs and by the other: 2,048 x 3,584 11 and 12, 4,096 x 3,584 21 and 12.5,
-  // 8,192 x 3,584 25 and 21, 12,288 x 5,120 both 44
+  // us by slabs and by the other: MXFP4, 2,048 x 3,584 11 and 12, 2,080 x 3,584 20 and 12,
+  // 4,096 x 3,584 22 and 12.5, 8,192 x 3,584 27 and 21, 8,192 x 896 11.5 and 8, 12,288 x 5,120
+  // both 44; FP8, 2,080 x 3,584 24 and 14, 4,096 x 5,120 36 and 19, 8,192 x 3,584 34 and 24,
+  // 8,192 x 896 13 and 9.  (40 tokens of 2,080 rows: 11 and 12, FP8 12.5 and 14)
   if (p.tokens > 32 && z.tiles > kLpCus / 2 && z.tiles <= 2 * kLpCus) return false;
   z.slabs = (p.cols / U::kValues + kSlabUnits - 1) / kSlabUnits;
   const uint64_t x_bytes = (p.tokens < 16 ? p.tokens : 16) * ((uint64_t)z.slabs * kSlabUnits * U::kValues * 2 + 16);
@@ -585,7 +589,9 @@ void launch_type(const LowpMatmulParams& p, hipStream_t stream) {
   // Each group of row tiles reads all tokens' values again, and a round of blocks takes as
   // long as its last: as few groups as fit one round; of many rounds, two tiles each.  16
   // tokens, MXFP4, in us with 1, 2 and 4 tiles: 5,120 x 27,648 (320 tiles) 75 and 51;
-  // 12,288 x 16,384 (768) 61 with 2, 47 with 4; one token, 40,000 x 5,056 (2,500) 33, 28, 33.
+  // 12,288 x 16,384 (768) 65 with 2, 52 with 4, 16,384 x 27,648 (1,024) 113 and 88, FP8 70 and
+  // 58, 125 and 104 (5 tokens: 48 and 43, FP8 58 and 52; the least gain at 513 tiles, 8,208 x
+  // 27,648: 65 and 70, FP8 68 and 79); one token, 40,000 x 5,056 (2,500) 33, 28, 33.
   const uint32_t tiles = (p.rows + 15) / 16;
   if (p.tokens <= 16 && tiles <= kLpCus) launch_shape<MX, 1, 1, false>(p, stream);
   else if (p.tokens <= 16 && tiles > 2 * kLpCus && tiles <= 4 * kLpCus) launch_shape<MX, 4, 1, false>(p, stream);
