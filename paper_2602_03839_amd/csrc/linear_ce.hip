@@ -26,8 +26,8 @@
 //
 // The three products of the backward pass and the one of the forward pass are
 // bound by the matrix cores for many tokens (4,096 at 152,064 x 3,584, 4.46 TFLOP
-// each: forward 3.5 ms, G 3.7, dx 3.6, dw 3.9), by the weight's bytes for few (61 at
-// 152,064 x 5,120, 1.56 GB: 297, 310 and 285 us to read it, 303 to write dw).
+// each: forward 3.5 ms, G 3.8, dx 3.5, dw 4.0), by the weight's bytes for few (61 at
+// 152,064 x 5,120, 1.56 GB: 288, 305 and 278 us to read it, 294 to write dw).
 #include "device_common.hpp"
 #include "gemm_tile.hpp"
 #include "head.hpp"
