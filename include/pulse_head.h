@@ -81,6 +81,64 @@ int pulse_layer_norm_backward(int dtype, const void *dy, uint64_t dy_stride, con
                               void *stream);
 
 /*
+ * pulse_block_norm_forward -- a block's output b joins the residual stream h, and
+ * the stream is normalised for the next block; per row, with N_post and N the norms
+ * of pulse_layer_norm_forward (PULSE_NORM_RMS for both) with the same eps,
+ *   h_out = residual_scale * h + gate * N_post(b),
+ *   y     = N(h_out)                    of the sum before it is rounded,
+ * each rounded once.
+ *   dtype         of b, h, h_out and y: PULSE_DTYPE_F32 or PULSE_DTYPE_BF16.
+ *   weight, bias  of N, [cols] of `param_dtype` (F32 or BF16); bias may be NULL.
+ *   post_weight, post_bias  of N_post; post_weight NULL: b is taken as it is
+ *                 (and post_bias is NULL too); post_bias may be NULL.
+ *   gate          [cols] of `param_dtype`, a factor per column; NULL: 1.
+ *   h_out         may be h itself (the same pointer and stride).
+ *   stats         FP32, rows of `rows` values stats_stride apart: rstd of N, rstd of
+ *                 N_post, then (without PULSE_NORM_RMS) mean of N, mean of N_post;
+ *                 N_post's are left as they were without post_weight.  NULL: not kept.
+ * cols is 1 to PULSE_NORM_MAX_COLS, residual_scale finite.
+ */
+int pulse_block_norm_forward(int dtype, const void *b, uint64_t b_stride, const void *h,
+                             uint64_t h_stride, float residual_scale, int param_dtype,
+                             const void *weight, const void *bias, const void *post_weight,
+                             const void *post_bias, const void *gate, void *y, uint64_t y_stride,
+                             void *h_out, uint64_t h_out_stride, float *stats,
+                             uint64_t stats_stride, uint64_t rows, uint32_t cols, float eps,
+                             uint32_t flags, void *stream);
+
+/* Workspace of pulse_block_norm_backward for rows of `cols` elements. */
+size_t pulse_block_norm_workspace_bytes(uint32_t cols);
+
+/*
+ * pulse_block_norm_backward -- the gradient of a forward pass that gave h_out and
+ * stats: with xh and bh the rows of h_out and b less their mean, times their rstd
+ * (bh = b without post_weight), a = dy * weight and, per row,
+ *   g  = dh_out + rstd * (a - sum(a)/n - xh * sum(a * xh)/n),
+ *   c  = g * gate * post_weight,
+ *   dh = residual_scale * g,
+ *   db = post_rstd * (c - sum(c)/n - bh * sum(c * bh)/n)   (without post_weight: c)
+ * (without the terms of sum(a) and sum(c) with PULSE_NORM_RMS), rounded once, and
+ * summed over the rows, FP32 [cols],
+ *   dweight = dy * xh,  dbias = dy,  dpost_weight = g * gate * bh,
+ *   dpost_bias = g * gate,  dgate = g * N_post(b).
+ *   dh_out   the gradient that reaches h_out elsewhere; NULL: none.
+ *   b        may be NULL with neither post_weight nor gate.
+ *   dbias, dpost_weight, dpost_bias, dgate  may each be NULL; dpost_weight,
+ *            dpost_bias need post_weight, dgate needs gate.
+ * rows == 0 sets the sums to zero.
+ */
+int pulse_block_norm_backward(int dtype, const void *dy, uint64_t dy_stride, const void *dh_out,
+                              uint64_t dh_out_stride, const void *b, uint64_t b_stride,
+                              const void *h_out, uint64_t h_out_stride, float residual_scale,
+                              int param_dtype, const void *weight, const void *post_weight,
+                              const void *post_bias, const void *gate, const float *stats,
+                              uint64_t stats_stride, void *db, uint64_t db_stride, void *dh,
+                              uint64_t dh_stride, float *dweight, float *dbias,
+                              float *dpost_weight, float *dpost_bias, float *dgate, uint64_t rows,
+                              uint32_t cols, uint32_t flags, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/*
  * Softmax cross entropy of a head's logits, which are never stored: with
  *   z[t][v] = logit_scale * sum_k x[t][k] weight[v][k]      (products exact,
  *             summed in FP32),

@@ -50,6 +50,69 @@ struct NormGradParams {
 hipError_t launch_layer_norm(bool bf16, const NormParams& p, hipStream_t stream);
 hipError_t launch_layer_norm_grad(bool bf16, const NormGradParams& p, hipStream_t stream);
 
+// ---------------------------------------------------------------- block norm
+
+constexpr uint32_t kBlockNormBlocks = 512;  // blocks of the backward pass, each with its column sums
+
+struct BlockNormParams {
+  const void* b;
+  uint64_t b_stride;
+  const void* h;
+  uint64_t h_stride;
+  float residual_scale;
+  const void* weight;
+  const void* bias;         // may be null
+  const void* post_weight;  // null: b is not normalised
+  const void* post_bias;    // may be null
+  const void* gate;         // may be null
+  void* y;
+  uint64_t y_stride;
+  void* h_out;  // h itself, or elsewhere
+  uint64_t h_out_stride;
+  float* stats;  // rows of rstd, post_rstd, mean, post_mean; null: not kept
+  uint64_t stats_stride;
+  uint64_t rows;
+  uint32_t cols;
+  float eps;
+  int param_bf16;
+  bool rms;
+};
+
+struct BlockNormGradParams {
+  const void* dy;
+  uint64_t dy_stride;
+  const void* dh_out;  // null: zeros
+  uint64_t dh_out_stride;
+  const void* b;  // null where nothing asks for it: neither post norm nor gate
+  uint64_t b_stride;
+  const void* h_out;
+  uint64_t h_out_stride;
+  float residual_scale;
+  const void* weight;
+  const void* post_weight;
+  const void* post_bias;
+  const void* gate;
+  const float* stats;
+  uint64_t stats_stride;
+  void* db;
+  uint64_t db_stride;
+  void* dh;
+  uint64_t dh_stride;
+  float* dweight;
+  float* dbias;  // this and the following may be null
+  float* dpost_weight;
+  float* dpost_bias;
+  float* dgate;
+  float* partial;  // [blocks][cols] of dy xh, then of g bh, dy and g
+  uint64_t rows;
+  uint32_t cols;
+  int param_bf16;
+  bool rms, biases;  // biases: the sums of dy and g are asked for
+};
+
+hipError_t launch_block_norm(bool bf16, const BlockNormParams& p, hipStream_t stream);
+hipError_t launch_block_norm_grad(bool bf16, const BlockNormGradParams& p, hipStream_t stream);
+
 // ---------------------------------------------------------------- low-bit products
 
 struct LowpMatmulParams {

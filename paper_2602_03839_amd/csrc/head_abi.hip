@@ -51,6 +51,25 @@ int check_matrix(const char* who, const char* name, const void* p, uint64_t stri
   return PULSE_OK;
 }
 
+// what both directions of the block norm ask of their arguments
+int check_block_norm(const char* who, int dtype, int param_dtype, uint64_t rows, uint32_t cols, uint32_t flags,
+                     float residual_scale, const void* weight, const void* post_weight, const void* post_bias,
+                     const void* gate, const float* stats, uint64_t stats_stride) {
+  // the statistics are checked apart: they may be absent
+  const float* none = (const float*)(uintptr_t)16;
+  if (int rc = check_norm(who, dtype, param_dtype, rows, cols, flags, weight, none, none)) return rc;
+  if (!(residual_scale - residual_scale == 0.0f))
+    return fail(PULSE_EINVAL, "%s: residual_scale is not finite", who);
+  if (post_bias && !post_weight) return fail(PULSE_EINVAL, "%s: post_bias without post_weight", who);
+  for (const void* v : {post_weight, post_bias, gate})
+    if (!aligned16(v)) return fail(PULSE_EALIGN, "%s: post_weight, post_bias or gate not 16-byte aligned", who);
+  if (!aligned(stats, 4)) return fail(PULSE_EALIGN, "%s: stats not 4-byte aligned", who);
+  if (stats && (stats_stride < rows || stats_stride > (1ull << 40)))
+    return fail(PULSE_EINVAL, "%s: stats stride %llu for %llu rows", who, (unsigned long long)stats_stride,
+                (unsigned long long)rows);
+  return PULSE_OK;
+}
+
 bool ce_handles(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   return tokens <= 0x7FFFFFFFu && vocab != 0 && vocab <= 0x7FFFFFFFu && hidden != 0 && hidden <= PULSE_CE_MAX_HIDDEN;
 }
@@ -117,6 +136,76 @@ int pulse_layer_norm_backward(int dtype, const void* dy, uint64_t dy_stride, con
                              (float*)workspace, rows, cols, param_dtype == PULSE_DTYPE_BF16};
   return hip_status(pulse::launch_layer_norm_grad(dtype == PULSE_DTYPE_BF16, p, (hipStream_t)stream),
                     "layer_norm backward launch");
+}
+
+int pulse_block_norm_forward(int dtype, const void* b, uint64_t b_stride, const void* h, uint64_t h_stride,
+                             float residual_scale, int param_dtype, const void* weight, const void* bias,
+                             const void* post_weight, const void* post_bias, const void* gate, void* y,
+                             uint64_t y_stride, void* h_out, uint64_t h_out_stride, float* stats,
+                             uint64_t stats_stride, uint64_t rows, uint32_t cols, float eps, uint32_t flags,
+                             void* stream) {
+  const char* who = "block_norm forward";
+  if (int rc = check_block_norm(who, dtype, param_dtype, rows, cols, flags, residual_scale, weight, post_weight,
+                                post_bias, gate, stats, stats_stride))
+    return rc;
+  if (int rc = check_matrix(who, "b", b, b_stride, rows, cols)) return rc;
+  if (int rc = check_matrix(who, "h", h, h_stride, rows, cols)) return rc;
+  if (int rc = check_matrix(who, "y", y, y_stride, rows, cols)) return rc;
+  if (int rc = check_matrix(who, "h_out", h_out, h_out_stride, rows, cols)) return rc;
+  if (!aligned16(bias)) return fail(PULSE_EALIGN, "%s: bias not 16-byte aligned", who);
+  if (!(eps >= 0.0f)) return fail(PULSE_EINVAL, "%s: eps is negative or NaN", who);
+  if (rows == 0) return ok();
+  if (h_out == h && h_out_stride != h_stride)
+    return fail(PULSE_EINVAL, "%s: h_out is h with another stride", who);
+  pulse::BlockNormParams p = {b, b_stride, h, h_stride, residual_scale, weight, bias, post_weight, post_bias, gate,
+                              y, y_stride, h_out, h_out_stride, stats, stats_stride, rows, cols, eps,
+                              param_dtype == PULSE_DTYPE_BF16, (flags & PULSE_NORM_RMS) != 0};
+  return hip_status(pulse::launch_block_norm(dtype == PULSE_DTYPE_BF16, p, (hipStream_t)stream),
+                    "block_norm launch");
+}
+
+size_t pulse_block_norm_workspace_bytes(uint32_t cols) {
+  return (size_t)pulse::kBlockNormBlocks * cols * 4 * sizeof(float);
+}
+
+int pulse_block_norm_backward(int dtype, const void* dy, uint64_t dy_stride, const void* dh_out,
+                              uint64_t dh_out_stride, const void* b, uint64_t b_stride, const void* h_out,
+                              uint64_t h_out_stride, float residual_scale, int param_dtype, const void* weight,
+                              const void* post_weight, const void* post_bias, const void* gate,
+                              const float* stats, uint64_t stats_stride, void* db, uint64_t db_stride, void* dh,
+                              uint64_t dh_stride, float* dweight, float* dbias, float* dpost_weight,
+                              float* dpost_bias, float* dgate, uint64_t rows, uint32_t cols, uint32_t flags,
+                              void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "block_norm backward";
+  if (int rc = check_block_norm(who, dtype, param_dtype, rows, cols, flags, residual_scale, weight, post_weight,
+                                post_bias, gate, stats, stats_stride))
+    return rc;
+  if (rows && !stats) return fail(PULSE_EINVAL, "%s: stats is NULL", who);
+  if (int rc = check_matrix(who, "dy", dy, dy_stride, rows, cols)) return rc;
+  if (dh_out)
+    if (int rc = check_matrix(who, "dh_out", dh_out, dh_out_stride, rows, cols)) return rc;
+  const bool reads_b = post_weight || gate;
+  if (reads_b)
+    if (int rc = check_matrix(who, "b", b, b_stride, rows, cols)) return rc;
+  if (int rc = check_matrix(who, "h_out", h_out, h_out_stride, rows, cols)) return rc;
+  if (int rc = check_matrix(who, "db", db, db_stride, rows, cols)) return rc;
+  if (int rc = check_matrix(who, "dh", dh, dh_stride, rows, cols)) return rc;
+  if (!dweight) return fail(PULSE_EINVAL, "%s: dweight is NULL", who);
+  if ((dpost_weight || dpost_bias) && !post_weight)
+    return fail(PULSE_EINVAL, "%s: dpost_weight or dpost_bias without post_weight", who);
+  if (dgate && !gate) return fail(PULSE_EINVAL, "%s: dgate without gate", who);
+  for (const void* v : {(const void*)dweight, (const void*)dbias, (const void*)dpost_weight,
+                        (const void*)dpost_bias, (const void*)dgate})
+    if (!aligned(v, 4)) return fail(PULSE_EALIGN, "%s: a parameter's gradient is not 4-byte aligned", who);
+  if (int rc = check_space(who, workspace, workspace_bytes, pulse_block_norm_workspace_bytes(cols))) return rc;
+  const bool biases = dbias || dpost_bias || (dgate && post_bias);
+  pulse::BlockNormGradParams p = {dy, dy_stride, dh_out, dh_out_stride, reads_b ? b : nullptr, b_stride, h_out,
+                                  h_out_stride, residual_scale, weight, post_weight, post_bias, gate, stats,
+                                  stats_stride, db, db_stride, dh, dh_stride, dweight, dbias, dpost_weight,
+                                  dpost_bias, dgate, (float*)workspace, rows, cols,
+                                  param_dtype == PULSE_DTYPE_BF16, (flags & PULSE_NORM_RMS) != 0, biases};
+  return hip_status(pulse::launch_block_norm_grad(dtype == PULSE_DTYPE_BF16, p, (hipStream_t)stream),
+                    "block_norm backward launch");
 }
 
 size_t pulse_linear_ce_workspace_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden) {

@@ -13,6 +13,7 @@ Outputs are allocated on the stream that the call runs on unless they are given.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import threading
 from typing import Optional
@@ -29,7 +30,8 @@ CE_MAX_HIDDEN = 65536
 MAX_SIZE = (1 << 31) - 1  # of a vocabulary, a weight's rows or columns, tokens
 
 EXPORTS = ("pulse_layer_norm_workspace_bytes", "pulse_layer_norm_forward",
-           "pulse_layer_norm_backward", "pulse_linear_ce_workspace_bytes", "pulse_linear_ce_forward",
+           "pulse_layer_norm_backward", "pulse_block_norm_workspace_bytes", "pulse_block_norm_forward",
+           "pulse_block_norm_backward", "pulse_linear_ce_workspace_bytes", "pulse_linear_ce_forward",
            "pulse_linear_ce_backward", "pulse_lowp_matmul")
 
 _lock = threading.Lock()
@@ -52,6 +54,12 @@ def lib():
                                                    u32, f32, u32, vp]
             L.pulse_layer_norm_backward.argtypes = [i32, vp, u64, vp, u64, i32, vp, vp, vp, vp, u64,
                                                     vp, vp, u64, u32, u32, vp, sz, vp]
+            L.pulse_block_norm_workspace_bytes.argtypes = [u32]
+            L.pulse_block_norm_forward.argtypes = [i32, vp, u64, vp, u64, f32, i32, vp, vp, vp, vp, vp, vp, u64,
+                                                   vp, u64, vp, u64, u64, u32, f32, u32, vp]
+            L.pulse_block_norm_backward.argtypes = [i32, vp, u64, vp, u64, vp, u64, vp, u64, f32, i32, vp, vp, vp,
+                                                    vp, vp, u64, vp, u64, vp, u64, vp, vp, vp, vp, vp, u64, u32,
+                                                    u32, vp, sz, vp]
             L.pulse_lowp_matmul.argtypes = [i32, vp, vp, f32, u32, u32, vp, u64, u32, i32, vp, u64, vp]
             L.pulse_linear_ce_workspace_bytes.argtypes = [u32, u32, u32]
             L.pulse_linear_ce_forward.argtypes = [vp, u64, vp, vp, u32, u32, u32, f32, vp, vp, vp, sz, vp]
@@ -123,6 +131,14 @@ def _vec(t, name, n, device, stream):
     return t, _f32(t, name, n, device)
 
 
+_NOTHING = contextlib.nullcontext()
+
+
+def _on(device):
+    """The device of a call's tensors as the current one, which a launch goes by."""
+    return _NOTHING if torch._C._cuda_getDevice() == device.index else torch.cuda.device(device)
+
+
 class LayerNorm:
     """Layer norm, or RMS norm with ``rms``, over the last axis.
 
@@ -189,6 +205,103 @@ class LayerNorm:
         if rc:
             _check(rc, "pulse_layer_norm_backward")
         return dx, dweight, dbias
+
+
+class BlockNorm:
+    """What joins two blocks: a block's output b is added to the residual stream h
+    and the stream is normalised for the next block,
+
+        h_out = residual_scale * h + gate * post_norm(b),    y = norm(h_out),
+
+    in one pass.  ``weight`` and ``bias`` (may be None) are the norm's, [cols];
+    ``post_weight``, ``post_bias`` those of the norm of the block's output, None for
+    none; ``gate`` a factor per column, None for none.  All parameters are float32 or
+    all bfloat16; activations are float32 or bfloat16 of their own.  Both norms are
+    RMS norms with ``rms``, layer norms without.
+    """
+
+    def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                 post_weight: Optional[torch.Tensor] = None, post_bias: Optional[torch.Tensor] = None,
+                 gate: Optional[torch.Tensor] = None, residual_scale: float = 1.0, eps: float = 1e-6,
+                 rms: bool = True):
+        self._dt = _dtype(weight, "weight")
+        self.device, self.cols = weight.device, weight.numel()
+        if not 1 <= self.cols <= NORM_MAX_COLS:
+            raise PulseError(f"weight has {self.cols} elements, 1 to {NORM_MAX_COLS} are handled")
+        if post_bias is not None and post_weight is None:
+            raise PulseError("post_bias needs post_weight")
+        self._params = [_p(t, name, dtype=weight.dtype, numel=self.cols, device=self.device, optional=k > 0)
+                        for k, (t, name) in enumerate(((weight, "weight"), (bias, "bias"),
+                                                       (post_weight, "post_weight"), (post_bias, "post_bias"),
+                                                       (gate, "gate")))]
+        self.weight, self.bias, self.post_weight, self.post_bias, self.gate = weight, bias, post_weight, post_bias, gate
+        self.residual_scale, self.eps, self.rms = float(residual_scale), float(eps), bool(rms)
+        self._flags, self._nstats, self._lib = (NORM_RMS, 2, lib()) if rms else (0, 4, lib())
+        self._nws = int(self._lib.pulse_block_norm_workspace_bytes(self.cols))
+        self.ws = None  # of the gradient: allocated by the first call that asks for one
+
+    def __call__(self, b: torch.Tensor, h: torch.Tensor, y: Optional[torch.Tensor] = None,
+                 h_out: Optional[torch.Tensor] = None, stats: Optional[torch.Tensor] = None,
+                 keep_stats: bool = True, stream=None):
+        """(y, h_out, stats) for b and h [rows, cols].  ``h_out`` may be h itself, which
+        is then brought up to date in place.  stats, float32 [2 or 4, rows], is what the
+        gradient asks for: rstd, post_rstd and, for layer norms, mean, post_mean (post:
+        only with post_weight); None with ``keep_stats`` false."""
+        dev, cols, dt = self.device, self.cols, _dtype(b, "b")
+        pb, sb = _matrix(b, "b", cols, device=dev)
+        rows = b.shape[0]
+        ph, sh = _matrix(h, "h", cols, rows, b.dtype, dev)
+        y, py, sy = _out(y, "y", cols, rows, b.dtype, dev, stream)
+        h_out, po, so = _out(h_out, "h_out", cols, rows, b.dtype, dev, stream)
+        if not keep_stats:
+            stats, ps, ss = None, None, 0
+        else:
+            stats, ps, ss = _out(stats, "stats", rows, self._nstats, torch.float32, dev, stream)
+        pw, pwb, pp, ppb, pg = self._params
+        with _on(dev):
+            rc = self._lib.pulse_block_norm_forward(dt, pb, sb, ph, sh, self.residual_scale, self._dt, pw, pwb, pp,
+                                                    ppb, pg, py, sy, po, so, ps, ss, rows, cols, self.eps,
+                                                    self._flags, _stream(stream, dev))
+        if rc:
+            _check(rc, "pulse_block_norm_forward")
+        return y, h_out, stats
+
+    def backward(self, dy: torch.Tensor, dh_out: Optional[torch.Tensor], b: Optional[torch.Tensor],
+                 h_out: torch.Tensor, stats: torch.Tensor, db: Optional[torch.Tensor] = None,
+                 dh: Optional[torch.Tensor] = None, stream=None):
+        """(db, dh, dweight, dbias, dpost_weight, dpost_bias, dgate) for the upstream
+        gradients of y and of h_out (None: zeros) and the forward pass's b (None will do
+        with neither post norm nor gate), h_out and stats; None for a parameter that is
+        not there, float32 for the others."""
+        dev, cols, dt = self.device, self.cols, _dtype(h_out, "h_out")
+        po, so = _matrix(h_out, "h_out", cols, device=dev)
+        rows, typ = h_out.shape[0], h_out.dtype
+        py, sy = _matrix(dy, "dy", cols, rows, typ, dev)
+        pd, sd = (None, 0) if dh_out is None else _matrix(dh_out, "dh_out", cols, rows, typ, dev)
+        if b is None and self.post_weight is None and self.gate is None:
+            pb, sb = None, 0
+        else:
+            pb, sb = _matrix(b, "b", cols, rows, typ, dev)
+        ps, ss = _matrix(stats, "stats", rows, self._nstats, torch.float32, dev)
+        db, pdb, sdb = _out(db, "db", cols, rows, typ, dev, stream)
+        dh, pdh, sdh = _out(dh, "dh", cols, rows, typ, dev, stream)
+        if self.ws is None:
+            self.ws = _new((self._nws,), torch.uint8, dev, stream)
+        pw, pwb, pp, ppb, pg = self._params
+        # one allocation for all parameters' gradients: a call of few rows is bound by the host
+        there = [k for k, p in enumerate(self._params) if p is not None]
+        sums, to = _new((len(there), cols), torch.float32, dev, stream), [None] * 5
+        out = [None] * 5
+        for k, g in zip(there, sums.unbind()):
+            out[k], to[k] = g, g.data_ptr()
+        with _on(dev):
+            rc = self._lib.pulse_block_norm_backward(dt, py, sy, pd, sd, pb, sb, po, so, self.residual_scale,
+                                                     self._dt, pw, pp, ppb, pg, ps, ss, pdb, sdb, pdh, sdh, *to,
+                                                     rows, cols, self._flags, self.ws.data_ptr(), self._nws,
+                                                     _stream(stream, dev))
+        if rc:
+            _check(rc, "pulse_block_norm_backward")
+        return (db, dh, *out)
 
 
 class LinearCE:
