@@ -189,6 +189,46 @@ int pulse_linear_ce_backward(const uint16_t *x, uint64_t x_stride, const uint16_
                              uint16_t *dweight, void *workspace, size_t workspace_bytes,
                              void *stream);
 
+/* The most drafted tokens of a sequence. */
+#define PULSE_VERIFY_MAX_DRAFTS 128
+
+/* A workspace for calls of up to `batch` sequences and `drafts` drafts each; 0 for sizes
+ * that no call handles. */
+size_t pulse_verify_drafts_workspace_bytes(uint32_t batch, uint32_t drafts, uint32_t vocab);
+
+/*
+ * pulse_verify_drafts -- which drafted tokens a target model keeps, and the token that
+ * follows them, so that all are distributed as the target's own.  With, for the k-th
+ * draft x of a sequence,
+ *   p = softmax(scale * target row k),  q = softmax(draft_scale * draft row k),
+ * the draft is taken if those before it were and u[k] * q(x) < p(x).  At the first that
+ * is not taken, a token is drawn from max(p - q, 0); where all were, from p of the
+ * next target row: the lowest v with
+ *   sum of the weights of 0 ... v  >  u[drafts] * sum of all weights.
+ * With drafts == 0 that is sampling from p.
+ *   dtype    of the logits: PULSE_DTYPE_F32 or PULSE_DTYPE_BF16.
+ *   target   [batch * (drafts + 1), vocab], a sequence's rows one after the other.
+ *   draft    [batch * drafts, vocab]; NULL: q is 1 at the draft.
+ *   tokens   int64 [batch, drafts]; one outside [0, vocab) is not taken.
+ *   lengths  int32 [batch], a sequence's number of drafts, brought into 0 ... drafts;
+ *            NULL: drafts of each.  Rows past them are not read.
+ *   uniform  FP32 [batch, drafts + 1], in [0, 1).
+ *   out      int64 [batch, drafts + 1]: the drafts taken, the token drawn, then -1.
+ *   count    int32 [batch]: how many drafts were taken.
+ *   logprob  FP32 [batch, drafts + 1]: log p of each token of `out`, 0 past them.
+ * A logit of -inf has probability 0.  A row that is -inf throughout, or holds a NaN or
+ * +inf, has p (or q) = 0 everywhere: where p has, the draft is refused, and where
+ * nothing can be drawn the token is -1 and its logprob -inf.
+ * Probabilities and their sums are FP64, and so are the scales: rounded to FP32 they
+ * would move every border by some 1e-7.  drafts is at most PULSE_VERIFY_MAX_DRAFTS,
+ * batch * (2 drafts + 1) and vocab are below 2^31, the scales positive and finite.
+ */
+int pulse_verify_drafts(int dtype, const void *target, uint64_t target_stride, const void *draft,
+                        uint64_t draft_stride, const int64_t *tokens, const int32_t *lengths,
+                        const float *uniform, uint32_t batch, uint32_t drafts, uint32_t vocab,
+                        double scale, double draft_scale, int64_t *out, int32_t *count,
+                        float *logprob, void *workspace, size_t workspace_bytes, void *stream);
+
 /*
  * pulse_lowp_matmul -- y = x W^T, W the receiver's copy of a [rows, cols]
  * weight as pulse_cast_lowp and pulse_apply_lowp_batch leave it (codes flat in

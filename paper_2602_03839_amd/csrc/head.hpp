@@ -167,6 +167,51 @@ uint64_t linear_ce_bytes(uint32_t tokens, uint32_t vocab, uint32_t hidden);
 hipError_t launch_linear_ce(const LinearCeParams& p, char* ws, hipStream_t stream);
 hipError_t launch_linear_ce_grad(const LinearCeGradParams& p, char* ws, hipStream_t stream);
 
+// ---------------------------------------------------------------- drafts
+
+constexpr uint32_t kVerifyMaxDrafts = 128;
+
+struct VerifyPart {  // of a row's tile: the sum of exponentials below its largest logit
+  double sum;
+  float top;
+};
+
+// A row's distribution: entry z has the probability 2^((z - top) by) inv; all of them 0
+// where inv is, that is, where the logits' exponentials have no finite positive sum.
+struct VerifyRow {
+  double by, inv;
+  float top;
+};
+
+// What is decided for a sequence: the rows at its first draft that is not taken.
+struct VerifyDecision {
+  VerifyRow p, q;
+  uint32_t taken, length;
+};
+
+struct VerifyParams {
+  const void* target;  // [batch][drafts + 1] rows
+  uint64_t target_stride;
+  const void* draft;  // [batch][drafts] rows; null: q is 1 at the draft
+  uint64_t draft_stride;
+  const int64_t* tokens;   // [batch][drafts]
+  const int32_t* lengths;  // [batch]; null: drafts of each
+  const float* uniform;    // [batch][drafts + 1]
+  uint32_t batch, drafts, vocab;
+  double scale, by, draft_by;  // the latter log2(e) times the scales
+  int64_t* out;
+  int32_t* count;
+  float* logprob;
+  // set by the launcher
+  uint32_t rows, tiles;  // of a sequence; of a row
+  VerifyPart* parts;     // [batch][rows][tiles]
+  double* rests;         // [batch][tiles]: sums of max(p - q, 0)
+  VerifyDecision* decisions;
+};
+
+uint64_t verify_workspace(uint32_t batch, uint32_t drafts, uint32_t vocab);
+hipError_t launch_verify(bool bf16, const VerifyParams& p, char* ws, hipStream_t stream);
+
 // ---------------------------------------------------------------- device helpers
 
 typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));

@@ -70,6 +70,11 @@ int check_block_norm(const char* who, int dtype, int param_dtype, uint64_t rows,
   return PULSE_OK;
 }
 
+bool verify_handles(uint32_t batch, uint32_t drafts, uint32_t vocab) {
+  return drafts <= PULSE_VERIFY_MAX_DRAFTS && vocab != 0 && vocab <= 0x7FFFFFFFu &&
+         (uint64_t)batch * (2 * drafts + 1) <= 0x7FFFFFFFull;
+}
+
 bool ce_handles(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   return tokens <= 0x7FFFFFFFu && vocab != 0 && vocab <= 0x7FFFFFFFu && hidden != 0 && hidden <= PULSE_CE_MAX_HIDDEN;
 }
@@ -248,6 +253,57 @@ int pulse_linear_ce_backward(const uint16_t* x, uint64_t x_stride, const uint16_
                                  dx, dx_stride, dweight};
   return hip_status(pulse::launch_linear_ce_grad(p, (char*)workspace, (hipStream_t)stream),
                     "linear_ce backward launch");
+}
+
+size_t pulse_verify_drafts_workspace_bytes(uint32_t batch, uint32_t drafts, uint32_t vocab) {
+  return batch && verify_handles(batch, drafts, vocab) ? pulse::verify_workspace(batch, drafts, vocab) : 0;
+}
+
+int pulse_verify_drafts(int dtype, const void* target, uint64_t target_stride, const void* draft,
+                        uint64_t draft_stride, const int64_t* tokens, const int32_t* lengths, const float* uniform,
+                        uint32_t batch, uint32_t drafts, uint32_t vocab, double scale, double draft_scale,
+                        int64_t* out, int32_t* count, float* logprob, void* workspace, size_t workspace_bytes,
+                        void* stream) {
+  const char* who = "verify_drafts";
+  if (dtype != PULSE_DTYPE_F32 && dtype != PULSE_DTYPE_BF16)
+    return fail(PULSE_EINVAL, "%s: dtype %d is neither F32 nor BF16", who, dtype);
+  if (!verify_handles(batch, drafts, vocab))
+    return fail(PULSE_EINVAL, "%s: %u sequences of %u drafts, vocabulary of %u", who, batch, drafts, vocab);
+  for (double v : {scale, draft_scale})
+    if (!(v > 0.0 && v - v == 0.0)) return fail(PULSE_EINVAL, "%s: a scale is not positive and finite", who);
+  if (batch == 0) return ok();
+  // rows are read from any element on
+  const uintptr_t size = dtype == PULSE_DTYPE_BF16 ? 2 : 4;
+  if (!target || (drafts && !tokens) || !uniform) return fail(PULSE_EINVAL, "%s: target, tokens or uniform is NULL", who);
+  if (!out || !count || !logprob) return fail(PULSE_EINVAL, "%s: out, count or logprob is NULL", who);
+  if (target_stride < vocab || target_stride > (1ull << 40) ||
+      (draft && (draft_stride < vocab || draft_stride > (1ull << 40))))
+    return fail(PULSE_EINVAL, "%s: row strides %llu and %llu for a vocabulary of %u", who,
+                (unsigned long long)target_stride, (unsigned long long)draft_stride, vocab);
+  if (!aligned(target, size) || !aligned(draft, size) || !aligned(tokens, 8) || !aligned(out, 8) ||
+      !aligned(lengths, 4) || !aligned(uniform, 4) || !aligned(count, 4) || !aligned(logprob, 4))
+    return fail(PULSE_EALIGN, "%s: a pointer is not aligned to its elements", who);
+  if (int rc = check_space(who, workspace, workspace_bytes, pulse::verify_workspace(batch, drafts, vocab))) return rc;
+  const double log2e = 1.4426950408889634;
+  pulse::VerifyParams p = {};
+  p.target = target;
+  p.target_stride = target_stride;
+  p.draft = drafts ? draft : nullptr;
+  p.draft_stride = draft_stride;
+  p.tokens = tokens;
+  p.lengths = lengths;
+  p.uniform = uniform;
+  p.batch = batch;
+  p.drafts = drafts;
+  p.vocab = vocab;
+  p.scale = scale;
+  p.by = scale * log2e;
+  p.draft_by = draft_scale * log2e;
+  p.out = out;
+  p.count = count;
+  p.logprob = logprob;
+  return hip_status(pulse::launch_verify(dtype == PULSE_DTYPE_BF16, p, (char*)workspace, (hipStream_t)stream),
+                    "verify_drafts launch");
 }
 
 int pulse_lowp_matmul(int dtype, const uint8_t* codes, const uint8_t* scales, float inv_scale,

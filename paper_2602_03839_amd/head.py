@@ -27,12 +27,13 @@ F32, BF16 = 3, 4  # PULSE_DTYPE_F32, PULSE_DTYPE_BF16
 NORM_RMS = 1      # PULSE_NORM_RMS
 NORM_MAX_COLS = 16384
 CE_MAX_HIDDEN = 65536
+VERIFY_MAX_DRAFTS = 128
 MAX_SIZE = (1 << 31) - 1  # of a vocabulary, a weight's rows or columns, tokens
 
 EXPORTS = ("pulse_layer_norm_workspace_bytes", "pulse_layer_norm_forward",
            "pulse_layer_norm_backward", "pulse_block_norm_workspace_bytes", "pulse_block_norm_forward",
            "pulse_block_norm_backward", "pulse_linear_ce_workspace_bytes", "pulse_linear_ce_forward",
-           "pulse_linear_ce_backward", "pulse_lowp_matmul")
+           "pulse_linear_ce_backward", "pulse_verify_drafts_workspace_bytes", "pulse_verify_drafts", "pulse_lowp_matmul")
 
 _lock = threading.Lock()
 _lib = None
@@ -48,7 +49,7 @@ def lib():
         if _lib is None:
             vp, u64, u32, f32, i32 = (ctypes.c_void_p, ctypes.c_uint64, ctypes.c_uint32,
                                       ctypes.c_float, ctypes.c_int)
-            sz = ctypes.c_size_t
+            sz, f64 = ctypes.c_size_t, ctypes.c_double
             L.pulse_layer_norm_workspace_bytes.argtypes = [u32]
             L.pulse_layer_norm_forward.argtypes = [i32, vp, u64, i32, vp, vp, vp, u64, vp, vp, u64,
                                                    u32, f32, u32, vp]
@@ -60,6 +61,9 @@ def lib():
             L.pulse_block_norm_backward.argtypes = [i32, vp, u64, vp, u64, vp, u64, vp, u64, f32, i32, vp, vp, vp,
                                                     vp, vp, u64, vp, u64, vp, u64, vp, vp, vp, vp, vp, u64, u32,
                                                     u32, vp, sz, vp]
+            L.pulse_verify_drafts_workspace_bytes.argtypes = [u32, u32, u32]
+            L.pulse_verify_drafts.argtypes = [i32, vp, u64, vp, u64, vp, vp, vp, u32, u32, u32, f64, f64, vp,
+                                              vp, vp, vp, sz, vp]
             L.pulse_lowp_matmul.argtypes = [i32, vp, vp, f32, u32, u32, vp, u64, u32, i32, vp, u64, vp]
             L.pulse_linear_ce_workspace_bytes.argtypes = [u32, u32, u32]
             L.pulse_linear_ce_forward.argtypes = [vp, u64, vp, vp, u32, u32, u32, f32, vp, vp, vp, sz, vp]
@@ -374,6 +378,83 @@ class LinearCE:
         return dx, dweight
 
 
+class VerifyDrafts:
+    """Which drafted tokens a target model keeps, and the token that follows them:
+    drafts are taken while u q(x) < p(x), then one token is drawn from max(p - q, 0),
+    or from p where all drafts were taken.  With p and q the softmax of logit_scale
+    times the target's and draft_scale times the draft's logits, the tokens are
+    distributed as the target's own.  Without drafts it samples.
+
+    One object serves up to ``max_batch`` sequences of up to ``max_drafts`` drafts a call.
+    """
+
+    def __init__(self, vocab: int, max_batch: int, max_drafts: int = 0, logit_scale: float = 1.0,
+                 draft_scale: Optional[float] = None, device=None):
+        if not 1 <= vocab <= MAX_SIZE:
+            raise PulseError(f"vocabulary of {vocab}, 1 to {MAX_SIZE} are handled")
+        if not 0 <= max_drafts <= VERIFY_MAX_DRAFTS:
+            raise PulseError(f"{max_drafts} drafts, 0 to {VERIFY_MAX_DRAFTS} are handled")
+        if not 1 <= max_batch <= MAX_SIZE // (2 * max_drafts + 1):
+            raise PulseError(f"batch of {max_batch} is out of range")
+        self.vocab, self.max_batch, self.max_drafts = vocab, max_batch, max_drafts
+        self.logit_scale = float(logit_scale)
+        self.draft_scale = self.logit_scale if draft_scale is None else float(draft_scale)
+        self._lib = lib()
+        self._nws = int(self._lib.pulse_verify_drafts_workspace_bytes(max_batch, max_drafts, vocab))
+        self.ws = torch.empty(self._nws, dtype=torch.uint8, device=device or "cuda")
+        self.device, self._pws = self.ws.device, self.ws.data_ptr()
+
+    def _rows(self, t, name, rows, dtype):
+        if isinstance(t, torch.Tensor) and t.dim() == 3:
+            try:
+                t = t.view(-1, t.shape[2])
+            except RuntimeError:
+                raise PulseError(f"{name}'s rows must be equally far apart (strides {t.stride()})") from None
+        return _matrix(t, name, self.vocab, rows, dtype, self.device)
+
+    def __call__(self, target: torch.Tensor, drafts: Optional[torch.Tensor], uniform: torch.Tensor,
+                 draft_logits: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
+                 tokens: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                 logprob: Optional[torch.Tensor] = None, stream=None):
+        """(tokens, count, logprob) for B sequences of K drafts: ``target`` logits
+        [B * (K + 1), V] or [B, K + 1, V], float32 or bfloat16; ``drafts`` int64 [B, K]
+        (None for K = 0); ``uniform`` float32 [B, K + 1] in [0, 1), a sequence's last for
+        the token that is drawn; ``draft_logits`` [B * K, V] or [B, K, V] (None: the draft
+        was certain of its tokens); ``lengths`` int32 [B], the drafts a sequence has (None:
+        K).  tokens, int64 [B, K + 1], holds the drafts taken, the token drawn, then -1;
+        count, int32 [B], how many were taken; logprob, float32 [B, K + 1], each token's
+        log p, 0 past them.  Where p is empty the token is -1, its logprob -inf."""
+        dev = self.device
+        if not isinstance(uniform, torch.Tensor) or uniform.dim() != 2 or uniform.shape[1] < 1:
+            raise PulseError("uniform must be a tensor [batch, drafts + 1]")
+        n, k = uniform.shape[0], uniform.shape[1] - 1
+        if n > self.max_batch or k > self.max_drafts:
+            raise PulseError(f"{n} sequences of {k} drafts, this object was built for {self.max_batch} of "
+                             f"{self.max_drafts}")
+        pu = _f32(uniform, "uniform", device=dev)
+        dt = _dtype(target, "target")
+        pt, st = self._rows(target, "target", n * (k + 1), target.dtype)
+        pd, sd = (None, 0) if draft_logits is None else self._rows(draft_logits, "draft_logits", n * k, target.dtype)
+        px = _p(drafts, "drafts", dtype=torch.int64, numel=n * k, device=dev, optional=k == 0)
+        pl = _p(lengths, "lengths", dtype=torch.int32, numel=n, device=dev)
+        if tokens is None:
+            tokens = _new((n, k + 1), torch.int64, dev, stream)
+        if count is None:
+            count = _new((n,), torch.int32, dev, stream)
+        if logprob is None:
+            logprob = _new((n, k + 1), torch.float32, dev, stream)
+        po = _p(tokens, "tokens", dtype=torch.int64, numel=n * (k + 1), device=dev)
+        pc = _p(count, "count", dtype=torch.int32, numel=n, device=dev)
+        pp = _f32(logprob, "logprob", n * (k + 1), dev)
+        with _on(dev):
+            rc = self._lib.pulse_verify_drafts(dt, pt, st, pd, sd, px, pl, pu, n, k, self.vocab, self.logit_scale,
+                                               self.draft_scale, po, pc, pp, self._pws, self._nws,
+                                               _stream(stream, dev))
+        if rc:
+            _check(rc, "pulse_verify_drafts")
+        return tokens, count, logprob
+
+
 class LowpLinear:
     """Products with a [rows, cols] weight that a receiver holds as MXFP4 or FP8
     codes (the tensors that ``pulse.ApplyLowpBatch`` patches in place)."""
@@ -408,5 +489,5 @@ class LowpLinear:
         rc = self._lib.pulse_lowp_matmul(self.dtype, self._codes, self._scales, self.inv_scale, self.rows,
                                          self.cols, px, sx, n, dt, py, sy, _stream(stream, dev))
         if rc:
-            _check(rc, "pulse_lowp_matmul")
+            _check(rc, "pulse_verify_drafts_workspace_bytes", "pulse_verify_drafts", "pulse_lowp_matmul")
         return out

@@ -64,3 +64,26 @@ def test_block_norm_backward_validation(L):
         (dict(ws=None), EINVAL, b"workspace"), (dict(wsb=size - 1), EINVAL, b"workspace"),
         (dict(ws=A + 16), EALIGN, b"workspace"), (dict(dgate=A + 2), EALIGN, b"gradient"),
         (dict(dy=A + 4), EALIGN, b"dy not"), (dict(dtype=7), EINVAL, b"dtype")))
+
+
+def test_verify_drafts_validation(L):
+    need = L.pulse_verify_drafts_workspace_bytes
+    size = need(4, 3, 1000)
+    assert 0 < size <= min(need(5, 3, 1000), need(4, 4, 1000), need(4, 3, 3000))
+    for sizes in ((0, 3, 1000), (4, 129, 1000), (4, 3, 0), (4, 3, 1 << 31), (1 << 31, 0, 10), (0xFFFFFFFF, 128, 10)):
+        assert need(*sizes) == 0, sizes
+    good = dict(dtype=BF16, z=A, zs=1000, d=A, ds=1000, x=A, lengths=A, u=A, batch=4, drafts=3, vocab=1000, scale=1.0,
+                dscale=1.0, out=A, count=A, lp=A, ws=A, wsb=size, stream=None)
+    assert L.pulse_verify_drafts(*{**good, **dict(batch=0, z=None, x=None, u=None, out=None, count=None, lp=None, ws=None,
+                                                  wsb=0)}.values()) == OK
+    refused(L.pulse_verify_drafts, good, L, (
+        (dict(dtype=FP8), EINVAL, b"dtype"), (dict(drafts=129), EINVAL, b"drafts"), (dict(vocab=0), EINVAL, b"vocabulary"),
+        (dict(vocab=1 << 31), EINVAL, b"vocabulary"), (dict(batch=1 << 31), EINVAL, b"sequences"),
+        (dict(scale=0.0), EINVAL, b"scale"), (dict(scale=INF), EINVAL, b"scale"), (dict(scale=NAN), EINVAL, b"scale"),
+        (dict(dscale=-1.0), EINVAL, b"scale"), (dict(z=None), EINVAL, b"target"), (dict(x=None), EINVAL, b"tokens"),
+        (dict(u=None), EINVAL, b"uniform"), (dict(out=None), EINVAL, b"out"), (dict(count=None), EINVAL, b"count"),
+        (dict(lp=None), EINVAL, b"logprob"), (dict(zs=999), EINVAL, b"stride"), (dict(ds=1), EINVAL, b"stride"),
+        (dict(zs=1 << 41), EINVAL, b"stride"), (dict(z=A + 1), EALIGN, b"aligned"), (dict(x=A + 4), EALIGN, b"aligned"),
+        (dict(out=A + 4), EALIGN, b"aligned"), (dict(lp=A + 2), EALIGN, b"aligned"), (dict(lengths=A + 2), EALIGN, b"aligned"),
+        (dict(dtype=F32, z=A + 2), EALIGN, b"aligned"), (dict(ws=None), EINVAL, b"workspace"),
+        (dict(wsb=size - 1), EINVAL, b"workspace"), (dict(ws=A + 64), EALIGN, b"workspace")))
