@@ -248,6 +248,77 @@ int pulse_lowp_matmul(int dtype, const uint8_t *codes, const uint8_t *scales, fl
                       uint32_t rows, uint32_t cols, const uint16_t *x, uint64_t x_stride,
                       uint32_t tokens, int y_dtype, void *y, uint64_t y_stride, void *stream);
 
+/* Activations; silu(v) = v / (1 + e^-v), gelu(v) = v (1 + erf(v / sqrt 2)) / 2,
+ * gelu_tanh(v) = v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2. */
+#define PULSE_ACT_NONE 0
+#define PULSE_ACT_RELU 1
+#define PULSE_ACT_SILU 2
+#define PULSE_ACT_GELU 3
+#define PULSE_ACT_GELU_TANH 4
+
+/*
+ * pulse_lowp_linear -- pulse_lowp_matmul with what follows it in a block, before the one
+ * rounding:
+ *   y = act(x W^T + bias) * times + residual.
+ *   bias      [rows] of `bias_dtype` (F32 or BF16); NULL: none.
+ *   times, residual  [tokens, rows] of `y_dtype`; NULL: none.  y may be one of them
+ *             (the same pointer and stride), and is then brought up to date in place.
+ */
+int pulse_lowp_linear(int dtype, const uint8_t *codes, const uint8_t *scales, float inv_scale,
+                      uint32_t rows, uint32_t cols, const uint16_t *x, uint64_t x_stride,
+                      uint32_t tokens, int bias_dtype, const void *bias, int activation,
+                      const void *times, uint64_t times_stride, const void *residual,
+                      uint64_t residual_stride, int y_dtype, void *y, uint64_t y_stride,
+                      void *stream);
+
+/* The largest weight that pulse_linear handles, and the most tokens of a call. */
+#define PULSE_LINEAR_MAX_WIDTH 1048576
+
+/* Up to so many tokens pulse_linear_forward needs no workspace (which may be NULL). */
+#define PULSE_LINEAR_FEW_TOKENS 32
+
+/* A workspace for calls of any number of tokens up to `tokens`, both directions; 0 for
+ * sizes that no call handles. */
+size_t pulse_linear_workspace_bytes(uint32_t tokens, uint32_t rows, uint32_t cols);
+
+/*
+ * pulse_linear_forward -- y = act(x W^T + bias) * times + residual, as pulse_lowp_linear,
+ * for a BF16 weight [rows, cols] (rows adjacent) and any number of tokens, with
+ *   pre   [tokens, rows] of `y_dtype`: x W^T + bias, rounded, which the gradient asks
+ *         for where there is an activation or a multiplier; NULL: not kept.
+ * rows, cols and tokens are at most PULSE_LINEAR_MAX_WIDTH, rows and cols at least 1.
+ * A cols that is no multiple of 8 costs, above PULSE_LINEAR_FEW_TOKENS, a copy of the weight with padded
+ * rows in the workspace.
+ */
+int pulse_linear_forward(const uint16_t *x, uint64_t x_stride, const uint16_t *weight,
+                         uint32_t tokens, uint32_t rows, uint32_t cols, int bias_dtype,
+                         const void *bias, int activation, const void *times,
+                         uint64_t times_stride, const void *residual, uint64_t residual_stride,
+                         int y_dtype, void *y, uint64_t y_stride, void *pre, uint64_t pre_stride,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * pulse_linear_backward -- the gradient at the forward pass's x, pre and times for the
+ * upstream dy (the residual's gradient is dy itself): with
+ *   d = dy * times * act'(pre),
+ *   dx = d W,   dweight = d^T x,   dbias = sum over tokens of d,   dtimes = dy * act(pre).
+ * For the two products d is rounded to BF16, unless it is a BF16 dy unchanged; they are
+ * summed in FP32 and rounded once to BF16.  dbias is summed from d as it is.  relu's
+ * derivative at 0 is 0.
+ *   dtype     of dy, pre, times and dtimes: F32 or BF16.
+ *   pre       may be NULL with neither an activation nor times.
+ *   dbias     FP32 [rows]; NULL: not asked for.
+ *   dtimes    [tokens, rows]; NULL: not asked for.  dweight: BF16 [rows, cols].
+ * tokens == 0 sets dweight and dbias to zero.
+ */
+int pulse_linear_backward(int dtype, const void *dy, uint64_t dy_stride, const uint16_t *x,
+                          uint64_t x_stride, const uint16_t *weight, const void *pre,
+                          uint64_t pre_stride, int activation, const void *times,
+                          uint64_t times_stride, uint32_t tokens, uint32_t rows, uint32_t cols,
+                          uint16_t *dx, uint64_t dx_stride, uint16_t *dweight, float *dbias,
+                          void *dtimes, uint64_t dtimes_stride, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,135 @@
+// epilogue.hpp -- what follows a product's sum before it is stored: bias, activation,
+// multiplier and residual, in FP32 and in this order; and the activations' derivatives.
+//
+//   silu(v) = v s(v), s(v) = 1 / (1 + e^-v)
+//   gelu(v) = v (1 + erf(v / sqrt 2)) / 2
+//   gelu_tanh(v) = v (1 + tanh y) / 2 = v s(2 y), y = sqrt(2 / pi) (v + 0.044715 v^3)
+// Exponentials and reciprocals are the hardware's (1 ulp each): a value is off by a few
+// ulp, and where it is a small fraction of v by a few ulp of v.
+#pragma once
+
+#include "device_common.hpp"
+#include "head.hpp"
+
+namespace pulse {
+
+namespace {
+
+__device__ __forceinline__ float sigmoid_of(float v) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.4426950408889634f * v));
+}
+
+constexpr float kGeluA = 0.7978845608028654f;  // sqrt(2 / pi)
+constexpr float kGeluB = 0.044715f;
+
+__device__ __forceinline__ float activate(int act, float v) {
+  switch (act) {
+    case kActRelu: return v < 0.0f ? 0.0f : v;  // a NaN stays one
+    case kActSilu: return v * sigmoid_of(v);
+    case kActGelu: return 0.5f * v * (1.0f + erff(0.7071067811865476f * v));
+    case kActGeluTanh: return v * sigmoid_of(2.0f * kGeluA * __builtin_fmaf(kGeluB * v * v, v, v));
+    default: return v;
+  }
+}
+
+// An activation and its derivative.
+__device__ __forceinline__ float2 activate2(int act, float v) {
+  switch (act) {
+    case kActRelu: return make_float2(v < 0.0f ? 0.0f : v, v > 0.0f ? 1.0f : v - v);
+    case kActSilu: {
+      const float s = sigmoid_of(v);
+      return make_float2(v * s, s * __builtin_fmaf(v, 1.0f - s, 1.0f));
+    }
+    case kActGelu: {
+      const float h = 0.5f * (1.0f + erff(0.7071067811865476f * v));
+      const float d = 0.3989422804014327f * __builtin_amdgcn_exp2f(-0.7213475204444817f * v * v);
+      return make_float2(v * h, __builtin_fmaf(v, d, h));
+    }
+    case kActGeluTanh: {
+      const float s = sigmoid_of(2.0f * kGeluA * __builtin_fmaf(kGeluB * v * v, v, v));
+      const float y = 2.0f * kGeluA * __builtin_fmaf(3.0f * kGeluB * v, v, 1.0f);
+      return make_float2(v * s, __builtin_fmaf(v * s * (1.0f - s), y, s));
+    }
+    default: return make_float2(v, 1.0f);
+  }
+}
+
+__device__ __forceinline__ float load_f32(const void* p, uint64_t at, int bf16) {
+  return bf16 ? __uint_as_float((uint32_t)((const uint16_t*)p)[at] << 16) : ((const float*)p)[at];
+}
+
+// Four adjacent values from element `at` on, of which `left` are there (the others 0).
+__device__ __forceinline__ f32x4_t load_four(const void* p, uint64_t at, int bf16, uint32_t left) {
+  f32x4_t v = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (left >= 4 && at % 4 == 0) {
+    if (!bf16) return *(const f32x4_t*)((const float*)p + at);
+    const uint2 w = *(const uint2*)((const uint16_t*)p + at);
+    return f32x4_t{__uint_as_float(w.x << 16), __uint_as_float(w.x & 0xFFFF0000u), __uint_as_float(w.y << 16),
+                   __uint_as_float(w.y & 0xFFFF0000u)};
+  }
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i)
+    if (i < left) v[i] = load_f32(p, at + i, bf16);
+  return v;
+}
+
+__device__ __forceinline__ void store_four(void* p, uint64_t at, int bf16, uint32_t left, f32x4_t v) {
+  if (bf16) {
+    uint16_t* const y = (uint16_t*)p + at;
+    const uint2 o = make_uint2(bf16x2_rne(__float_as_uint(v[0]), __float_as_uint(v[1])),
+                               bf16x2_rne(__float_as_uint(v[2]), __float_as_uint(v[3])));
+    if (left >= 4 && at % 4 == 0) {
+      *(uint2*)y = o;
+    } else {
+      const uint32_t w[2] = {o.x, o.y};
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+        if (i < left) y[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+    }
+  } else {
+    float* const y = (float*)p + at;
+    if (left >= 4 && at % 4 == 0) {
+      *(f32x4_t*)y = v;
+    } else {
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+        if (i < left) y[i] = v[i];
+    }
+  }
+}
+
+// The four features from `row` on of token t (`left` of them are there): what is stored
+// as y; `pre`, if it is kept, is stored here.
+__device__ __forceinline__ f32x4_t finish_four(const Epilogue& e, f32x4_t v, uint64_t t, uint64_t row, uint32_t left) {
+  // all loads first
+  f32x4_t bias = {0.0f, 0.0f, 0.0f, 0.0f}, times = {1.0f, 1.0f, 1.0f, 1.0f}, residual = bias;
+  if (e.bias) bias = load_four(e.bias, row, e.bias_bf16, left);
+  if (e.times) times = load_four(e.times, t * e.times_stride + row, e.out_bf16, left);
+  if (e.residual) residual = load_four(e.residual, t * e.residual_stride + row, e.out_bf16, left);
+  if (e.bias) v += bias;
+  if (e.pre) store_four(e.pre, t * e.pre_stride + row, e.out_bf16, left, v);
+  if (e.act) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = activate(e.act, v[i]);
+  }
+  if (e.times) v *= times;
+  if (e.residual) v += residual;
+  return v;
+}
+
+__device__ __forceinline__ float finish_one(const Epilogue& e, float v, uint64_t t, uint64_t row) {
+  if (e.bias) v += load_f32(e.bias, row, e.bias_bf16);
+  if (e.pre) {
+    const uint64_t at = t * e.pre_stride + row;
+    if (e.out_bf16) ((uint16_t*)e.pre)[at] = (uint16_t)bf16x2_rne(__float_as_uint(v), 0u);
+    else ((float*)e.pre)[at] = v;
+  }
+  v = activate(e.act, v);
+  if (e.times) v *= load_f32(e.times, t * e.times_stride + row, e.out_bf16);
+  if (e.residual) v += load_f32(e.residual, t * e.residual_stride + row, e.out_bf16);
+  return v;
+}
+
+}  // namespace
+
+}  // namespace pulse

@@ -113,10 +113,31 @@ struct BlockNormGradParams {
 hipError_t launch_block_norm(bool bf16, const BlockNormParams& p, hipStream_t stream);
 hipError_t launch_block_norm_grad(bool bf16, const BlockNormGradParams& p, hipStream_t stream);
 
-// ---------------------------------------------------------------- low-bit products
+// ---------------------------------------------------------------- products with an epilogue
+
+enum Activation { kActNone, kActRelu, kActSilu, kActGelu, kActGeluTanh, kActs };
+
+// y = act(product + bias) * times + residual; what is null is left out.  times, residual
+// and pre are rows of y's type, [tokens][rows of the weight].
+struct Epilogue {
+  const void* bias;
+  int bias_bf16;
+  int act;
+  const void* times;
+  uint64_t times_stride;
+  const void* residual;
+  uint64_t residual_stride;
+  void* pre;  // product + bias, kept for the gradient
+  uint64_t pre_stride;
+  int out_bf16;
+};
+
+// ---------------------------------------------------------------- few-token products
+
+enum WeightForm { kWeightFp8, kWeightMxfp4, kWeightBf16 };
 
 struct LowpMatmulParams {
-  const uint8_t* codes;
+  const uint8_t* codes;   // BF16: the weight itself
   const uint8_t* scales;  // MXFP4
   float inv_scale;        // FP8
   uint32_t rows, cols;
@@ -127,9 +148,51 @@ struct LowpMatmulParams {
   void* y;
   uint64_t y_stride;
   int y_bf16;
+  Epilogue e;
 };
 
-hipError_t launch_lowp_matmul(bool mxfp4, const LowpMatmulParams& p, hipStream_t stream);
+// `epilogue`: e is looked at; always so for BF16 weights.
+hipError_t launch_lowp_matmul(WeightForm form, bool epilogue, const LowpMatmulParams& p, hipStream_t stream);
+
+// ---------------------------------------------------------------- linear
+
+constexpr uint32_t kLinearFewTokens = 32;  // up to here the forward pass needs no workspace
+
+struct LinearParams {
+  const uint16_t* x;
+  uint64_t x_stride;
+  const uint16_t* weight;
+  uint32_t tokens, rows, cols;
+  void* y;
+  uint64_t y_stride;
+  Epilogue e;
+};
+
+struct LinearGradParams {
+  const void* dy;
+  uint64_t dy_stride;
+  const uint16_t* x;
+  uint64_t x_stride;
+  const uint16_t* weight;
+  const void* pre;  // null: neither activation nor multiplier
+  uint64_t pre_stride;
+  const void* times;  // may be null
+  uint64_t times_stride;
+  int act, bf16;  // bf16: type of dy, pre, times and dtimes
+  uint32_t tokens, rows, cols;
+  uint16_t* dx;
+  uint64_t dx_stride;
+  uint16_t* dweight;
+  float* dbias;  // may be null
+  void* dtimes;  // may be null
+  uint64_t dtimes_stride;
+};
+
+uint64_t linear_needs(bool forward, uint32_t tokens, uint32_t rows, uint32_t cols);  // one call's workspace
+// a workspace for any call of up to `tokens` tokens
+uint64_t linear_bytes(uint32_t tokens, uint32_t rows, uint32_t cols);
+hipError_t launch_linear(const LinearParams& p, char* ws, hipStream_t stream);
+hipError_t launch_linear_grad(const LinearGradParams& p, char* ws, hipStream_t stream);
 
 // ---------------------------------------------------------------- cross entropy
 

@@ -75,6 +75,75 @@ bool verify_handles(uint32_t batch, uint32_t drafts, uint32_t vocab) {
          (uint64_t)batch * (2 * drafts + 1) <= 0x7FFFFFFFull;
 }
 
+bool linear_handles(uint32_t tokens, uint32_t rows, uint32_t cols) {
+  return tokens <= PULSE_LINEAR_MAX_WIDTH && rows != 0 && rows <= PULSE_LINEAR_MAX_WIDTH && cols != 0 &&
+         cols <= PULSE_LINEAR_MAX_WIDTH;
+}
+
+// what both directions of the linear layer ask of their arguments
+int check_linear(const char* who, bool forward, const void* x, uint64_t x_stride, const void* weight, uint32_t tokens, uint32_t rows,
+                 uint32_t cols, const void* ws, size_t ws_bytes) {
+  if (!linear_handles(tokens, rows, cols))
+    return fail(PULSE_EINVAL, "%s: %u tokens, a weight of %u x %u", who, tokens, rows, cols);
+  if (tokens == 0) return PULSE_OK;
+  if (int rc = check_matrix(who, "x", x, x_stride, tokens, cols)) return rc;
+  if (!weight) return fail(PULSE_EINVAL, "%s: weight is NULL", who);
+  if (!aligned16(weight)) return fail(PULSE_EALIGN, "%s: weight not 16-byte aligned", who);
+  const uint64_t needs = pulse::linear_needs(forward, tokens, rows, cols);
+  return needs ? check_space(who, ws, ws_bytes, needs) : PULSE_OK;
+}
+
+// what every product with codes asks of its arguments
+int check_lowp(const char* who, int dtype, const void* codes, const void* scales, float inv_scale, uint32_t rows,
+               uint32_t cols, const void* x, uint64_t x_stride, uint32_t tokens, int y_dtype, const void* y,
+               uint64_t y_stride) {
+  const bool mx = dtype == PULSE_DTYPE_MXFP4;
+  if (!mx && dtype != PULSE_DTYPE_FP8_E4M3)
+    return fail(PULSE_EINVAL, "%s: dtype %d is neither FP8_E4M3 nor MXFP4", who, dtype);
+  if (y_dtype != PULSE_DTYPE_F32 && y_dtype != PULSE_DTYPE_BF16)
+    return fail(PULSE_EINVAL, "%s: y_dtype %d is neither F32 nor BF16", who, y_dtype);
+  if (rows == 0 || rows > 0x7FFFFFFFu || cols == 0 || cols > 0x7FFFFFFFu)
+    return fail(PULSE_EINVAL, "%s: a weight of %u x %u", who, rows, cols);
+  if (tokens > 1u << 20) return fail(PULSE_EINVAL, "%s: more than 2^20 tokens", who);
+  if (tokens == 0) return PULSE_OK;
+  if (!codes) return fail(PULSE_EINVAL, "%s: codes is NULL", who);
+  if (mx && !scales) return fail(PULSE_EINVAL, "%s: scales is NULL", who);
+  if (!aligned(codes, mx ? 4 : 8)) return fail(PULSE_EALIGN, "%s: codes not %d-byte aligned", who, mx ? 4 : 8);
+  if (!mx && !(inv_scale - inv_scale == 0.0f && inv_scale != 0.0f))
+    return fail(PULSE_EINVAL, "%s: inv_scale is zero or not finite", who);
+  if (int rc = check_matrix(who, "x", x, x_stride, tokens, cols)) return rc;
+  return check_matrix(who, "y", y, y_stride, tokens, rows);
+}
+
+pulse::LowpMatmulParams lowp_params(int dtype, const uint8_t* codes, const uint8_t* scales, float inv_scale,
+                                    uint32_t rows, uint32_t cols, const uint16_t* x, uint64_t x_stride,
+                                    uint32_t tokens, int y_dtype, void* y, uint64_t y_stride) {
+  const uint64_t n = (uint64_t)rows * cols;
+  return {codes, scales, inv_scale, rows, cols, dtype == PULSE_DTYPE_MXFP4 ? (n + 1) / 2 : n, (n + 31) / 32, x, x_stride,
+          tokens, y, y_stride, y_dtype == PULSE_DTYPE_BF16, {}};
+}
+
+// The epilogue's arguments, checked, as `e` (whose `pre` is none).
+int check_epilogue(const char* who, uint32_t rows, uint32_t tokens, int bias_dtype, const void* bias, int activation,
+                   const void* times, uint64_t times_stride, const void* residual, uint64_t residual_stride,
+                   int y_dtype, const void* y, uint64_t y_stride, pulse::Epilogue& e) {
+  if (bias && bias_dtype != PULSE_DTYPE_F32 && bias_dtype != PULSE_DTYPE_BF16)
+    return fail(PULSE_EINVAL, "%s: bias_dtype %d is neither F32 nor BF16", who, bias_dtype);
+  if (!aligned16(bias)) return fail(PULSE_EALIGN, "%s: bias not 16-byte aligned", who);
+  if (activation < 0 || activation >= pulse::kActs)
+    return fail(PULSE_EINVAL, "%s: activation %d is not known", who, activation);
+  if (times)
+    if (int rc = check_matrix(who, "times", times, times_stride, tokens, rows)) return rc;
+  if (residual)
+    if (int rc = check_matrix(who, "residual", residual, residual_stride, tokens, rows)) return rc;
+  if (tokens && ((times && y == times && y_stride != times_stride) ||
+                 (residual && y == residual && y_stride != residual_stride)))
+    return fail(PULSE_EINVAL, "%s: y is times or residual with another stride", who);
+  e = {bias, bias_dtype == PULSE_DTYPE_BF16, activation, times, times_stride, residual, residual_stride, nullptr, 0,
+       y_dtype == PULSE_DTYPE_BF16};
+  return PULSE_OK;
+}
+
 bool ce_handles(uint32_t tokens, uint32_t vocab, uint32_t hidden) {
   return tokens <= 0x7FFFFFFFu && vocab != 0 && vocab <= 0x7FFFFFFFu && hidden != 0 && hidden <= PULSE_CE_MAX_HIDDEN;
 }
@@ -310,26 +379,95 @@ int pulse_lowp_matmul(int dtype, const uint8_t* codes, const uint8_t* scales, fl
                       uint32_t rows, uint32_t cols, const uint16_t* x, uint64_t x_stride,
                       uint32_t tokens, int y_dtype, void* y, uint64_t y_stride, void* stream) {
   const char* who = "lowp matmul";
-  const bool mx = dtype == PULSE_DTYPE_MXFP4;
-  if (!mx && dtype != PULSE_DTYPE_FP8_E4M3)
-    return fail(PULSE_EINVAL, "%s: dtype %d is neither FP8_E4M3 nor MXFP4", who, dtype);
+  if (int rc = check_lowp(who, dtype, codes, scales, inv_scale, rows, cols, x, x_stride, tokens, y_dtype, y, y_stride))
+    return rc;
+  if (tokens == 0) return ok();
+  return hip_status(pulse::launch_lowp_matmul(dtype == PULSE_DTYPE_MXFP4 ? pulse::kWeightMxfp4 : pulse::kWeightFp8, false,
+                                              lowp_params(dtype, codes, scales, inv_scale, rows, cols, x, x_stride,
+                                                          tokens, y_dtype, y, y_stride),
+                                              (hipStream_t)stream),
+                    "lowp matmul launch");
+}
+
+int pulse_lowp_linear(int dtype, const uint8_t* codes, const uint8_t* scales, float inv_scale, uint32_t rows,
+                      uint32_t cols, const uint16_t* x, uint64_t x_stride, uint32_t tokens, int bias_dtype,
+                      const void* bias, int activation, const void* times, uint64_t times_stride,
+                      const void* residual, uint64_t residual_stride, int y_dtype, void* y, uint64_t y_stride,
+                      void* stream) {
+  const char* who = "lowp linear";
+  if (int rc = check_lowp(who, dtype, codes, scales, inv_scale, rows, cols, x, x_stride, tokens, y_dtype, y, y_stride))
+    return rc;
+  pulse::Epilogue e;
+  if (int rc = check_epilogue(who, rows, tokens, bias_dtype, bias, activation, times, times_stride, residual,
+                              residual_stride, y_dtype, y, y_stride, e))
+    return rc;
+  if (tokens == 0) return ok();
+  pulse::LowpMatmulParams p = lowp_params(dtype, codes, scales, inv_scale, rows, cols, x, x_stride, tokens, y_dtype, y,
+                                          y_stride);
+  p.e = e;
+  return hip_status(pulse::launch_lowp_matmul(dtype == PULSE_DTYPE_MXFP4 ? pulse::kWeightMxfp4 : pulse::kWeightFp8, true,
+                                              p, (hipStream_t)stream),
+                    "lowp linear launch");
+}
+
+size_t pulse_linear_workspace_bytes(uint32_t tokens, uint32_t rows, uint32_t cols) {
+  return tokens && linear_handles(tokens, rows, cols) ? pulse::linear_bytes(tokens, rows, cols) : 0;
+}
+
+int pulse_linear_forward(const uint16_t* x, uint64_t x_stride, const uint16_t* weight, uint32_t tokens, uint32_t rows,
+                         uint32_t cols, int bias_dtype, const void* bias, int activation, const void* times,
+                         uint64_t times_stride, const void* residual, uint64_t residual_stride, int y_dtype, void* y,
+                         uint64_t y_stride, void* pre, uint64_t pre_stride, void* workspace, size_t workspace_bytes,
+                         void* stream) {
+  const char* who = "linear forward";
+  if (int rc = check_linear(who, true, x, x_stride, weight, tokens, rows, cols, workspace, workspace_bytes)) return rc;
   if (y_dtype != PULSE_DTYPE_F32 && y_dtype != PULSE_DTYPE_BF16)
     return fail(PULSE_EINVAL, "%s: y_dtype %d is neither F32 nor BF16", who, y_dtype);
-  if (rows == 0 || rows > 0x7FFFFFFFu || cols == 0 || cols > 0x7FFFFFFFu)
-    return fail(PULSE_EINVAL, "%s: a weight of %u x %u", who, rows, cols);
-  if (tokens > 1u << 20) return fail(PULSE_EINVAL, "%s: more than 2^20 tokens", who);
-  if (tokens == 0) return ok();
-  if (!codes) return fail(PULSE_EINVAL, "%s: codes is NULL", who);
-  if (mx && !scales) return fail(PULSE_EINVAL, "%s: scales is NULL", who);
-  if (!aligned(codes, mx ? 4 : 8)) return fail(PULSE_EALIGN, "%s: codes not %d-byte aligned", who, mx ? 4 : 8);
-  if (!mx && !(inv_scale - inv_scale == 0.0f && inv_scale != 0.0f))
-    return fail(PULSE_EINVAL, "%s: inv_scale is zero or not finite", who);
-  if (int rc = check_matrix(who, "x", x, x_stride, tokens, cols)) return rc;
   if (int rc = check_matrix(who, "y", y, y_stride, tokens, rows)) return rc;
-  const uint64_t n = (uint64_t)rows * cols;
-  pulse::LowpMatmulParams p = {codes, scales, inv_scale, rows, cols, mx ? (n + 1) / 2 : n, (n + 31) / 32,
-                               x, x_stride, tokens, y, y_stride, y_dtype == PULSE_DTYPE_BF16};
-  return hip_status(pulse::launch_lowp_matmul(mx, p, (hipStream_t)stream), "lowp matmul launch");
+  pulse::LinearParams p = {x, x_stride, weight, tokens, rows, cols, y, y_stride, {}};
+  if (int rc = check_epilogue(who, rows, tokens, bias_dtype, bias, activation, times, times_stride, residual,
+                              residual_stride, y_dtype, y, y_stride, p.e))
+    return rc;
+  if (pre)
+    if (int rc = check_matrix(who, "pre", pre, pre_stride, tokens, rows)) return rc;
+  if (tokens == 0) return ok();
+  p.e.pre = pre;
+  p.e.pre_stride = pre_stride;
+  return hip_status(pulse::launch_linear(p, (char*)workspace, (hipStream_t)stream), "linear launch");
+}
+
+int pulse_linear_backward(int dtype, const void* dy, uint64_t dy_stride, const uint16_t* x, uint64_t x_stride,
+                          const uint16_t* weight, const void* pre, uint64_t pre_stride, int activation,
+                          const void* times, uint64_t times_stride, uint32_t tokens, uint32_t rows, uint32_t cols,
+                          uint16_t* dx, uint64_t dx_stride, uint16_t* dweight, float* dbias, void* dtimes,
+                          uint64_t dtimes_stride, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "linear backward";
+  if (dtype != PULSE_DTYPE_F32 && dtype != PULSE_DTYPE_BF16)
+    return fail(PULSE_EINVAL, "%s: dtype %d is neither F32 nor BF16", who, dtype);
+  if (activation < 0 || activation >= pulse::kActs)
+    return fail(PULSE_EINVAL, "%s: activation %d is not known", who, activation);
+  if (int rc = check_linear(who, false, x, x_stride, weight, tokens, rows, cols, workspace, workspace_bytes)) return rc;
+  if (!dweight) return fail(PULSE_EINVAL, "%s: dweight is NULL", who);
+  if (!aligned16(dweight)) return fail(PULSE_EALIGN, "%s: dweight not 16-byte aligned", who);
+  if (!aligned(dbias, 4)) return fail(PULSE_EALIGN, "%s: dbias not 4-byte aligned", who);
+  if (tokens == 0) {
+    hipError_t e = pulse::launch_zero_bytes(dweight, (uint64_t)rows * cols * 2, (hipStream_t)stream);
+    if (e == hipSuccess && dbias) e = pulse::launch_zero_bytes(dbias, (uint64_t)rows * 4, (hipStream_t)stream);
+    return hip_status(e, "linear backward launch");
+  }
+  if (int rc = check_matrix(who, "dy", dy, dy_stride, tokens, rows)) return rc;
+  if (activation || times)
+    if (int rc = check_matrix(who, "pre", pre, pre_stride, tokens, rows)) return rc;
+  if (times)
+    if (int rc = check_matrix(who, "times", times, times_stride, tokens, rows)) return rc;
+  if (dtimes && !times) return fail(PULSE_EINVAL, "%s: dtimes without times", who);
+  if (dtimes)
+    if (int rc = check_matrix(who, "dtimes", dtimes, dtimes_stride, tokens, rows)) return rc;
+  if (int rc = check_matrix(who, "dx", dx, dx_stride, tokens, cols)) return rc;
+  pulse::LinearGradParams p = {dy, dy_stride, x, x_stride, weight, pre, pre_stride, times, times_stride, activation,
+                               dtype == PULSE_DTYPE_BF16, tokens, rows, cols, dx, dx_stride, dweight, dbias, dtimes,
+                               dtimes_stride};
+  return hip_status(pulse::launch_linear_grad(p, (char*)workspace, (hipStream_t)stream), "linear backward launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,530 @@
+// linear.hip -- y = act(x W^T + bias) * times + residual for a BF16 weight and BF16
+// tokens, and its gradient.
+//
+// Up to 32 tokens the weight's way from HBM bounds it: lowp_matmul.hip, which reads it
+// once.  For more, the matrix cores: tiles of gemm_tile.hpp, whose sums go through LDS
+// as FP32 rows, so that multiplier, residual and results move 16 bytes a lane and whole
+// lines at a time, and the epilogue's code is there once, not once per accumulator.
+//
+// Backward, with d = dy * times * act'(pre) rounded to BF16 (the products need a BF16
+// operand; for a BF16 dy without activation and multiplier it is dy itself):
+//   dx = d W,   dW = d^T x,   dbias = sum over tokens of d before its rounding,
+//   dtimes = dy * act(pre).
+// One elementwise kernel makes d, dtimes and parts of dbias.
+//
+// Where the tiles are too few for the chip, k is split over blocks, whose FP32 sums are
+// added by a further kernel, with the epilogue.  Tile and split are chosen by a cost.
+#include "device_common.hpp"
+#include "epilogue.hpp"
+#include "gemm_tile.hpp"
+#include "head.hpp"
+
+namespace pulse {
+
+namespace {
+
+// out[n][m] = sum_k A[m][k] B[n][k], then the epilogue, whose tokens are n and rows m.
+struct ProductParams {
+  GemmOperand a, b;
+  uint32_t m, n, k;
+  uint32_t tiles_m, tiles_n, first_tile;
+  uint32_t k_split;  // a multiple of 64
+  float* sums;       // null: no split; [splits][n][m_ld]
+  uint32_t m_ld;     // a multiple of 4
+  void* out;
+  uint64_t out_ld;
+  bool wide;  // every row of the epilogue starts at 16 bytes
+  Epilogue e;
+};
+
+// Eight adjacent values from element `at` on, `left` of them there.
+__device__ __forceinline__ void load_eight(const void* p, uint64_t at, int bf16, bool wide, uint32_t left,
+                                           float (&v)[8]) {
+  if (wide && left >= 8) {
+    if (bf16) {
+      const uint4 w = load16((const uint16_t*)p + at);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        v[e] = __uint_as_float(e & 1 ? get_u32(w, e >> 1) & 0xFFFF0000u : get_u32(w, e >> 1) << 16);
+    } else {
+      const uint4 a = load16((const float*)p + at), b = load16((const float*)p + at + 4);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[e] = __uint_as_float(get_u32(a, e));
+        v[4 + e] = __uint_as_float(get_u32(b, e));
+      }
+    }
+    return;
+  }
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e) v[e] = e < left ? load_f32(p, at + e, bf16) : 0.0f;
+}
+
+__device__ __forceinline__ uint4 pack_eight(const float (&v)[8]) {
+  uint4 o;
+  o.x = bf16x2_rne(__float_as_uint(v[0]), __float_as_uint(v[1]));
+  o.y = bf16x2_rne(__float_as_uint(v[2]), __float_as_uint(v[3]));
+  o.z = bf16x2_rne(__float_as_uint(v[4]), __float_as_uint(v[5]));
+  o.w = bf16x2_rne(__float_as_uint(v[6]), __float_as_uint(v[7]));
+  return o;
+}
+
+__device__ __forceinline__ void store_eight(void* p, uint64_t at, int bf16, bool wide, uint32_t left,
+                                            const float (&v)[8]) {
+  if (bf16) {
+    uint16_t* const y = (uint16_t*)p + at;
+    const uint4 o = pack_eight(v);
+    if (wide && left >= 8) {
+      store16(y, o);
+    } else if (left >= 8) {
+      store16_any(y, o);
+    } else {
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e)
+        if (e < left) y[e] = (uint16_t)(get_u32(o, e >> 1) >> (16 * (e & 1)));
+    }
+  } else {
+    float* const y = (float*)p + at;
+    if (wide && left >= 8) {
+      *(f32x4_t*)y = f32x4_t{v[0], v[1], v[2], v[3]};
+      *(f32x4_t*)(y + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+    } else {
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e)
+        if (e < left) y[e] = v[e];
+    }
+  }
+}
+
+// Token t's eight features from `row` on, from their sums to what is stored.
+__device__ __forceinline__ void finish_eight(const ProductParams& p, float (&v)[8], uint64_t t, uint32_t row) {
+  const Epilogue& e = p.e;
+  const uint32_t left = p.m - row;
+  float bias[8], times[8], residual[8];
+  if (e.bias) load_eight(e.bias, row, e.bias_bf16, true, left, bias);
+  if (e.times) load_eight(e.times, t * e.times_stride + row, e.out_bf16, p.wide, left, times);
+  if (e.residual) load_eight(e.residual, t * e.residual_stride + row, e.out_bf16, p.wide, left, residual);
+  if (e.bias) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += bias[i];
+  }
+  if (e.pre) store_eight(e.pre, t * e.pre_stride + row, e.out_bf16, p.wide, left, v);
+  if (e.act) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = activate(e.act, v[i]);
+  }
+  if (e.times) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= times[i];
+  }
+  if (e.residual) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += residual[i];
+  }
+  store_eight(p.out, t * p.out_ld + row, e.out_bf16, p.wide, left, v);
+}
+
+template <typename T, bool AK, bool BK>
+__global__ __launch_bounds__(T::kThreads) void product_kernel(ProductParams p) {
+  // the tile's FP32 rows pass through LDS, as many fragments' columns at a time as fit
+  constexpr int kFit = T::kLds / (T::BM * 4 * 16 * T::WN), kAtOnce = kFit < T::FN ? kFit : T::FN;
+  static_assert(kFit >= 1 && T::FN % kAtOnce == 0, "whole fragments at a time");
+  __shared__ alignas(1024) char lds[T::kLds];
+  uint32_t tm, tn;
+  gemm_tile_of(p.first_tile + blockIdx.x, p.tiles_m, p.tiles_n, 8, tm, tn);
+  const uint32_t m0 = tm * T::BM, n0 = tn * T::BN;
+  const GemmOperand a = {p.a.p + (AK ? (uint64_t)m0 : m0 * p.a.ld), p.a.ld, p.a.limit - m0};
+  const GemmOperand b = {p.b.p + (BK ? (uint64_t)n0 : n0 * p.b.ld), p.b.ld, p.b.limit - n0};
+  const uint32_t k0 = p.sums ? blockIdx.y * p.k_split : 0;
+  // a split past the end has no k and gives zeros
+  const uint32_t k1 = !p.sums ? p.k : k0 >= p.k ? k0 : p.k - k0 < p.k_split ? p.k : k0 + p.k_split;
+  typename T::Acc acc;
+  T::run(lds, a, b, k0, k1, acc);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (p.sums) {
+    float* const sums = p.sums + (uint64_t)blockIdx.y * p.n * p.m_ld;
+#pragma unroll
+    for (int j = 0; j < T::FN; ++j) {
+      const uint32_t n = n0 + T::n_of(j, lane, wave);
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i) {
+        const uint32_t m = m0 + T::m_of(i, lane, wave);
+        if (n < p.n && m < p.m) *(f32x4_t*)(sums + (uint64_t)n * p.m_ld + m) = acc[i][j];
+      }
+    }
+    return;
+  }
+  // group c (4 values) of a row lies at place c ^ (n & 15)
+#pragma unroll
+  for (int j0 = 0; j0 < T::FN; j0 += kAtOnce) {
+    if (j0) __syncthreads();
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      const uint32_t n = (wave % T::WN) * (kAtOnce * 16) + j * 16 + (lane & 15);
+#pragma unroll
+      for (int i = 0; i < T::FM; ++i) {
+        const uint32_t c = T::m_of(i, lane, wave) >> 2;
+        *(f32x4_t*)(lds + n * (T::BM * 4) + ((c ^ (n & 15)) << 4)) = acc[i][j0 + j];
+      }
+    }
+    __syncthreads();
+    constexpr uint32_t kRows = kAtOnce * 16 * T::WN, kEights = T::BM / 8;
+#pragma unroll 2
+    for (uint32_t q = threadIdx.x; q < kRows * kEights; q += T::kThreads) {
+      const uint32_t r = q / kEights, g = q % kEights;
+      // row r of the staged ones is this token of the tile
+      const uint32_t n = n0 + r / (kAtOnce * 16) * (T::FN * 16) + j0 * 16 + r % (kAtOnce * 16), m = m0 + g * 8;
+      if (n >= p.n || m >= p.m) continue;
+      const f32x4_t lo = *(const f32x4_t*)(lds + r * (T::BM * 4) + (((2 * g) ^ (r & 15)) << 4));
+      const f32x4_t hi = *(const f32x4_t*)(lds + r * (T::BM * 4) + (((2 * g + 1) ^ (r & 15)) << 4));
+      float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      finish_eight(p, v, n, m);
+    }
+  }
+}
+
+// The splits' sums, added in order, and the epilogue: a thread an eight of a row.
+__global__ __launch_bounds__(256) void join_kernel(ProductParams p, uint32_t splits) {
+  const uint32_t eights = (p.m + 7) / 8;
+  const uint64_t id = (uint64_t)blockIdx.x * 256 + threadIdx.x, n = id / eights;
+  if (n >= p.n) return;
+  const uint32_t m = (uint32_t)(id % eights) * 8;
+  const bool second = m + 4 < p.m_ld;
+  f32x4_t lo = {0.0f, 0.0f, 0.0f, 0.0f}, hi = lo;
+#pragma unroll 4
+  for (uint32_t s = 0; s < splits; ++s) {
+    const float* const from = p.sums + ((uint64_t)s * p.n + n) * p.m_ld + m;
+    lo += *(const f32x4_t*)from;
+    if (second) hi += *(const f32x4_t*)(from + 4);
+  }
+  float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+  finish_eight(p, v, n, m);
+}
+
+// ---------------------------------------------------------------- the elementwise part of the gradient
+
+struct SlopeParams {
+  const void* dy;
+  uint64_t dy_stride;
+  const void* pre;  // null: neither activation nor multiplier
+  uint64_t pre_stride;
+  const void* times;
+  uint64_t times_stride;
+  void* dtimes;
+  uint64_t dtimes_stride;
+  uint16_t* d;  // null: dy serves; rows of d_ld, zeros past the last feature
+  uint32_t d_ld;
+  float* partial;  // null: no bias; [chunks][rows]
+  uint32_t tokens, rows, chunk;
+  int act, bf16;
+  bool wide;
+};
+
+// A block takes 512 features (8 a lane) of `chunk` tokens, its waves the tokens in turn.
+__global__ __launch_bounds__(256) void slope_kernel(SlopeParams p) {
+  __shared__ float s_sum[3][512];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t row = blockIdx.x * 512 + lane * 8, left = row < p.rows ? p.rows - row : 0;
+  const uint32_t end = p.tokens - blockIdx.y * p.chunk < p.chunk ? p.tokens : (blockIdx.y + 1) * p.chunk;
+  float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  if (left)
+    for (uint64_t t = blockIdx.y * p.chunk + wave; t < end; t += 4) {
+      float v[8], pre[8], times[8];
+      load_eight(p.dy, t * p.dy_stride + row, p.bf16, p.wide, left, v);
+      if (p.pre) load_eight(p.pre, t * p.pre_stride + row, p.bf16, p.wide, left, pre);
+      if (p.times) load_eight(p.times, t * p.times_stride + row, p.bf16, p.wide, left, times);
+      if (p.pre) {
+        float g[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 a = activate2(p.act, pre[i]);
+          g[i] = v[i] * a.x;
+          v[i] *= p.times ? a.y * times[i] : a.y;
+          // past the row's end, where a derivative is no number's
+          if ((uint32_t)i >= left) v[i] = 0.0f;
+        }
+        if (p.dtimes) store_eight(p.dtimes, t * p.dtimes_stride + row, p.bf16, p.wide, left, g);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] += v[i];
+      if (p.d) store16(p.d + t * p.d_ld + row, pack_eight(v));
+    }
+  if (!p.partial) return;
+  if (wave) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s_sum[wave - 1][i * 64 + lane] = sum[i];
+  }
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float v = (sum[i] + s_sum[0][i * 64 + lane]) + (s_sum[1][i * 64 + lane] + s_sum[2][i * 64 + lane]);
+    if ((uint32_t)i < left) p.partial[(uint64_t)blockIdx.y * p.rows + row + i] = v;
+  }
+}
+
+// dbias from the chunks' sums: 64 features a block, its 4 waves a slice of the chunks each.
+__global__ __launch_bounds__(256) void dbias_kernel(const float* partial, uint32_t chunks, uint32_t rows, float* dbias) {
+  __shared__ float s[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t row = blockIdx.x * 64 + lane;
+  float v = 0.0f;
+  if (row < rows) {
+#pragma unroll 4
+    for (uint32_t c = wave; c < chunks; c += 4) v += partial[(uint64_t)c * rows + row];
+  }
+  s[wave][lane] = v;
+  __syncthreads();
+  if (wave == 0 && row < rows) dbias[row] = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
+}
+
+// Rows of `cols` padded with zeros to `ld`.
+__global__ __launch_bounds__(256) void pad_kernel(const uint16_t* from, uint64_t from_ld, uint64_t rows, uint32_t cols,
+                                                  uint16_t* to, uint32_t ld) {
+  const uint64_t groups = ld / 8, all = rows * groups;
+  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
+    const uint64_t r = i / groups;
+    const uint32_t c = (uint32_t)(i % groups) * 8;
+    const uint16_t* const row = from + r * from_ld;
+    uint4 v;
+    if (c + 8 <= cols) {
+      v = load16_any(row + c);
+    } else {
+      uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e)
+        if (c + e < cols) w[e >> 1] |= (uint32_t)row[c + e] << (16 * (e & 1));
+      v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    store16(to + r * ld + c, v);
+  }
+}
+
+// ---------------------------------------------------------------- shapes
+
+uint32_t up(uint32_t v, uint32_t to) { return (v + to - 1) / to * to; }
+uint32_t parts(uint64_t v, uint32_t of) { return (uint32_t)((v + of - 1) / of); }
+
+constexpr uint64_t kMaxStride = 1u << 20;    // a tile's byte offsets stay in 32 bits
+constexpr uint32_t kTilesAtOnce = 1u << 22;  // of up to 512 threads; a multiple of 8, the XCDs
+constexpr uint64_t kSumBytes = 32ull << 20;  // the most that splits' sums take
+constexpr uint32_t kMinSplit = 256;          // of k
+constexpr uint32_t kFewTokens = kLinearFewTokens;
+
+// Time of a product in thousands of cycles: rounds of blocks, each with a fixed part and
+// one per 64 of k, and, with splits, their sums' way and a launch.
+struct TileCost {
+  uint32_t bm, bn;
+  float fixed, step, shared;
+};
+constexpr TileCost kCosts[3] = {{256, 256, 18.0f, 2.2f, 0.0f}, {256, 128, 11.0f, 1.2f, 1.1f}, {128, 64, 6.0f, 0.9f, 0.6f}};
+
+struct Shape {
+  int tile;
+  uint32_t splits;
+};
+
+Shape shape_of(uint32_t m, uint32_t n, uint32_t k) {
+  constexpr float kCus = 256.0f;
+  Shape best = {2, 1};
+  float least = 0.0f;
+  const uint64_t bytes = (uint64_t)n * up(m, 4) * 4;
+  for (int i = 0; i < 3; ++i) {
+    const TileCost& c = kCosts[i];
+    const float tiles = (float)parts(m, c.bm) * (float)parts(n, c.bn);
+    for (uint32_t splits = 1; splits <= 64; ++splits) {
+      if (splits > 1 && (splits * bytes > kSumBytes || k < splits * kMinSplit || tiles * splits > 2 * kCus)) break;
+      const float blocks = tiles * splits;
+      const float rounds = (float)(uint64_t)((blocks + kCus - 1) / kCus), busy = blocks < kCus ? blocks / kCus : 1.0f;
+      const float steps = (float)parts(parts(k, splits), kGemmK);
+      float cost = rounds * (c.fixed + (c.step + c.shared * busy) * steps);
+      if (splits > 1) cost += 8.0f + (float)((splits + 1) * bytes) / 2e6f;
+      if (least == 0.0f || cost < least) {
+        least = cost;
+        best = {i, splits};
+      }
+    }
+  }
+  return best;
+}
+
+template <bool AK, bool BK>
+void run_product(ProductParams p, float* sums, hipStream_t stream) {
+  const Shape s = shape_of(p.m, p.n, p.k);
+  p.m_ld = up(p.m, 4);
+  p.sums = s.splits > 1 ? sums : nullptr;
+  p.k_split = up(parts(p.k, s.splits), kGemmK);
+  auto launch = [&](auto tile) {
+    typedef decltype(tile) T;
+    p.tiles_m = parts(p.m, T::BM);
+    p.tiles_n = parts(p.n, T::BN);
+    const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
+    for (uint64_t first = 0; first < tiles; first += kTilesAtOnce) {
+      p.first_tile = (uint32_t)first;
+      const uint64_t left = tiles - first;
+      hipLaunchKernelGGL((product_kernel<T, AK, BK>), dim3(left < kTilesAtOnce ? (uint32_t)left : kTilesAtOnce, s.splits),
+                         dim3(T::kThreads), 0, stream, p);
+    }
+  };
+  if (s.tile == 0) launch(Gemm<256, 256, 2, 4, 2, AK, BK>{});
+  else if (s.tile == 1) launch(Gemm<256, 128, 4, 2, 3, AK, BK>{});
+  else launch(Gemm<128, 64, 4, 1, 4, AK, BK>{});
+  if (s.splits > 1) {
+    const uint64_t threads = (uint64_t)p.n * parts(p.m, 8);
+    hipLaunchKernelGGL(join_kernel, dim3(parts(threads, 256)), dim3(256), 0, stream, p, s.splits);
+  }
+}
+
+struct Plan {
+  uint32_t ld, d_ld, chunk, chunks;
+  uint64_t w, x, d, partial, sums, total;
+};
+
+Plan plan_of(uint32_t tokens, uint32_t rows, uint32_t cols) {
+  Plan q;
+  q.ld = up(cols, 8);
+  q.d_ld = up(rows, 8);
+  // chunks of tokens for some eight blocks a CU
+  const uint32_t strips = parts(rows, 512), wanted = strips < 2048 ? 2048 / strips : 1;
+  q.chunk = up(parts(tokens, wanted), 16);
+  q.chunks = parts(tokens, q.chunk);
+  uint64_t at = 0;
+  auto take = [&](uint64_t bytes) {
+    const uint64_t here = at;
+    at += (bytes + 255) & ~255ull;
+    return here;
+  };
+  q.w = take(cols % 8 ? (uint64_t)rows * q.ld * 2 : 0);
+  q.x = take((uint64_t)tokens * q.ld * 2);
+  q.d = take((uint64_t)tokens * q.d_ld * 2);
+  q.partial = take((uint64_t)q.chunks * rows * 4);
+  auto sums = [&](uint32_t m, uint32_t n, uint32_t k) -> uint64_t {
+    const Shape s = shape_of(m, n, k);
+    return s.splits > 1 ? (uint64_t)s.splits * n * up(m, 4) * 4 : 0;
+  };
+  uint64_t most = sums(rows, tokens, cols);
+  for (uint64_t v : {sums(cols, tokens, rows), sums(cols, rows, tokens)})
+    if (v > most) most = v;
+  q.sums = take(most);
+  q.total = at;
+  return q;
+}
+
+// x as the products take it: rows of 16-byte groups, not too far apart.
+const uint16_t* tidy(const uint16_t* from, uint64_t& stride, uint64_t rows, uint32_t cols, uint16_t* to, uint32_t ld,
+                     hipStream_t stream) {
+  if (cols % 8 == 0 && stride % 8 == 0 && stride <= kMaxStride) return from;
+  uint64_t blocks = (rows * (ld / 8) + 255) / 256;
+  if (blocks > 8192) blocks = 8192;
+  hipLaunchKernelGGL(pad_kernel, dim3((uint32_t)blocks), dim3(256), 0, stream, from, stride, rows, cols, to, ld);
+  stride = ld;
+  return to;
+}
+
+}  // namespace
+
+uint64_t linear_needs(bool forward, uint32_t tokens, uint32_t rows, uint32_t cols) {
+  return forward && tokens <= kFewTokens ? 0 : plan_of(tokens, rows, cols).total;
+}
+
+// A call of fewer tokens may take more splits, and shorter chunks: bounds on those parts.
+uint64_t linear_bytes(uint32_t tokens, uint32_t rows, uint32_t cols) {
+  const Plan q = plan_of(tokens, rows, cols);
+  const uint32_t strips = parts(rows, 512);
+  const uint64_t chunks = strips < 2048 ? 2048 / strips : 1;
+  uint64_t sums = 0;  // at most k / kMinSplit splits
+  auto product = [&](uint64_t m, uint64_t n, uint64_t k) {
+    const uint64_t bytes = k / kMinSplit * n * (m + 3) * 4;
+    if (bytes > sums) sums = bytes;
+  };
+  product(rows, tokens, q.ld);
+  product(cols, tokens, rows);
+  product(cols, rows, tokens);
+  if (sums > kSumBytes) sums = kSumBytes;
+  return q.partial + ((chunks * rows * 4 + 255) & ~255ull) + ((sums + 255) & ~255ull);
+}
+
+hipError_t launch_linear(const LinearParams& c, char* ws, hipStream_t stream) {
+  if (c.tokens <= kFewTokens) {
+    const uint64_t n = (uint64_t)c.rows * c.cols;
+    LowpMatmulParams p = {(const uint8_t*)c.weight, nullptr, 1.0f, c.rows, c.cols, 2 * n, 0, c.x, c.x_stride, c.tokens,
+                          c.y, c.y_stride, c.e.out_bf16, c.e};
+    return launch_lowp_matmul(kWeightBf16, true, p, stream);
+  }
+  const Plan q = plan_of(c.tokens, c.rows, c.cols);
+  ProductParams p = {};
+  uint64_t w_ld = c.cols, x_ld = c.x_stride;
+  const uint16_t* const w = tidy(c.weight, w_ld, c.rows, c.cols, (uint16_t*)(ws + q.w), q.ld, stream);
+  const uint16_t* const x = tidy(c.x, x_ld, c.tokens, c.cols, (uint16_t*)(ws + q.x), q.ld, stream);
+  p.a = {w, w_ld, c.rows};
+  p.b = {x, x_ld, c.tokens};
+  p.m = c.rows;
+  p.n = c.tokens;
+  p.k = q.ld;
+  p.out = c.y;
+  p.out_ld = c.y_stride;
+  p.e = c.e;
+  const uint64_t unit = c.e.out_bf16 ? 8 : 4;
+  p.wide = c.y_stride % unit == 0 && (!c.e.pre || c.e.pre_stride % unit == 0) &&
+           (!c.e.times || c.e.times_stride % unit == 0) && (!c.e.residual || c.e.residual_stride % unit == 0);
+  run_product<false, false>(p, (float*)(ws + q.sums), stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t stream) {
+  const Plan q = plan_of(c.tokens, c.rows, c.cols);
+  uint64_t w_ld = c.cols, x_ld = c.x_stride;
+  const uint16_t* const w = tidy(c.weight, w_ld, c.rows, c.cols, (uint16_t*)(ws + q.w), q.ld, stream);
+  const uint16_t* const x = tidy(c.x, x_ld, c.tokens, c.cols, (uint16_t*)(ws + q.x), q.ld, stream);
+  // d, dtimes and dbias
+  const bool serves = !c.act && !c.times && c.bf16 && c.rows % 8 == 0 && c.dy_stride % 8 == 0 && c.dy_stride <= kMaxStride;
+  SlopeParams s = {};
+  s.dy = c.dy;
+  s.dy_stride = c.dy_stride;
+  s.pre = c.act || c.times ? c.pre : nullptr;
+  s.pre_stride = c.pre_stride;
+  s.times = c.times;
+  s.times_stride = c.times_stride;
+  s.dtimes = c.dtimes;
+  s.dtimes_stride = c.dtimes_stride;
+  s.d = serves ? nullptr : (uint16_t*)(ws + q.d);
+  s.d_ld = q.d_ld;
+  s.partial = c.dbias ? (float*)(ws + q.partial) : nullptr;
+  s.tokens = c.tokens;
+  s.rows = c.rows;
+  s.chunk = q.chunk;
+  s.act = c.act;
+  s.bf16 = c.bf16;
+  const uint64_t unit = c.bf16 ? 8 : 4;
+  s.wide = c.dy_stride % unit == 0 && (!s.pre || c.pre_stride % unit == 0) &&
+           (!c.times || (c.times_stride % unit == 0 && (!c.dtimes || c.dtimes_stride % unit == 0)));
+  if (s.d || s.partial)
+    hipLaunchKernelGGL(slope_kernel, dim3(parts(c.rows, 512), q.chunks), dim3(256), 0, stream, s);
+  if (c.dbias)
+    hipLaunchKernelGGL(dbias_kernel, dim3(parts(c.rows, 64)), dim3(256), 0, stream, s.partial, q.chunks, c.rows, c.dbias);
+  const uint16_t* const d = serves ? (const uint16_t*)c.dy : s.d;
+  const uint64_t d_ld = serves ? c.dy_stride : q.d_ld;
+  ProductParams p = {};
+  p.e.out_bf16 = 1;
+  p.a = {w, w_ld, q.ld};
+  p.b = {d, d_ld, c.tokens};
+  p.m = c.cols;
+  p.n = c.tokens;
+  p.k = c.rows;
+  p.out = c.dx;
+  p.out_ld = c.dx_stride;
+  p.wide = c.dx_stride % 8 == 0;
+  run_product<true, false>(p, (float*)(ws + q.sums), stream);
+  p.a = {x, x_ld, q.ld};
+  p.b = {d, d_ld, q.d_ld};
+  p.m = c.cols;
+  p.n = c.rows;
+  p.k = c.tokens;
+  p.out = c.dweight;
+  p.out_ld = c.cols;
+  p.wide = c.cols % 8 == 0;
+  run_product<true, true>(p, (float*)(ws + q.sums), stream);
+  return hipGetLastError();
+}
+
+}  // namespace pulse

@@ -26,6 +26,7 @@
 // products are the same as before, and only the row's first and last chunk are
 // masked.
 #include "device_common.hpp"
+#include "epilogue.hpp"
 #include "head.hpp"
 #include "lds_load.hpp"
 
@@ -35,18 +36,19 @@ namespace {
 
 constexpr uint32_t kLpGroups = 4;  // lane groups of a wave: units side by side in a chunk
 
-template <bool MX>
+template <int FORM>
 struct Unit {
-  static constexpr uint32_t kValues = MX ? 32 : 16;  // in 16 bytes of codes
+  static constexpr uint32_t kValues = FORM == kWeightMxfp4 ? 32 : FORM == kWeightFp8 ? 16 : 8;  // in 16 bytes of codes
   static constexpr uint32_t kFrags = kValues / 8;    // MFMA operands of 8 values
   static constexpr uint32_t kChunk = kValues * kLpGroups;
 };
 
-template <bool MX>
+template <int FORM>
 __device__ __forceinline__ bf16x8_t decode8(const uint4& c, int f, float scale) {
+  if constexpr (FORM == kWeightBf16) return __builtin_bit_cast(bf16x8_t, c);
   typedef __bf16 pair_t __attribute__((ext_vector_type(2)));
   pair_t v[4];
-  if constexpr (MX) {
+  if constexpr (FORM == kWeightMxfp4) {
     const uint32_t w = get_u32(c, f);
     v[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
     v[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
@@ -63,10 +65,10 @@ __device__ __forceinline__ bf16x8_t decode8(const uint4& c, int f, float scale) 
 }
 
 // Codes of a unit, of which only the values [lo, hi) count; the others become
-// code 0, which is zero in both types.
-template <bool MX>
+// code 0, which is zero in every type.
+template <int FORM>
 __device__ __forceinline__ uint4 mask_codes(uint4 c, int lo, int hi) {
-  constexpr int kBits = MX ? 4 : 8, kPer = 32 / kBits;
+  constexpr int kBits = FORM == kWeightMxfp4 ? 4 : FORM == kWeightFp8 ? 8 : 16, kPer = 32 / kBits;
   uint32_t w[4] = {c.x, c.y, c.z, c.w};
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -82,20 +84,20 @@ __device__ __forceinline__ uint4 mask_codes(uint4 c, int lo, int hi) {
 
 // What a lane holds of one chunk: its unit's codes and scale byte for RT row
 // tiles, its unit's values of one token in each of NT token tiles.
-template <bool MX, int RT, int NT>
+template <int FORM, int RT, int NT>
 struct Held {
   uint4 codes[RT];
   uint32_t scale[RT];
-  uint4 x[NT][Unit<MX>::kFrags];
+  uint4 x[NT][Unit<FORM>::kFrags];
 };
 
 // A wave's chunks are w, w + nwk, ...; `base` holds each row tile's first unit
 // (a byte offset of its codes), `shift` where in that unit the row starts.
-template <bool MX, int RT, int NT, bool SHIFT>
+template <int FORM, int RT, int NT, bool SHIFT>
 __device__ __forceinline__ void load_chunk(const LowpMatmulParams& p, const uint64_t (&unit)[RT],
                                            const uint16_t* const (&xrow)[NT], uint32_t chunk, int g,
-                                           uint32_t shift, Held<MX, RT, NT>& h) {
-  typedef Unit<MX> U;
+                                           uint32_t shift, Held<FORM, RT, NT>& h) {
+  typedef Unit<FORM> U;
   const uint32_t u = chunk * kLpGroups + g;                        // the lane's unit in its row
   const int64_t k = (int64_t)u * U::kValues - (SHIFT ? shift : 0);  // its first value's column
   const int64_t k0 = (int64_t)chunk * U::kChunk - (SHIFT ? shift : 0);
@@ -103,7 +105,7 @@ __device__ __forceinline__ void load_chunk(const LowpMatmulParams& p, const uint
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
       h.codes[r] = load16_any(p.codes + (unit[r] + u) * 16);
-      if constexpr (MX) h.scale[r] = p.scales[unit[r] + u];
+      if constexpr (FORM == kWeightMxfp4) h.scale[r] = p.scales[unit[r] + u];
     }
 #pragma unroll
     for (int n = 0; n < NT; ++n)
@@ -128,8 +130,8 @@ __device__ __forceinline__ void load_chunk(const LowpMatmulParams& p, const uint
           if (at + b < p.code_bytes) w[b >> 2] |= (uint32_t)p.codes[at + b] << (8 * (b & 3));
         c = make_uint4(w[0], w[1], w[2], w[3]);
       }
-      if constexpr (MX) h.scale[r] = p.scales[unit[r] + u];
-      c = mask_codes<MX>(c, lo, hi);
+      if constexpr (FORM == kWeightMxfp4) h.scale[r] = p.scales[unit[r] + u];
+      c = mask_codes<FORM>(c, lo, hi);
     }
     h.codes[r] = c;
   }
@@ -147,16 +149,16 @@ __device__ __forceinline__ void load_chunk(const LowpMatmulParams& p, const uint
     }
 }
 
-template <bool MX, int RT, int NT>
-__device__ __forceinline__ void multiply_chunk(const Held<MX, RT, NT>& h, f32x4_t (&acc)[RT][NT]) {
+template <int FORM, int RT, int NT>
+__device__ __forceinline__ void multiply_chunk(const Held<FORM, RT, NT>& h, f32x4_t (&acc)[RT][NT]) {
 #pragma unroll
   for (int r = 0; r < RT; ++r) {
     // the scale byte is the exponent field of its FP32 value; the conversion
     // takes 0 as 2^-127 and 255 as NaN
-    const float scale = MX ? __uint_as_float(h.scale[r] << 23) : 1.0f;
+    const float scale = FORM == kWeightMxfp4 ? __uint_as_float(h.scale[r] << 23) : 1.0f;
 #pragma unroll
-    for (uint32_t f = 0; f < Unit<MX>::kFrags; ++f) {
-      const bf16x8_t a = decode8<MX>(h.codes[r], f, scale);
+    for (uint32_t f = 0; f < Unit<FORM>::kFrags; ++f) {
+      const bf16x8_t a = decode8<FORM>(h.codes[r], f, scale);
 #pragma unroll
       for (int n = 0; n < NT; ++n)
         acc[r][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
@@ -167,9 +169,9 @@ __device__ __forceinline__ void multiply_chunk(const Held<MX, RT, NT>& h, f32x4_
 
 // grid.x: groups of RT row tiles from `first` on; grid.y: groups of NT token tiles.  The
 // block's waves share the chunks of one group and add their sums at the end.
-template <bool MX, int RT, int NT, bool SHIFT>
+template <int FORM, int RT, int NT, bool SHIFT, bool EPILOGUE>
 __global__ __launch_bounds__(1024) void lowp_matmul_kernel(LowpMatmulParams p, uint32_t classes, uint32_t first) {
-  typedef Unit<MX> U;
+  typedef Unit<FORM> U;
   extern __shared__ f32x4_t s_part[];  // [waves - 1][RT * NT][64]
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   const int r16 = lane & 15, g = lane >> 4;
@@ -207,15 +209,15 @@ __global__ __launch_bounds__(1024) void lowp_matmul_kernel(LowpMatmulParams p, u
   const uint32_t chunks = (uint32_t)(((uint64_t)p.cols + shift + U::kChunk - 1) / U::kChunk);
   uint32_t c = wave;
   if (c < chunks) {
-    Held<MX, RT, NT> h;
-    load_chunk<MX, RT, NT, SHIFT>(p, unit, xrow, c, g, shift, h);
+    Held<FORM, RT, NT> h;
+    load_chunk<FORM, RT, NT, SHIFT>(p, unit, xrow, c, g, shift, h);
     for (c += waves; c < chunks; c += waves) {
-      Held<MX, RT, NT> next;
-      load_chunk<MX, RT, NT, SHIFT>(p, unit, xrow, c, g, shift, next);
-      multiply_chunk<MX, RT, NT>(h, acc);
+      Held<FORM, RT, NT> next;
+      load_chunk<FORM, RT, NT, SHIFT>(p, unit, xrow, c, g, shift, next);
+      multiply_chunk<FORM, RT, NT>(h, acc);
       h = next;
     }
-    multiply_chunk<MX, RT, NT>(h, acc);
+    multiply_chunk<FORM, RT, NT>(h, acc);
   }
 
   if (waves > 1) {
@@ -244,50 +246,26 @@ __global__ __launch_bounds__(1024) void lowp_matmul_kernel(LowpMatmulParams p, u
       for (int i = 0; i < 4; ++i) {
         const uint64_t row = row_of(r, 4 * g + i);
         if (row >= p.rows) continue;
-        const float v = MX ? acc[r][n][i] : acc[r][n][i] / p.inv_scale;
+        float v = FORM == kWeightFp8 ? acc[r][n][i] / p.inv_scale : acc[r][n][i];
+        if constexpr (EPILOGUE) v = finish_one(p.e, v, t, row);
         if (p.y_bf16) ((uint16_t*)p.y)[t * p.y_stride + row] = (uint16_t)bf16x2_rne(__float_as_uint(v), 0u);
         else ((float*)p.y)[t * p.y_stride + row] = v;
       }
   }
 }
 
-// The sum of a tile's parts and its rows' results: lane (token r16, group g) has
-// the rows row0 + 4 g + i.
-__device__ __forceinline__ void store_result(const LowpMatmulParams& p, bool mx, f32x4_t v, uint32_t t,
-                                             uint64_t row) {
-  if (t >= p.tokens) return;
-  if (!mx) {
+// A tile's results of one token: the four rows from `row` on.
+template <int FORM, bool EPILOGUE>
+__device__ __forceinline__ void store_result(const LowpMatmulParams& p, f32x4_t v, uint32_t t, uint64_t row) {
+  if (t >= p.tokens || row >= p.rows) return;
+  if constexpr (FORM == kWeightFp8) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] /= p.inv_scale;
   }
-  const uint64_t at = t * p.y_stride + row;
-  if (p.y_bf16) {
-    uint16_t* y = (uint16_t*)p.y + at;
-    const uint2 o = make_uint2(bf16x2_rne(__float_as_uint(v[0]), __float_as_uint(v[1])),
-                               bf16x2_rne(__float_as_uint(v[2]), __float_as_uint(v[3])));
-    if (at % 4 == 0 && row + 4 <= p.rows) {
-      *(uint2*)y = o;
-    } else {
-      const uint32_t w[2] = {o.x, o.y};
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (row + i < p.rows) y[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-    }
-  } else {
-    float* y = (float*)p.y + at;
-    if (at % 4 == 0 && row + 4 <= p.rows) {
-      *(f32x4_t*)y = v;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (row + i < p.rows) y[i] = v[i];
-    }
-  }
+  const uint32_t left = p.rows - row < 4 ? (uint32_t)(p.rows - row) : 4;
+  if constexpr (EPILOGUE) v = finish_four(p.e, v, t, row, left);
+  store_four(p.y, t * p.y_stride + row, p.y_bf16, left, v);
 }
-
-struct __attribute__((packed)) Bytes4 {
-  uint32_t w;
-};
 
 // ---------------------------------------------------------------- slabs
 //
@@ -318,7 +296,7 @@ __device__ __forceinline__ uint32_t afresh(uint32_t lane) {
   return lane;
 }
 
-template <bool MX, bool TIGHT>
+template <int FORM, bool TIGHT>
 struct SlabStream {
   const LowpMatmulParams& p;
   const SlabShape& z;
@@ -350,7 +328,7 @@ struct SlabStream {
       u = u < left ? u : left - 1;
       load_to_lds<true>(to + i * 1024, (r * units + u) * 16, codes);
     }
-    if constexpr (MX) {
+    if constexpr (FORM == kWeightMxfp4) {
       uint32_t r = lane >> 2, u = (lane & 3) * 4;
       r = r < rows ? r : rows - 1;
       u = u < left ? u : left - 4;
@@ -368,7 +346,7 @@ struct SlabStream {
 
   // Waits until the oldest slab has landed.
   __device__ __forceinline__ void wait() {
-    constexpr int kLoads = MX ? 5 : 4;
+    constexpr int kLoads = FORM == kWeightMxfp4 ? 5 : 4;
     if (flying >= 4) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * kLoads) : "memory");
     else if (flying == 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * kLoads) : "memory");
     else if (flying == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads) : "memory");
@@ -380,9 +358,9 @@ struct SlabStream {
 // NS > 0: each wave has up to NS slabs of k for good (slabs <= NS wk) and the tokens'
 // values of them in registers; otherwise all tokens' values lie in LDS.  A block
 // takes NT tiles of 16 tokens.
-template <bool MX, int NS, int NT>
+template <int FORM, int NS, int NT, bool EPILOGUE>
 __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulParams p, SlabShape z) {
-  typedef Unit<MX> U;
+  typedef Unit<FORM> U;
   constexpr bool XREG = NS > 0;
   // units of a lane's codes, and parts of a sum, in registers at once
   constexpr int kAtOnce = NT == 1 ? 4 : 2, kAdds = NT == 1 ? 5 : 2;
@@ -415,7 +393,7 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
       }
     }
   }
-  SlabStream<MX, (NT > 1)> in = {p, z, s_lds + wave * z.depth * kSlabBytes, units, kw, rw, lane, blockIdx.x * z.run, kw};
+  SlabStream<FORM, (NT > 1)> in = {p, z, s_lds + wave * z.depth * kSlabBytes, units, kw, rw, lane, blockIdx.x * z.run, kw};
   for (uint32_t i = 0; i < z.depth && in.more(); ++i) in.load();
   if constexpr (!XREG) {
     const uint32_t pieces = (ld - 16) / 16, filled = p.cols / 8;  // of 16 bytes, in a row
@@ -438,7 +416,7 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
       const uint32_t now = afresh<(NT > 1)>(lane), r16 = now & 15, g = now >> 4;
       slot = slot + 1 == z.depth ? 0 : slot + 1;
       uint32_t scales = 0;
-      if constexpr (MX) scales = *(const uint32_t*)(from + 4096 + (r16 * 4 + g) * 4);
+      if constexpr (FORM == kWeightMxfp4) scales = *(const uint32_t*)(from + 4096 + (r16 * 4 + g) * 4);
       // past the row's end the tokens are zeros; the scale has to be finite there
       if (slab * kSlabUnits + g * 4 >= units) scales = 0x7F7F7F7Fu;
       uint4 c[kAtOnce];
@@ -453,10 +431,12 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
             if (in.more()) in.load();
           }
         }
-        const float scale = MX ? __uint_as_float((scales >> (8 * s) & 255u) << 23) : 1.0f;
+        const float scale = FORM == kWeightMxfp4 ? __uint_as_float((scales >> (8 * s) & 255u) << 23) : 1.0f;
 #pragma unroll
         for (uint32_t f = 0; f < U::kFrags; ++f) {
-          const bf16x8_t a = decode8<MX>(c[s % kAtOnce], f, scale);
+          bf16x8_t a = decode8<FORM>(c[s % kAtOnce], f, scale);
+          // past the row's end lies a value of the row again, which may be infinite
+          if (FORM == kWeightBf16 && slab * kSlabUnits + g * 4 + s >= units) a = bf16x8_t{};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
             uint4 v;
@@ -489,12 +469,12 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
         acc[n] = part[(rw * z.wk * NT + n) * 64 + lane];
 #pragma unroll kAdds
         for (uint32_t w = 1; w < z.wk; ++w) acc[n] += part[((rw * z.wk + w) * NT + n) * 64 + lane];
-        if (tile < z.tiles) store_result(p, MX, acc[n], t0 + n * 16 + r16, (uint64_t)tile * 16 + 4 * g);
+        if (tile < z.tiles) store_result<FORM, EPILOGUE>(p, acc[n], t0 + n * 16 + r16, (uint64_t)tile * 16 + 4 * g);
       }
     } else if (tile < z.tiles) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
-        store_result(p, MX, acc[n], t0 + n * 16 + r16, (uint64_t)tile * 16 + 4 * g);
+        store_result<FORM, EPILOGUE>(p, acc[n], t0 + n * 16 + r16, (uint64_t)tile * 16 + 4 * g);
     }
   }
 }
@@ -503,9 +483,16 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
 constexpr uint32_t kGroupsAtOnce = 1u << 21;
 constexpr uint32_t kTokensAtOnce = 1u << 15;
 
-template <bool MX, int RT, int NT, bool SHIFT>
-void launch_shape(const LowpMatmulParams& p, hipStream_t stream) {
-  typedef Unit<MX> U;
+// BF16 weights have the epilogue's form alone: without one it costs them nothing.
+template <int FORM, typename F>
+void by_epilogue(bool epilogue, F f) {
+  if (FORM == kWeightBf16 || epilogue) f(std::true_type{});
+  else f(std::integral_constant<bool, FORM == kWeightBf16>{});
+}
+
+template <int FORM, int RT, int NT, bool SHIFT>
+void launch_shape(const LowpMatmulParams& p, bool epilogue, hipStream_t stream) {
+  typedef Unit<FORM> U;
   const uint32_t classes = SHIFT ? U::kValues : 1;
   const uint64_t per_class = (p.rows + classes - 1) / classes;
   const uint64_t groups = (per_class + 16 * RT - 1) / (16 * RT) * classes;
@@ -517,9 +504,11 @@ void launch_shape(const LowpMatmulParams& p, hipStream_t stream) {
   const size_t lds = (size_t)(waves - 1) * RT * NT * 64 * sizeof(f32x4_t);
   for (uint64_t first = 0; first < groups; first += kGroupsAtOnce) {
     const uint64_t left = groups - first;
-    hipLaunchKernelGGL((lowp_matmul_kernel<MX, RT, NT, SHIFT>),
-                       dim3(left < kGroupsAtOnce ? (uint32_t)left : kGroupsAtOnce, tgroups), dim3(64 * waves), lds,
-                       stream, p, classes, (uint32_t)first);
+    const dim3 grid(left < kGroupsAtOnce ? (uint32_t)left : kGroupsAtOnce, tgroups), block(64 * waves);
+    by_epilogue<FORM>(epilogue, [&](auto e) {
+      hipLaunchKernelGGL((lowp_matmul_kernel<FORM, RT, NT, SHIFT, decltype(e)::value>), grid, block, lds, stream, p,
+                         classes, (uint32_t)first);
+    });
   }
 }
 
@@ -531,9 +520,10 @@ constexpr uint32_t kLpLds = 160 * 1024;
 // units (MXFP4, whose scales are loaded by fours: groups of four), other alignment, or too
 // many values of the tokens.  FP8 rows of whole units, 27,648 x 5,136, 1 and 64 tokens: 25
 // and 84 us (30 and 96 by the other kernel).
-template <bool MX>
-bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
-  typedef Unit<MX> U;
+template <int FORM>
+bool launch_slabs(const LowpMatmulParams& p, bool epilogue, hipStream_t stream) {
+  typedef Unit<FORM> U;
+  constexpr bool MX = FORM == kWeightMxfp4;
   if (p.tokens > 64 || p.cols % (MX ? U::kChunk : U::kValues) || ((uintptr_t)p.codes & 15) ||
       (MX && ((uintptr_t)p.scales & 3)))
     return false;
@@ -550,10 +540,11 @@ bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
   const uint64_t x_bytes = (p.tokens < 16 ? p.tokens : 16) * ((uint64_t)z.slabs * kSlabUnits * U::kValues * 2 + 16);
   // the tokens in registers where a block's waves cover k; then as many rows of waves
   // as make twelve
-  constexpr uint32_t kEach = MX ? 1 : 2;  // 64 registers of them
+  constexpr uint32_t kEach = MX ? 1 : FORM == kWeightFp8 ? 2 : 4;  // 64 registers of them
   const bool xreg = z.slabs <= 12 * kEach;
   if (xreg) {
-    z.wk = z.slabs <= 12 ? z.slabs : (z.slabs + 1) / 2;
+    const uint32_t each = (z.slabs + 11) / 12;
+    z.wk = (z.slabs + each - 1) / each;
     z.wr = 12 / z.wk;
     while (z.wr > 1 && z.wr * kLpCus > z.tiles) --z.wr;
   } else {
@@ -574,18 +565,21 @@ bool launch_slabs(const LowpMatmulParams& p, hipStream_t stream) {
   z.run = groups >= 16 * kLpCus ? 2 : 1;
   const dim3 grid(groups < kLpCus ? groups : kLpCus, (p.tokens + 16 * nt - 1) / (16 * nt)), block(64 * waves);
   const size_t lds = (size_t)(rest + (uint64_t)z.depth * waves * kSlabBytes);
-  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, lds, stream, p, z); };
-  if (!xreg) launch(lowp_slab_kernel<MX, 0, 1>);
-  else if (z.slabs <= z.wk) launch(nt == 1 ? lowp_slab_kernel<MX, 1, 1> : lowp_slab_kernel<MX, 1, 2>);
-  else launch(nt == 1 ? lowp_slab_kernel<MX, kEach, 1> : lowp_slab_kernel<MX, kEach, 2>);
+  by_epilogue<FORM>(epilogue, [&](auto e) {
+    constexpr bool E = decltype(e)::value;
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, lds, stream, p, z); };
+    if (!xreg) launch(lowp_slab_kernel<FORM, 0, 1, E>);
+    else if (z.slabs <= z.wk) launch(nt == 1 ? lowp_slab_kernel<FORM, 1, 1, E> : lowp_slab_kernel<FORM, 1, 2, E>);
+    else launch(nt == 1 ? lowp_slab_kernel<FORM, kEach, 1, E> : lowp_slab_kernel<FORM, kEach, 2, E>);
+  });
   return true;
 }
 
-template <bool MX>
-void launch_type(const LowpMatmulParams& p, hipStream_t stream) {
-  typedef Unit<MX> U;
-  if (p.cols % U::kValues) return launch_shape<MX, 1, 1, true>(p, stream);
-  if (launch_slabs<MX>(p, stream)) return;
+template <int FORM>
+void launch_type(const LowpMatmulParams& p, bool epilogue, hipStream_t stream) {
+  typedef Unit<FORM> U;
+  if (p.cols % U::kValues) return launch_shape<FORM, 1, 1, true>(p, epilogue, stream);
+  if (launch_slabs<FORM>(p, epilogue, stream)) return;
   // Each group of row tiles reads all tokens' values again, and a round of blocks takes as
   // long as its last: as few groups as fit one round; of many rounds, two tiles each.  16
   // tokens, MXFP4, in us with 1, 2 and 4 tiles: 5,120 x 27,648 (320 tiles) 75 and 51;
@@ -593,22 +587,27 @@ void launch_type(const LowpMatmulParams& p, hipStream_t stream) {
   // 58, 125 and 104 (5 tokens: 48 and 43, FP8 58 and 52; the least gain at 513 tiles, 8,208 x
   // 27,648: 65 and 70, FP8 68 and 79); one token, 40,000 x 5,056 (2,500) 33, 28, 33.
   const uint32_t tiles = (p.rows + 15) / 16;
-  if (p.tokens <= 16 && tiles <= kLpCus) launch_shape<MX, 1, 1, false>(p, stream);
-  else if (p.tokens <= 16 && tiles > 2 * kLpCus && tiles <= 4 * kLpCus) launch_shape<MX, 4, 1, false>(p, stream);
-  else if (p.tokens <= 16) launch_shape<MX, 2, 1, false>(p, stream);
-  else launch_shape<MX, 2, 2, false>(p, stream);
+  if (p.tokens <= 16 && tiles <= kLpCus) launch_shape<FORM, 1, 1, false>(p, epilogue, stream);
+  else if (p.tokens <= 16 && tiles > 2 * kLpCus && tiles <= 4 * kLpCus) launch_shape<FORM, 4, 1, false>(p, epilogue, stream);
+  else if (p.tokens <= 16) launch_shape<FORM, 2, 1, false>(p, epilogue, stream);
+  else launch_shape<FORM, 2, 2, false>(p, epilogue, stream);
 }
 
 }  // namespace
 
-hipError_t launch_lowp_matmul(bool mxfp4, const LowpMatmulParams& p, hipStream_t stream) {
+hipError_t launch_lowp_matmul(WeightForm form, bool epilogue, const LowpMatmulParams& p, hipStream_t stream) {
+  const uint64_t size = p.y_bf16 ? 2 : 4;
   for (uint32_t first = 0; first < p.tokens; first += kTokensAtOnce) {
     LowpMatmulParams q = p;
     q.x = p.x + first * p.x_stride;
-    q.y = (char*)p.y + first * p.y_stride * (p.y_bf16 ? 2 : 4);
+    q.y = (char*)p.y + first * p.y_stride * size;
+    if (p.e.times) q.e.times = (const char*)p.e.times + first * p.e.times_stride * size;
+    if (p.e.residual) q.e.residual = (const char*)p.e.residual + first * p.e.residual_stride * size;
+    if (p.e.pre) q.e.pre = (char*)p.e.pre + first * p.e.pre_stride * size;
     q.tokens = p.tokens - first < kTokensAtOnce ? p.tokens - first : kTokensAtOnce;
-    if (mxfp4) launch_type<true>(q, stream);
-    else launch_type<false>(q, stream);
+    if (form == kWeightMxfp4) launch_type<kWeightMxfp4>(q, epilogue, stream);
+    else if (form == kWeightFp8) launch_type<kWeightFp8>(q, epilogue, stream);
+    else launch_type<kWeightBf16>(q, epilogue, stream);
   }
   return hipGetLastError();
 }

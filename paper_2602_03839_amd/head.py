@@ -28,12 +28,17 @@ NORM_RMS = 1      # PULSE_NORM_RMS
 NORM_MAX_COLS = 16384
 CE_MAX_HIDDEN = 65536
 VERIFY_MAX_DRAFTS = 128
+LINEAR_MAX_WIDTH = 1 << 20  # of a weight's rows and columns, and tokens
+LINEAR_FEW_TOKENS = 32  # up to which Linear's forward pass needs no workspace
+# PULSE_ACT_*
+ACTIVATIONS = {None: 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 MAX_SIZE = (1 << 31) - 1  # of a vocabulary, a weight's rows or columns, tokens
 
 EXPORTS = ("pulse_layer_norm_workspace_bytes", "pulse_layer_norm_forward",
            "pulse_layer_norm_backward", "pulse_block_norm_workspace_bytes", "pulse_block_norm_forward",
            "pulse_block_norm_backward", "pulse_linear_ce_workspace_bytes", "pulse_linear_ce_forward",
-           "pulse_linear_ce_backward", "pulse_verify_drafts_workspace_bytes", "pulse_verify_drafts", "pulse_lowp_matmul")
+           "pulse_linear_ce_backward", "pulse_verify_drafts_workspace_bytes", "pulse_verify_drafts", "pulse_lowp_matmul", "pulse_lowp_linear",
+           "pulse_linear_workspace_bytes", "pulse_linear_forward", "pulse_linear_backward")
 
 _lock = threading.Lock()
 _lib = None
@@ -65,6 +70,13 @@ def lib():
             L.pulse_verify_drafts.argtypes = [i32, vp, u64, vp, u64, vp, vp, vp, u32, u32, u32, f64, f64, vp,
                                               vp, vp, vp, sz, vp]
             L.pulse_lowp_matmul.argtypes = [i32, vp, vp, f32, u32, u32, vp, u64, u32, i32, vp, u64, vp]
+            L.pulse_lowp_linear.argtypes = [i32, vp, vp, f32, u32, u32, vp, u64, u32, i32, vp, i32, vp, u64, vp, u64,
+                                            i32, vp, u64, vp]
+            L.pulse_linear_workspace_bytes.argtypes = [u32, u32, u32]
+            L.pulse_linear_forward.argtypes = [vp, u64, vp, u32, u32, u32, i32, vp, i32, vp, u64, vp, u64, i32, vp,
+                                               u64, vp, u64, vp, sz, vp]
+            L.pulse_linear_backward.argtypes = [i32, vp, u64, vp, u64, vp, vp, u64, i32, vp, u64, u32, u32, u32, vp,
+                                                u64, vp, vp, vp, u64, vp, sz, vp]
             L.pulse_linear_ce_workspace_bytes.argtypes = [u32, u32, u32]
             L.pulse_linear_ce_forward.argtypes = [vp, u64, vp, vp, u32, u32, u32, f32, vp, vp, vp, sz, vp]
             L.pulse_linear_ce_backward.argtypes = [vp, u64, vp, vp, u32, u32, u32, f32, vp, vp, vp, u64,
@@ -455,12 +467,133 @@ class VerifyDrafts:
         return tokens, count, logprob
 
 
+def _activation(name) -> int:
+    try:
+        return ACTIVATIONS[name]
+    except (KeyError, TypeError):
+        raise PulseError(f"activation must be one of {list(ACTIVATIONS)}, got {name!r}") from None
+
+
+class Linear:
+    """y = act(x W^T + bias) * times + residual for a BF16 weight [rows, cols], from one
+    token to many, and its gradient.
+
+    ``weight`` may change in place between calls.  ``bias`` is [rows], float32 or
+    bfloat16, or None; ``activation`` None, "relu", "silu", "gelu" or "gelu_tanh".  One
+    object serves up to ``max_tokens`` tokens a call.  Its workspace is allocated by the
+    first call that needs one (forward, more than LINEAR_FEW_TOKENS tokens), or given: a
+    uint8 tensor of at least ``workspace_bytes``, which objects whose calls are ordered
+    on one stream may share.
+    """
+
+    def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                 activation: Optional[str] = None, max_tokens: int = 32,
+                 workspace: Optional[torch.Tensor] = None):
+        if not isinstance(weight, torch.Tensor) or weight.dim() != 2:
+            raise PulseError("weight must be a tensor [rows, cols]")
+        self._pw = _p(weight, "weight", dtype=torch.bfloat16, optional=False)
+        self.device, (self.rows, self.cols) = weight.device, weight.shape
+        if not (1 <= self.rows <= LINEAR_MAX_WIDTH and 1 <= self.cols <= LINEAR_MAX_WIDTH):
+            raise PulseError(f"a weight of {self.rows} x {self.cols}, 1 to {LINEAR_MAX_WIDTH} of each are handled")
+        if not 0 <= max_tokens <= LINEAR_MAX_WIDTH:
+            raise PulseError(f"max_tokens {max_tokens} is out of range")
+        self._act, self._bias = _activation(activation), _p(bias, "bias", numel=self.rows, device=self.device)
+        self._bias_dt = 0 if bias is None else _dtype(bias, "bias")
+        self.weight, self.bias, self.activation, self.max_tokens = weight, bias, activation, max_tokens
+        self._lib = lib()
+        self.workspace_bytes = int(self._lib.pulse_linear_workspace_bytes(max_tokens, self.rows, self.cols))
+        self.ws = workspace
+        if workspace is not None:
+            _p(workspace, "workspace", dtype=torch.uint8, min_numel=self.workspace_bytes, device=self.device)
+
+    def _tokens(self, x, few, stream):
+        px, sx = _matrix(x, "x", self.cols, dtype=torch.bfloat16, device=self.device)
+        n = x.shape[0]
+        if n > self.max_tokens:
+            raise PulseError(f"{n} tokens, this object was built for {self.max_tokens}")
+        if n <= few:
+            return px, sx, n, None, 0
+        if self.ws is None:
+            self.ws = _new((self.workspace_bytes,), torch.uint8, self.device, stream)
+        return px, sx, n, self.ws.data_ptr(), self.ws.numel()
+
+    def __call__(self, x: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                 times: Optional[torch.Tensor] = None, keep_pre: bool = False,
+                 out: Optional[torch.Tensor] = None, out_dtype: torch.dtype = torch.bfloat16,
+                 pre: Optional[torch.Tensor] = None, stream=None):
+        """y, or (y, pre) with ``keep_pre`` (or a ``pre`` to write), for BF16 x [tokens,
+        cols]: y, pre = x W^T + bias, residual and times are [tokens, rows], all float32
+        or all bfloat16.  ``out`` may be the residual or the multiplier."""
+        dev = self.device
+        px, sx, n, pws, nws = self._tokens(x, LINEAR_FEW_TOKENS, stream)
+        if out is None:
+            dt, typ = _DTYPES.get(out_dtype), out_dtype
+            if dt is None:
+                raise PulseError(f"out_dtype must be float32 or bfloat16, got {out_dtype}")
+        else:
+            dt, typ = _dtype(out, "out"), out.dtype
+        pt, st = (None, 0) if times is None else _matrix(times, "times", self.rows, n, typ, dev)
+        pr, sr = (None, 0) if residual is None else _matrix(residual, "residual", self.rows, n, typ, dev)
+        out, py, sy = _out(out, "out", self.rows, n, typ, dev, stream)
+        pp, sp = None, 0
+        if keep_pre or pre is not None:
+            pre, pp, sp = _out(pre, "pre", self.rows, n, typ, dev, stream)
+        with _on(dev):
+            rc = self._lib.pulse_linear_forward(px, sx, self._pw, n, self.rows, self.cols, self._bias_dt, self._bias,
+                                                self._act, pt, st, pr, sr, dt, py, sy, pp, sp, pws, nws,
+                                                _stream(stream, dev))
+        if rc:
+            _check(rc, "pulse_linear_forward")
+        return out if pp is None and pre is None else (out, pre)
+
+    def backward(self, dy: torch.Tensor, x: torch.Tensor, pre: Optional[torch.Tensor] = None,
+                 times: Optional[torch.Tensor] = None, dx: Optional[torch.Tensor] = None,
+                 dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
+                 dtimes: Optional[torch.Tensor] = None, stream=None):
+        """(dx, dweight, dbias, dtimes) for the upstream gradient dy [tokens, rows] and
+        the forward pass's x, pre (needed with an activation or a multiplier) and times,
+        all of dy's type but x.  dx and dweight are bfloat16, dbias float32, dtimes of
+        dy's type; None where there is no bias or multiplier.  The residual's gradient is
+        dy itself."""
+        dev = self.device
+        px, sx, n, pws, nws = self._tokens(x, 0, stream)
+        dt, typ = _dtype(dy, "dy"), dy.dtype
+        py, sy = _matrix(dy, "dy", self.rows, n, typ, dev)
+        pp, sp = None, 0
+        if self._act or times is not None:
+            pp, sp = _matrix(pre, "pre", self.rows, n, typ, dev)
+        pt, st = (None, 0) if times is None else _matrix(times, "times", self.rows, n, typ, dev)
+        dx, pdx, sdx = _out(dx, "dx", self.cols, n, torch.bfloat16, dev, stream)
+        if dweight is None:
+            dweight = _new((self.rows, self.cols), torch.bfloat16, dev, stream)
+        pdw = _p(dweight, "dweight", dtype=torch.bfloat16, numel=self.rows * self.cols, device=dev)
+        dbias, pdb = (None, None) if self.bias is None else _vec(dbias, "dbias", self.rows, dev, stream)
+        pdt, sdt = None, 0
+        if times is None:
+            dtimes = None
+        else:
+            dtimes, pdt, sdt = _out(dtimes, "dtimes", self.rows, n, typ, dev, stream)
+        with _on(dev):
+            rc = self._lib.pulse_linear_backward(dt, py, sy, px, sx, self._pw, pp, sp, self._act, pt, st, n, self.rows,
+                                                 self.cols, pdx, sdx, pdw, pdb, pdt, sdt, pws, nws,
+                                                 _stream(stream, dev))
+        if rc:
+            _check(rc, "pulse_linear_backward")
+        return dx, dweight, dbias, dtimes
+
+
 class LowpLinear:
     """Products with a [rows, cols] weight that a receiver holds as MXFP4 or FP8
-    codes (the tensors that ``pulse.ApplyLowpBatch`` patches in place)."""
+    codes (the tensors that ``pulse.ApplyLowpBatch`` patches in place), with what
+    follows them in a block: y = act(x W^T + bias) * times + residual.
+
+    ``bias`` is [rows], float32 or bfloat16, or None; ``activation`` None, "relu",
+    "silu", "gelu" or "gelu_tanh".
+    """
 
     def __init__(self, dtype: int, codes: torch.Tensor, scales: Optional[torch.Tensor], rows: int,
-                 cols: int, inv_scale: float = 1.0):
+                 cols: int, inv_scale: float = 1.0, bias: Optional[torch.Tensor] = None,
+                 activation: Optional[str] = None):
         if not (1 <= rows <= MAX_SIZE and 1 <= cols <= MAX_SIZE):
             raise PulseError(f"a weight of {rows} x {cols}, 1 to {MAX_SIZE} of each are handled")
         nc, ns = pulse.lowp_sizes(dtype, rows * cols)
@@ -469,11 +602,17 @@ class LowpLinear:
         self._scales = _p(scales, "scales", esize=1, min_numel=ns, device=self.device,
                           optional=dtype != pulse.MXFP4)
         self.dtype, self.rows, self.cols, self.inv_scale = dtype, rows, cols, float(inv_scale)
+        self._act, self._bias = _activation(activation), _p(bias, "bias", numel=rows, device=self.device)
+        self._bias_dt = 0 if bias is None else _dtype(bias, "bias")
+        self.bias, self.activation = bias, activation
         self.keep, self._lib = (codes, scales), lib()
 
     def __call__(self, x: torch.Tensor, out: Optional[torch.Tensor] = None,
-                 out_dtype: torch.dtype = torch.float32, stream=None) -> torch.Tensor:
-        """x W^T for BF16 x [tokens, cols]: [tokens, rows], float32 or bfloat16."""
+                 out_dtype: torch.dtype = torch.float32, stream=None, times: Optional[torch.Tensor] = None,
+                 residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """act(x W^T + bias) * times + residual for BF16 x [tokens, cols]: [tokens,
+        rows], float32 or bfloat16.  times and residual are of the same shape and type;
+        ``out`` may be either of them."""
         dev = self.device
         px, sx = _matrix(x, "x", self.cols, dtype=torch.bfloat16, device=dev)
         n = x.shape[0]
@@ -486,8 +625,18 @@ class LowpLinear:
         else:
             dt = _dtype(out, "out")
             py, sy = _matrix(out, "out", self.rows, n, device=dev)
-        rc = self._lib.pulse_lowp_matmul(self.dtype, self._codes, self._scales, self.inv_scale, self.rows,
-                                         self.cols, px, sx, n, dt, py, sy, _stream(stream, dev))
+        if times is None and residual is None and self._bias is None and not self._act:
+            rc = self._lib.pulse_lowp_matmul(self.dtype, self._codes, self._scales, self.inv_scale, self.rows,
+                                             self.cols, px, sx, n, dt, py, sy, _stream(stream, dev))
+            if rc:
+                _check(rc, "pulse_lowp_matmul")
+            return out
+        pt, st = (None, 0) if times is None else _matrix(times, "times", self.rows, n, out.dtype, dev)
+        pr, sr = (None, 0) if residual is None else _matrix(residual, "residual", self.rows, n, out.dtype, dev)
+        with _on(dev):
+            rc = self._lib.pulse_lowp_linear(self.dtype, self._codes, self._scales, self.inv_scale, self.rows,
+                                             self.cols, px, sx, n, self._bias_dt, self._bias, self._act, pt, st,
+                                             pr, sr, dt, py, sy, _stream(stream, dev))
         if rc:
-            _check(rc, "pulse_verify_drafts_workspace_bytes", "pulse_verify_drafts", "pulse_lowp_matmul")
+            _check(rc, "pulse_lowp_linear")
         return out

@@ -87,3 +87,62 @@ def test_verify_drafts_validation(L):
         (dict(out=A + 4), EALIGN, b"aligned"), (dict(lp=A + 2), EALIGN, b"aligned"), (dict(lengths=A + 2), EALIGN, b"aligned"),
         (dict(dtype=F32, z=A + 2), EALIGN, b"aligned"), (dict(ws=None), EINVAL, b"workspace"),
         (dict(wsb=size - 1), EINVAL, b"workspace"), (dict(ws=A + 64), EALIGN, b"workspace")))
+
+
+def test_lowp_linear_validation(L):
+    good = dict(dtype=MX, codes=A, scales=A, inv=1.0, rows=64, cols=128, x=A, xs=128, tokens=4, bd=F32, bias=A, act=2,
+                times=A, ts=64, res=A, rs=64, yd=BF16, y=A + 4096, ys=64, stream=None)
+    assert L.pulse_lowp_linear(*{**good, **dict(tokens=0, x=None, y=None, codes=None, times=None, res=None)}.values()) == OK
+    refused(L.pulse_lowp_linear, good, L, (
+        (dict(dtype=9), EINVAL, b"dtype"), (dict(yd=FP8), EINVAL, b"y_dtype"), (dict(rows=0), EINVAL, b"weight of"),
+        (dict(cols=1 << 31), EINVAL, b"weight of"), (dict(tokens=(1 << 20) + 1), EINVAL, b"tokens"),
+        (dict(codes=None), EINVAL, b"codes"), (dict(scales=None), EINVAL, b"scales"), (dict(codes=A + 2), EALIGN, b"codes"),
+        (dict(dtype=FP8, inv=0.0), EINVAL, b"inv_scale"), (dict(dtype=FP8, inv=NAN), EINVAL, b"inv_scale"),
+        (dict(x=None), EINVAL, b"x is NULL"), (dict(xs=100), EINVAL, b"x stride"), (dict(y=None), EINVAL, b"y is NULL"),
+        (dict(ys=63), EINVAL, b"y stride"), (dict(bd=0), EINVAL, b"bias_dtype"), (dict(bias=A + 4), EALIGN, b"bias"),
+        (dict(act=5), EINVAL, b"activation"), (dict(act=-1), EINVAL, b"activation"), (dict(ts=3), EINVAL, b"times stride"),
+        (dict(rs=3), EINVAL, b"residual stride"), (dict(times=A + 8), EALIGN, b"times"), (dict(res=A + 2), EALIGN, b"residual"),
+        (dict(y=A, ys=72), EINVAL, b"another stride")))
+
+
+def test_linear_validation(L):
+    need = L.pulse_linear_workspace_bytes
+    top = 1 << 20
+    assert need(0, 64, 128) == 0
+    for sizes in ((1, 0, 8), (1, 8, 0), (top + 1, 8, 8), (1, top + 1, 8), (1, 8, top + 1), (0xFFFFFFFF,) * 3):
+        assert need(*sizes) == 0, sizes
+    for sizes in ((1, 1, 1), (top, 1, 1), (1, top, 1), (1, 1, top), (top, top, top), (4096, 18944, 3584)):
+        assert need(*sizes) > 0, sizes
+    size = need(100, 64, 128)
+    good = dict(x=A, xs=128, w=A, tokens=100, rows=64, cols=128, bd=BF16, bias=A, act=1, times=A, ts=64, res=A, rs=64,
+                yd=F32, y=A + (1 << 16), ys=64, pre=A, ps=64, ws=A, wsb=size, stream=None)
+    assert L.pulse_linear_forward(*{**good, **dict(tokens=0, x=None, w=None, y=None, ws=None, wsb=0)}.values()) == OK
+    shared = ((dict(rows=0), EINVAL, b"weight of"), (dict(cols=top + 1), EINVAL, b"weight of"),
+              (dict(tokens=top + 1), EINVAL, b"tokens"), (dict(x=None), EINVAL, b"x is NULL"), (dict(xs=9), EINVAL, b"x stride"),
+              (dict(w=None), EINVAL, b"weight is NULL"), (dict(w=A + 8), EALIGN, b"weight"), (dict(ws=None), EINVAL, b"workspace"),
+              (dict(ws=A + 8), EALIGN, b"workspace"), (dict(wsb=64), EINVAL, b"workspace"),
+              (dict(act=7), EINVAL, b"activation"), (dict(times=A + 4), EALIGN, b"times"), (dict(ts=1), EINVAL, b"times stride"))
+    refused(L.pulse_linear_forward, good, L, shared + (
+        (dict(yd=0), EINVAL, b"y_dtype"), (dict(y=None), EINVAL, b"y is NULL"), (dict(ys=8), EINVAL, b"y stride"),
+        (dict(bd=1), EINVAL, b"bias_dtype"), (dict(res=A + 4), EALIGN, b"residual"), (dict(pre=A + 8), EALIGN, b"pre"),
+        (dict(ps=63), EINVAL, b"pre stride"), (dict(y=A, ys=65), EINVAL, b"another stride")))
+    good = dict(dtype=BF16, dy=A, dys=64, x=A, xs=128, w=A, pre=A, ps=64, act=2, times=A, ts=64, tokens=100, rows=64,
+                cols=128, dx=A, dxs=128, dw=A, db=A, dt=A, dts=64, ws=A, wsb=size, stream=None)
+    refused(L.pulse_linear_backward, good, L, shared + (
+        (dict(dtype=1), EINVAL, b"dtype"), (dict(dy=None), EINVAL, b"dy is NULL"), (dict(dys=3), EINVAL, b"dy stride"),
+        (dict(pre=None), EINVAL, b"pre is NULL"), (dict(pre=None, act=0), EINVAL, b"pre is NULL"),
+        (dict(times=None, ts=0), EINVAL, b"dtimes without"), (dict(dts=3), EINVAL, b"dtimes stride"),
+        (dict(dx=None), EINVAL, b"dx is NULL"), (dict(dxs=1), EINVAL, b"dx stride"), (dict(dw=None), EINVAL, b"dweight"),
+        (dict(dw=A + 2), EALIGN, b"dweight"), (dict(db=A + 2), EALIGN, b"dbias")))
+
+
+def test_linear_workspace_serves_fewer_tokens(L):
+    """What a call asks for is within the workspace of any larger number of tokens."""
+    for rows, cols in ((64, 128), (1003, 203), (18944, 3584), (3584, 18944), (64, 64), (1, 1), (7, 27648)):
+        for most in (40, 700, 9000):
+            size = L.pulse_linear_workspace_bytes(most, rows, cols)
+            for tokens in range(33, most + 1, max(1, most // 50)):
+                # a wrong pointer at the end: the workspace is looked at before
+                rc = L.pulse_linear_forward(A, cols, A, tokens, rows, cols, 0, None, 0, None, 0, None, 0, BF16, None,
+                                            rows, None, 0, A, size, None)
+                assert rc == EINVAL and b"y is NULL" in L.pulse_last_error(), (rows, cols, most, tokens, L.pulse_last_error())
