@@ -11,13 +11,14 @@
 // Probabilities are FP64.  The draw is the first entry whose cumulated probability
 // exceeds u times the total: in FP32 each of some 150,000 borders would be off by 1e-7
 // of the total, so that one draw in 30 gave another token than the definition's.  With
-// borders off by 1e-12 it is one in a million.  An exponential is 9 FMAs and a handful
-// of other FP64 instructions, which issue as fast as FP32's here.
+// borders off by 5e-11 it is one in 100,000.  An exponential is 15 FP64 instructions,
+// which issue as fast as FP32's here, and these bound the first kernel for BF16 logits.
 //
-// Three kernels: per row and tile of the vocabulary the largest logit and the sum of
-// exponentials below it; per sequence and tile the decisions (each block joins its
-// sequence's sums again: some KB from the L2) and a refused row's sum of max(p - q, 0);
-// per sequence the tile that holds the draw, then the entry in it.
+// A wave takes a segment of a row by itself: 1,024 adjacent entries, or 512 where that
+// would leave CUs without work.  Four kernels: per segment the largest logit and the sum
+// of exponentials below it; per sequence the decisions; per segment of a refused draft's
+// rows the sums of max(p - q, 0), of 512 entries each; per sequence the segment that
+// holds the draw, then the entry in it.  Without drafts the first and the last.
 #include "device_common.hpp"
 #include "head.hpp"
 
@@ -25,64 +26,105 @@ namespace pulse {
 
 namespace {
 
-constexpr double kNoEntry = -1100.0;  // 2^x is 0
-
-// 2^x for x <= 0, or a little above, off by 1.1e-12: x to the nearest integer and a
-// polynomial for the rest, interpolated at the 9 Chebyshev nodes of [-1/2, 1/2].
+// 2^x for x <= 0, or a little above, off by 5.5e-11: a polynomial for what x is from the
+// nearest integer, interpolated at the 8 Chebyshev nodes of [-1/2, 1/2].  The integer is
+// in the low bits of x + 1.5 * 2^52, and goes into the exponent by an addition; 2^-1000
+// stands for 0.
+template <bool CLAMP = true>  // without: x > -1000
 __device__ __forceinline__ double exp2_64(double x) {
-  x = __builtin_fmax(x, kNoEntry);
-  const double k = __builtin_rint(x), f = x - k;
-  double v = 1.3255224878668817e-06;
-  v = __builtin_fma(v, f, 1.5310079402249296e-05);
-  v = __builtin_fma(v, f, 0.00015403455852453838);
-  v = __builtin_fma(v, f, 0.0013333450568000645);
-  v = __builtin_fma(v, f, 0.009618129159402558);
-  v = __builtin_fma(v, f, 0.05550410941205933);
-  v = __builtin_fma(v, f, 0.2402265069581299);
-  v = __builtin_fma(v, f, 0.6931471805459335);
-  v = __builtin_fma(v, f, 1.0);
-  return __builtin_ldexp(v, (int)k);
+  if constexpr (CLAMP) x = __builtin_fmax(x, -1000.0);
+  const double shifted = x + 0x1.8p52, f = x - (shifted - 0x1.8p52);
+  double v = __builtin_fma(1.5303700711365693e-05, f, 0.00015469729214118296);
+  v = __builtin_fma(v, f, 0.0013333478473685416);
+  v = __builtin_fma(v, f, 0.009618025613318034);
+  v = __builtin_fma(v, f, 0.055504109063258665);
+  v = __builtin_fma(v, f, 0.24022651213498092);
+  v = __builtin_fma(v, f, 0.6931471805568324);
+  v = __builtin_fma(v, f, 0.9999999999595618);
+  return __hiloint2double(__double2hiint(v) + (__double2loint(shifted) << 20), __double2loint(v));
 }
 
 __device__ __forceinline__ float logit_of(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
 __device__ __forceinline__ float logit_of(float v) { return v; }
 
-// Entries c to c + 7 of a row, -inf past its end.
-__device__ __forceinline__ void load_logits(const uint16_t* row, uint32_t c, uint32_t vocab, float (&z)[8]) {
+// Entries c to c + 7 of a row as they lie in memory, -inf past its end.
+template <typename T>
+struct RawLogits {
+  uint4 v[sizeof(T) / 2];
+};
+
+template <typename T>
+__device__ __forceinline__ void load_raw(const T* row, uint32_t c, uint32_t vocab, RawLogits<T>& r) {
+  constexpr int kPer = 16 / sizeof(T);
   if (c + 8 <= vocab) {
-    const uint4 v = load16_any(row + c);
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      z[e] = __uint_as_float(e & 1 ? get_u32(v, e >> 1) & 0xFFFF0000u : get_u32(v, e >> 1) << 16);
+    for (int i = 0; i < 8 / kPer; ++i) r.v[i] = load16_any(row + c + i * kPer);
+    return;
+  }
+  uint32_t w[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    w[e] = __float_as_uint(c < vocab && e < vocab - c ? logit_of(row[c + e]) : -INFINITY);
+  if constexpr (sizeof(T) == 2) {
+    r.v[0] = make_uint4(w[0] >> 16 | w[1], w[2] >> 16 | w[3], w[4] >> 16 | w[5], w[6] >> 16 | w[7]);
   } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = c < vocab && e < vocab - c ? logit_of(row[c + e]) : -INFINITY;
+    r.v[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    r.v[1] = make_uint4(w[4], w[5], w[6], w[7]);
   }
 }
-__device__ __forceinline__ void load_logits(const float* row, uint32_t c, uint32_t vocab, float (&z)[8]) {
-  if (c + 8 <= vocab) {
-    const uint4 a = load16_any(row + c), b = load16_any(row + c + 4);
+
+template <typename T>
+__device__ __forceinline__ void unpack(const RawLogits<T>& r, float (&z)[8]) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      z[e] = __uint_as_float(get_u32(a, e));
-      z[4 + e] = __uint_as_float(get_u32(b, e));
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (sizeof(T) == 2) {
+      const uint32_t w = get_u32(r.v[0], e >> 1);
+      z[e] = __uint_as_float(e & 1 ? w & 0xFFFF0000u : w << 16);
+    } else {
+      z[e] = __uint_as_float(get_u32(r.v[e >> 2], e & 3));
     }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) z[e] = c < vocab && e < vocab - c ? row[c + e] : -INFINITY;
   }
 }
 
-__device__ __forceinline__ double shuffle_xor(double v, int mask) {
-  const uint64_t b = __builtin_bit_cast(uint64_t, v);
-  const uint32_t lo = __shfl_xor((uint32_t)b, mask), hi = __shfl_xor((uint32_t)(b >> 32), mask);
-  return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+template <typename T>
+__device__ __forceinline__ void load_logits(const T* row, uint32_t c, uint32_t vocab, float (&z)[8]) {
+  RawLogits<T> r;
+  load_raw(row, c, vocab, r);
+  unpack(r, z);
 }
 
+// A lane's value (the same lane for all) in every lane.
+__device__ __forceinline__ double lane_value(double v, int lane) {
+  return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane),
+                          __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+
+template <int CTRL>
+__device__ __forceinline__ double dpp64(double v) {
+  return __hiloint2double(__builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xF, 0xF, true),
+                          __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xF, 0xF, true));
+}
+
+// The wave's sum and maximum in every lane, as wave_sum.
 __device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int x = 1; x < 64; x *= 2) v += shuffle_xor(v, x);
-  return v;
+  v += dpp64<0xB1>(v);   // quad_perm 1,0,3,2
+  v += dpp64<0x4E>(v);   // quad_perm 2,3,0,1
+  v += dpp64<0x141>(v);  // row_half_mirror
+  v += dpp64<0x140>(v);  // row_mirror
+  return (lane_value(v, 0) + lane_value(v, 16)) + (lane_value(v, 32) + lane_value(v, 48));
+}
+
+__device__ __forceinline__ float wave_max(float v) {
+  auto with = [&](auto ctrl) {
+    v = __builtin_fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, 0xF,
+                                                                      0xF, true)));
+  };
+  with(std::integral_constant<int, 0xB1>{});
+  with(std::integral_constant<int, 0x4E>{});
+  with(std::integral_constant<int, 0x141>{});
+  with(std::integral_constant<int, 0x140>{});
+  auto row = [&](int l) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), l)); };
+  return __builtin_fmaxf(__builtin_fmaxf(row(0), row(16)), __builtin_fmaxf(row(32), row(48)));
 }
 
 // The sum over lanes 0 to this one.
@@ -90,9 +132,8 @@ __device__ __forceinline__ double wave_scan64(double v) {
   const int lane = lane_id();
 #pragma unroll
   for (int x = 1; x < 64; x *= 2) {
-    const uint64_t b = __builtin_bit_cast(uint64_t, v);
-    const uint32_t lo = __shfl_up((uint32_t)b, x), hi = __shfl_up((uint32_t)(b >> 32), x);
-    if (lane >= x) v += __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+    const double up = __hiloint2double(__shfl_up(__double2hiint(v), x), __shfl_up(__double2loint(v), x));
+    if (lane >= x) v += up;
   }
   return v;
 }
@@ -112,67 +153,76 @@ __device__ __forceinline__ const char* row_at(const VerifyParams& p, uint32_t b,
 
 __device__ __forceinline__ double probability(const VerifyRow& d, float z) {
   // the largest logit is infinite where the row is empty: no difference is taken then
-  return d.inv == 0.0 ? 0.0 : exp2_64(((double)z - (double)d.top) * d.by) * d.inv;
+  const double x = ((double)z - (double)d.top) * d.by;
+  return d.inv == 0.0 || !(x > -1000.0) ? 0.0 : exp2_64(x) * d.inv;
 }
 
-// A tile of a row: the largest logit, and the sum of exponentials below it (NaN where a
-// logit is NaN or the largest is infinite; 0 where every one is -inf).
-template <typename T, int TILE>
-__global__ __launch_bounds__(256) void verify_sums_kernel(VerifyParams p, uint64_t first) {
-  constexpr int kGroups = TILE / 2048;
-  const uint64_t block = first + blockIdx.x;
-  const uint64_t id = block / p.tiles;
-  const uint32_t tile = (uint32_t)(block % p.tiles), b = (uint32_t)(id / p.rows), r = (uint32_t)(id % p.rows);
+// Where a wave's entries lie: eight a lane and 512 at a time, from its segment's first on.
+template <int SEG>
+__device__ __forceinline__ uint32_t entry_at(uint32_t segment, int j) {
+  return segment * SEG + j * 512 + (threadIdx.x & 63) * 8;
+}
+
+// A segment of a row, a wave each: the largest logit, and the sum of exponentials below
+// it (NaN where a logit is NaN or the largest is +inf; 0 where every one is -inf).
+template <typename T, int SEG>
+__global__ __launch_bounds__(256) void verify_sums_kernel(VerifyParams p, uint32_t first_row) {
+  constexpr int kGroups = SEG / 512;
+  const uint32_t blocks = (p.segments + 3) / 4, id = first_row + blockIdx.x / blocks;
+  const uint32_t segment = blockIdx.x % blocks * 4 + (threadIdx.x >> 6), b = id / p.rows, r = id % p.rows;
   const uint32_t length = length_of(p, b);
-  if (r <= p.drafts ? r > length : r - p.drafts - 1 >= length) return;  // nobody asks
+  if (segment >= p.segments || (r <= p.drafts ? r > length : r - p.drafts - 1 >= length)) return;  // nobody asks
   const T* const row = (const T*)row_at(p, b, r, sizeof(T));
-  const uint32_t c0 = tile * TILE + threadIdx.x * 8;
   float z[kGroups][8];
 #pragma unroll
-  for (int j = 0; j < kGroups; ++j) load_logits(row, c0 + j * 2048, p.vocab, z[j]);
+  for (int j = 0; j < kGroups; ++j) load_logits(row, entry_at<SEG>(segment, j), p.vocab, z[j]);
+  // the largest value; the largest bits as whole numbers with and without a sign, which
+  // are a NaN's where there is one, and the latter's else the most negative value's
   float top = -INFINITY;
-  bool nan = false;
+  int32_t bits = 0;
+  uint32_t ubits = 0;
 #pragma unroll
   for (int j = 0; j < kGroups; ++j)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       top = __builtin_fmaxf(top, z[j][e]);
-      nan |= z[j][e] != z[j][e];
+      const int32_t v = __float_as_int(z[j][e]);
+      bits = v > bits ? v : bits;
+      ubits = (uint32_t)v > ubits ? (uint32_t)v : ubits;
     }
-  __shared__ float s_top[4];
-  __shared__ double s_sum[4];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  top = wave_max(top);
+  const bool nan = bits > 0x7F800000 || ubits > 0xFF800000u;
+  const double by = r <= p.drafts ? p.by : p.draft_by, from = -(double)top * by;
+  const double least = __builtin_fma((double)(ubits >> 31 ? __uint_as_float(ubits) : 0.0f), by, from);
+  double sum[2] = {0.0, 0.0};
+  auto add = [&](auto clamp) {
 #pragma unroll
-  for (int x = 1; x < 64; x *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, x));
-  if (lane == 0) s_top[wave] = top;
-  __syncthreads();
-  top = __builtin_fmaxf(__builtin_fmaxf(s_top[0], s_top[1]), __builtin_fmaxf(s_top[2], s_top[3]));
-  const double by = r <= p.drafts ? p.by : p.draft_by;
-  const double from = top == -INFINITY ? 0.0 : (double)top;
-  double sum[2] = {nan || top == INFINITY ? (double)NAN : 0.0, 0.0};
+    for (int j = 0; j < kGroups; ++j)
 #pragma unroll
-  for (int j = 0; j < kGroups; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum[e & 1] += exp2_64(((double)z[j][e] - from) * by);
+      for (int e = 0; e < 8; ++e)
+        sum[e & 1] += exp2_64<decltype(clamp)::value>(__builtin_fma((double)z[j][e], by, from));
+  };
+  // the same for the whole wave
+  if (!__builtin_amdgcn_ballot_w64(!(least > -1000.0))) add(std::false_type{});
+  else if (top > -INFINITY) add(std::true_type{});
+  if (nan || top == INFINITY) sum[0] = (double)NAN;
   const double all = wave_sum64(sum[0] + sum[1]);
-  if (lane == 0) s_sum[wave] = all;
-  __syncthreads();
-  if (threadIdx.x == 0)
-    p.parts[id * p.tiles + tile] = {(s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]), top};
+  if ((threadIdx.x & 63) == 0) p.parts[(uint64_t)id * p.segments + segment] = {all, top};
 }
 
-// A row from its tiles' sums, in every lane of the wave.
+// A row from its segments' sums, in every lane of the wave.
 __device__ __forceinline__ VerifyRow join_row(const VerifyParams& p, uint32_t b, uint32_t r) {
-  const VerifyPart* const parts = p.parts + ((uint64_t)b * p.rows + r) * p.tiles;
+  const VerifyPart* const parts = p.parts + ((uint64_t)b * p.rows + r) * p.segments;
   const int lane = threadIdx.x & 63;
   float top = -INFINITY;
-  for (uint32_t i = lane; i < p.tiles; i += 64) top = __builtin_fmaxf(top, parts[i].top);
-#pragma unroll
-  for (int x = 1; x < 64; x *= 2) top = __builtin_fmaxf(top, __shfl_xor(top, x));
+#pragma unroll 4
+  for (uint32_t i = lane; i < p.segments; i += 64) top = __builtin_fmaxf(top, parts[i].top);
+  top = wave_max(top);
   VerifyRow d = {r <= p.drafts ? p.by : p.draft_by, 0.0, top};
   double sum = 0.0;
   if (top > -INFINITY)
-    for (uint32_t i = lane; i < p.tiles; i += 64) {
+#pragma unroll 4
+    for (uint32_t i = lane; i < p.segments; i += 64) {
       const VerifyPart q = parts[i];
       sum += q.sum * (q.top == top ? 1.0 : exp2_64(((double)q.top - (double)top) * d.by));
     }
@@ -189,247 +239,251 @@ __device__ __forceinline__ double rest_of(const VerifyParams& v, const VerifyDec
   return p > q ? p - q : 0.0;
 }
 
-template <typename T, int TILE>
-__global__ __launch_bounds__(256) void verify_decide_kernel(VerifyParams p, uint64_t first) {
+// One block a sequence: its rows joined, a wave each, then its drafts looked at, a thread
+// each, and what is known written.
+template <typename T>
+__global__ __launch_bounds__(512) void verify_decide_kernel(VerifyParams p, uint32_t first) {
   constexpr uint32_t kMost = kVerifyMaxDrafts;
   __shared__ VerifyRow s_row[2 * kMost + 1];
   __shared__ uint32_t s_taken;
-  __shared__ double s_sum[4];
-  const uint64_t block = first + blockIdx.x;
-  const uint32_t b = (uint32_t)(block / p.tiles), tile = (uint32_t)(block % p.tiles);
+  const uint32_t b = first + blockIdx.x;
   const uint32_t length = length_of(p, b);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   if (threadIdx.x == 0) s_taken = length;
-  for (uint32_t r = wave; r <= length; r += 4) {
-    const VerifyRow d = join_row(p, b, r);
-    if (lane == 0) s_row[r] = d;
-  }
-  if (p.draft)
-    for (uint32_t r = wave; r < length; r += 4) {
-      const VerifyRow d = join_row(p, b, p.drafts + 1 + r);
-      if (lane == 0) s_row[kMost + 1 + r] = d;
-    }
-  __syncthreads();
-  for (uint32_t k = threadIdx.x; k < length; k += 256) {
-    const int64_t x = p.tokens[(uint64_t)b * p.drafts + k];
-    bool taken = false;
+  // the drafts' logits are on their way meanwhile
+  const uint32_t k = threadIdx.x;
+  int64_t x = -1;
+  float z = -INFINITY, zd = -INFINITY, u = 0.0f;
+  if (k < length) {
+    x = p.tokens[(uint64_t)b * p.drafts + k];
+    u = p.uniform[(uint64_t)b * (p.drafts + 1) + k];
     if (x >= 0 && x < (int64_t)p.vocab) {
-      const double at = probability(s_row[k], logit_of(((const T*)row_at(p, b, k, sizeof(T)))[x]));
-      const double of = p.draft ? probability(s_row[kMost + 1 + k],
-                                              logit_of(((const T*)row_at(p, b, p.drafts + 1 + k, sizeof(T)))[x]))
-                                : 1.0;
-      taken = (double)p.uniform[(uint64_t)b * (p.drafts + 1) + k] * of < at;
+      z = logit_of(((const T*)row_at(p, b, k, sizeof(T)))[x]);
+      if (p.draft) zd = logit_of(((const T*)row_at(p, b, p.drafts + 1 + k, sizeof(T)))[x]);
     }
-    if (!taken) atomicMin(&s_taken, k);
+  }
+  const uint32_t rows = p.draft ? 2 * length + 1 : length + 1;
+  for (uint32_t i = wave; i < rows; i += 8) {
+    const VerifyRow d = join_row(p, b, i <= length ? i : p.drafts + i - length);
+    if (lane == 0) s_row[i] = d;
+  }
+  __syncthreads();
+  if (k < length) {
+    const double at = probability(s_row[k], z), of = p.draft ? probability(s_row[length + 1 + k], zd) : 1.0;
+    if (!(x >= 0 && x < (int64_t)p.vocab && (double)u * of < at)) atomicMin(&s_taken, k);
   }
   __syncthreads();
   const uint32_t taken = s_taken;
-  const VerifyDecision d = {s_row[taken], taken < length && p.draft ? s_row[kMost + 1 + taken] : VerifyRow{}, taken, length};
-  if (tile == 0) {
-    if (threadIdx.x == 0) {
-      p.count[b] = (int32_t)taken;
-      p.decisions[b] = d;
-    }
-    // the tokens that are taken, and what follows the one that will be drawn
-    for (uint32_t k = threadIdx.x; k <= p.drafts; k += 256) {
-      if (k == taken) continue;
-      int64_t x = -1;
-      float logp = 0.0f;
-      if (k < taken) {
-        x = p.tokens[(uint64_t)b * p.drafts + k];
-        const float z = logit_of(((const T*)row_at(p, b, k, sizeof(T)))[x]);
-        logp = (float)(((double)z - (double)s_row[k].top) * p.scale + log(s_row[k].inv));
-      }
-      p.out[(uint64_t)b * (p.drafts + 1) + k] = x;
-      p.logprob[(uint64_t)b * (p.drafts + 1) + k] = logp;
-    }
+  if (threadIdx.x == 0) {
+    p.count[b] = (int32_t)taken;
+    VerifyRow q = {};
+    if (taken < length && p.draft) q = s_row[length + 1 + taken];
+    p.decisions[b] = {s_row[taken], q, taken, length};
   }
-  if (taken == length) return;  // drawn from p, whose tiles' sums are there
-  const T* const row = (const T*)row_at(p, b, taken, sizeof(T));
-  const T* const draft_row = p.draft ? (const T*)row_at(p, b, p.drafts + 1 + taken, sizeof(T)) : nullptr;
-  const int64_t draft = p.tokens[(uint64_t)b * p.drafts + taken];
-  const uint32_t c0 = tile * TILE + threadIdx.x * 8;
-  float z[TILE / 2048][8], zd[TILE / 2048][8];
-#pragma unroll
-  for (int j = 0; j < TILE / 2048; ++j) {
-    load_logits(row, c0 + j * 2048, p.vocab, z[j]);
-    if (draft_row) load_logits(draft_row, c0 + j * 2048, p.vocab, zd[j]);
+  // the tokens that are taken, and what follows the one that will be drawn
+  if (k <= p.drafts && k != taken) {
+    const uint64_t at = (uint64_t)b * (p.drafts + 1) + k;
+    p.out[at] = k < taken ? x : -1;
+    p.logprob[at] =
+        k < taken ? (float)(((double)z - (double)s_row[k].top) * p.scale + log(s_row[k].inv)) : 0.0f;
   }
-  double sum = 0.0;
-#pragma unroll
-  for (int j = 0; j < TILE / 2048; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) sum += rest_of(p, d, draft, z[j][e], zd[j][e], c0 + j * 2048 + e);
-  sum = wave_sum64(sum);
-  if (lane == 0) s_sum[wave] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) p.rests[block] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
 }
 
-// One block a sequence, 8 entries of the tile a thread.
-template <typename T, int TILE>
-__global__ __launch_bounds__(TILE / 8) void verify_draw_kernel(VerifyParams p, uint32_t first) {
-  __shared__ double s_wave[16];
-  __shared__ double s_from, s_left;
-  __shared__ uint32_t s_tile, s_first, s_last;
-  __shared__ float s_z;
-  const uint32_t b = first + blockIdx.x;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+// The rests of refused sequences, by 512 entries, a wave each.
+template <typename T>
+__global__ __launch_bounds__(256) void verify_rests_kernel(VerifyParams p, uint32_t first) {
+  const uint32_t blocks = (p.rest_count + 3) / 4, b = first + blockIdx.x / blocks;
+  const uint32_t at = blockIdx.x % blocks * 4 + (threadIdx.x >> 6), c = entry_at<512>(at, 0);
   const VerifyDecision d = p.decisions[b];
-  const VerifyPart* const parts = p.parts + ((uint64_t)b * p.rows + d.taken) * p.tiles;
-  const double* const rests = p.rests + (uint64_t)b * p.tiles;
+  if (at >= p.rest_count || d.taken == d.length) return;
+  const int64_t draft = p.tokens[(uint64_t)b * p.drafts + d.taken];
+  float z[8], zd[8];
+  load_logits((const T*)row_at(p, b, d.taken, sizeof(T)), c, p.vocab, z);
+  if (p.draft) load_logits((const T*)row_at(p, b, p.drafts + 1 + d.taken, sizeof(T)), c, p.vocab, zd);
+  double sum = 0.0;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum += rest_of(p, d, draft, z[e], zd[e], c + e);
+  sum = wave_sum64(sum);
+  if ((threadIdx.x & 63) == 0) p.rests[(uint64_t)b * p.rest_count + at] = sum;
+}
+
+// One wave a sequence.  ALONE: there are no drafts, so nothing was decided before, and
+// the row's sums are joined here.
+template <typename T, int SEG, bool ALONE>
+__global__ __launch_bounds__(64) void verify_draw_kernel(VerifyParams p, uint32_t first) {
+  constexpr uint32_t kKept = 5;  // of 64 sums each, in registers
+  const uint32_t b = first + blockIdx.x;
+  const int lane = threadIdx.x;
   const double u = (double)p.uniform[(uint64_t)b * (p.drafts + 1) + p.drafts];
-  if (threadIdx.x == 0) {
-    s_first = ~0u;
-    s_last = 0;
-    s_tile = ~0u;
-  }
-  __syncthreads();
+  VerifyDecision d;
+  if constexpr (ALONE) d = {join_row(p, b, 0), {}, 0, 0};
+  else d = p.decisions[b];
+  const VerifyPart* const parts = p.parts + ((uint64_t)b * p.rows + d.taken) * p.segments;
+  const double* const rests = p.rests + (uint64_t)b * p.rest_count;
   // what is drawn from: the rests, or p (where nothing was refused, and where by the
   // roundings nothing is left)
-  bool rest = d.taken < d.length;
-  if (wave == 0) {
-    auto mass = [&](uint32_t i) {
-      if (i >= p.tiles) return 0.0;
-      if (rest) return rests[i];
-      if (d.p.inv == 0.0) return 0.0;
-      const VerifyPart q = parts[i];
-      return q.sum * (q.top == d.p.top ? 1.0 : exp2_64(((double)q.top - (double)d.p.top) * d.p.by)) * d.p.inv;
-    };
-    auto total_of = [&] {
-      double total = 0.0;
-      for (uint32_t i = 0; i < p.tiles; i += 64) total += wave_sum64(mass(i + lane));
-      return total;
-    };
-    double total = total_of();
-    if (rest && !(total > 0.0)) {
-      rest = false;
-      total = total_of();
-    }
-    // the first tile whose cumulated sum exceeds u total; else the last that has any
-    const double goal = u * total;
-    double before = 0.0;
-    bool found = false;
-    for (uint32_t i = 0; i < p.tiles && !found; i += 64) {
-      const double m = mass(i + lane), upto = before + wave_scan64(m);
-      const uint64_t over = __builtin_amdgcn_ballot_w64(m > 0.0 && upto > goal);
-      const uint64_t any = __builtin_amdgcn_ballot_w64(m > 0.0);
-      found = over != 0;
-      const int at = over ? __builtin_ctzll(over) : any ? 63 - __builtin_clzll(any) : -1;
-      if (lane == at) {
-        s_tile = i + lane;
-        s_from = upto - m;
-      }
-      before = before + wave_sum64(m);
-    }
-    if (lane == 0) {
-      s_left = rest ? 1.0 : 0.0;
-      s_wave[0] = goal;
-    }
+  bool rest = !ALONE && d.taken < d.length;
+  uint32_t count = rest ? p.rest_count : p.segments;
+  double kept[kKept];
+  auto mass = [&](uint32_t i) {
+    if (i >= count) return 0.0;
+    if (rest) return rests[i];
+    if (d.p.inv == 0.0) return 0.0;
+    const VerifyPart q = parts[i];
+    return q.sum * (q.top == d.p.top ? 1.0 : exp2_64(((double)q.top - (double)d.p.top) * d.p.by)) * d.p.inv;
+  };
+  auto total_of = [&] {
+    double mine = 0.0;
+#pragma unroll
+    for (uint32_t c = 0; c < kKept; ++c) mine += kept[c] = mass(c * 64 + lane);
+    for (uint32_t i = kKept * 64; i < count; i += 64) mine += mass(i + lane);
+    return wave_sum64(mine);
+  };
+  double total = total_of();
+  if (rest && !(total > 0.0)) {
+    rest = false;
+    count = p.segments;
+    total = total_of();
   }
-  __syncthreads();
-  const uint32_t tile = s_tile;
+  // the first whose cumulated sum exceeds u total; else the last that has any
+  const double goal = u * total;
+  double before = 0.0, from = 0.0;
+  int64_t where = -1;
+  bool found = false;
+  auto look = [&](uint32_t i, double m) {
+    const double upto = before + wave_scan64(m);
+    const uint64_t over = __builtin_amdgcn_ballot_w64(m > 0.0 && upto > goal);
+    const uint64_t any = __builtin_amdgcn_ballot_w64(m > 0.0);
+    found = over != 0;
+    if (any) {
+      const int at = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any);
+      where = i + at;
+      from = lane_value(upto - m, at);
+    }
+    before = lane_value(upto, 63);
+  };
+#pragma unroll
+  for (uint32_t c = 0; c < kKept; ++c)
+    if (!found && c * 64 < count) look(c * 64, kept[c]);
+  for (uint32_t i = kKept * 64; i < count && !found; i += 64) look(i, mass(i + lane));
   const uint64_t at = (uint64_t)b * (p.drafts + 1) + d.taken;
-  if (tile == ~0u) {  // an empty row: the whole block
-    if (threadIdx.x == 0) {
+  if (ALONE && lane == 0) p.count[b] = 0;
+  if (where < 0) {  // an empty row
+    if (lane == 0) {
       p.out[at] = -1;
       p.logprob[at] = -INFINITY;
     }
     return;
   }
-  rest = s_left != 0.0;
-  const double goal = s_wave[0] - s_from;
-  __syncthreads();
   const T* const row = (const T*)row_at(p, b, d.taken, sizeof(T));
-  const uint32_t c0 = tile * TILE + threadIdx.x * 8;
-  float z[8], zd[8];
-  load_logits(row, c0, p.vocab, z);
-  if (rest && p.draft) load_logits((const T*)row_at(p, b, p.drafts + 1 + d.taken, sizeof(T)), c0, p.vocab, zd);
+  const T* const draft_row =
+      rest && p.draft ? (const T*)row_at(p, b, p.drafts + 1 + d.taken, sizeof(T)) : nullptr;
   const int64_t draft = rest ? p.tokens[(uint64_t)b * p.drafts + d.taken] : -1;
-  double m[8], mine = 0.0;
+  // the entry, 512 at a time; where the roundings leave the sum below the goal, the last
+  // that has any
+  const uint32_t begin = rest ? (uint32_t)where * 512 : (uint32_t)where * SEG;
+  const int steps = rest ? 1 : SEG / 512;
+  uint32_t entry = begin;
+  float logit = 0.0f;
+  before = from;
+  found = false;
+  for (int j = 0; j < steps && !found; ++j) {
+    const uint32_t c = begin + j * 512 + lane * 8;
+    float z[8], zd[8];
+    load_logits(row, c, p.vocab, z);
+    if (draft_row) load_logits(draft_row, c, p.vocab, zd);
+    double m[8], mine = 0.0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    m[e] = rest ? rest_of(p, d, draft, z[e], zd[e], c0 + e) : probability(d.p, z[e]);
-    mine += m[e];
-  }
-  const double upto = wave_scan64(mine);
-  if (lane == 63) s_wave[wave] = upto;
-  __syncthreads();
-  double sum = upto - mine;
-  for (int w = 0; w < wave; ++w) sum += s_wave[w];
-  uint32_t hit = ~0u, last = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    sum += m[e];
-    if (m[e] > 0.0) {
-      if (hit == ~0u && sum > goal) hit = threadIdx.x * 8 + e;
-      last = threadIdx.x * 8 + e + 1;
+    for (int e = 0; e < 8; ++e) {
+      m[e] = rest ? rest_of(p, d, draft, z[e], zd[e], c + e) : probability(d.p, z[e]);
+      mine += m[e];
     }
-  }
-  if (hit != ~0u) atomicMin(&s_first, hit);
-  if (last) atomicMax(&s_last, last);
-  __syncthreads();
-  // where the roundings leave the tile's sum below the goal: its last entry that has any
-  const uint32_t v = s_first != ~0u ? s_first : s_last ? s_last - 1 : 0;
-  if (v / 8 == threadIdx.x) {
+    const double upto = before + wave_scan64(mine);
+    double sum = upto - mine;
+    int hit = -1, last = -1;
+    float z_hit = 0.0f, z_last = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (v % 8 == (uint32_t)e) s_z = z[e];
+    for (int e = 0; e < 8; ++e) {
+      sum += m[e];
+      if (m[e] > 0.0) {
+        if (hit < 0 && sum > goal) {
+          hit = e;
+          z_hit = z[e];
+        }
+        last = e;
+        z_last = z[e];
+      }
+    }
+    const uint64_t over = __builtin_amdgcn_ballot_w64(hit >= 0), any = __builtin_amdgcn_ballot_w64(last >= 0);
+    found = over != 0;
+    if (any) {
+      const int l = over ? __builtin_ctzll(over) : 63 - __builtin_clzll(any);
+      entry = begin + j * 512 + l * 8 + __builtin_amdgcn_readlane(over ? hit : last, l);
+      logit = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(over ? z_hit : z_last), l));
+    }
+    before = lane_value(upto, 63);
   }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    p.out[at] = (int64_t)tile * TILE + v;
-    p.logprob[at] = (float)(((double)s_z - (double)d.p.top) * p.scale + log(d.p.inv));
+  if (lane == 0) {
+    p.out[at] = (int64_t)entry;
+    p.logprob[at] = (float)(((double)logit - (double)d.p.top) * p.scale + log(d.p.inv));
   }
 }
 
-constexpr uint32_t kTileL = 8192, kTileS = 2048;
-// the larger tile where that still gives every CU eight blocks
-constexpr uint64_t kEnoughTiles = 2048;
+constexpr uint32_t kSegL = 1024, kSegS = 512;
+// the longer segments where they still give every SIMD eight waves
+constexpr uint64_t kEnoughSegments = 8192;
 // A launch has fewer than 2^32 threads.
-constexpr uint64_t kBlocksAtOnce = 1u << 21;  // of up to 1,024
+constexpr uint32_t kUnitsAtOnce = 1u << 22;  // of up to 512
 
-uint32_t tiles_of(uint32_t vocab, uint32_t tile) { return (vocab - 1) / tile + 1; }
+uint32_t parts_of(uint32_t n, uint32_t of) { return (n - 1) / of + 1; }
 
 uint64_t up256(uint64_t v) { return (v + 255) & ~255ull; }
 
-template <typename T, int TILE>
-void run_verify(VerifyParams p, hipStream_t stream) {
-  const uint64_t sums = (uint64_t)p.batch * p.rows * p.tiles, decide = (uint64_t)p.batch * p.tiles;
-  auto in_parts = [&](uint64_t blocks, auto launch) {
-    for (uint64_t first = 0; first < blocks; first += kBlocksAtOnce)
-      launch(first, dim3((uint32_t)(blocks - first < kBlocksAtOnce ? blocks - first : kBlocksAtOnce)));
+template <typename T, int SEG>
+void run_verify(const VerifyParams& p, hipStream_t stream) {
+  // `count` rows, or sequences, of `each` units
+  auto in_parts = [&](uint64_t count, uint32_t each, auto launch) {
+    const uint32_t most = kUnitsAtOnce / each;
+    for (uint64_t first = 0; first < count; first += most)
+      launch((uint32_t)first, (uint32_t)(count - first < most ? count - first : most) * each);
   };
-  in_parts(sums, [&](uint64_t first, dim3 grid) {
-    hipLaunchKernelGGL((verify_sums_kernel<T, TILE>), grid, dim3(256), 0, stream, p, first);
+  in_parts((uint64_t)p.batch * p.rows, parts_of(p.segments, 4), [&](uint32_t first, uint32_t all) {
+    hipLaunchKernelGGL((verify_sums_kernel<T, SEG>), dim3(all), dim3(256), 0, stream, p, first);
   });
-  in_parts(decide, [&](uint64_t first, dim3 grid) {
-    hipLaunchKernelGGL((verify_decide_kernel<T, TILE>), grid, dim3(256), 0, stream, p, first);
-  });
-  in_parts(p.batch, [&](uint64_t first, dim3 grid) {
-    hipLaunchKernelGGL((verify_draw_kernel<T, TILE>), grid, dim3(TILE / 8), 0, stream, p, (uint32_t)first);
+  if (p.drafts) {
+    in_parts(p.batch, 1, [&](uint32_t first, uint32_t all) {
+      hipLaunchKernelGGL(verify_decide_kernel<T>, dim3(all), dim3(512), 0, stream, p, first);
+    });
+    in_parts(p.batch, parts_of(p.rest_count, 4), [&](uint32_t first, uint32_t all) {
+      hipLaunchKernelGGL(verify_rests_kernel<T>, dim3(all), dim3(256), 0, stream, p, first);
+    });
+  }
+  in_parts(p.batch, 1, [&](uint32_t first, uint32_t all) {
+    if (p.drafts) hipLaunchKernelGGL((verify_draw_kernel<T, SEG, false>), dim3(all), dim3(64), 0, stream, p, first);
+    else hipLaunchKernelGGL((verify_draw_kernel<T, SEG, true>), dim3(all), dim3(64), 0, stream, p, first);
   });
 }
 
 }  // namespace
 
 uint64_t verify_workspace(uint32_t batch, uint32_t drafts, uint32_t vocab) {
-  const uint64_t tiles = tiles_of(vocab, kTileS), rows = (uint64_t)batch * (2 * drafts + 1);
-  return up256(rows * tiles * sizeof(VerifyPart)) + up256(batch * tiles * sizeof(double)) +
+  const uint64_t segments = parts_of(vocab, kSegS), rows = (uint64_t)batch * (2 * drafts + 1);
+  return up256(rows * segments * sizeof(VerifyPart)) + up256(batch * segments * sizeof(double)) +
          up256(batch * sizeof(VerifyDecision));
 }
 
 hipError_t launch_verify(bool bf16, const VerifyParams& c, char* ws, hipStream_t stream) {
   VerifyParams p = c;
   p.rows = p.drafts + 1 + (p.draft ? p.drafts : 0);
-  const bool large = (uint64_t)p.batch * p.rows * tiles_of(p.vocab, kTileL) >= kEnoughTiles;
-  p.tiles = tiles_of(p.vocab, large ? kTileL : kTileS);
-  const uint64_t tiles = tiles_of(p.vocab, kTileS), rows = (uint64_t)p.batch * (2 * p.drafts + 1);
+  const bool large = (uint64_t)p.batch * p.rows * parts_of(p.vocab, kSegL) >= kEnoughSegments;
+  p.segments = parts_of(p.vocab, large ? kSegL : kSegS);
+  p.rest_count = parts_of(p.vocab, kSegS);
+  const uint64_t rows = (uint64_t)p.batch * (2 * p.drafts + 1);
   p.parts = (VerifyPart*)ws;
-  p.rests = (double*)(ws + up256(rows * tiles * sizeof(VerifyPart)));
-  p.decisions = (VerifyDecision*)((char*)p.rests + up256(p.batch * tiles * sizeof(double)));
-  if (bf16) large ? run_verify<uint16_t, kTileL>(p, stream) : run_verify<uint16_t, kTileS>(p, stream);
-  else large ? run_verify<float, kTileL>(p, stream) : run_verify<float, kTileS>(p, stream);
+  p.rests = (double*)(ws + up256(rows * p.rest_count * sizeof(VerifyPart)));
+  p.decisions = (VerifyDecision*)((char*)p.rests + up256((uint64_t)p.batch * p.rest_count * sizeof(double)));
+  if (bf16) large ? run_verify<uint16_t, kSegL>(p, stream) : run_verify<uint16_t, kSegS>(p, stream);
+  else large ? run_verify<float, kSegL>(p, stream) : run_verify<float, kSegS>(p, stream);
   return hipGetLastError();
 }
 
