@@ -275,7 +275,7 @@ int pulse_lowp_linear(int dtype, const uint8_t *codes, const uint8_t *scales, fl
 #define PULSE_LINEAR_MAX_WIDTH 1048576
 
 /* Up to so many tokens pulse_linear_forward needs no workspace (which may be NULL). */
-#define PULSE_LINEAR_FEW_TOKENS 32
+#define PULSE_LINEAR_FEW_TOKENS 16
 
 /* A workspace for calls of any number of tokens up to `tokens`, both directions; 0 for
  * sizes that no call handles. */

@@ -156,7 +156,7 @@ hipError_t launch_lowp_matmul(WeightForm form, bool epilogue, const LowpMatmulPa
 
 // ---------------------------------------------------------------- linear
 
-constexpr uint32_t kLinearFewTokens = 32;  // up to here the forward pass needs no workspace
+constexpr uint32_t kLinearFewTokens = 16;  // up to here the forward pass needs no workspace
 
 struct LinearParams {
   const uint16_t* x;
@@ -234,7 +234,7 @@ hipError_t launch_linear_ce_grad(const LinearCeGradParams& p, char* ws, hipStrea
 
 constexpr uint32_t kVerifyMaxDrafts = 128;
 
-struct VerifyPart {  // of a row's tile: the sum of exponentials below its largest logit
+struct VerifyPart {  // of a row's segment: the sum of exponentials below its largest logit
   double sum;
   float top;
 };
@@ -266,9 +266,11 @@ struct VerifyParams {
   int32_t* count;
   float* logprob;
   // set by the launcher
-  uint32_t rows, tiles;  // of a sequence; of a row
-  VerifyPart* parts;     // [batch][rows][tiles]
-  double* rests;         // [batch][tiles]: sums of max(p - q, 0)
+  uint32_t rows;        // of a sequence
+  uint32_t segments;    // of a row
+  uint32_t rest_count;  // 512 entries each
+  VerifyPart* parts;    // [batch][rows][segments]
+  double* rests;        // [batch][rest_count]: sums of max(p - q, 0)
   VerifyDecision* decisions;
 };
 

@@ -124,25 +124,25 @@ __device__ __forceinline__ void finish_eight(const ProductParams& p, float (&v)[
   store_eight(p.out, t * p.out_ld + row, e.out_bf16, p.wide, left, v);
 }
 
+// Block `id` of a product's tiles, and its split's share of k.
 template <typename T, bool AK, bool BK>
-__global__ __launch_bounds__(T::kThreads) void product_kernel(ProductParams p) {
+__device__ __forceinline__ void product_block(const ProductParams& p, char* lds, uint32_t id, uint32_t split) {
   // the tile's FP32 rows pass through LDS, as many fragments' columns at a time as fit
   constexpr int kFit = T::kLds / (T::BM * 4 * 16 * T::WN), kAtOnce = kFit < T::FN ? kFit : T::FN;
   static_assert(kFit >= 1 && T::FN % kAtOnce == 0, "whole fragments at a time");
-  __shared__ alignas(1024) char lds[T::kLds];
   uint32_t tm, tn;
-  gemm_tile_of(p.first_tile + blockIdx.x, p.tiles_m, p.tiles_n, 8, tm, tn);
+  gemm_tile_of(id, p.tiles_m, p.tiles_n, 8, tm, tn);
   const uint32_t m0 = tm * T::BM, n0 = tn * T::BN;
   const GemmOperand a = {p.a.p + (AK ? (uint64_t)m0 : m0 * p.a.ld), p.a.ld, p.a.limit - m0};
   const GemmOperand b = {p.b.p + (BK ? (uint64_t)n0 : n0 * p.b.ld), p.b.ld, p.b.limit - n0};
-  const uint32_t k0 = p.sums ? blockIdx.y * p.k_split : 0;
+  const uint32_t k0 = p.sums ? split * p.k_split : 0;
   // a split past the end has no k and gives zeros
   const uint32_t k1 = !p.sums ? p.k : k0 >= p.k ? k0 : p.k - k0 < p.k_split ? p.k : k0 + p.k_split;
   typename T::Acc acc;
   T::run(lds, a, b, k0, k1, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (p.sums) {
-    float* const sums = p.sums + (uint64_t)blockIdx.y * p.n * p.m_ld;
+    float* const sums = p.sums + (uint64_t)split * p.n * p.m_ld;
 #pragma unroll
     for (int j = 0; j < T::FN; ++j) {
       const uint32_t n = n0 + T::n_of(j, lane, wave);
@@ -183,6 +183,22 @@ __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductParams p) {
   }
 }
 
+template <typename T, bool AK, bool BK>
+__global__ __launch_bounds__(T::kThreads) void product_kernel(ProductParams p) {
+  __shared__ alignas(1024) char lds[T::kLds];
+  product_block<T, AK, BK>(p, lds, p.first_tile + blockIdx.x, blockIdx.y);
+}
+
+// dx's and dW's products in one launch: dx's blocks, whose sums are the longer ones, first.
+template <typename TX, typename TW>
+__global__ __launch_bounds__(TX::kThreads) void both_kernel(ProductParams x, ProductParams w) {
+  static_assert(TX::kThreads == TW::kThreads && TX::kLds == TW::kLds, "blocks of one shape");
+  __shared__ alignas(1024) char lds[TX::kLds];
+  const uint32_t first = x.tiles_m * x.tiles_n;
+  if (blockIdx.x < first) product_block<TX, true, false>(x, lds, blockIdx.x, 0);
+  else product_block<TW, true, true>(w, lds, blockIdx.x - first, 0);
+}
+
 // The splits' sums, added in order, and the epilogue: a thread an eight of a row.
 __global__ __launch_bounds__(256) void join_kernel(ProductParams p, uint32_t splits) {
   const uint32_t eights = (p.m + 7) / 8;
@@ -201,7 +217,35 @@ __global__ __launch_bounds__(256) void join_kernel(ProductParams p, uint32_t spl
   finish_eight(p, v, n, m);
 }
 
-// ---------------------------------------------------------------- the elementwise part of the gradient
+// ---------------------------------------------------------------- what goes before the products
+
+// Rows to be padded with zeros from `cols` to `ld`; rows 0: none.
+struct PadJob {
+  const uint16_t* from;
+  uint64_t from_ld, rows;
+  uint32_t cols, ld;
+  uint16_t* to;
+};
+
+__device__ __forceinline__ void pad_rows(const PadJob& j, uint32_t block, uint32_t blocks) {
+  const uint64_t groups = j.ld / 8, all = j.rows * groups;
+  for (uint64_t i = (uint64_t)block * blockDim.x + threadIdx.x; i < all; i += (uint64_t)blocks * blockDim.x) {
+    const uint64_t r = i / groups;
+    const uint32_t c = (uint32_t)(i % groups) * 8;
+    const uint16_t* const row = j.from + r * j.from_ld;
+    uint4 v;
+    if (c + 8 <= j.cols) {
+      v = load16_any(row + c);
+    } else {
+      uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e)
+        if (c + e < j.cols) w[e >> 1] |= (uint32_t)row[c + e] << (16 * (e & 1));
+      v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    store16(j.to + r * j.ld + c, v);
+  }
+}
 
 struct SlopeParams {
   const void* dy;
@@ -214,53 +258,91 @@ struct SlopeParams {
   uint64_t dtimes_stride;
   uint16_t* d;  // null: dy serves; rows of d_ld, zeros past the last feature
   uint32_t d_ld;
-  float* partial;  // null: no bias; [chunks][rows]
+  float* partial;  // null: no bias; [chunks][rows] (one chunk: dbias itself)
   uint32_t tokens, rows, chunk;
   int act, bf16;
   bool wide;
 };
 
-// A block takes 512 features (8 a lane) of `chunk` tokens, its waves the tokens in turn.
-__global__ __launch_bounds__(256) void slope_kernel(SlopeParams p) {
-  __shared__ float s_sum[3][512];
+// d, dtimes and sums of d: a block takes 64 W features, W a lane, of `chunk` tokens, its
+// waves the tokens in turn, two or four at a time.
+template <int W, int WAVES>
+__device__ __forceinline__ void slope_rows(const SlopeParams& p, uint32_t strip, uint32_t chunk) {
+  constexpr int kAtOnce = W == 8 ? 2 : 4;
+  __shared__ float s_sum[WAVES - 1][64 * W];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t row = blockIdx.x * 512 + lane * 8, left = row < p.rows ? p.rows - row : 0;
-  const uint32_t end = p.tokens - blockIdx.y * p.chunk < p.chunk ? p.tokens : (blockIdx.y + 1) * p.chunk;
-  float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-  if (left)
-    for (uint64_t t = blockIdx.y * p.chunk + wave; t < end; t += 4) {
-      float v[8], pre[8], times[8];
-      load_eight(p.dy, t * p.dy_stride + row, p.bf16, p.wide, left, v);
-      if (p.pre) load_eight(p.pre, t * p.pre_stride + row, p.bf16, p.wide, left, pre);
-      if (p.times) load_eight(p.times, t * p.times_stride + row, p.bf16, p.wide, left, times);
-      if (p.pre) {
-        float g[8];
+  const uint32_t row = (strip * 64 + lane) * W, left = row < p.rows ? p.rows - row : 0;
+  const uint32_t end = p.tokens - chunk * p.chunk < p.chunk ? p.tokens : (chunk + 1) * p.chunk;
+  auto load = [&](const void* from, uint64_t at, float(&v)[W]) {
+    if constexpr (W == 8) load_eight(from, at, p.bf16, p.wide, left, v);
+    else v[0] = left ? load_f32(from, at, p.bf16) : 0.0f;
+  };
+  float sum[W] = {};
+  if (row < p.d_ld)
+    for (uint64_t t0 = chunk * p.chunk + wave; t0 < end; t0 += WAVES * kAtOnce) {
+      float v[kAtOnce][W], pre[kAtOnce][W], times[kAtOnce][W];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float2 a = activate2(p.act, pre[i]);
-          g[i] = v[i] * a.x;
-          v[i] *= p.times ? a.y * times[i] : a.y;
-          // past the row's end, where a derivative is no number's
-          if ((uint32_t)i >= left) v[i] = 0.0f;
-        }
-        if (p.dtimes) store_eight(p.dtimes, t * p.dtimes_stride + row, p.bf16, p.wide, left, g);
+      for (int k = 0; k < kAtOnce; ++k) {
+        const uint64_t t = t0 + k * WAVES < end ? t0 + k * WAVES : t0;
+        load(p.dy, t * p.dy_stride + row, v[k]);
+        if (p.pre) load(p.pre, t * p.pre_stride + row, pre[k]);
+        if (p.times) load(p.times, t * p.times_stride + row, times[k]);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += v[i];
-      if (p.d) store16(p.d + t * p.d_ld + row, pack_eight(v));
+      for (int k = 0; k < kAtOnce; ++k) {
+        const uint64_t t = t0 + k * WAVES;
+        if (t >= end) break;
+        if (p.pre) {
+          float g[W];
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            const float2 a = activate2(p.act, pre[k][i]);
+            g[i] = v[k][i] * a.x;
+            v[k][i] *= p.times ? a.y * times[k][i] : a.y;
+            if ((uint32_t)i >= left) v[k][i] = 0.0f;
+          }
+          if (p.dtimes) {
+            const uint64_t at = t * p.dtimes_stride + row;
+            if constexpr (W == 8) {
+              store_eight(p.dtimes, at, p.bf16, p.wide, left, g);
+            } else if (left) {
+              if (p.bf16) ((uint16_t*)p.dtimes)[at] = (uint16_t)bf16x2_rne(__float_as_uint(g[0]), 0u);
+              else ((float*)p.dtimes)[at] = g[0];
+            }
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < W; ++i) sum[i] += v[k][i];
+        if (p.d) {
+          if constexpr (W == 8) store16(p.d + t * p.d_ld + row, pack_eight(v[k]));
+          else p.d[t * p.d_ld + row] = (uint16_t)bf16x2_rne(__float_as_uint(v[k][0]), 0u);
+        }
+      }
     }
   if (!p.partial) return;
   if (wave) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s_sum[wave - 1][i * 64 + lane] = sum[i];
+    for (int i = 0; i < W; ++i) s_sum[wave - 1][i * 64 + lane] = sum[i];
   }
   __syncthreads();
   if (wave) return;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float v = (sum[i] + s_sum[0][i * 64 + lane]) + (s_sum[1][i * 64 + lane] + s_sum[2][i * 64 + lane]);
-    if ((uint32_t)i < left) p.partial[(uint64_t)blockIdx.y * p.rows + row + i] = v;
+  for (int i = 0; i < W; ++i) {
+#pragma unroll
+    for (int w = 0; w < WAVES - 1; ++w) sum[i] += s_sum[w][i * 64 + lane];
+    if ((uint32_t)i < left) p.partial[(uint64_t)chunk * p.rows + row + i] = sum[i];
   }
+}
+
+// One launch for the copies and the gradient's elementwise part: `pad_w` and `pad_x`
+// blocks, then strips * chunks.
+template <int W, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void prepare_kernel(PadJob w, PadJob x, SlopeParams s, uint32_t pad_w,
+                                                             uint32_t pad_x, uint32_t strips) {
+  if (blockIdx.x < pad_w) return pad_rows(w, blockIdx.x, pad_w);
+  if (blockIdx.x < pad_w + pad_x) return pad_rows(x, blockIdx.x - pad_w, pad_x);
+  const uint32_t block = blockIdx.x - pad_w - pad_x;
+  slope_rows<W, WAVES>(s, block % strips, block / strips);
 }
 
 // dbias from the chunks' sums: 64 features a block, its 4 waves a slice of the chunks each.
@@ -278,28 +360,6 @@ __global__ __launch_bounds__(256) void dbias_kernel(const float* partial, uint32
   if (wave == 0 && row < rows) dbias[row] = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
 }
 
-// Rows of `cols` padded with zeros to `ld`.
-__global__ __launch_bounds__(256) void pad_kernel(const uint16_t* from, uint64_t from_ld, uint64_t rows, uint32_t cols,
-                                                  uint16_t* to, uint32_t ld) {
-  const uint64_t groups = ld / 8, all = rows * groups;
-  for (uint64_t i = (uint64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (uint64_t)gridDim.x * 256) {
-    const uint64_t r = i / groups;
-    const uint32_t c = (uint32_t)(i % groups) * 8;
-    const uint16_t* const row = from + r * from_ld;
-    uint4 v;
-    if (c + 8 <= cols) {
-      v = load16_any(row + c);
-    } else {
-      uint32_t w[4] = {0, 0, 0, 0};
-#pragma unroll
-      for (uint32_t e = 0; e < 8; ++e)
-        if (c + e < cols) w[e >> 1] |= (uint32_t)row[c + e] << (16 * (e & 1));
-      v = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    store16(to + r * ld + c, v);
-  }
-}
-
 // ---------------------------------------------------------------- shapes
 
 uint32_t up(uint32_t v, uint32_t to) { return (v + to - 1) / to * to; }
@@ -310,6 +370,7 @@ constexpr uint32_t kTilesAtOnce = 1u << 22;  // of up to 512 threads; a multiple
 constexpr uint64_t kSumBytes = 32ull << 20;  // the most that splits' sums take
 constexpr uint32_t kMinSplit = 256;          // of k
 constexpr uint32_t kFewTokens = kLinearFewTokens;
+constexpr uint32_t kOneChunk = 128;  // tokens up to which dbias is summed by one block a strip
 
 // Time of a product in thousands of cycles: rounds of blocks, each with a fixed part and
 // one per 64 of k, and, with splits, their sums' way and a launch.
@@ -348,6 +409,19 @@ Shape shape_of(uint32_t m, uint32_t n, uint32_t k) {
   return best;
 }
 
+template <typename T>
+void set_tiles(ProductParams& p) {
+  p.tiles_m = parts(p.m, T::BM);
+  p.tiles_n = parts(p.n, T::BN);
+}
+
+template <bool AK, bool BK>
+using TileL = Gemm<256, 256, 2, 4, 2, AK, BK>;
+template <bool AK, bool BK>
+using TileM = Gemm<256, 128, 4, 2, 3, AK, BK>;
+template <bool AK, bool BK>
+using TileS = Gemm<128, 64, 4, 1, 4, AK, BK>;
+
 template <bool AK, bool BK>
 void run_product(ProductParams p, float* sums, hipStream_t stream) {
   const Shape s = shape_of(p.m, p.n, p.k);
@@ -356,8 +430,7 @@ void run_product(ProductParams p, float* sums, hipStream_t stream) {
   p.k_split = up(parts(p.k, s.splits), kGemmK);
   auto launch = [&](auto tile) {
     typedef decltype(tile) T;
-    p.tiles_m = parts(p.m, T::BM);
-    p.tiles_n = parts(p.n, T::BN);
+    set_tiles<T>(p);
     const uint64_t tiles = (uint64_t)p.tiles_m * p.tiles_n;
     for (uint64_t first = 0; first < tiles; first += kTilesAtOnce) {
       p.first_tile = (uint32_t)first;
@@ -366,13 +439,29 @@ void run_product(ProductParams p, float* sums, hipStream_t stream) {
                          dim3(T::kThreads), 0, stream, p);
     }
   };
-  if (s.tile == 0) launch(Gemm<256, 256, 2, 4, 2, AK, BK>{});
-  else if (s.tile == 1) launch(Gemm<256, 128, 4, 2, 3, AK, BK>{});
-  else launch(Gemm<128, 64, 4, 1, 4, AK, BK>{});
+  if (s.tile == 0) launch(TileL<AK, BK>{});
+  else if (s.tile == 1) launch(TileM<AK, BK>{});
+  else launch(TileS<AK, BK>{});
   if (s.splits > 1) {
     const uint64_t threads = (uint64_t)p.n * parts(p.m, 8);
     hipLaunchKernelGGL(join_kernel, dim3(parts(threads, 256)), dim3(256), 0, stream, p, s.splits);
   }
+}
+
+// dx and dW: where the smallest tiles of both are fewer than CUs, and dx's sums short,
+// one launch instead of two or three (each costs 3 us on the host and as much on the GPU).
+void run_gradients(ProductParams x, ProductParams w, float* sums, hipStream_t stream) {
+  typedef TileS<true, false> TX;
+  typedef TileS<true, true> TW;
+  set_tiles<TX>(x);
+  set_tiles<TW>(w);
+  const uint64_t tiles = (uint64_t)x.tiles_m * x.tiles_n + (uint64_t)w.tiles_m * w.tiles_n;
+  if (tiles <= 256 && x.k <= 2048 && w.k <= 2048) {
+    hipLaunchKernelGGL((both_kernel<TX, TW>), dim3((uint32_t)tiles), dim3(TX::kThreads), 0, stream, x, w);
+    return;
+  }
+  run_product<true, false>(x, sums, stream);
+  run_product<true, true>(w, sums, stream);
 }
 
 struct Plan {
@@ -384,9 +473,9 @@ Plan plan_of(uint32_t tokens, uint32_t rows, uint32_t cols) {
   Plan q;
   q.ld = up(cols, 8);
   q.d_ld = up(rows, 8);
-  // chunks of tokens for some eight blocks a CU
+  // chunks of tokens for some eight blocks a CU; few tokens in one
   const uint32_t strips = parts(rows, 512), wanted = strips < 2048 ? 2048 / strips : 1;
-  q.chunk = up(parts(tokens, wanted), 16);
+  q.chunk = tokens <= kOneChunk ? tokens : up(parts(tokens, wanted), 16);
   q.chunks = parts(tokens, q.chunk);
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) {
@@ -410,15 +499,20 @@ Plan plan_of(uint32_t tokens, uint32_t rows, uint32_t cols) {
   return q;
 }
 
-// x as the products take it: rows of 16-byte groups, not too far apart.
-const uint16_t* tidy(const uint16_t* from, uint64_t& stride, uint64_t rows, uint32_t cols, uint16_t* to, uint32_t ld,
-                     hipStream_t stream) {
-  if (cols % 8 == 0 && stride % 8 == 0 && stride <= kMaxStride) return from;
-  uint64_t blocks = (rows * (ld / 8) + 255) / 256;
-  if (blocks > 8192) blocks = 8192;
-  hipLaunchKernelGGL(pad_kernel, dim3((uint32_t)blocks), dim3(256), 0, stream, from, stride, rows, cols, to, ld);
-  stride = ld;
-  return to;
+// A matrix as the products take it, rows of 16-byte groups and not too far apart: itself,
+// or a copy in `to`.
+struct Tidy {
+  const uint16_t* p;
+  uint64_t ld;
+  PadJob job;
+  uint32_t blocks;
+};
+
+Tidy tidy(const uint16_t* from, uint64_t stride, uint64_t rows, uint32_t cols, uint16_t* to, uint32_t ld,
+          uint32_t threads) {
+  if (cols % 8 == 0 && stride % 8 == 0 && stride <= kMaxStride) return {from, stride, {}, 0};
+  const uint64_t blocks = (rows * (ld / 8) + threads - 1) / threads;
+  return {to, ld, {from, stride, rows, cols, ld, to}, blocks < 8192 ? (uint32_t)blocks : 8192};
 }
 
 }  // namespace
@@ -452,12 +546,14 @@ hipError_t launch_linear(const LinearParams& c, char* ws, hipStream_t stream) {
     return launch_lowp_matmul(kWeightBf16, true, p, stream);
   }
   const Plan q = plan_of(c.tokens, c.rows, c.cols);
+  const Tidy w = tidy(c.weight, c.cols, c.rows, c.cols, (uint16_t*)(ws + q.w), q.ld, 256);
+  const Tidy x = tidy(c.x, c.x_stride, c.tokens, c.cols, (uint16_t*)(ws + q.x), q.ld, 256);
+  if (w.blocks + x.blocks)
+    hipLaunchKernelGGL((prepare_kernel<8, 4>), dim3(w.blocks + x.blocks), dim3(256), 0, stream, w.job, x.job,
+                       SlopeParams{}, w.blocks, x.blocks, 1u);
   ProductParams p = {};
-  uint64_t w_ld = c.cols, x_ld = c.x_stride;
-  const uint16_t* const w = tidy(c.weight, w_ld, c.rows, c.cols, (uint16_t*)(ws + q.w), q.ld, stream);
-  const uint16_t* const x = tidy(c.x, x_ld, c.tokens, c.cols, (uint16_t*)(ws + q.x), q.ld, stream);
-  p.a = {w, w_ld, c.rows};
-  p.b = {x, x_ld, c.tokens};
+  p.a = {w.p, w.ld, c.rows};
+  p.b = {x.p, x.ld, c.tokens};
   p.m = c.rows;
   p.n = c.tokens;
   p.k = q.ld;
@@ -473,9 +569,10 @@ hipError_t launch_linear(const LinearParams& c, char* ws, hipStream_t stream) {
 
 hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t stream) {
   const Plan q = plan_of(c.tokens, c.rows, c.cols);
-  uint64_t w_ld = c.cols, x_ld = c.x_stride;
-  const uint16_t* const w = tidy(c.weight, w_ld, c.rows, c.cols, (uint16_t*)(ws + q.w), q.ld, stream);
-  const uint16_t* const x = tidy(c.x, x_ld, c.tokens, c.cols, (uint16_t*)(ws + q.x), q.ld, stream);
+  const bool few = c.tokens <= kOneChunk;
+  const uint32_t threads = few ? 1024 : 256;
+  const Tidy w = tidy(c.weight, c.cols, c.rows, c.cols, (uint16_t*)(ws + q.w), q.ld, threads);
+  const Tidy x = tidy(c.x, c.x_stride, c.tokens, c.cols, (uint16_t*)(ws + q.x), q.ld, threads);
   // d, dtimes and dbias
   const bool serves = !c.act && !c.times && c.bf16 && c.rows % 8 == 0 && c.dy_stride % 8 == 0 && c.dy_stride <= kMaxStride;
   SlopeParams s = {};
@@ -489,7 +586,7 @@ hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t s
   s.dtimes_stride = c.dtimes_stride;
   s.d = serves ? nullptr : (uint16_t*)(ws + q.d);
   s.d_ld = q.d_ld;
-  s.partial = c.dbias ? (float*)(ws + q.partial) : nullptr;
+  s.partial = !c.dbias ? nullptr : q.chunks == 1 ? c.dbias : (float*)(ws + q.partial);
   s.tokens = c.tokens;
   s.rows = c.rows;
   s.chunk = q.chunk;
@@ -498,15 +595,22 @@ hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t s
   const uint64_t unit = c.bf16 ? 8 : 4;
   s.wide = c.dy_stride % unit == 0 && (!s.pre || c.pre_stride % unit == 0) &&
            (!c.times || (c.times_stride % unit == 0 && (!c.dtimes || c.dtimes_stride % unit == 0)));
-  if (s.d || s.partial)
-    hipLaunchKernelGGL(slope_kernel, dim3(parts(c.rows, 512), q.chunks), dim3(256), 0, stream, s);
-  if (c.dbias)
+  // few tokens: a feature a lane and 16 waves, for more blocks and fewer turns
+  const uint32_t strips = parts(c.rows, few ? 64 : 512);
+  const uint32_t blocks = w.blocks + x.blocks + (s.d || s.partial ? strips * q.chunks : 0);
+  if (blocks && few)
+    hipLaunchKernelGGL((prepare_kernel<1, 16>), dim3(blocks), dim3(1024), 0, stream, w.job, x.job, s, w.blocks, x.blocks,
+                       strips);
+  else if (blocks)
+    hipLaunchKernelGGL((prepare_kernel<8, 4>), dim3(blocks), dim3(256), 0, stream, w.job, x.job, s, w.blocks, x.blocks,
+                       strips);
+  if (c.dbias && q.chunks > 1)
     hipLaunchKernelGGL(dbias_kernel, dim3(parts(c.rows, 64)), dim3(256), 0, stream, s.partial, q.chunks, c.rows, c.dbias);
   const uint16_t* const d = serves ? (const uint16_t*)c.dy : s.d;
   const uint64_t d_ld = serves ? c.dy_stride : q.d_ld;
   ProductParams p = {};
   p.e.out_bf16 = 1;
-  p.a = {w, w_ld, q.ld};
+  p.a = {w.p, w.ld, q.ld};
   p.b = {d, d_ld, c.tokens};
   p.m = c.cols;
   p.n = c.tokens;
@@ -514,16 +618,15 @@ hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t s
   p.out = c.dx;
   p.out_ld = c.dx_stride;
   p.wide = c.dx_stride % 8 == 0;
-  run_product<true, false>(p, (float*)(ws + q.sums), stream);
-  p.a = {x, x_ld, q.ld};
-  p.b = {d, d_ld, q.d_ld};
-  p.m = c.cols;
-  p.n = c.rows;
-  p.k = c.tokens;
-  p.out = c.dweight;
-  p.out_ld = c.cols;
-  p.wide = c.cols % 8 == 0;
-  run_product<true, true>(p, (float*)(ws + q.sums), stream);
+  ProductParams g = p;
+  g.a = {x.p, x.ld, q.ld};
+  g.b = {d, d_ld, q.d_ld};
+  g.n = c.rows;
+  g.k = c.tokens;
+  g.out = c.dweight;
+  g.out_ld = c.cols;
+  g.wide = c.cols % 8 == 0;
+  run_gradients(p, g, (float*)(ws + q.sums), stream);
   return hipGetLastError();
 }
 

@@ -29,7 +29,7 @@ NORM_MAX_COLS = 16384
 CE_MAX_HIDDEN = 65536
 VERIFY_MAX_DRAFTS = 128
 LINEAR_MAX_WIDTH = 1 << 20  # of a weight's rows and columns, and tokens
-LINEAR_FEW_TOKENS = 32  # up to which Linear's forward pass needs no workspace
+LINEAR_FEW_TOKENS = 16  # up to which Linear's forward pass needs no workspace
 # PULSE_ACT_*
 ACTIVATIONS = {None: 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}
 MAX_SIZE = (1 << 31) - 1  # of a vocabulary, a weight's rows or columns, tokens
