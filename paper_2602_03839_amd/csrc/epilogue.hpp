@@ -98,22 +98,30 @@ __device__ __forceinline__ void store_four(void* p, uint64_t at, int bf16, uint3
   }
 }
 
-// The four features from `row` on of token t (`left` of them are there): what is stored
-// as y; `pre`, if it is kept, is stored here.
-__device__ __forceinline__ f32x4_t finish_four(const Epilogue& e, f32x4_t v, uint64_t t, uint64_t row, uint32_t left) {
-  // all loads first
-  f32x4_t bias = {0.0f, 0.0f, 0.0f, 0.0f}, times = {1.0f, 1.0f, 1.0f, 1.0f}, residual = bias;
-  if (e.bias) bias = load_four(e.bias, row, e.bias_bf16, left);
-  if (e.times) times = load_four(e.times, t * e.times_stride + row, e.out_bf16, left);
-  if (e.residual) residual = load_four(e.residual, t * e.residual_stride + row, e.out_bf16, left);
-  if (e.bias) v += bias;
+// The operands of the four features from `row` on of token t (`left` of them are there).
+struct FourOperands {
+  f32x4_t bias, times, residual;
+};
+
+__device__ __forceinline__ FourOperands load_operands(const Epilogue& e, uint64_t t, uint64_t row, uint32_t left) {
+  FourOperands o = {};
+  if (e.bias) o.bias = load_four(e.bias, row, e.bias_bf16, left);
+  if (e.times) o.times = load_four(e.times, t * e.times_stride + row, e.out_bf16, left);
+  if (e.residual) o.residual = load_four(e.residual, t * e.residual_stride + row, e.out_bf16, left);
+  return o;
+}
+
+// What is stored as y; `pre`, if it is kept, is stored here.
+__device__ __forceinline__ f32x4_t finish_four(const Epilogue& e, const FourOperands& o, f32x4_t v, uint64_t t,
+                                               uint64_t row, uint32_t left) {
+  if (e.bias) v += o.bias;
   if (e.pre) store_four(e.pre, t * e.pre_stride + row, e.out_bf16, left, v);
   if (e.act) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = activate(e.act, v[i]);
   }
-  if (e.times) v *= times;
-  if (e.residual) v += residual;
+  if (e.times) v *= o.times;
+  if (e.residual) v += o.residual;
   return v;
 }
 

@@ -167,6 +167,28 @@ __device__ __forceinline__ void multiply_chunk(const Held<FORM, RT, NT>& h, f32x
   }
 }
 
+// The epilogue's part of the kernel's first argument, read where it is used: kept in
+// registers throughout it would push the scalars of the loops out of theirs (FP8 27,648 x
+// 5,120, one token and a bias: .. us, .. with).
+__device__ __forceinline__ Epilogue epilogue_here() {
+  typedef const __attribute__((address_space(4))) uint64_t* args_t;
+  args_t args = (args_t)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(LowpMatmulParams, e) / 8;
+  asm volatile("" : "+s"(args));
+  struct {
+    uint64_t v[sizeof(Epilogue) / 8];
+  } words;
+#pragma unroll
+  for (size_t i = 0; i < sizeof(Epilogue) / 8; ++i) words.v[i] = args[i];
+  Epilogue e = __builtin_bit_cast(Epilogue, words);
+  // global memory: loads that could be LDS's too would be waited for with LDS's
+  auto global = [](const void* v) { return (void*)(__attribute__((address_space(1))) void*)(uintptr_t)v; };
+  e.bias = global(e.bias);
+  e.times = global(e.times);
+  e.residual = global(e.residual);
+  e.pre = global(e.pre);
+  return e;
+}
+
 // grid.x: groups of RT row tiles from `first` on; grid.y: groups of NT token tiles.  The
 // block's waves share the chunks of one group and add their sums at the end.
 template <int FORM, int RT, int NT, bool SHIFT, bool EPILOGUE>
@@ -247,7 +269,7 @@ __global__ __launch_bounds__(1024) void lowp_matmul_kernel(LowpMatmulParams p, u
         const uint64_t row = row_of(r, 4 * g + i);
         if (row >= p.rows) continue;
         float v = FORM == kWeightFp8 ? acc[r][n][i] / p.inv_scale : acc[r][n][i];
-        if constexpr (EPILOGUE) v = finish_one(p.e, v, t, row);
+        if constexpr (EPILOGUE) v = finish_one(epilogue_here(), v, t, row);
         if (p.y_bf16) ((uint16_t*)p.y)[t * p.y_stride + row] = (uint16_t)bf16x2_rne(__float_as_uint(v), 0u);
         else ((float*)p.y)[t * p.y_stride + row] = v;
       }
@@ -263,7 +285,13 @@ __device__ __forceinline__ void store_result(const LowpMatmulParams& p, f32x4_t 
     for (int i = 0; i < 4; ++i) v[i] /= p.inv_scale;
   }
   const uint32_t left = p.rows - row < 4 ? (uint32_t)(p.rows - row) : 4;
-  if constexpr (EPILOGUE) v = finish_four(p.e, v, t, row, left);
+  if constexpr (EPILOGUE) {
+    const Epilogue e = epilogue_here();
+    v = finish_four(e, load_operands(e, t, row, left), v, t, row, left);
+    // vmcnt(0): without it the compiler, for whom an operand may be loaded and not used,
+    // waits in the products' loop, at every slab and for the slabs too
+    __builtin_amdgcn_s_waitcnt(0x0F70);
+  }
   store_four(p.y, t * p.y_stride + row, p.y_bf16, left, v);
 }
 
@@ -287,6 +315,7 @@ struct SlabShape {
   uint32_t tiles, slabs;   // of 16 rows; of a row
   uint32_t wk, wr, depth;  // waves side by side in k, in rows; slabs ahead
   uint32_t run;            // groups of wr tiles that a block takes in a row
+  bool apart;              // a further wave adds the parts and finishes the tiles
 };
 
 // TIGHT: places are computed where they are used, since no registers are left to keep them in.
@@ -355,6 +384,11 @@ struct SlabStream {
   }
 };
 
+// With an epilogue the parts are added by a wave of their own, if there is room for one
+// and tiles are one at a time: its loads would have the wave that makes them wait for
+// its slabs too, and the others wait for it.  FP8 27,648 x 5,120, 16 tokens, silu and
+// multiplier: .. us, .. with the waves taking turns (.. without an epilogue).
+//
 // NS > 0: each wave has up to NS slabs of k for good (slabs <= NS wk) and the tokens'
 // values of them in registers; otherwise all tokens' values lie in LDS.  A block
 // takes NT tiles of 16 tokens.
@@ -377,6 +411,7 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
   // row to other banks
   const uint32_t ld = z.slabs * kSlabUnits * U::kValues * 2 + 16;
 
+  const bool apart = EPILOGUE && z.apart, finisher = apart && wave == waves;
   uint4 x[NT][XREG ? 4 * NS : 1][U::kFrags];
   uint32_t t[NT];  // the lane's token of each tile, or some other: its sums are dropped
 #pragma unroll
@@ -388,13 +423,13 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
         const uint32_t u = (kw + s / 4 * z.wk) * kSlabUnits + g * 4 + s % 4;
 #pragma unroll
         for (uint32_t f = 0; f < U::kFrags; ++f)
-          x[n][s][f] = u < units ? load16_any(p.x + (t0 + t[n]) * p.x_stride + (uint64_t)u * U::kValues + 8 * f)
+          x[n][s][f] = u < units && !finisher ? load16_any(p.x + (t0 + t[n]) * p.x_stride + (uint64_t)u * U::kValues + 8 * f)
                                  : make_uint4(0, 0, 0, 0);
       }
     }
   }
   SlabStream<FORM, (NT > 1)> in = {p, z, s_lds + wave * z.depth * kSlabBytes, units, kw, rw, lane, blockIdx.x * z.run, kw};
-  for (uint32_t i = 0; i < z.depth && in.more(); ++i) in.load();
+  for (uint32_t i = 0; i < z.depth && in.more() && !finisher; ++i) in.load();
   if constexpr (!XREG) {
     const uint32_t pieces = (ld - 16) / 16, filled = p.cols / 8;  // of 16 bytes, in a row
     for (uint32_t i = threadIdx.x; i < tokens * pieces; i += blockDim.x) {
@@ -405,6 +440,39 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
     __syncthreads();
   }
 
+  if constexpr (EPILOGUE) {
+    if (finisher) {
+      const Epilogue e = epilogue_here();
+      uint32_t turn = 0;
+      for (uint32_t tile = blockIdx.x * z.run; tile < z.tiles; tile = in.after(tile), ++turn) {
+        const uint64_t row = (uint64_t)tile * 16 + 4 * g;
+        const uint32_t left = row >= p.rows ? 0 : p.rows - row < 4 ? (uint32_t)(p.rows - row) : 4;
+        FourOperands o[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) o[n] = load_operands(e, t0 + t[n], row, left);
+        __syncthreads();
+        const f32x4_t* const part = s_part + (turn & 1) * waves * NT * 64;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          f32x4_t v = part[n * 64 + lane];
+#pragma unroll kAdds
+          for (uint32_t w = 1; w < z.wk; ++w) v += part[(w * NT + n) * 64 + lane];
+          if constexpr (FORM == kWeightFp8) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] /= p.inv_scale;
+          }
+          const uint32_t token = t0 + n * 16 + r16, stored = token < p.tokens ? left : 0;
+          v = finish_four(e, o[n], v, token, row, stored);
+          store_four(p.y, (uint64_t)token * p.y_stride + row, p.y_bf16, stored, v);
+        }
+      }
+      return;
+    }
+  }
+
+  // vmcnt(0): the tokens are there.  Else the compiler waits for them at every slab, and so
+  // for the slabs that are on their way
+  if constexpr (XREG && EPILOGUE) __builtin_amdgcn_s_waitcnt(0x0F70);
   uint32_t slot = 0, turn = 0;
   for (uint32_t group = blockIdx.x * z.run; group * z.wr < z.tiles; group = in.after(group), ++turn) {
     f32x4_t acc[NT];
@@ -463,6 +531,7 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
 #pragma unroll
       for (int n = 0; n < NT; ++n) part[(wave * NT + n) * 64 + lane] = acc[n];
       __syncthreads();
+      if (apart) continue;
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
         if ((turn * NT + n) % z.wk != kw) continue;
@@ -563,7 +632,8 @@ bool launch_slabs(const LowpMatmulParams& p, bool epilogue, hipStream_t stream) 
   z.depth = (uint32_t)((kLpLds - rest) / (waves * kSlabBytes));
   if (z.depth > 4) z.depth = 4;
   z.run = groups >= 16 * kLpCus ? 2 : 1;
-  const dim3 grid(groups < kLpCus ? groups : kLpCus, (p.tokens + 16 * nt - 1) / (16 * nt)), block(64 * waves);
+  z.apart = (epilogue || FORM == kWeightBf16) && z.wr == 1 && z.wk > 1 && waves < 12;
+  const dim3 grid(groups < kLpCus ? groups : kLpCus, (p.tokens + 16 * nt - 1) / (16 * nt)), block(64 * (waves + z.apart));
   const size_t lds = (size_t)(rest + (uint64_t)z.depth * waves * kSlabBytes);
   by_epilogue<FORM>(epilogue, [&](auto e) {
     constexpr bool E = decltype(e)::value;
