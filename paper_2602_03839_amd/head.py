@@ -139,6 +139,15 @@ def _out(t, name, cols, rows, dtype, device, stream):
     return (t, *_matrix(t, name, cols, rows, dtype, device))
 
 
+def _like(t, like, stride, name, stream):
+    """A matrix of `like`'s shape and type to write, as _out; `stride`: of its rows."""
+    rows, cols = like.shape
+    if t is None and stream is None and stride == cols:
+        t = torch.empty_like(like)  # the cheapest of allocations
+        return t, t.data_ptr(), cols
+    return _out(t, name, cols, rows, like.dtype, like.device, stream)
+
+
 def _vec(t, name, n, device, stream):
     """A float32 vector to write: the caller's, checked, or a new one; with its pointer."""
     if t is None:
@@ -267,8 +276,11 @@ class BlockNorm:
         pb, sb = _matrix(b, "b", cols, device=dev)
         rows = b.shape[0]
         ph, sh = _matrix(h, "h", cols, rows, b.dtype, dev)
-        y, py, sy = _out(y, "y", cols, rows, b.dtype, dev, stream)
-        h_out, po, so = _out(h_out, "h_out", cols, rows, b.dtype, dev, stream)
+        y, py, sy = _like(y, b, sb, "y", stream)
+        if h_out is h:
+            po, so = ph, sh
+        else:
+            h_out, po, so = _like(h_out, b, sb, "h_out", stream)
         if not keep_stats:
             stats, ps, ss = None, None, 0
         else:
@@ -299,17 +311,18 @@ class BlockNorm:
         else:
             pb, sb = _matrix(b, "b", cols, rows, typ, dev)
         ps, ss = _matrix(stats, "stats", rows, self._nstats, torch.float32, dev)
-        db, pdb, sdb = _out(db, "db", cols, rows, typ, dev, stream)
-        dh, pdh, sdh = _out(dh, "dh", cols, rows, typ, dev, stream)
+        db, pdb, sdb = _like(db, h_out, so, "db", stream)
+        dh, pdh, sdh = _like(dh, h_out, so, "dh", stream)
         if self.ws is None:
             self.ws = _new((self._nws,), torch.uint8, dev, stream)
         pw, pwb, pp, ppb, pg = self._params
         # one allocation for all parameters' gradients: a call of few rows is bound by the host
         there = [k for k, p in enumerate(self._params) if p is not None]
         sums, to = _new((len(there), cols), torch.float32, dev, stream), [None] * 5
-        out = [None] * 5
+        out, at = [None] * 5, sums.data_ptr()
         for k, g in zip(there, sums.unbind()):
-            out[k], to[k] = g, g.data_ptr()
+            out[k], to[k] = g, at
+            at += 4 * cols
         with _on(dev):
             rc = self._lib.pulse_block_norm_backward(dt, py, sy, pd, sd, pb, sb, po, so, self.residual_scale,
                                                      self._dt, pw, pp, ppb, pg, ps, ss, pdb, sdb, pdh, sdh, *to,
@@ -451,13 +464,19 @@ class VerifyDrafts:
         pl = _p(lengths, "lengths", dtype=torch.int32, numel=n, device=dev)
         if tokens is None:
             tokens = _new((n, k + 1), torch.int64, dev, stream)
+            po = tokens.data_ptr()
+        else:
+            po = _p(tokens, "tokens", dtype=torch.int64, numel=n * (k + 1), device=dev)
         if count is None:
             count = _new((n,), torch.int32, dev, stream)
+            pc = count.data_ptr()
+        else:
+            pc = _p(count, "count", dtype=torch.int32, numel=n, device=dev)
         if logprob is None:
-            logprob = _new((n, k + 1), torch.float32, dev, stream)
-        po = _p(tokens, "tokens", dtype=torch.int64, numel=n * (k + 1), device=dev)
-        pc = _p(count, "count", dtype=torch.int32, numel=n, device=dev)
-        pp = _f32(logprob, "logprob", n * (k + 1), dev)
+            logprob = _new((n, k + 1), torch.float32, dev, stream) if stream is not None else torch.empty_like(uniform)
+            pp = logprob.data_ptr()
+        else:
+            pp = _f32(logprob, "logprob", n * (k + 1), dev)
         with _on(dev):
             rc = self._lib.pulse_verify_drafts(dt, pt, st, pd, sd, px, pl, pu, n, k, self.vocab, self.logit_scale,
                                                self.draft_scale, po, pc, pp, self._pws, self._nws,
