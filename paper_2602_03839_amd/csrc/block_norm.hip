@@ -144,7 +144,7 @@ __global__ __launch_bounds__(block_of(G)) void block_norm_kernel(BlockNormParams
   }
 }
 
-constexpr int block_grad_of(int g) { return g == 64 ? 256 : g == 1024 ? 1024 : 512; }
+constexpr int block_grad_of(int g) { return g < 256 ? 256 : g; }
 
 // Each group of G lanes takes a row at a time, the next one on its way (but for rows of
 // more than 8,192 elements, whose 1,024 threads have 128 registers each and keep part
@@ -202,20 +202,10 @@ __global__ __launch_bounds__(block_grad_of(G)) void block_norm_grad_kernel(Block
     if (!kAhead) fetch(row);
     float x[E], g[E], bh[E];
     R::unpack(nx, x);
-    float dy[E], dh[E];
+    float dy[E];
     R::unpack(ndy, dy);
-    if (p.dh_out) {
-      R::unpack(ndh, dh);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) dh[e] = 0.0f;
-    }
-    if (p.b) {
-      R::unpack(nb, bh);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) bh[e] = 0.0f;
-    }
+    // as they lie in memory until they are needed
+    const typename R::template Raw<T> raw_dh = ndh, raw_b = nb;
     const float rstd = nrstd, mean = nmean, pr = npr, pm = npm;
     if (kAhead && k + 1 < turns) fetch(row + step);
     float sa = 0.0f, sax = 0.0f;
@@ -234,6 +224,13 @@ __global__ __launch_bounds__(block_grad_of(G)) void block_norm_grad_kernel(Block
     float2 sum = group_sum2<G>(sa, sax, s[0]);
     sa = p.rms ? 0.0f : sum.x * inv_n;
     sax = sum.y * inv_n;
+    float dh[E];
+    if (p.dh_out) {
+      R::unpack(raw_dh, dh);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) dh[e] = 0.0f;
+    }
 #pragma unroll
     for (int e = 0; e < E; ++e)
       g[e] = R::in(e, p.cols, t) ? __builtin_fmaf(g[e] - sa - x[e] * sax, rstd, dh[e]) : 0.0f;
@@ -241,6 +238,12 @@ __global__ __launch_bounds__(block_grad_of(G)) void block_norm_grad_kernel(Block
     for (int e = 0; e < E; ++e) x[e] = g[e] * p.residual_scale;
     if (valid) R::store((T*)p.dh + row * p.dh_stride, p.cols, t, x);
     float sc = 0.0f, scb = 0.0f;
+    if (p.b) {
+      R::unpack(raw_b, bh);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) bh[e] = 0.0f;
+    }
     if (post) {
 #pragma unroll
       for (int e = 0; e < E; ++e) bh[e] = R::in(e, p.cols, t) ? (bh[e] - pm) * pr : 0.0f;
