@@ -108,6 +108,8 @@ struct BlockNormGradParams {
   uint32_t cols;
   int param_bf16;
   bool rms, biases;  // biases: the sums of dy and g are asked for
+  float* means;      // of wide rows: the means of a and of a xh (set by the launcher)
+  uint64_t means_stride;
 };
 
 hipError_t launch_block_norm(bool bf16, const BlockNormParams& p, hipStream_t stream);

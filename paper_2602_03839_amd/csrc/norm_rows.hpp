@@ -1,6 +1,6 @@
 // norm_rows.hpp -- how the norms hold a row: in the registers of G lanes, E elements
-// each, groups of 8 side by side (rows of 16-byte groups) or element by element,
-// and the sums over those lanes.
+// each, groups of 8 side by side (rows of 16-byte groups, or any rows) or element by
+// element, and the sums over those lanes.
 #pragma once
 
 #include <type_traits>
@@ -125,6 +125,89 @@ struct Row {
                                                 float (&v)[E]) {
     if (bf16) load<false>((const uint16_t*)p, cols, t, v);
     else load<false>((const float*)p, cols, t, v);
+  }
+};
+
+// Groups of 8 of a row of any length and alignment: loaded 16 bytes at a time wherever
+// they lie, but for the row's last one, which may be cut short.
+template <int E, int G>
+struct AnyRow {
+  static __device__ __forceinline__ uint32_t at(int j, uint32_t t) { return (uint32_t)(j * G + t) * 8; }
+
+  template <typename T>
+  struct Raw {
+    Raw8<T> v[E / 8];
+  };
+  template <bool STREAM, typename T>
+  static __device__ __forceinline__ void load(const T* p, uint32_t cols, uint32_t t, Raw<T>& r) {
+    constexpr int kPer = 16 / sizeof(T);
+#pragma unroll
+    for (int j = 0; j < E / 8; ++j) {
+      const uint32_t c = at(j, t);
+      if (c + 8 <= cols) {
+#pragma unroll
+        for (size_t i = 0; i < sizeof(T) / 2; ++i) r.v[j].v[i] = load16_any(p + c + kPer * i);
+        continue;
+      }
+      uint32_t w[2 * sizeof(T)] = {};
+#pragma unroll
+      for (uint32_t i = 0; i < 8; ++i)
+        if (c + i < cols) {
+          if constexpr (sizeof(T) == 2) w[i >> 1] |= (uint32_t)p[c + i] << (16 * (i & 1));
+          else w[i] = __float_as_uint(p[c + i]);
+        }
+#pragma unroll
+      for (size_t i = 0; i < sizeof(T) / 2; ++i)
+        r.v[j].v[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+    }
+  }
+  template <typename T>
+  static __device__ __forceinline__ void unpack(const Raw<T>& r, float (&v)[E]) {
+#pragma unroll
+    for (int j = 0; j < E / 8; ++j) unpack8(r.v[j], v + 8 * j);
+  }
+  static __device__ __forceinline__ void store_group(uint16_t* p, uint32_t left, const float* v) {
+    uint4 o;
+    o.x = bf16x2_rne(__float_as_uint(v[0]), __float_as_uint(v[1]));
+    o.y = bf16x2_rne(__float_as_uint(v[2]), __float_as_uint(v[3]));
+    o.z = bf16x2_rne(__float_as_uint(v[4]), __float_as_uint(v[5]));
+    o.w = bf16x2_rne(__float_as_uint(v[6]), __float_as_uint(v[7]));
+    if (left >= 8) return store16_any(p, o);
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+      if (i < left) p[i] = (uint16_t)(get_u32(o, i >> 1) >> (16 * (i & 1)));
+  }
+  static __device__ __forceinline__ void store_group(float* p, uint32_t left, const float* v) {
+    if (left >= 8) {
+#pragma unroll
+      for (int i = 0; i < 8; i += 4)
+        store16_any(p + i, make_uint4(__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]),
+                                      __float_as_uint(v[i + 3])));
+      return;
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i)
+      if (i < left) p[i] = v[i];
+  }
+  template <typename T>
+  static __device__ __forceinline__ void store(T* p, uint32_t cols, uint32_t t, const float (&v)[E]) {
+#pragma unroll
+    for (int j = 0; j < E / 8; ++j) {
+      const uint32_t c = at(j, t);
+      if (c < cols) store_group(p + c, cols - c, v + 8 * j);
+    }
+  }
+  static __device__ __forceinline__ bool in(int e, uint32_t cols, uint32_t t) { return at(e / 8, t) + e % 8 < cols; }
+  static __device__ __forceinline__ void params(const void* p, int bf16, uint32_t cols, uint32_t t, float (&v)[E]) {
+    if (bf16) {
+      Raw<uint16_t> r;
+      load<false>((const uint16_t*)p, cols, t, r);
+      unpack(r, v);
+    } else {
+      Raw<float> r;
+      load<false>((const float*)p, cols, t, r);
+      unpack(r, v);
+    }
   }
 };
 

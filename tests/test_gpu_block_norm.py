@@ -368,3 +368,13 @@ def test_refusals():
         norm.backward(x, None, x, h_out, stats[:1])
     with pytest.raises(pulse.PulseError, match="must be"):
         head.BlockNorm(w, gate=w).backward(x, None, None, h_out, stats)
+
+
+@pytest.mark.parametrize("cols", [4099, 8193, 12000])
+@pytest.mark.parametrize("rows", [1, 63, 65, 1200])
+def test_wide_rows(rows, cols):
+    """Rows whose columns' sums are taken in a pass of their own."""
+    for dtype, rms, post, gate in ((torch.float32, False, True, True), (torch.bfloat16, True, True, False),
+                                   (torch.bfloat16, False, False, True), (torch.float32, True, False, False)):
+        b, h, dy, dh, p = make(rows, cols, dtype, rows + cols, rms, post, gate)
+        check(b, h, dy, dh, p, rms, 0.5, dtype)
