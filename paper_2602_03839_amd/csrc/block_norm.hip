@@ -548,7 +548,9 @@ hipError_t launch_block_norm_grad(bool bf16, const BlockNormGradParams& p, hipSt
     grad_lanes<!kIsBf16<T> || !V>(p.cols, [&](auto lanes) {
       constexpr int E = decltype(lanes)::kE, G = decltype(lanes)::kG;
       constexpr uint32_t kGroups = block_grad_of(G) / G, kMost = G < 512 ? kBlockNormBlocks : kBlockNormBlocks / 2;
-      const uint64_t blocks = (p.rows + kGroups - 1) / kGroups;
+      uint64_t blocks = (p.rows + kGroups - 1) / kGroups;
+      // two turns of a block rather than a second one for a CU, whose sums are read again
+      if (blocks > kMost / 2) blocks = blocks / 2 + 1 < kMost / 2 ? kMost / 2 : blocks / 2 + 1;
       sums = blocks < kMost ? (uint32_t)blocks : kMost;
       if (blocks == 0) return;
       const dim3 block(block_grad_of(G)), grid(sums);

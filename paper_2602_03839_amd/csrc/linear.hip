@@ -33,19 +33,23 @@ struct ProductParams {
   uint32_t m_ld;     // a multiple of 4
   void* out;
   uint64_t out_ld;
-  bool wide;  // every row of the epilogue starts at 16 bytes
+  bool wide;    // every row of the epilogue starts at 16 bytes
+  bool stream;  // what is read and written there is more than the caches keep
   Epilogue e;
 };
+
+__device__ __forceinline__ void unpack_eight(const uint4& w, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    v[e] = __uint_as_float(e & 1 ? get_u32(w, e >> 1) & 0xFFFF0000u : get_u32(w, e >> 1) << 16);
+}
 
 // Eight adjacent values from element `at` on, `left` of them there.
 __device__ __forceinline__ void load_eight(const void* p, uint64_t at, int bf16, bool wide, uint32_t left,
                                            float (&v)[8]) {
   if (wide && left >= 8) {
     if (bf16) {
-      const uint4 w = load16((const uint16_t*)p + at);
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        v[e] = __uint_as_float(e & 1 ? get_u32(w, e >> 1) & 0xFFFF0000u : get_u32(w, e >> 1) << 16);
+      unpack_eight(load16((const uint16_t*)p + at), v);
     } else {
       const uint4 a = load16((const float*)p + at), b = load16((const float*)p + at + 4);
 #pragma unroll
@@ -69,13 +73,14 @@ __device__ __forceinline__ uint4 pack_eight(const float (&v)[8]) {
   return o;
 }
 
-__device__ __forceinline__ void store_eight(void* p, uint64_t at, int bf16, bool wide, uint32_t left,
+__device__ __forceinline__ void store_eight(void* p, uint64_t at, int bf16, bool wide, bool stream, uint32_t left,
                                             const float (&v)[8]) {
   if (bf16) {
     uint16_t* const y = (uint16_t*)p + at;
     const uint4 o = pack_eight(v);
     if (wide && left >= 8) {
-      store16(y, o);
+      if (stream) store16_stream(y, o);
+      else store16(y, o);
     } else if (left >= 8) {
       store16_any(y, o);
     } else {
@@ -96,22 +101,37 @@ __device__ __forceinline__ void store_eight(void* p, uint64_t at, int bf16, bool
   }
 }
 
-// Token t's eight features from `row` on, from their sums to what is stored.
-__device__ __forceinline__ void finish_eight(const ProductParams& p, float (&v)[8], uint64_t t, uint32_t row) {
+// Multiplier and residual of eight features, fetched before the sums are there.
+struct Fetched {
+  uint4 times, residual;
+};
+
+// Token t's eight features from `row` on, from their sums to what is stored.  FETCHED: `f`
+// holds the operands, of whole eights of BF16.  act: p.e.act, where it is known a
+// constant, so that the others' code is not there.
+template <bool FETCHED>
+__device__ __forceinline__ void finish_eight(const ProductParams& p, const Fetched& f, int act, float (&v)[8],
+                                             uint64_t t, uint32_t row) {
   const Epilogue& e = p.e;
   const uint32_t left = p.m - row;
   float bias[8], times[8], residual[8];
   if (e.bias) load_eight(e.bias, row, e.bias_bf16, true, left, bias);
-  if (e.times) load_eight(e.times, t * e.times_stride + row, e.out_bf16, p.wide, left, times);
-  if (e.residual) load_eight(e.residual, t * e.residual_stride + row, e.out_bf16, p.wide, left, residual);
+  if (e.times) {
+    if (FETCHED && left >= 8) unpack_eight(f.times, times);
+    else load_eight(e.times, t * e.times_stride + row, e.out_bf16, p.wide, left, times);
+  }
+  if (e.residual) {
+    if (FETCHED && left >= 8) unpack_eight(f.residual, residual);
+    else load_eight(e.residual, t * e.residual_stride + row, e.out_bf16, p.wide, left, residual);
+  }
   if (e.bias) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += bias[i];
   }
-  if (e.pre) store_eight(e.pre, t * e.pre_stride + row, e.out_bf16, p.wide, left, v);
-  if (e.act) {
+  if (e.pre) store_eight(e.pre, t * e.pre_stride + row, e.out_bf16, p.wide, p.stream, left, v);
+  if (act) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = activate(e.act, v[i]);
+    for (int i = 0; i < 8; ++i) v[i] = activate(act, v[i]);
   }
   if (e.times) {
 #pragma unroll
@@ -121,15 +141,18 @@ __device__ __forceinline__ void finish_eight(const ProductParams& p, float (&v)[
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += residual[i];
   }
-  store_eight(p.out, t * p.out_ld + row, e.out_bf16, p.wide, left, v);
+  store_eight(p.out, t * p.out_ld + row, e.out_bf16, p.wide, p.stream, left, v);
 }
 
-// Block `id` of a product's tiles, and its split's share of k.
-template <typename T, bool AK, bool BK>
+// Block `id` of a product's tiles, and its split's share of k.  ACT: the epilogue's
+// activation, or kPlain: there is no epilogue.
+constexpr int kPlain = -1;
+
+template <typename T, bool AK, bool BK, int ACT>
 __device__ __forceinline__ void product_block(const ProductParams& p, char* lds, uint32_t id, uint32_t split) {
   // the tile's FP32 rows pass through LDS, as many fragments' columns at a time as fit
   constexpr int kFit = T::kLds / (T::BM * 4 * 16 * T::WN), kAtOnce = kFit < T::FN ? kFit : T::FN;
-  static_assert(kFit >= 1 && T::FN % kAtOnce == 0, "whole fragments at a time");
+  static_assert(kFit >= 1 && (T::FN == kAtOnce || T::FN == 2 * kAtOnce), "in one or two passes");
   uint32_t tm, tn;
   gemm_tile_of(id, p.tiles_m, p.tiles_n, 8, tm, tn);
   const uint32_t m0 = tm * T::BM, n0 = tn * T::BN;
@@ -154,10 +177,34 @@ __device__ __forceinline__ void product_block(const ProductParams& p, char* lds,
     }
     return;
   }
-  // group c (4 values) of a row lies at place c ^ (n & 15)
+  // The operands of all of a thread's eights leave together and before the sums are
+  // staged: one after the other they took as long as the bytes of seven (4,096 tokens,
+  // 18,944 x 3,584, silu and multiplier: 515 us, .. so).
+  constexpr uint32_t kRows = kAtOnce * 16 * T::WN, kEights = T::BM / 8, kItems = kRows * kEights / T::kThreads;
+  const bool fetch = ACT != kPlain && p.wide && p.e.out_bf16 && (p.e.times || p.e.residual);
+  auto pass = [&](auto first) {
+    constexpr int j0 = decltype(first)::value;
+    // a thread's i-th eight: row r of the staged ones, which is this token of the tile
+    auto place = [&](uint32_t i, uint32_t& r, uint32_t& g, uint32_t& n, uint32_t& m) {
+      const uint32_t q = threadIdx.x + i * T::kThreads;
+      r = q / kEights;
+      g = q % kEights;
+      n = n0 + r / (kAtOnce * 16) * (T::FN * 16) + j0 * 16 + r % (kAtOnce * 16);
+      m = m0 + g * 8;
+      return n < p.n && m < p.m;
+    };
+    Fetched f[kItems];
+    if (fetch) {
 #pragma unroll
-  for (int j0 = 0; j0 < T::FN; j0 += kAtOnce) {
+      for (uint32_t i = 0; i < kItems; ++i) {
+        uint32_t r, g, n, m;
+        if (!place(i, r, g, n, m) || m + 8 > p.m) continue;
+        if (p.e.times) f[i].times = load16_stream((const uint16_t*)p.e.times + n * p.e.times_stride + m);
+        if (p.e.residual) f[i].residual = load16_stream((const uint16_t*)p.e.residual + n * p.e.residual_stride + m);
+      }
+    }
     if (j0) __syncthreads();
+    // group c (4 values) of a row lies at place c ^ (n & 15)
 #pragma unroll
     for (int j = 0; j < kAtOnce; ++j) {
       const uint32_t n = (wave % T::WN) * (kAtOnce * 16) + j * 16 + (lane & 15);
@@ -168,25 +215,34 @@ __device__ __forceinline__ void product_block(const ProductParams& p, char* lds,
       }
     }
     __syncthreads();
-    constexpr uint32_t kRows = kAtOnce * 16 * T::WN, kEights = T::BM / 8;
-#pragma unroll 2
-    for (uint32_t q = threadIdx.x; q < kRows * kEights; q += T::kThreads) {
-      const uint32_t r = q / kEights, g = q % kEights;
-      // row r of the staged ones is this token of the tile
-      const uint32_t n = n0 + r / (kAtOnce * 16) * (T::FN * 16) + j0 * 16 + r % (kAtOnce * 16), m = m0 + g * 8;
-      if (n >= p.n || m >= p.m) continue;
+    auto finish = [&](uint32_t i, const Fetched& o, auto fetched) {
+      uint32_t r, g, n, m;
+      if (!place(i, r, g, n, m)) return;
       const f32x4_t lo = *(const f32x4_t*)(lds + r * (T::BM * 4) + (((2 * g) ^ (r & 15)) << 4));
       const f32x4_t hi = *(const f32x4_t*)(lds + r * (T::BM * 4) + (((2 * g + 1) ^ (r & 15)) << 4));
       float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      finish_eight(p, v, n, m);
+      if constexpr (ACT == kPlain)
+        store_eight(p.out, n * p.out_ld + m, true, p.wide, p.stream, p.m - m, v);
+      else
+        finish_eight<decltype(fetched)::value>(p, o, ACT, v, n, m);
+    };
+    if (fetch) {
+#pragma unroll
+      for (uint32_t i = 0; i < kItems; ++i) finish(i, f[i], std::true_type{});
+    } else {
+#pragma unroll 2
+      for (uint32_t i = 0; i < kItems; ++i) finish(i, f[0], std::false_type{});
     }
-  }
+  };
+  // (a loop of this size the compiler would not unroll, as the sums' registers need)
+  pass(std::integral_constant<int, 0>{});
+  if constexpr (T::FN > kAtOnce) pass(std::integral_constant<int, kAtOnce>{});
 }
 
-template <typename T, bool AK, bool BK>
+template <typename T, bool AK, bool BK, int ACT>
 __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductParams p) {
   __shared__ alignas(1024) char lds[T::kLds];
-  product_block<T, AK, BK>(p, lds, p.first_tile + blockIdx.x, blockIdx.y);
+  product_block<T, AK, BK, ACT>(p, lds, p.first_tile + blockIdx.x, blockIdx.y);
 }
 
 // dx's and dW's products in one launch: dx's blocks, whose sums are the longer ones, first.
@@ -195,8 +251,8 @@ __global__ __launch_bounds__(TX::kThreads) void both_kernel(ProductParams x, Pro
   static_assert(TX::kThreads == TW::kThreads && TX::kLds == TW::kLds, "blocks of one shape");
   __shared__ alignas(1024) char lds[TX::kLds];
   const uint32_t first = x.tiles_m * x.tiles_n;
-  if (blockIdx.x < first) product_block<TX, true, false>(x, lds, blockIdx.x, 0);
-  else product_block<TW, true, true>(w, lds, blockIdx.x - first, 0);
+  if (blockIdx.x < first) product_block<TX, true, false, kPlain>(x, lds, blockIdx.x, 0);
+  else product_block<TW, true, true, kPlain>(w, lds, blockIdx.x - first, 0);
 }
 
 // The splits' sums, added in order, and the epilogue: a thread an eight of a row.
@@ -214,7 +270,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductParams p, uint32_t spl
     if (second) hi += *(const f32x4_t*)(from + 4);
   }
   float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-  finish_eight(p, v, n, m);
+  finish_eight<false>(p, Fetched{}, p.e.act, v, n, m);
 }
 
 // ---------------------------------------------------------------- what goes before the products
@@ -304,7 +360,7 @@ __device__ __forceinline__ void slope_rows(const SlopeParams& p, uint32_t strip,
           if (p.dtimes) {
             const uint64_t at = t * p.dtimes_stride + row;
             if constexpr (W == 8) {
-              store_eight(p.dtimes, at, p.bf16, p.wide, left, g);
+              store_eight(p.dtimes, at, p.bf16, p.wide, true, left, g);
             } else if (left) {
               if (p.bf16) ((uint16_t*)p.dtimes)[at] = (uint16_t)bf16x2_rne(__float_as_uint(g[0]), 0u);
               else ((float*)p.dtimes)[at] = g[0];
@@ -370,6 +426,7 @@ constexpr uint32_t kTilesAtOnce = 1u << 22;  // of up to 512 threads; a multiple
 constexpr uint64_t kSumBytes = 32ull << 20;  // the most that splits' sums take
 constexpr uint32_t kMinSplit = 256;          // of k
 constexpr uint32_t kFewTokens = kLinearFewTokens;
+constexpr uint64_t kStreamBytes = 64ull << 20;  // results of more are written past the caches
 constexpr uint32_t kOneChunk = 128;  // tokens up to which dbias is summed by one block a strip
 
 // Time of a product in thousands of cycles: rounds of blocks, each with a fixed part and
@@ -418,13 +475,16 @@ void set_tiles(ProductParams& p) {
 template <bool AK, bool BK>
 using TileL = Gemm<256, 256, 2, 4, 2, AK, BK>;
 template <bool AK, bool BK>
+using TileH = Gemm<256, 128, 2, 2, 3, AK, BK, false, 32>;
+template <bool AK, bool BK>
 using TileM = Gemm<256, 128, 4, 2, 3, AK, BK>;
 template <bool AK, bool BK>
 using TileS = Gemm<128, 64, 4, 1, 4, AK, BK>;
 
-template <bool AK, bool BK>
+template <bool AK, bool BK, int ACT>
 void run_product(ProductParams p, float* sums, hipStream_t stream) {
   const Shape s = shape_of(p.m, p.n, p.k);
+  p.stream = (uint64_t)p.m * p.n * (p.e.out_bf16 ? 2 : 4) >= kStreamBytes;
   p.m_ld = up(p.m, 4);
   p.sums = s.splits > 1 ? sums : nullptr;
   p.k_split = up(parts(p.k, s.splits), kGemmK);
@@ -435,7 +495,7 @@ void run_product(ProductParams p, float* sums, hipStream_t stream) {
     for (uint64_t first = 0; first < tiles; first += kTilesAtOnce) {
       p.first_tile = (uint32_t)first;
       const uint64_t left = tiles - first;
-      hipLaunchKernelGGL((product_kernel<T, AK, BK>), dim3(left < kTilesAtOnce ? (uint32_t)left : kTilesAtOnce, s.splits),
+      hipLaunchKernelGGL((product_kernel<T, AK, BK, ACT>), dim3(left < kTilesAtOnce ? (uint32_t)left : kTilesAtOnce, s.splits),
                          dim3(T::kThreads), 0, stream, p);
     }
   };
@@ -460,8 +520,8 @@ void run_gradients(ProductParams x, ProductParams w, float* sums, hipStream_t st
     hipLaunchKernelGGL((both_kernel<TX, TW>), dim3((uint32_t)tiles), dim3(TX::kThreads), 0, stream, x, w);
     return;
   }
-  run_product<true, false>(x, sums, stream);
-  run_product<true, true>(w, sums, stream);
+  run_product<true, false, kPlain>(x, sums, stream);
+  run_product<true, true, kPlain>(w, sums, stream);
 }
 
 struct Plan {
@@ -563,7 +623,14 @@ hipError_t launch_linear(const LinearParams& c, char* ws, hipStream_t stream) {
   const uint64_t unit = c.e.out_bf16 ? 8 : 4;
   p.wide = c.y_stride % unit == 0 && (!c.e.pre || c.e.pre_stride % unit == 0) &&
            (!c.e.times || c.e.times_stride % unit == 0) && (!c.e.residual || c.e.residual_stride % unit == 0);
-  run_product<false, false>(p, (float*)(ws + q.sums), stream);
+  float* const sums = (float*)(ws + q.sums);
+  switch (c.e.act) {
+    case kActRelu: run_product<false, false, kActRelu>(p, sums, stream); break;
+    case kActSilu: run_product<false, false, kActSilu>(p, sums, stream); break;
+    case kActGelu: run_product<false, false, kActGelu>(p, sums, stream); break;
+    case kActGeluTanh: run_product<false, false, kActGeluTanh>(p, sums, stream); break;
+    default: run_product<false, false, kActNone>(p, sums, stream);
+  }
   return hipGetLastError();
 }
 
