@@ -14,7 +14,7 @@
 // which group.
 //   k-contiguous: rows of 128 bytes (8 groups).  Group c of row r lies at
 //     place c ^ ((r >> 1) & 7): the 16 rows that a fragment read touches at
-//     one c then cover all 64 banks once.  (32 k: rows of 64 bytes, c ^ ((r >> 2) & 3).)
+//     one c then cover all 64 banks once.
 //   k-major: rows of all the tile's m (or n).  Pairs of groups (16 elements, one
 //     fragment's width) are permuted by k: the transposing read takes 4
 //     rows of 32 bytes for each of its lane groups, 8 rows apart, which then
@@ -55,12 +55,11 @@ __device__ __forceinline__ void wait_and_meet() {
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4_t lds_s16x4_t;
 
-constexpr int kGemmK = 64;  // k per buffer, unless said otherwise
+constexpr int kGemmK = 64;  // k per buffer
 
-template <int ROWS, int WAVES, bool KMAJOR, int KS = kGemmK>
+template <int ROWS, int WAVES, bool KMAJOR>
 struct GemmTile {
-  static_assert(KS == 64 || KS == 32, "");
-  static constexpr int kBytes = ROWS * KS * 2;
+  static constexpr int kBytes = ROWS * kGemmK * 2;
   static constexpr int kLoads = kBytes / 1024 / WAVES;  // per wave and buffer
   static_assert(kBytes % (1024 * WAVES) == 0, "whole wave loads");
 
@@ -72,10 +71,9 @@ struct GemmTile {
   const char* at;
   uint64_t step;
 
-  // k (of the KS) that the lane's i-th load starts at
+  // k (of the 64) that the lane's i-th load starts at
   static __device__ __forceinline__ int32_t k_of(int i, int wave, int lane) {
-    if constexpr (!KMAJOR && KS == 32) return ((lane & 3) ^ ((lane >> 4) & 3)) * 8;
-    else if constexpr (!KMAJOR) return (((lane & 7) ^ (((lane >> 4) & 3) | (((i * WAVES + wave) & 1) << 2))) * 8);
+    if constexpr (!KMAJOR) return (((lane & 7) ^ (((lane >> 4) & 3) | (((i * WAVES + wave) & 1) << 2))) * 8);
     else return (i * WAVES + wave) * (512 / ROWS) + lane / (ROWS / 8);
   }
 
@@ -83,7 +81,7 @@ struct GemmTile {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       if constexpr (!KMAJOR) {
-        uint32_t r = KS == 64 ? (i * WAVES + wave) * 8 + (lane >> 3) : (i * WAVES + wave) * 16 + (lane >> 2);
+        uint32_t r = (i * WAVES + wave) * 8 + (lane >> 3);
         if (r >= o.limit) r = o.limit - 1;
         off[i] = (uint32_t)(r * o.ld * 2 + k_of(i, wave, lane) * 2);
       } else {
@@ -94,7 +92,7 @@ struct GemmTile {
       }
     }
     at = (const char*)o.p + (KMAJOR ? k0 * o.ld * 2 : (uint64_t)k0 * 2);
-    step = KMAJOR ? KS * o.ld * 2 : KS * 2;
+    step = KMAJOR ? kGemmK * o.ld * 2 : kGemmK * 2;
   }
 
   // The i-th load of the next 64 k, all in the matrix, into `lds`; then next().
@@ -141,7 +139,6 @@ struct GemmTile {
   // constants, so one register serves all of a wave's reads.
   static __device__ __forceinline__ uint32_t lane_place(uint32_t first, int lane) {
     const uint32_t r = lane & 15, g = lane >> 4;
-    if constexpr (!KMAJOR && KS == 32) return (first + r) * 64 + ((g ^ ((r >> 2) & 3)) << 4);
     if constexpr (!KMAJOR) return (first + r) * 128 + ((g ^ ((r >> 1) & 7)) << 4);
     const uint32_t k = g * 8 + (r >> 2);
     return k * (ROWS * 2) + ((first * 2) ^ (mix(k) << 5)) + (r & 3) * 8;
@@ -149,9 +146,7 @@ struct GemmTile {
 
   // The lane's fragment of rows 16 i ..., k = 32 ks ..., `at`: its place and the tile's.
   static __device__ __forceinline__ bf16x8_t fragment(uint32_t at, int i, int ks) {
-    if constexpr (!KMAJOR && KS == 32) {
-      return *(const __attribute__((address_space(3))) bf16x8_t*)(at + i * 1024);
-    } else if constexpr (!KMAJOR) {
+    if constexpr (!KMAJOR) {
       return *(const __attribute__((address_space(3))) bf16x8_t*)((at ^ (ks << 6)) + i * 2048);
     } else {
       const uint32_t to = (at ^ (i << 5)) + ks * 32 * ROWS * 2;
@@ -163,16 +158,13 @@ struct GemmTile {
   }
 };
 
-// KS_: k per buffer.  With 32 the buffers of two blocks fit a CU, so that one's epilogue
-// goes on while the other multiplies, for half as much again to load per product.
-template <int BM_, int BN_, int WM_, int WN_, int NST_, bool AK_, bool BK_, bool STREAM_ = false, int KS_ = kGemmK>
+template <int BM_, int BN_, int WM_, int WN_, int NST_, bool AK_, bool BK_, bool STREAM_ = false>
 struct Gemm {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NST = NST_;
   static constexpr int kWaves = WM * WN, kThreads = 64 * kWaves;
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;  // fragments of a wave
-  static constexpr int KS = KS_;
-  typedef GemmTile<BM, kWaves, AK_, KS> A;
-  typedef GemmTile<BN, kWaves, BK_, KS> B;
+  typedef GemmTile<BM, kWaves, AK_> A;
+  typedef GemmTile<BN, kWaves, BK_> B;
   static constexpr int kStage = A::kBytes + B::kBytes;
   static constexpr int kLds = NST * kStage;
   static constexpr int kLoads = A::kLoads + B::kLoads;  // of a wave and step
@@ -262,9 +254,9 @@ struct Gemm {
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    const int32_t full = (int32_t)((k1 - k0) / KS), steps = (int32_t)((k1 - k0 + KS - 1) / KS);
+    const int32_t full = (int32_t)((k1 - k0) / kGemmK), steps = (int32_t)((k1 - k0 + kGemmK - 1) / kGemmK);
     if (steps == 0) return;
-    const int32_t rest = (int32_t)((k1 - k0) % KS);
+    const int32_t rest = (int32_t)((k1 - k0) % kGemmK);
     const uint32_t at_a = lds_address(lds) + A::lane_place((wave / WN) * (FM * 16), lane);
     const uint32_t at_b = lds_address(lds) + A::kBytes + B::lane_place((wave % WN) * (FN * 16), lane);
 
@@ -334,32 +326,6 @@ struct Gemm {
 #pragma unroll
     for (int i = 0; i < FM + FN; ++i) read(f0, 0, 0, i);
     int32_t s = 0;
-    if constexpr (KS == 32) {
-      // a step is one set of fragments: the next step's are read while one's are multiplied
-      auto turn = [&](Frags& next, const Frags& now) {
-        wait_and_meet<(NST - 2) * kLoads>();
-        half(next, after, 0, now, true, here);
-        la.next();
-        lb.next();
-        advance();
-      };
-      for (; s + 1 + NST < full; s += 2) {
-        turn(f1, f0);
-        turn(f0, f1);
-      }
-      for (; s < steps; ++s) {
-#pragma unroll
-        for (int i = 0; i < FM; ++i) multiply(f0, i);
-        if (s + 1 == steps) break;
-        wait_and_meet<0>();
-        if (s + NST < steps) load_step(here, s + NST);
-#pragma unroll
-        for (int i = 0; i < FM + FN; ++i) read(f0, after, 0, i);
-        advance();
-      }
-      __syncthreads();
-      return;
-    }
     for (; s + NST < full; ++s) {
       half(f1, here, 1, f0, false, 0);
       wait_and_meet<(NST - 2) * kLoads>();

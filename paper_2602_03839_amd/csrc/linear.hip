@@ -179,7 +179,7 @@ __device__ __forceinline__ void product_block(const ProductParams& p, char* lds,
   }
   // The operands of all of a thread's eights leave together and before the sums are
   // staged: one after the other they took as long as the bytes of seven (4,096 tokens,
-  // 18,944 x 3,584, silu and multiplier: 515 us, .. so).
+  // 18,944 x 3,584, silu and multiplier: 515 us, 458 so).
   constexpr uint32_t kRows = kAtOnce * 16 * T::WN, kEights = T::BM / 8, kItems = kRows * kEights / T::kThreads;
   const bool fetch = ACT != kPlain && p.wide && p.e.out_bf16 && (p.e.times || p.e.residual);
   auto pass = [&](auto first) {
@@ -474,8 +474,6 @@ void set_tiles(ProductParams& p) {
 
 template <bool AK, bool BK>
 using TileL = Gemm<256, 256, 2, 4, 2, AK, BK>;
-template <bool AK, bool BK>
-using TileH = Gemm<256, 128, 2, 2, 3, AK, BK, false, 32>;
 template <bool AK, bool BK>
 using TileM = Gemm<256, 128, 4, 2, 3, AK, BK>;
 template <bool AK, bool BK>
