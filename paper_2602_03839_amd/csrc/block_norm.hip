@@ -62,6 +62,14 @@ __device__ __forceinline__ void normalise(float (&v)[N][E], const BlockNormParam
   rstd[1] = 1.0f / __builtin_sqrtf(sum.y * inv_n + p.eps);
 }
 
+// stream: rows that the caches will not keep until they are read again are written past
+// them (16,384 x 3,584 BF16: forward 87 us, 82 so, backward 142 and 134).
+template <typename R, typename T, int E>
+__device__ __forceinline__ void store_row(bool stream, T* p, uint32_t cols, uint32_t t, const float (&v)[E]) {
+  if (stream) R::template store<true>(p, cols, t, v);
+  else R::store(p, cols, t, v);
+}
+
 // N rows at a time by each group of G lanes, and no loop, as the layer norm's.
 template <typename T, int E, int G, bool VEC, int N>
 __global__ __launch_bounds__(block_of(G)) void block_norm_kernel(BlockNormParams p) {
@@ -125,7 +133,7 @@ __global__ __launch_bounds__(block_of(G)) void block_norm_kernel(BlockNormParams
       // past the row's end zeros, whatever rstd is
       u[k][e] = R::in(e, p.cols, t) ? __builtin_fmaf(p.residual_scale, h[e], u[k][e]) : 0.0f;
     // where h_out is h these lanes have read what they write
-    if (row + k <= last) R::store((T*)p.h_out + (row + k) * p.h_out_stride, p.cols, t, u[k]);
+    if (row + k <= last) store_row<R>(p.stream, (T*)p.h_out + (row + k) * p.h_out_stride, p.cols, t, u[k]);
   }
   normalise<T, E, G, VEC, N>(u, p, t, inv_n, s, mean, rstd);
   R::params(p.weight, p.param_bf16, p.cols, t, w);
@@ -143,7 +151,7 @@ __global__ __launch_bounds__(block_of(G)) void block_norm_kernel(BlockNormParams
 #pragma unroll
   for (int k = 0; k < N; ++k) {
     if (row + k > last) break;
-    R::store((T*)p.y + (row + k) * p.y_stride, p.cols, t, u[k]);
+    store_row<R>(p.stream, (T*)p.y + (row + k) * p.y_stride, p.cols, t, u[k]);
     if (t == 0 && p.stats) {
       p.stats[row + k] = rstd[k];
       if (!p.rms) p.stats[2 * p.stats_stride + row + k] = mean[k];
@@ -249,7 +257,7 @@ __global__ __launch_bounds__(block_grad_of(G)) void block_norm_grad_kernel(Block
       g[e] = R::in(e, p.cols, t) ? __builtin_fmaf(g[e] - sa - x[e] * sax, rstd, dh[e]) : 0.0f;
 #pragma unroll
     for (int e = 0; e < E; ++e) x[e] = g[e] * p.residual_scale;
-    if (valid) R::store((T*)p.dh + row * p.dh_stride, p.cols, t, x);
+    if (valid) store_row<R>(p.stream, (T*)p.dh + row * p.dh_stride, p.cols, t, x);
     float sc = 0.0f, scb = 0.0f;
     if (p.b) {
       R::unpack(raw_b, bh);
@@ -285,7 +293,7 @@ __global__ __launch_bounds__(block_grad_of(G)) void block_norm_grad_kernel(Block
 #pragma unroll
       for (int e = 0; e < E; ++e) g[e] = (g[e] - sc - bh[e] * scb) * pr;
     }
-    if (valid) R::store((T*)p.db + row * p.db_stride, p.cols, t, g);
+    if (valid) store_row<R>(p.stream, (T*)p.db + row * p.db_stride, p.cols, t, g);
   }
   if constexpr (!SUMS) return;
   // the groups' sums one after the other, then one row of each sum for the block
@@ -470,13 +478,17 @@ void run_block_norm(bool bf16, const BlockNormParams& p, hipStream_t stream) {
   });
 }
 
+constexpr uint64_t kStreamBytes = 64ull << 20;  // of one matrix
+
 // A launch has fewer than 2^32 threads; the widest form takes 512 for a row.
 constexpr uint64_t kRowsAtOnce = 1u << 22;
 
 }  // namespace
 
-hipError_t launch_block_norm(bool bf16, const BlockNormParams& p, hipStream_t stream) {
+hipError_t launch_block_norm(bool bf16, const BlockNormParams& all, hipStream_t stream) {
   const uint64_t size = bf16 ? 2 : 4;
+  BlockNormParams p = all;
+  p.stream = p.rows * p.cols * size >= kStreamBytes;
   for (uint64_t first = 0; first < p.rows; first += kRowsAtOnce) {
     BlockNormParams q = p;
     q.rows = p.rows - first < kRowsAtOnce ? p.rows - first : kRowsAtOnce;
@@ -534,7 +546,9 @@ uint32_t run_wide_grad(const BlockNormGradParams& p, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_block_norm_grad(bool bf16, const BlockNormGradParams& p, hipStream_t stream) {
+hipError_t launch_block_norm_grad(bool bf16, const BlockNormGradParams& all, hipStream_t stream) {
+  BlockNormGradParams p = all;
+  p.stream = p.rows * p.cols * (bf16 ? 2 : 4) >= kStreamBytes;
   const bool vec = p.cols % 8 == 0 && p.dy_stride % 8 == 0 && p.h_out_stride % 8 == 0 && p.dh_stride % 8 == 0 &&
                    p.db_stride % 8 == 0 && (!p.dh_out || p.dh_out_stride % 8 == 0) && (!p.b || p.b_stride % 8 == 0);
   uint32_t sums = 0;

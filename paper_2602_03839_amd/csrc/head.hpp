@@ -76,6 +76,7 @@ struct BlockNormParams {
   float eps;
   int param_bf16;
   bool rms;
+  bool stream;  // set by the launcher, as below
 };
 
 struct BlockNormGradParams {
@@ -108,7 +109,9 @@ struct BlockNormGradParams {
   uint32_t cols;
   int param_bf16;
   bool rms, biases;  // biases: the sums of dy and g are asked for
-  float* means;      // of wide rows: the means of a and of a xh (set by the launcher)
+  // set by the launcher
+  bool stream;   // the results are more than the caches keep
+  float* means;  // of wide rows: the means of a and of a xh
   uint64_t means_stride;
 };
 

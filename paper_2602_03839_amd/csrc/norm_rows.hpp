@@ -45,20 +45,26 @@ __device__ __forceinline__ void unpack8(const Raw8<float>& r, float* v) {
   for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(get_u32(r.v[i / 4], i & 3));
 }
 
+template <bool STREAM>
 __device__ __forceinline__ void store8(uint16_t* p, const float* v) {
   uint4 o;
   o.x = bf16x2_rne(__float_as_uint(v[0]), __float_as_uint(v[1]));
   o.y = bf16x2_rne(__float_as_uint(v[2]), __float_as_uint(v[3]));
   o.z = bf16x2_rne(__float_as_uint(v[4]), __float_as_uint(v[5]));
   o.w = bf16x2_rne(__float_as_uint(v[6]), __float_as_uint(v[7]));
-  store16(p, o);
+  if (STREAM) store16_stream(p, o);
+  else store16(p, o);
 }
 
+template <bool STREAM>
 __device__ __forceinline__ void store8(float* p, const float* v) {
 #pragma unroll
-  for (int i = 0; i < 8; i += 4)
-    store16(p + i, make_uint4(__float_as_uint(v[i]), __float_as_uint(v[i + 1]),
-                              __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])));
+  for (int i = 0; i < 8; i += 4) {
+    const uint4 o = make_uint4(__float_as_uint(v[i]), __float_as_uint(v[i + 1]),
+                               __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3]));
+    if (STREAM) store16_stream(p + i, o);
+    else store16(p + i, o);
+  }
 }
 
 __device__ __forceinline__ void store1(uint16_t* p, float v) {
@@ -107,13 +113,13 @@ struct Row {
     load<STREAM>(p, cols, t, r);
     unpack(r, v);
   }
-  template <typename T>
+  template <bool STREAM = false, typename T>
   static __device__ __forceinline__ void store(T* p, uint32_t cols, uint32_t t, const float (&v)[E]) {
 #pragma unroll
     for (int j = 0; j < E / kStep; ++j) {
       const uint32_t c = at(j, t);
       if (c < cols) {
-        if constexpr (VEC) store8(p + c, v + 8 * j);
+        if constexpr (VEC) store8<STREAM>(p + c, v + 8 * j);
         else store1(p + c, v[j]);
       }
     }
@@ -189,7 +195,7 @@ struct AnyRow {
     for (uint32_t i = 0; i < 8; ++i)
       if (i < left) p[i] = v[i];
   }
-  template <typename T>
+  template <bool STREAM = false, typename T>
   static __device__ __forceinline__ void store(T* p, uint32_t cols, uint32_t t, const float (&v)[E]) {
 #pragma unroll
     for (int j = 0; j < E / 8; ++j) {
