@@ -11,7 +11,7 @@
 // Probabilities are FP64.  The draw is the first entry whose cumulated probability
 // exceeds u times the total: in FP32 each of some 150,000 borders would be off by 1e-7
 // of the total, so that one draw in 30 gave another token than the definition's.  With
-// borders off by 5e-11 it is one in 100,000.  An exponential is 15 FP64 instructions,
+// borders off by 1e-12 it is one in a million.  An exponential is 16 FP64 instructions,
 // which issue as fast as FP32's here, and these bound the first kernel for BF16 logits.
 //
 // A wave takes a segment of a row by itself: 1,024 adjacent entries, or 512 where that
@@ -26,21 +26,22 @@ namespace pulse {
 
 namespace {
 
-// 2^x for x <= 0, or a little above, off by 5.5e-11: a polynomial for what x is from the
-// nearest integer, interpolated at the 8 Chebyshev nodes of [-1/2, 1/2].  The integer is
-// in the low bits of x + 1.5 * 2^52, and goes into the exponent by an addition; 2^-1000
-// stands for 0.
+// 2^x for x <= 0, or a little above, off by 1.1e-12 and 1 at 0, so that no probability
+// is above 1: a polynomial for what x is from the nearest integer, interpolated at the 9
+// Chebyshev nodes of [-1/2, 1/2].  The integer is in the low bits of x + 1.5 * 2^52, and
+// goes into the exponent by an addition; 2^-1000 stands for 0.
 template <bool CLAMP = true>  // without: x > -1000
 __device__ __forceinline__ double exp2_64(double x) {
   if constexpr (CLAMP) x = __builtin_fmax(x, -1000.0);
   const double shifted = x + 0x1.8p52, f = x - (shifted - 0x1.8p52);
-  double v = __builtin_fma(1.5303700711365693e-05, f, 0.00015469729214118296);
-  v = __builtin_fma(v, f, 0.0013333478473685416);
-  v = __builtin_fma(v, f, 0.009618025613318034);
-  v = __builtin_fma(v, f, 0.055504109063258665);
-  v = __builtin_fma(v, f, 0.24022651213498092);
-  v = __builtin_fma(v, f, 0.6931471805568324);
-  v = __builtin_fma(v, f, 0.9999999999595618);
+  double v = __builtin_fma(1.3255224878668817e-06, f, 1.5310079402249296e-05);
+  v = __builtin_fma(v, f, 0.00015403455852453838);
+  v = __builtin_fma(v, f, 0.0013333450568000645);
+  v = __builtin_fma(v, f, 0.009618129159402558);
+  v = __builtin_fma(v, f, 0.05550410941205933);
+  v = __builtin_fma(v, f, 0.2402265069581299);
+  v = __builtin_fma(v, f, 0.6931471805459335);
+  v = __builtin_fma(v, f, 1.0);
   return __hiloint2double(__double2hiint(v) + (__double2loint(shifted) << 20), __double2loint(v));
 }
 

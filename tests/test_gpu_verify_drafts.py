@@ -132,6 +132,28 @@ def test_large_vocabulary():
     check(z.float(), x, u, None)
 
 
+def test_more_segments_than_are_kept():
+    """Vocabularies whose sums a wave does not hold at once: 512 entries a sum, 320 sums."""
+    for vocab in (163841, 400003):
+        z, x, u, zd = make(3, 1, vocab, torch.bfloat16, vocab, sd=1.0)
+        check(z, x, u, zd)
+        # the draw in the last entries
+        z[:, :-300] = -math.inf
+        check(z, x.clamp(min=vocab - 300), u, None)
+
+
+def test_more_sequences_than_a_launch_takes():
+    """2^22 units of work are one launch's."""
+    n = (1 << 22) + 3
+    z = torch.zeros(n, 2, device="cuda")
+    z[:, 0] = -math.inf
+    z[0, 0], z[n - 1, 1], z[n - 1, 0] = 0.0, -math.inf, 1.0
+    u = torch.full((n, 1), 0.25, device="cuda")
+    tokens, count, logprob = head.VerifyDrafts(2, n)(z, None, u)
+    assert (count == 0).all() and (tokens[1:n - 1] == 1).all() and tokens[0] == 0 and tokens[n - 1] == 0
+    assert (logprob[1:] == 0).all() and abs(logprob[0].item() + math.log(2)) < 1e-6
+
+
 def test_lengths():
     z, x, u, zd = make(9, 4, 400, torch.float32, 2, noise=0.05)
     lengths = torch.tensor([0, 1, 2, 3, 4, -5, 99, 2, 0], dtype=torch.int32)
