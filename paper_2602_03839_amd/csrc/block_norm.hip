@@ -342,7 +342,7 @@ __global__ __launch_bounds__(1024) void block_norm_wide_sums_kernel(BlockNormGra
   __shared__ float s[4][16][64];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const uint32_t c = blockIdx.x * 64 + lane;
-  const uint64_t begin = (uint64_t)blockIdx.y * chunk, end = p.rows - begin < chunk ? p.rows : begin + chunk;
+  const uint64_t begin = (uint64_t)blockIdx.y * chunk, end = begin + chunk < p.rows ? begin + chunk : p.rows;
   const bool post = p.post_weight != nullptr;
   float dw = 0.0f, s1 = 0.0f, db = 0.0f, s2 = 0.0f;
   if (c < p.cols) {

@@ -22,12 +22,20 @@ __device__ __forceinline__ float sigmoid_of(float v) {
 constexpr float kGeluA = 0.7978845608028654f;  // sqrt(2 / pi)
 constexpr float kGeluB = 0.044715f;
 
+// The logistic function's argument for gelu_tanh, whose cube would overflow far from 0:
+// from 30 on it is 0 or 1 in FP32 anyway.
+__device__ __forceinline__ float near_zero(float v) { return __builtin_fminf(__builtin_fmaxf(v, -30.0f), 30.0f); }
+__device__ __forceinline__ float gelu_tanh_gate(float v) {
+  const float u = near_zero(v);
+  return v == v ? sigmoid_of(2.0f * kGeluA * __builtin_fmaf(kGeluB * u * u, u, u)) : v;
+}
+
 __device__ __forceinline__ float activate(int act, float v) {
   switch (act) {
     case kActRelu: return v < 0.0f ? 0.0f : v;  // a NaN stays one
     case kActSilu: return v * sigmoid_of(v);
     case kActGelu: return 0.5f * v * (1.0f + erff(0.7071067811865476f * v));
-    case kActGeluTanh: return v * sigmoid_of(2.0f * kGeluA * __builtin_fmaf(kGeluB * v * v, v, v));
+    case kActGeluTanh: return v * gelu_tanh_gate(v);
     default: return v;
   }
 }
@@ -35,7 +43,7 @@ __device__ __forceinline__ float activate(int act, float v) {
 // An activation and its derivative.
 __device__ __forceinline__ float2 activate2(int act, float v) {
   switch (act) {
-    case kActRelu: return make_float2(v < 0.0f ? 0.0f : v, v > 0.0f ? 1.0f : v - v);
+    case kActRelu: return make_float2(v < 0.0f ? 0.0f : v, v > 0.0f ? 1.0f : v == v ? 0.0f : v);
     case kActSilu: {
       const float s = sigmoid_of(v);
       return make_float2(v * s, s * __builtin_fmaf(v, 1.0f - s, 1.0f));
@@ -46,9 +54,9 @@ __device__ __forceinline__ float2 activate2(int act, float v) {
       return make_float2(v * h, __builtin_fmaf(v, d, h));
     }
     case kActGeluTanh: {
-      const float s = sigmoid_of(2.0f * kGeluA * __builtin_fmaf(kGeluB * v * v, v, v));
-      const float y = 2.0f * kGeluA * __builtin_fmaf(3.0f * kGeluB * v, v, 1.0f);
-      return make_float2(v * s, __builtin_fmaf(v * s * (1.0f - s), y, s));
+      const float s = gelu_tanh_gate(v), u = near_zero(v);
+      const float y = 2.0f * kGeluA * __builtin_fmaf(3.0f * kGeluB * u, u, 1.0f);
+      return make_float2(v * s, __builtin_fmaf(u * s * (1.0f - s), y, s));
     }
     default: return make_float2(v, 1.0f);
   }

@@ -1,19 +1,20 @@
 // lowp_matmul.hip -- y = x W^T for a few BF16 tokens x and a weight W that a
-// receiver holds as MXFP4 or FP8 codes.
+// receiver holds as MXFP4 or FP8 codes, or in BF16; with or without an epilogue.
 //
 // The codes' way from HBM bounds the kernels: half a byte and a thirty-second of a byte
-// of scale a value (MXFP4), or a byte (FP8).  They are read once for every 32 tokens, or
+// of scale a value (MXFP4), a byte (FP8), or two (BF16, whose codes are the values, for up
+// to 16 tokens).  They are read once for every 32 tokens, or
 // 16 (rows that start inside a unit, tokens in LDS, fewer blocks than CUs), after the
 // first time from the last level cache if they fit there.  A wave
 // takes 16 rows and converts 16 bytes of each lane's codes to BF16 in registers:
-// exact, since a code has at most 3 (FP8: 4) significant bits and a power-of-two
+// exact, since a code has at most 3 (FP8: 4, BF16: 8) significant bits and a power-of-two
 // scale moves only the exponent.  v_mfma_f32_16x16x32_bf16 multiplies them with 16
 // tokens; its columns past the last token are computed and dropped, which costs
 // nothing here.  Products are exact in FP32 and summed in FP32.
 //
 // Two kernels: the slab kernel below for rows of whole chunks (FP8: units), up to 64 tokens, whose
 // values fit LDS or registers (152,064 x 5,120 MXFP4, 1 and 16 tokens: 65 and 79 us,
-// 6.4 and 5.3 TB/s); and lowp_matmul_kernel for every other call.
+// 6.4 and 5.3 TB/s; BF16 18,944 x 3,584: 23.4 and 26.9, 5.8 and 5.0); and lowp_matmul_kernel for every other call.
 //
 // Any order of k serves a dot product as long as both operands use the same:
 // lane (row r, group g) holds one block of 32 values (FP8: 16) with one scale,
@@ -168,8 +169,8 @@ __device__ __forceinline__ void multiply_chunk(const Held<FORM, RT, NT>& h, f32x
 }
 
 // The epilogue's part of the kernel's first argument, read where it is used: kept in
-// registers throughout it would push the scalars of the loops out of theirs (FP8 27,648 x
-// 5,120, one token and a bias: .. us, .. with).
+// registers throughout it pushes what the loops need out of theirs (FP8 27,648 x 5,120, 32
+// tokens and a bias: 49 us, 40 so).
 __device__ __forceinline__ Epilogue epilogue_here() {
   typedef const __attribute__((address_space(4))) uint64_t* args_t;
   args_t args = (args_t)__builtin_amdgcn_kernarg_segment_ptr() + offsetof(LowpMatmulParams, e) / 8;
@@ -258,6 +259,8 @@ __global__ __launch_bounds__(1024) void lowp_matmul_kernel(LowpMatmulParams p, u
         for (int n = 0; n < NT; ++n) acc[r][n] += s_part[(w * RT * NT + r * NT + n) * 64 + lane];
   }
   // lane (token r16, group g) has the rows 4 g + i of each tile
+  Epilogue e = {};
+  if constexpr (EPILOGUE) e = epilogue_here();
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     const uint32_t t = (blockIdx.y * NT + n) * 16 + r16;
@@ -269,7 +272,7 @@ __global__ __launch_bounds__(1024) void lowp_matmul_kernel(LowpMatmulParams p, u
         const uint64_t row = row_of(r, 4 * g + i);
         if (row >= p.rows) continue;
         float v = FORM == kWeightFp8 ? acc[r][n][i] / p.inv_scale : acc[r][n][i];
-        if constexpr (EPILOGUE) v = finish_one(epilogue_here(), v, t, row);
+        if constexpr (EPILOGUE) v = finish_one(e, v, t, row);
         if (p.y_bf16) ((uint16_t*)p.y)[t * p.y_stride + row] = (uint16_t)bf16x2_rne(__float_as_uint(v), 0u);
         else ((float*)p.y)[t * p.y_stride + row] = v;
       }
@@ -387,7 +390,7 @@ struct SlabStream {
 // With an epilogue the parts are added by a wave of their own, if there is room for one
 // and tiles are one at a time: its loads would have the wave that makes them wait for
 // its slabs too, and the others wait for it.  FP8 27,648 x 5,120, 16 tokens, silu and
-// multiplier: .. us, .. with the waves taking turns (.. without an epilogue).
+// multiplier: 32 us, 35.4 with the waves taking turns (30.9 without an epilogue).
 //
 // NS > 0: each wave has up to NS slabs of k for good (slabs <= NS wk) and the tokens'
 // values of them in registers; otherwise all tokens' values lie in LDS.  A block
@@ -471,7 +474,7 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
   }
 
   // vmcnt(0): the tokens are there.  Else the compiler waits for them at every slab, and so
-  // for the slabs that are on their way
+  // for the slabs that are on their way (one token and a bias: 25.5 us, 22.0 with this)
   if constexpr (XREG && EPILOGUE) __builtin_amdgcn_s_waitcnt(0x0F70);
   uint32_t slot = 0, turn = 0;
   for (uint32_t group = blockIdx.x * z.run; group * z.wr < z.tiles; group = in.after(group), ++turn) {
@@ -638,9 +641,10 @@ bool launch_slabs(const LowpMatmulParams& p, bool epilogue, hipStream_t stream) 
   by_epilogue<FORM>(epilogue, [&](auto e) {
     constexpr bool E = decltype(e)::value;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, lds, stream, p, z); };
+    constexpr int kMost = FORM == kWeightBf16 ? 1 : 2;  // tiles of tokens: BF16 has 16 tokens at most
     if (!xreg) launch(lowp_slab_kernel<FORM, 0, 1, E>);
-    else if (z.slabs <= z.wk) launch(nt == 1 ? lowp_slab_kernel<FORM, 1, 1, E> : lowp_slab_kernel<FORM, 1, 2, E>);
-    else launch(nt == 1 ? lowp_slab_kernel<FORM, kEach, 1, E> : lowp_slab_kernel<FORM, kEach, 2, E>);
+    else if (z.slabs <= z.wk) launch(nt == 1 ? lowp_slab_kernel<FORM, 1, 1, E> : lowp_slab_kernel<FORM, 1, kMost, E>);
+    else launch(nt == 1 ? lowp_slab_kernel<FORM, kEach, 1, E> : lowp_slab_kernel<FORM, kEach, kMost, E>);
   });
   return true;
 }
@@ -660,7 +664,7 @@ void launch_type(const LowpMatmulParams& p, bool epilogue, hipStream_t stream) {
   if (p.tokens <= 16 && tiles <= kLpCus) launch_shape<FORM, 1, 1, false>(p, epilogue, stream);
   else if (p.tokens <= 16 && tiles > 2 * kLpCus && tiles <= 4 * kLpCus) launch_shape<FORM, 4, 1, false>(p, epilogue, stream);
   else if (p.tokens <= 16) launch_shape<FORM, 2, 1, false>(p, epilogue, stream);
-  else launch_shape<FORM, 2, 2, false>(p, epilogue, stream);
+  else if constexpr (FORM != kWeightBf16) launch_shape<FORM, 2, 2, false>(p, epilogue, stream);
 }
 
 }  // namespace

@@ -146,3 +146,17 @@ def test_linear_workspace_serves_fewer_tokens(L):
                 rc = L.pulse_linear_forward(A, cols, A, tokens, rows, cols, 0, None, 0, None, 0, None, 0, BF16, None,
                                             rows, None, 0, A, size, None)
                 assert rc == EINVAL and b"y is NULL" in L.pulse_last_error(), (rows, cols, most, tokens, L.pulse_last_error())
+
+
+def test_constants(L):
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "pulse_head.h")).read()
+    for macro, value in (("PULSE_VERIFY_MAX_DRAFTS", head.VERIFY_MAX_DRAFTS), ("PULSE_LINEAR_MAX_WIDTH", head.LINEAR_MAX_WIDTH),
+                         ("PULSE_LINEAR_FEW_TOKENS", head.LINEAR_FEW_TOKENS),
+                         *((f"PULSE_ACT_{(name or 'none').upper()}", v) for name, v in head.ACTIVATIONS.items())):
+        assert f"#define {macro} {value}\n" in text, macro
+    # up to so many tokens no workspace is asked for
+    n = head.LINEAR_FEW_TOKENS
+    for tokens, status in ((n, b"y is NULL"), (n + 1, b"workspace")):
+        assert L.pulse_linear_forward(A, 64, A, tokens, 64, 64, 0, None, 0, None, 0, None, 0, BF16, None, 64, None, 0, None, 0,
+                                      None) == EINVAL
+        assert status in L.pulse_last_error()

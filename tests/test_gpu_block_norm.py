@@ -378,3 +378,20 @@ def test_wide_rows(rows, cols):
                                    (torch.bfloat16, False, False, True), (torch.float32, True, False, False)):
         b, h, dy, dh, p = make(rows, cols, dtype, rows + cols, rms, post, gate)
         check(b, h, dy, dh, p, rms, 0.5, dtype)
+
+
+def test_more_rows_than_a_launch_takes():
+    """2^22 rows are one launch's; each of few elements."""
+    rows = (1 << 22) + 5
+    w = torch.ones(8, device="cuda")
+    norm = head.BlockNorm(w, gate=2 * w)
+    b = torch.ones(rows, 8, dtype=torch.bfloat16, device="cuda")
+    h = torch.full_like(b, -1.0)
+    h[-1], b[-2] = 3.0, 0.5
+    y, h_out, stats = norm(b, h)
+    assert (h_out[:-2] == 1).all() and (h_out[-1] == 5).all() and (h_out[-2] == 0).all()
+    assert (y[:-2] == 1).all() and (y[-1] == 1).all() and (y[-2] == 0).all()
+    got = norm.backward(y, h_out, b, h_out, stats)
+    # y is constant along a row, so nothing comes through the norm: g = dh_out
+    assert (got[1][:-2] == 1).all() and (got[1][-1] == 5).all() and (got[0][:-2] == 2).all()
+    assert abs(got[6][0].item() / (rows - 2 + 5) - 1) < 1e-4

@@ -285,6 +285,24 @@ def test_activations_over_their_range():
         within(dx, slope, 2.0 ** -7 * 1.01 * slope.abs() + 1e-5, f"{act}'")
 
 
+def test_activations_far_from_zero():
+    """The largest BF16 values, where a cube or an exponential overflows, and NaN."""
+    top = torch.finfo(torch.bfloat16).max
+    v = torch.tensor([top, -top, 1e30, -1e30, 1e20, -1e20, 1e13, -1e13]).cuda().bfloat16()[:, None]
+    w = torch.ones(1, 1, dtype=torch.bfloat16, device="cuda")
+    for act in ACTS[1:]:
+        for tokens in (8, 40):
+            x = v.repeat(tokens // 8, 1)
+            h = head.Linear(w, activation=act, max_tokens=tokens)
+            y, pre = h(x, keep_pre=True)
+            assert torch.equal(y, x.clamp(min=0)), act
+            assert torch.equal(h.backward(torch.ones_like(pre), x, pre=pre)[0], (x > 0).bfloat16()), act
+            x[3] = math.nan
+            y, pre = h(x, keep_pre=True)
+            dx = h.backward(torch.ones_like(pre), x, pre=pre)[0]
+            assert y[3].isnan().all() and dx[3].isnan().all() and y.isnan().sum() == 1 and dx.isnan().sum() == 1
+
+
 @pytest.mark.parametrize("form", [pulse.MXFP4, pulse.FP8_E4M3])
 @pytest.mark.parametrize("tokens,rows,cols", [(1, 3584, 3584), (1, 40, 96), (2, 100, 129), (5, 1003, 203), (16, 300, 5120),
                                               (17, 256, 640), (33, 4100, 512), (64, 512, 1024), (90, 72, 256),
