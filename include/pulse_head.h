@@ -1,10 +1,13 @@
 /*
- * pulse_head.h -- C ABI of libpulse's operators at a model's output end.
+ * pulse_head.h -- C ABI of libpulse's operators at a model's output end and
+ * between its blocks.
  *
  * The weights whose changes the codec of pulse.h carries are trained and used
  * here: the trainer normalises the last hidden states, takes the cross entropy
  * of the head's logits and its gradient; a receiver multiplies its current
- * tokens with weights that it holds as FP8 or MXFP4 codes.
+ * tokens with weights that it holds as FP8 or MXFP4 codes.  Before that, on both
+ * sides, blocks' outputs join the residual stream through norms and linear
+ * layers; after it, drafted tokens are held against the target's probabilities.
  *
  * Conventions: those of pulse.h (device pointers, a hipStream_t passed as
  * void*, work enqueued and not waited for, no device memory allocated,
@@ -18,7 +21,7 @@
  *     between calls, and serves any calls ordered on one stream;
  *   - results are the same bits for the same inputs: every sum has a fixed
  *     order.
- * Sums, statistics and products are accumulated in FP32.
+ * Sums, statistics and products are accumulated in FP32 (the verification's in FP64).
  */
 #ifndef PULSE_HEAD_H
 #define PULSE_HEAD_H

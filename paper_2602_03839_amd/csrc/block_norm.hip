@@ -6,7 +6,7 @@
 //   y  = norm(h')                  of the sum before it is rounded
 //
 // Bound by HBM: forward b and h in, h' and y out; backward dy, dh', h' and b in, dh
-// and db out.  A row lies in the registers of G lanes as in layer_norm.hip, so that
+// and db out (16,384 x 3,584 BF16: 82 us, 5.8 TB/s, and 134, 5.3).  A row lies in the registers of G lanes as in layer_norm.hip, so that
 // everything in between stays there.
 //
 // Backward, with xh and bh the normalised rows of h' and b and a = dy * weight:

@@ -1,5 +1,5 @@
-"""ctypes binding to libpulse.so's operators at a model's output end (C ABI in
-include/pulse_head.h).
+"""ctypes binding to libpulse.so's operators at a model's output end and between its
+blocks (C ABI in include/pulse_head.h).
 
 Argument marshalling only, like ``pulse``: every call takes torch tensors that
 already live on the GPU, passes their device pointers and the current HIP
