@@ -554,7 +554,7 @@ Plan plan_of(uint32_t tokens, uint32_t rows, uint32_t cols) {
     const Shape s = shape_of(m, n, k);
     return s.splits > 1 ? (uint64_t)s.splits * n * up(m, 4) * 4 : 0;
   };
-  uint64_t most = sums(rows, tokens, cols);
+  uint64_t most = sums(rows, tokens, q.ld);
   for (uint64_t v : {sums(cols, tokens, rows), sums(cols, rows, tokens)})
     if (v > most) most = v;
   q.sums = take(most);

@@ -148,6 +148,24 @@ def test_linear_workspace_serves_fewer_tokens(L):
                 assert rc == EINVAL and b"y is NULL" in L.pulse_last_error(), (rows, cols, most, tokens, L.pulse_last_error())
 
 
+def test_linear_workspace_of_padded_sums(L):
+    """8,191 columns are padded to 8,192, which may be split in 32 by 256 (8,191 in 31 at
+    most): the workspace has to hold the splits that are run.  512 rows and 32 tokens: the
+    padded weight and tokens, d, one chunk's sums and 32 splits' FP32 sums, 256-byte
+    multiples all."""
+    rows, tokens, ld = 512, 32, 8192
+    least = 2 * rows * ld + 2 * tokens * ld + 2 * tokens * rows + 4 * rows + 32 * 4 * tokens * rows
+    assert L.pulse_linear_workspace_bytes(tokens, rows, ld - 1) >= least
+
+    def forward(size):  # a NULL y at the end: nothing is launched
+        rc = L.pulse_linear_forward(A, ld, A, tokens, rows, ld - 1, 0, None, 0, None, 0, None, 0, BF16, None, rows, None, 0,
+                                    A, size, None)
+        assert rc == EINVAL
+        return L.pulse_last_error()
+    assert b"workspace" in forward(least - 1)
+    assert b"y is NULL" in forward(least)
+
+
 def test_constants(L):
     text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "pulse_head.h")).read()
     for macro, value in (("PULSE_VERIFY_MAX_DRAFTS", head.VERIFY_MAX_DRAFTS), ("PULSE_LINEAR_MAX_WIDTH", head.LINEAR_MAX_WIDTH),
