@@ -224,7 +224,7 @@ size_t pulse_verify_drafts_workspace_bytes(uint32_t batch, uint32_t drafts, uint
  * nothing can be drawn the token is -1 and its logprob -inf.
  * Probabilities and their sums are FP64, and so are the scales: rounded to FP32 they
  * would move every border by some 1e-7.  drafts is at most PULSE_VERIFY_MAX_DRAFTS,
- * batch * (2 drafts + 1) and vocab are below 2^31, the scales positive and finite.
+ * batch * (2 drafts + 1) and vocab are below 2^31, the scales from 1e-100 to 1e100.
  */
 int pulse_verify_drafts(int dtype, const void *target, uint64_t target_stride, const void *draft,
                         uint64_t draft_stride, const int64_t *tokens, const int32_t *lengths,

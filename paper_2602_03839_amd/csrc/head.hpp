@@ -267,6 +267,7 @@ struct VerifyParams {
   const float* uniform;    // [batch][drafts + 1]
   uint32_t batch, drafts, vocab;
   double scale, by, draft_by;  // the latter log2(e) times the scales
+  double floor, draft_floor;   // the difference of logits that these take to -1000
   int64_t* out;
   int32_t* count;
   float* logprob;

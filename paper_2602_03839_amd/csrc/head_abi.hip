@@ -339,7 +339,7 @@ int pulse_verify_drafts(int dtype, const void* target, uint64_t target_stride, c
   if (!verify_handles(batch, drafts, vocab))
     return fail(PULSE_EINVAL, "%s: %u sequences of %u drafts, vocabulary of %u", who, batch, drafts, vocab);
   for (double v : {scale, draft_scale})
-    if (!(v > 0.0 && v - v == 0.0)) return fail(PULSE_EINVAL, "%s: a scale is not positive and finite", who);
+    if (!(v >= 1e-100 && v <= 1e100)) return fail(PULSE_EINVAL, "%s: a scale is not from 1e-100 to 1e100", who);
   if (batch == 0) return ok();
   // rows are read from any element on
   const uintptr_t size = dtype == PULSE_DTYPE_BF16 ? 2 : 4;
@@ -368,6 +368,8 @@ int pulse_verify_drafts(int dtype, const void* target, uint64_t target_stride, c
   p.scale = scale;
   p.by = scale * log2e;
   p.draft_by = draft_scale * log2e;
+  p.floor = -1000.0 / p.by;
+  p.draft_floor = -1000.0 / p.draft_by;
   p.out = out;
   p.count = count;
   p.logprob = logprob;

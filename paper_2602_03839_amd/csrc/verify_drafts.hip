@@ -19,7 +19,7 @@
 // of exponentials below it; per sequence the decisions; per segment of a refused draft's
 // rows the sums of max(p - q, 0), of 512 entries each; per sequence the segment that
 // holds the draw, then the entry in it.  Without drafts the first and the last.  64
-// sequences of up to 7 drafts, 152,064 BF16 logits: 83 us; one sequence sampled from
+// sequences of up to 7 drafts, 152,064 BF16 logits: 84 us; one sequence sampled from
 // 151,936: 3 and 6.5 us, and the host's way.
 #include "device_common.hpp"
 #include "head.hpp"
@@ -28,14 +28,13 @@ namespace pulse {
 
 namespace {
 
-// 2^x for x <= 0, or a little above, off by 1.1e-12 and 1 at 0, so that no probability
-// is above 1: a polynomial for what x is from the nearest integer, interpolated at the 9
-// Chebyshev nodes of [-1/2, 1/2].  The integer is in the low bits of x + 1.5 * 2^52, and
-// goes into the exponent by an addition; 2^-1000 stands for 0.
-template <bool CLAMP = true>  // without: x > -1000
-__device__ __forceinline__ double exp2_64(double x) {
-  if constexpr (CLAMP) x = __builtin_fmax(x, -1000.0);
-  const double shifted = x + 0x1.8p52, f = x - (shifted - 0x1.8p52);
+// 2^(d by) for d <= 0 and d by >= -1000, off by 1.1e-12 and 1 at d = 0, so that no
+// probability is above 1: a polynomial for what d by is from the nearest integer,
+// interpolated at the 9 Chebyshev nodes of [-1/2, 1/2].  The integer is in the low bits of
+// d by + 1.5 * 2^52, and goes into the exponent by an addition.  d is a difference of logits:
+// of products with `by` first it would hold their roundings, all of it for logits of 1e20.
+__device__ __forceinline__ double exp2_64(double d, double by) {
+  const double shifted = __builtin_fma(d, by, 0x1.8p52), f = __builtin_fma(d, by, -(shifted - 0x1.8p52));
   double v = __builtin_fma(1.3255224878668817e-06, f, 1.5310079402249296e-05);
   v = __builtin_fma(v, f, 0.00015403455852453838);
   v = __builtin_fma(v, f, 0.0013333450568000645);
@@ -45,6 +44,14 @@ __device__ __forceinline__ double exp2_64(double x) {
   v = __builtin_fma(v, f, 0.6931471805459335);
   v = __builtin_fma(v, f, 1.0);
   return __hiloint2double(__double2hiint(v) + (__double2loint(shifted) << 20), __double2loint(v));
+}
+
+// The same for every d <= 0: below 2^-1000 it is 0.
+__device__ __forceinline__ double exp2_or_0(double d, double by) { return d * by > -1000.0 ? exp2_64(d, by) : 0.0; }
+
+// A segment's sum, of exponentials below its own largest logit, as a part of its row's.
+__device__ __forceinline__ double part_of(const VerifyPart& q, float top, double by) {
+  return q.sum * (q.top == top ? 1.0 : exp2_or_0((double)q.top - (double)top, by));
 }
 
 __device__ __forceinline__ float logit_of(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
@@ -156,8 +163,7 @@ __device__ __forceinline__ const char* row_at(const VerifyParams& p, uint32_t b,
 
 __device__ __forceinline__ double probability(const VerifyRow& d, float z) {
   // the largest logit is infinite where the row is empty: no difference is taken then
-  const double x = ((double)z - (double)d.top) * d.by;
-  return d.inv == 0.0 || !(x > -1000.0) ? 0.0 : exp2_64(x) * d.inv;
+  return d.inv == 0.0 ? 0.0 : exp2_or_0((double)z - (double)d.top, d.by) * d.inv;
 }
 
 // Where a wave's entries lie: eight a lane and 512 at a time, from its segment's first on.
@@ -195,18 +201,22 @@ __global__ __launch_bounds__(256) void verify_sums_kernel(VerifyParams p, uint32
     }
   top = wave_max(top);
   const bool nan = bits > 0x7F800000 || ubits > 0xFF800000u;
-  const double by = r <= p.drafts ? p.by : p.draft_by, from = -(double)top * by;
-  const double least = __builtin_fma((double)(ubits >> 31 ? __uint_as_float(ubits) : 0.0f), by, from);
+  const double by = r <= p.drafts ? p.by : p.draft_by;
+  const double least = (double)(ubits >> 31 ? __uint_as_float(ubits) : 0.0f) - (double)top;
+  const double floor = r <= p.drafts ? p.floor : p.draft_floor;  // there 2^-1000 stands for 0
   double sum[2] = {0.0, 0.0};
   auto add = [&](auto clamp) {
 #pragma unroll
     for (int j = 0; j < kGroups; ++j)
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        sum[e & 1] += exp2_64<decltype(clamp)::value>(__builtin_fma((double)z[j][e], by, from));
+      for (int e = 0; e < 8; ++e) {
+        double d = (double)z[j][e] - (double)top;
+        if constexpr (decltype(clamp)::value) d = __builtin_fmax(d, floor);
+        sum[e & 1] += exp2_64(d, by);
+      }
   };
   // the same for the whole wave
-  if (!__builtin_amdgcn_ballot_w64(!(least > -1000.0))) add(std::false_type{});
+  if (!__builtin_amdgcn_ballot_w64(!(least > floor))) add(std::false_type{});
   else if (top > -INFINITY) add(std::true_type{});
   if (nan || top == INFINITY) sum[0] = (double)NAN;
   const double all = wave_sum64(sum[0] + sum[1]);
@@ -227,7 +237,7 @@ __device__ __forceinline__ VerifyRow join_row(const VerifyParams& p, uint32_t b,
 #pragma unroll 4
     for (uint32_t i = lane; i < p.segments; i += 64) {
       const VerifyPart q = parts[i];
-      sum += q.sum * (q.top == top ? 1.0 : exp2_64(((double)q.top - (double)top) * d.by));
+      sum += part_of(q, top, d.by);
     }
   sum = wave_sum64(sum);
   if (sum > 0.0 && sum < (double)INFINITY) d.inv = 1.0 / sum;  // not where it is NaN
@@ -333,7 +343,7 @@ __global__ __launch_bounds__(64) void verify_draw_kernel(VerifyParams p, uint32_
     if (rest) return rests[i];
     if (d.p.inv == 0.0) return 0.0;
     const VerifyPart q = parts[i];
-    return q.sum * (q.top == d.p.top ? 1.0 : exp2_64(((double)q.top - (double)d.p.top) * d.p.by)) * d.p.inv;
+    return part_of(q, d.p.top, d.p.by) * d.p.inv;
   };
   auto total_of = [&] {
     double mine = 0.0;

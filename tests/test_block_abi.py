@@ -80,7 +80,8 @@ def test_verify_drafts_validation(L):
         (dict(dtype=FP8), EINVAL, b"dtype"), (dict(drafts=129), EINVAL, b"drafts"), (dict(vocab=0), EINVAL, b"vocabulary"),
         (dict(vocab=1 << 31), EINVAL, b"vocabulary"), (dict(batch=1 << 31), EINVAL, b"sequences"),
         (dict(scale=0.0), EINVAL, b"scale"), (dict(scale=INF), EINVAL, b"scale"), (dict(scale=NAN), EINVAL, b"scale"),
-        (dict(dscale=-1.0), EINVAL, b"scale"), (dict(z=None), EINVAL, b"target"), (dict(x=None), EINVAL, b"tokens"),
+        (dict(dscale=-1.0), EINVAL, b"scale"), (dict(scale=9e-101), EINVAL, b"scale"),
+        (dict(dscale=1.1e100), EINVAL, b"scale"), (dict(z=None), EINVAL, b"target"), (dict(x=None), EINVAL, b"tokens"),
         (dict(u=None), EINVAL, b"uniform"), (dict(out=None), EINVAL, b"out"), (dict(count=None), EINVAL, b"count"),
         (dict(lp=None), EINVAL, b"logprob"), (dict(zs=999), EINVAL, b"stride"), (dict(ds=1), EINVAL, b"stride"),
         (dict(zs=1 << 41), EINVAL, b"stride"), (dict(z=A + 1), EALIGN, b"aligned"), (dict(x=A + 4), EALIGN, b"aligned"),

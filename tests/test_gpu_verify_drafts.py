@@ -193,6 +193,41 @@ def test_bfloat16_masks_of_the_lowest_value():
     check(z, x.clamp(max=99), u, None)
 
 
+FLAT = [0.3, -5.0, 77.0, -1e9, 3e20, -1e30, "lowest", "largest"]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("scale", [1.0, 0.7, 1.3, 1e-20, 1e20])
+def test_flat_rows_of_any_value(scale, dtype):
+    """Equal logits have equal weights, whatever their size: u = v / 4096 gives v, and each
+    logprob is log(1 / 4096) in FP32; where others lie far below they do not count."""
+    vocab = 4096
+    info = torch.finfo(dtype)
+    values = [{"lowest": info.min, "largest": info.max}.get(v, v) for v in FLAT]
+    v = torch.arange(len(values)) * 511
+    z = torch.tensor(values).to(dtype)[:, None].repeat(1, vocab)
+    u = (v.double() / vocab).float()[:, None]
+    h = head.VerifyDrafts(2 * vocab, len(v), logit_scale=scale)
+    for mask in (-math.inf, info.min):
+        if mask == info.min:  # 1e-20 * 3e20 is not far
+            z, v, u = (t[[0, 1, 2, 7]] for t in (z, v, u))
+            if scale < 1e-3:
+                continue
+        wide = torch.cat([z, torch.full_like(z, mask)], 1)
+        tokens, count, logprob = h(wide.cuda(), None, u.cuda())
+        assert torch.equal(tokens.cpu()[:, 0], v)
+        assert torch.equal(logprob.cpu(), torch.full((len(v), 1), -math.log(4096)))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_the_only_token_has_a_logprob_of_zero(dtype):
+    z = torch.tensor(FLAT[:-2] + [0.1, 0.7, 11.3, -0.01], dtype=torch.float64).to(dtype)[:, None]
+    for scale in (1.0, 0.7, 1.3):
+        h = head.VerifyDrafts(1, len(z), logit_scale=scale)
+        tokens, count, logprob = h(z.cuda(), None, torch.full((len(z), 1), 0.5).cuda())
+        assert (tokens == 0).all() and (logprob == 0).all()
+
+
 def test_drafts_out_of_range_are_refused():
     z, x, u, zd = make(6, 2, 500, torch.float32, 5, noise=0.01)
     x[0, 0], x[1, 1], x[2, 0], x[3, 1], x[4, 0] = -1, 500, 1 << 33, -(1 << 40), -100
