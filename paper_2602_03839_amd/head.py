@@ -37,8 +37,9 @@ MAX_SIZE = (1 << 31) - 1  # of a vocabulary, a weight's rows or columns, tokens
 EXPORTS = ("pulse_layer_norm_workspace_bytes", "pulse_layer_norm_forward",
            "pulse_layer_norm_backward", "pulse_block_norm_workspace_bytes", "pulse_block_norm_forward",
            "pulse_block_norm_backward", "pulse_linear_ce_workspace_bytes", "pulse_linear_ce_forward",
-           "pulse_linear_ce_backward", "pulse_verify_drafts_workspace_bytes", "pulse_verify_drafts", "pulse_lowp_matmul", "pulse_lowp_linear",
-           "pulse_linear_workspace_bytes", "pulse_linear_forward", "pulse_linear_backward")
+           "pulse_linear_ce_backward", "pulse_verify_drafts_workspace_bytes", "pulse_verify_drafts",
+           "pulse_lowp_matmul", "pulse_lowp_linear", "pulse_linear_workspace_bytes",
+           "pulse_linear_forward", "pulse_linear_backward")
 
 _lock = threading.Lock()
 _lib = None
@@ -410,7 +411,8 @@ class VerifyDrafts:
     times the target's and draft_scale times the draft's logits, the tokens are
     distributed as the target's own.  Without drafts it samples.
 
-    One object serves up to ``max_batch`` sequences of up to ``max_drafts`` drafts a call.
+    One object serves up to ``max_batch`` sequences of up to ``max_drafts`` drafts a call,
+    which are ordered on one stream.  The scales are from 1e-100 to 1e100.
     """
 
     def __init__(self, vocab: int, max_batch: int, max_drafts: int = 0, logit_scale: float = 1.0,
@@ -429,13 +431,15 @@ class VerifyDrafts:
         self.ws = torch.empty(self._nws, dtype=torch.uint8, device=device or "cuda")
         self.device, self._pws = self.ws.device, self.ws.data_ptr()
 
-    def _rows(self, t, name, rows, dtype):
+    def _rows(self, t, name, n, k, dtype):
         if isinstance(t, torch.Tensor) and t.dim() == 3:
+            if t.shape[:2] != (n, k):
+                raise PulseError(f"{name} must be [{n}, {k}, {self.vocab}], got {tuple(t.shape)}")
             try:
                 t = t.view(-1, t.shape[2])
             except RuntimeError:
                 raise PulseError(f"{name}'s rows must be equally far apart (strides {t.stride()})") from None
-        return _matrix(t, name, self.vocab, rows, dtype, self.device)
+        return _matrix(t, name, self.vocab, n * k, dtype, self.device)
 
     def __call__(self, target: torch.Tensor, drafts: Optional[torch.Tensor], uniform: torch.Tensor,
                  draft_logits: Optional[torch.Tensor] = None, lengths: Optional[torch.Tensor] = None,
@@ -458,9 +462,11 @@ class VerifyDrafts:
                              f"{self.max_drafts}")
         pu = _f32(uniform, "uniform", device=dev)
         dt = _dtype(target, "target")
-        pt, st = self._rows(target, "target", n * (k + 1), target.dtype)
-        pd, sd = (None, 0) if draft_logits is None else self._rows(draft_logits, "draft_logits", n * k, target.dtype)
+        pt, st = self._rows(target, "target", n, k + 1, target.dtype)
+        pd, sd = (None, 0) if draft_logits is None else self._rows(draft_logits, "draft_logits", n, k, target.dtype)
         px = _p(drafts, "drafts", dtype=torch.int64, numel=n * k, device=dev, optional=k == 0)
+        if px and drafts.dim() == 2 and drafts.shape != (n, k):
+            raise PulseError(f"drafts must be [{n}, {k}], got {tuple(drafts.shape)}")
         pl = _p(lengths, "lengths", dtype=torch.int32, numel=n, device=dev)
         if tokens is None:
             tokens = _new((n, k + 1), torch.int64, dev, stream)

@@ -348,6 +348,19 @@ def test_another_stream():
     same(got, oracle(z, x, u, zd, None, 1.0, 1.0))
 
 
+def test_drafts_before_sequences_are_refused():
+    z, x, u, zd = cuda(*make(3, 1, 50, torch.float32, 15))
+    h = head.VerifyDrafts(50, 3, 2)
+    good = h(z.view(3, 2, 50), x, u, draft_logits=zd.view(3, 1, 50))
+    assert all(torch.equal(a, b) for a, b in zip(good, h(z, x.view(-1), u, draft_logits=zd)))
+    with pytest.raises(pulse.PulseError, match="target must"):
+        h(z.view(2, 3, 50), x, u)
+    with pytest.raises(pulse.PulseError, match="draft_logits must"):
+        h(z, x, u, draft_logits=zd.view(1, 3, 50))
+    with pytest.raises(pulse.PulseError, match="drafts must"):
+        h(z, x.view(1, 3), u)
+
+
 def test_refusals():
     z, x, u, zd = cuda(*make(3, 2, 50, torch.float32, 14))
     h = head.VerifyDrafts(50, 3, 2)
