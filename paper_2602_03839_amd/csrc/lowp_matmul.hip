@@ -282,20 +282,20 @@ __global__ __launch_bounds__(1024) void lowp_matmul_kernel(LowpMatmulParams p, u
 // A tile's results of one token: the four rows from `row` on.
 template <int FORM, bool EPILOGUE>
 __device__ __forceinline__ void store_result(const LowpMatmulParams& p, f32x4_t v, uint32_t t, uint64_t row) {
-  if (t >= p.tokens || row >= p.rows) return;
+  if (t >= p.tokens || (EPILOGUE && row >= p.rows)) return;
   if constexpr (FORM == kWeightFp8) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] /= p.inv_scale;
   }
-  const uint32_t left = p.rows - row < 4 ? (uint32_t)(p.rows - row) : 4;
   if constexpr (EPILOGUE) {
+    const uint32_t left = p.rows - row < 4 ? (uint32_t)(p.rows - row) : 4;
     const Epilogue e = epilogue_here();
     v = finish_four(e, load_operands(e, t, row, left), v, t, row, left);
     // vmcnt(0): without it the compiler, for whom an operand may be loaded and not used,
     // waits in the products' loop, at every slab and for the slabs too
     __builtin_amdgcn_s_waitcnt(0x0F70);
   }
-  store_four(p.y, t * p.y_stride + row, p.y_bf16, left, v);
+  store_four(p.y, t * p.y_stride + row, p.y_bf16, row, p.rows, v);
 }
 
 // ---------------------------------------------------------------- slabs
@@ -466,7 +466,7 @@ __global__ __launch_bounds__(NS ? 768 : 1024) void lowp_slab_kernel(LowpMatmulPa
           }
           const uint32_t token = t0 + n * 16 + r16, stored = token < p.tokens ? left : 0;
           v = finish_four(e, o[n], v, token, row, stored);
-          store_four(p.y, (uint64_t)token * p.y_stride + row, p.y_bf16, stored, v);
+          store_four(p.y, (uint64_t)token * p.y_stride + row, p.y_bf16, 0, stored, v);
         }
       }
       return;
