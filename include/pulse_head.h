@@ -305,8 +305,9 @@ int pulse_linear_forward(const uint16_t *x, uint64_t x_stride, const uint16_t *w
  * upstream dy (the residual's gradient is dy itself): with
  *   d = dy * times * act'(pre),
  *   dx = d W,   dweight = d^T x,   dbias = sum over tokens of d,   dtimes = dy * act(pre).
- * For the two products d is rounded to BF16, unless it is a BF16 dy unchanged; they are
- * summed in FP32 and rounded once to BF16.  dbias is summed from d as it is.  relu's
+ * The two products take d as the sum of two BF16 values, which leaves 2^-16 of it at
+ * most (nothing of a BF16 dy without multiplier and with no activation or relu); they
+ * are summed in FP32 and rounded once to BF16.  dbias is summed from d as it is.  relu's
  * derivative at 0 is 0.
  *   dtype     of dy, pre, times and dtimes: F32 or BF16.
  *   pre       may be NULL with neither an activation nor times.

@@ -242,9 +242,12 @@ struct Gemm {
   }
 
   // Sums over k0 <= k < k1 (k0 a multiple of 64).  Every wave calls it; ends with
-  // a barrier, after which `lds` is free.
+  // a barrier, after which `lds` is free.  PAIRS: B's values are pairs of BF16 whose sums
+  // are meant, the second ones `low` bytes behind the first; each 64 k of A are then
+  // two steps.
+  template <bool PAIRS = false>
   static __device__ __forceinline__ void run(char* lds, const GemmOperand& a, const GemmOperand& b, uint32_t k0,
-                                             uint32_t k1, Acc& acc) {
+                                             uint32_t k1, Acc& acc, uint64_t low = 0) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     A la;
     B lb;
@@ -254,7 +257,9 @@ struct Gemm {
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    const int32_t full = (int32_t)((k1 - k0) / kGemmK), steps = (int32_t)((k1 - k0 + kGemmK - 1) / kGemmK);
+    constexpr int32_t kEach = PAIRS ? 2 : 1;
+    const int32_t full = (int32_t)((k1 - k0) / kGemmK) * kEach;
+    const int32_t steps = (int32_t)((k1 - k0 + kGemmK - 1) / kGemmK) * kEach;
     if (steps == 0) return;
     const int32_t rest = (int32_t)((k1 - k0) % kGemmK);
     const uint32_t at_a = lds_address(lds) + A::lane_place((wave / WN) * (FM * 16), lane);
@@ -268,6 +273,17 @@ struct Gemm {
     auto advance = [&] {
       here = after;
       after = after + kStage == kLds ? 0 : after + kStage;
+    };
+    bool second = false;  // the next step is the second of its 64 k
+    auto next = [&] {
+      if constexpr (PAIRS) {
+        la.at += second ? la.step : 0;
+        lb.at += second ? lb.step - low : low;
+        second = !second;
+      } else {
+        la.next();
+        lb.next();
+      }
     };
     auto load = [&](uint32_t buffer, int i) {  // the i-th load of the next step, which is whole
       char* to = lds + buffer;
@@ -283,8 +299,7 @@ struct Gemm {
         la.load_end(to, rest, wave, lane);
         lb.load_end(to + A::kBytes, rest, wave, lane);
       }
-      la.next();
-      lb.next();
+      next();
     };
     auto read = [&](Frags& f, uint32_t from, int ks, int i) {  // fragment i of that half of a buffer
       if (i < FN) f.b[i] = B::fragment(from + at_b, i, ks);
@@ -330,8 +345,7 @@ struct Gemm {
       half(f1, here, 1, f0, false, 0);
       wait_and_meet<(NST - 2) * kLoads>();
       half(f0, after, 0, f1, true, here);
-      la.next();
-      lb.next();
+      next();
       advance();
     }
     // the last steps (and short sums), one half after the other

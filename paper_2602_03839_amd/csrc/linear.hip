@@ -9,10 +9,13 @@
 // 3,584: forward 412 us (1.35 PFLOP/s), with silu, multiplier and pre-activation 477 to
 // 500 for the 466 MB that these move; dx 444 and dW 498 (1.25 and 1.12).
 //
-// Backward, with d = dy * times * act'(pre) rounded to BF16 (the products need a BF16
-// operand; for a BF16 dy without activation and multiplier it is dy itself):
-//   dx = d W,   dW = d^T x,   dbias = sum over tokens of d before its rounding,
-//   dtimes = dy * act(pre).
+// Backward, with d = dy * times * act'(pre):
+//   dx = d W,   dW = d^T x,   dbias = sum over tokens of d,   dtimes = dy * act(pre).
+// The matrix cores take BF16, which would cut d to 8 bits: dx and dW 0.0023 off where
+// their own rounding is 0.0017, and a direction that the rows of W (or x) share would not
+// cancel in sums over d.  So d is two BF16 values, both products have twice the steps, and
+// 2^-16 of d is what is left out (4,096 tokens, 18,944 x 3,584: 1,930 us, 1,070 with one).
+// For a BF16 dy without multiplier, and no activation or relu, one holds it.
 // One elementwise kernel makes d, dtimes and parts of dbias (158 us there: 776 MB at 4.9
 // TB/s).
 //
@@ -37,6 +40,7 @@ struct ProductParams {
   uint32_t m_ld;     // a multiple of 4
   void* out;
   uint64_t out_ld;
+  uint64_t low;  // PAIRS: bytes from b's upper parts to its lower ones
   bool wide;    // every row of the epilogue starts at 16 bytes
   bool stream;  // what is read and written there is more than the caches keep
   Epilogue e;
@@ -152,7 +156,7 @@ __device__ __forceinline__ void finish_eight(const ProductParams& p, const Fetch
 // activation, or kPlain: there is no epilogue.
 constexpr int kPlain = -1;
 
-template <typename T, bool AK, bool BK, int ACT>
+template <typename T, bool AK, bool BK, int ACT, bool PAIRS>
 __device__ __forceinline__ void product_block(const ProductParams& p, char* lds, uint32_t id, uint32_t split) {
   // the tile's FP32 rows pass through LDS, as many fragments' columns at a time as fit
   constexpr int kFit = T::kLds / (T::BM * 4 * 16 * T::WN), kAtOnce = kFit < T::FN ? kFit : T::FN;
@@ -166,7 +170,7 @@ __device__ __forceinline__ void product_block(const ProductParams& p, char* lds,
   // a split past the end has no k and gives zeros
   const uint32_t k1 = !p.sums ? p.k : k0 >= p.k ? k0 : p.k - k0 < p.k_split ? p.k : k0 + p.k_split;
   typename T::Acc acc;
-  T::run(lds, a, b, k0, k1, acc);
+  T::template run<PAIRS>(lds, a, b, k0, k1, acc, p.low);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (p.sums) {
     float* const sums = p.sums + (uint64_t)split * p.n * p.m_ld;
@@ -243,20 +247,20 @@ __device__ __forceinline__ void product_block(const ProductParams& p, char* lds,
   if constexpr (T::FN > kAtOnce) pass(std::integral_constant<int, kAtOnce>{});
 }
 
-template <typename T, bool AK, bool BK, int ACT>
+template <typename T, bool AK, bool BK, int ACT, bool PAIRS>
 __global__ __launch_bounds__(T::kThreads) void product_kernel(ProductParams p) {
   __shared__ alignas(1024) char lds[T::kLds];
-  product_block<T, AK, BK, ACT>(p, lds, p.first_tile + blockIdx.x, blockIdx.y);
+  product_block<T, AK, BK, ACT, PAIRS>(p, lds, p.first_tile + blockIdx.x, blockIdx.y);
 }
 
 // dx's and dW's products in one launch: dx's blocks, whose sums are the longer ones, first.
-template <typename TX, typename TW>
+template <typename TX, typename TW, bool PAIRS>
 __global__ __launch_bounds__(TX::kThreads) void both_kernel(ProductParams x, ProductParams w) {
   static_assert(TX::kThreads == TW::kThreads && TX::kLds == TW::kLds, "blocks of one shape");
   __shared__ alignas(1024) char lds[TX::kLds];
   const uint32_t first = x.tiles_m * x.tiles_n;
-  if (blockIdx.x < first) product_block<TX, true, false, kPlain>(x, lds, blockIdx.x, 0);
-  else product_block<TW, true, true, kPlain>(w, lds, blockIdx.x - first, 0);
+  if (blockIdx.x < first) product_block<TX, true, false, kPlain, PAIRS>(x, lds, blockIdx.x, 0);
+  else product_block<TW, true, true, kPlain, PAIRS>(w, lds, blockIdx.x - first, 0);
 }
 
 // The splits' sums, added in order, and the epilogue: a thread an eight of a row.
@@ -307,6 +311,18 @@ __device__ __forceinline__ void pad_rows(const PadJob& j, uint32_t block, uint32
   }
 }
 
+// d as two BF16 values of one sign: `v` becomes its upper half, and what that leaves is
+// given back, whose rounding is off by 2^-16 of d at most.  Cut, not rounded, so that no
+// finite d becomes infinite, and never 0 but for d = 0: an infinite weight or token makes
+// of the second product the infinity that it makes of the first, not a NaN (where nothing
+// is left 2^-126 stands there, FP32's smallest).
+__device__ __forceinline__ float take_upper(float& v) {
+  v = __builtin_canonicalizef(v);  // a NaN's upper half is one then
+  const float all = __builtin_fabsf(v);
+  v = __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);
+  return __builtin_copysignf(__builtin_fmaxf(all - __builtin_fabsf(v), __builtin_fminf(all, 0x1p-126f)), v);
+}
+
 struct SlopeParams {
   const void* dy;
   uint64_t dy_stride;
@@ -318,6 +334,7 @@ struct SlopeParams {
   uint64_t dtimes_stride;
   uint16_t* d;  // null: dy serves; rows of d_ld, zeros past the last feature
   uint32_t d_ld;
+  uint64_t low;  // elements from d's upper parts to its lower ones; 0: d is BF16 as it is
   float* partial;  // null: no bias; [chunks][rows] (one chunk: dbias itself)
   uint32_t tokens, rows, chunk;
   int act, bf16;
@@ -374,8 +391,16 @@ __device__ __forceinline__ void slope_rows(const SlopeParams& p, uint32_t strip,
 #pragma unroll
         for (int i = 0; i < W; ++i) sum[i] += v[k][i];
         if (p.d) {
-          if constexpr (W == 8) store16(p.d + t * p.d_ld + row, pack_eight(v[k]));
-          else p.d[t * p.d_ld + row] = (uint16_t)bf16x2_rne(__float_as_uint(v[k][0]), 0u);
+          uint16_t* const d = p.d + t * p.d_ld + row;
+          if (p.low) {
+            float rest[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) rest[i] = take_upper(v[k][i]);
+            if constexpr (W == 8) store16(d + p.low, pack_eight(rest));
+            else d[p.low] = (uint16_t)bf16x2_rne(__float_as_uint(rest[0]), 0u);
+          }
+          if constexpr (W == 8) store16(d, pack_eight(v[k]));
+          else *d = (uint16_t)bf16x2_rne(__float_as_uint(v[k][0]), 0u);
         }
       }
     }
@@ -447,7 +472,8 @@ struct Shape {
   uint32_t splits;
 };
 
-Shape shape_of(uint32_t m, uint32_t n, uint32_t k) {
+// each: steps of 64 k, two for pairs.
+Shape shape_of(uint32_t m, uint32_t n, uint32_t k, uint32_t each) {
   constexpr float kCus = 256.0f;
   Shape best = {2, 1};
   float least = 0.0f;
@@ -459,7 +485,7 @@ Shape shape_of(uint32_t m, uint32_t n, uint32_t k) {
       if (splits > 1 && (splits * bytes > kSumBytes || k < splits * kMinSplit || tiles * splits > 2 * kCus)) break;
       const float blocks = tiles * splits;
       const float rounds = (float)(uint64_t)((blocks + kCus - 1) / kCus), busy = blocks < kCus ? blocks / kCus : 1.0f;
-      const float steps = (float)parts(parts(k, splits), kGemmK);
+      const float steps = (float)(parts(parts(k, splits), kGemmK) * each);
       float cost = rounds * (c.fixed + (c.step + c.shared * busy) * steps);
       if (splits > 1) cost += 8.0f + (float)((splits + 1) * bytes) / 2e6f;
       if (least == 0.0f || cost < least) {
@@ -484,9 +510,9 @@ using TileM = Gemm<256, 128, 4, 2, 3, AK, BK>;
 template <bool AK, bool BK>
 using TileS = Gemm<128, 64, 4, 1, 4, AK, BK>;
 
-template <bool AK, bool BK, int ACT>
+template <bool AK, bool BK, int ACT, bool PAIRS>
 void run_product(ProductParams p, float* sums, hipStream_t stream) {
-  const Shape s = shape_of(p.m, p.n, p.k);
+  const Shape s = shape_of(p.m, p.n, p.k, PAIRS ? 2 : 1);
   p.stream = (uint64_t)p.m * p.n * (p.e.out_bf16 ? 2 : 4) >= kStreamBytes;
   p.m_ld = up(p.m, 4);
   p.sums = s.splits > 1 ? sums : nullptr;
@@ -498,7 +524,7 @@ void run_product(ProductParams p, float* sums, hipStream_t stream) {
     for (uint64_t first = 0; first < tiles; first += kTilesAtOnce) {
       p.first_tile = (uint32_t)first;
       const uint64_t left = tiles - first;
-      hipLaunchKernelGGL((product_kernel<T, AK, BK, ACT>), dim3(left < kTilesAtOnce ? (uint32_t)left : kTilesAtOnce, s.splits),
+      hipLaunchKernelGGL((product_kernel<T, AK, BK, ACT, PAIRS>), dim3(left < kTilesAtOnce ? (uint32_t)left : kTilesAtOnce, s.splits),
                          dim3(T::kThreads), 0, stream, p);
     }
   };
@@ -513,6 +539,7 @@ void run_product(ProductParams p, float* sums, hipStream_t stream) {
 
 // dx and dW: where the smallest tiles of both are fewer than CUs, and dx's sums short,
 // one launch instead of two or three (each costs 3 us on the host and as much on the GPU).
+template <bool PAIRS>
 void run_gradients(ProductParams x, ProductParams w, float* sums, hipStream_t stream) {
   typedef TileS<true, false> TX;
   typedef TileS<true, true> TW;
@@ -520,11 +547,11 @@ void run_gradients(ProductParams x, ProductParams w, float* sums, hipStream_t st
   set_tiles<TW>(w);
   const uint64_t tiles = (uint64_t)x.tiles_m * x.tiles_n + (uint64_t)w.tiles_m * w.tiles_n;
   if (tiles <= 256 && x.k <= 2048 && w.k <= 2048) {
-    hipLaunchKernelGGL((both_kernel<TX, TW>), dim3((uint32_t)tiles), dim3(TX::kThreads), 0, stream, x, w);
+    hipLaunchKernelGGL((both_kernel<TX, TW, PAIRS>), dim3((uint32_t)tiles), dim3(TX::kThreads), 0, stream, x, w);
     return;
   }
-  run_product<true, false, kPlain>(x, sums, stream);
-  run_product<true, true, kPlain>(w, sums, stream);
+  run_product<true, false, kPlain, PAIRS>(x, sums, stream);
+  run_product<true, true, kPlain, PAIRS>(w, sums, stream);
 }
 
 struct Plan {
@@ -548,15 +575,16 @@ Plan plan_of(uint32_t tokens, uint32_t rows, uint32_t cols) {
   };
   q.w = take(cols % 8 ? (uint64_t)rows * q.ld * 2 : 0);
   q.x = take((uint64_t)tokens * q.ld * 2);
-  q.d = take((uint64_t)tokens * q.d_ld * 2);
+  q.d = take((uint64_t)tokens * q.d_ld * 4);
   q.partial = take((uint64_t)q.chunks * rows * 4);
-  auto sums = [&](uint32_t m, uint32_t n, uint32_t k) -> uint64_t {
-    const Shape s = shape_of(m, n, k);
+  auto sums = [&](uint32_t m, uint32_t n, uint32_t k, uint32_t each) -> uint64_t {
+    const Shape s = shape_of(m, n, k, each);
     return s.splits > 1 ? (uint64_t)s.splits * n * up(m, 4) * 4 : 0;
   };
-  uint64_t most = sums(rows, tokens, q.ld);
-  for (uint64_t v : {sums(cols, tokens, rows), sums(cols, rows, tokens)})
-    if (v > most) most = v;
+  uint64_t most = sums(rows, tokens, q.ld, 1);
+  for (uint32_t each : {1u, 2u})
+    for (uint64_t v : {sums(cols, tokens, rows, each), sums(cols, rows, tokens, each)})
+      if (v > most) most = v;
   q.sums = take(most);
   q.total = at;
   return q;
@@ -628,11 +656,11 @@ hipError_t launch_linear(const LinearParams& c, char* ws, hipStream_t stream) {
            (!c.e.times || c.e.times_stride % unit == 0) && (!c.e.residual || c.e.residual_stride % unit == 0);
   float* const sums = (float*)(ws + q.sums);
   switch (c.e.act) {
-    case kActRelu: run_product<false, false, kActRelu>(p, sums, stream); break;
-    case kActSilu: run_product<false, false, kActSilu>(p, sums, stream); break;
-    case kActGelu: run_product<false, false, kActGelu>(p, sums, stream); break;
-    case kActGeluTanh: run_product<false, false, kActGeluTanh>(p, sums, stream); break;
-    default: run_product<false, false, kActNone>(p, sums, stream);
+    case kActRelu: run_product<false, false, kActRelu, false>(p, sums, stream); break;
+    case kActSilu: run_product<false, false, kActSilu, false>(p, sums, stream); break;
+    case kActGelu: run_product<false, false, kActGelu, false>(p, sums, stream); break;
+    case kActGeluTanh: run_product<false, false, kActGeluTanh, false>(p, sums, stream); break;
+    default: run_product<false, false, kActNone, false>(p, sums, stream);
   }
   return hipGetLastError();
 }
@@ -644,7 +672,8 @@ hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t s
   const Tidy w = tidy(c.weight, c.cols, c.rows, c.cols, (uint16_t*)(ws + q.w), q.ld, threads);
   const Tidy x = tidy(c.x, c.x_stride, c.tokens, c.cols, (uint16_t*)(ws + q.x), q.ld, threads);
   // d, dtimes and dbias
-  const bool serves = !c.act && !c.times && c.bf16 && c.rows % 8 == 0 && c.dy_stride % 8 == 0 && c.dy_stride <= kMaxStride;
+  const bool exact = c.bf16 && !c.times && (c.act == kActNone || c.act == kActRelu);  // d is dy or 0
+  const bool serves = exact && !c.act && c.rows % 8 == 0 && c.dy_stride % 8 == 0 && c.dy_stride <= kMaxStride;
   SlopeParams s = {};
   s.dy = c.dy;
   s.dy_stride = c.dy_stride;
@@ -656,6 +685,7 @@ hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t s
   s.dtimes_stride = c.dtimes_stride;
   s.d = serves ? nullptr : (uint16_t*)(ws + q.d);
   s.d_ld = q.d_ld;
+  s.low = exact ? 0 : (uint64_t)c.tokens * q.d_ld;
   s.partial = !c.dbias ? nullptr : q.chunks == 1 ? c.dbias : (float*)(ws + q.partial);
   s.tokens = c.tokens;
   s.rows = c.rows;
@@ -687,6 +717,7 @@ hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t s
   p.k = c.rows;
   p.out = c.dx;
   p.out_ld = c.dx_stride;
+  p.low = s.low * 2;
   p.wide = c.dx_stride % 8 == 0;
   ProductParams g = p;
   g.a = {x.p, x.ld, q.ld};
@@ -696,7 +727,8 @@ hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t s
   g.out = c.dweight;
   g.out_ld = c.cols;
   g.wide = c.cols % 8 == 0;
-  run_gradients(p, g, (float*)(ws + q.sums), stream);
+  if (exact) run_gradients<false>(p, g, (float*)(ws + q.sums), stream);
+  else run_gradients<true>(p, g, (float*)(ws + q.sums), stream);
   return hipGetLastError();
 }
 
