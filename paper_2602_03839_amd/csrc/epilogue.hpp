@@ -2,10 +2,13 @@
 // multiplier and residual, in FP32 and in this order; and the activations' derivatives.
 //
 //   silu(v) = v s(v), s(v) = 1 / (1 + e^-v)
-//   gelu(v) = v (1 + erf(v / sqrt 2)) / 2
+//   gelu(v) = v (1 + erf(v / sqrt 2)) / 2 = v erfc(-v / sqrt 2) / 2
 //   gelu_tanh(v) = v (1 + tanh y) / 2 = v s(2 y), y = sqrt(2 / pi) (v + 0.044715 v^3)
-// Exponentials and reciprocals are the hardware's (1 ulp each): a value is off by a few
-// ulp, and where it is a small fraction of v by a few ulp of v.
+// Exponentials and reciprocals are the hardware's (1 ulp each).  An exponential makes of its
+// argument's rounding a relative error: silu is off by (6 + 2 |v|) 2^-24 of itself at most,
+// gelu by (36 + 3 v^2) 2^-24, gelu_tanh by (6 + 12 |y|) 2^-24; what is below 2e-36 may be 0.
+// (1 + erf cancels: 4% off at v = -5, and 0 from -5.5 on.  4,096 tokens, 4,864 x 896: 87 us
+// with it, 95 with erfc; 18,944 x 3,584: 600 with either.)
 #pragma once
 
 #include "device_common.hpp"
@@ -34,7 +37,7 @@ __device__ __forceinline__ float activate(int act, float v) {
   switch (act) {
     case kActRelu: return v < 0.0f ? 0.0f : v;  // a NaN stays one
     case kActSilu: return v * sigmoid_of(v);
-    case kActGelu: return 0.5f * v * (1.0f + erff(0.7071067811865476f * v));
+    case kActGelu: return 0.5f * v * erfcf(-0.7071067811865476f * v);
     case kActGeluTanh: return v * gelu_tanh_gate(v);
     default: return v;
   }
@@ -49,7 +52,7 @@ __device__ __forceinline__ float2 activate2(int act, float v) {
       return make_float2(v * s, s * __builtin_fmaf(v, 1.0f - s, 1.0f));
     }
     case kActGelu: {
-      const float h = 0.5f * (1.0f + erff(0.7071067811865476f * v));
+      const float h = 0.5f * erfcf(-0.7071067811865476f * v);
       const float d = 0.3989422804014327f * __builtin_amdgcn_exp2f(-0.7213475204444817f * v * v);
       return make_float2(v * h, __builtin_fmaf(v, d, h));
     }
