@@ -252,7 +252,8 @@ int pulse_lowp_matmul(int dtype, const uint8_t *codes, const uint8_t *scales, fl
                       uint32_t tokens, int y_dtype, void *y, uint64_t y_stride, void *stream);
 
 /* Activations; silu(v) = v / (1 + e^-v), gelu(v) = v (1 + erf(v / sqrt 2)) / 2,
- * gelu_tanh(v) = v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2. */
+ * gelu_tanh(v) = v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) / 2.  At -inf and inf they
+ * and their slopes are what they tend to: 0 and inf, 0 and 1. */
 #define PULSE_ACT_NONE 0
 #define PULSE_ACT_RELU 1
 #define PULSE_ACT_SILU 2

@@ -11,6 +11,8 @@
 // with it, 95 with erfc; 18,944 x 3,584: 600 with either.)
 #pragma once
 
+#include <cfloat>
+
 #include "device_common.hpp"
 #include "head.hpp"
 
@@ -33,12 +35,17 @@ __device__ __forceinline__ float gelu_tanh_gate(float v) {
   return v == v ? sigmoid_of(2.0f * kGeluA * __builtin_fmaf(kGeluB * u * u, u, u)) : v;
 }
 
+// Factors beside one that is 0 where v is infinite: -inf and what is far below 0 give 0, the
+// activations' limit there, and a slope has its limits 0 and 1 (a NaN comes from the other factor).
+__device__ __forceinline__ float not_minus_inf(float v) { return __builtin_fmaxf(v, -FLT_MAX); }
+__device__ __forceinline__ float not_inf(float v) { return __builtin_fminf(not_minus_inf(v), FLT_MAX); }
+
 __device__ __forceinline__ float activate(int act, float v) {
   switch (act) {
     case kActRelu: return v < 0.0f ? 0.0f : v;  // a NaN stays one
-    case kActSilu: return v * sigmoid_of(v);
-    case kActGelu: return 0.5f * v * erfcf(-0.7071067811865476f * v);
-    case kActGeluTanh: return v * gelu_tanh_gate(v);
+    case kActSilu: return not_minus_inf(v) * sigmoid_of(v);
+    case kActGelu: return 0.5f * not_minus_inf(v) * erfcf(-0.7071067811865476f * v);
+    case kActGeluTanh: return not_minus_inf(v) * gelu_tanh_gate(v);
     default: return v;
   }
 }
@@ -49,17 +56,17 @@ __device__ __forceinline__ float2 activate2(int act, float v) {
     case kActRelu: return make_float2(v < 0.0f ? 0.0f : v, v > 0.0f ? 1.0f : v == v ? 0.0f : v);
     case kActSilu: {
       const float s = sigmoid_of(v);
-      return make_float2(v * s, s * __builtin_fmaf(v, 1.0f - s, 1.0f));
+      return make_float2(not_minus_inf(v) * s, s * __builtin_fmaf(not_inf(v), 1.0f - s, 1.0f));
     }
     case kActGelu: {
       const float h = 0.5f * erfcf(-0.7071067811865476f * v);
       const float d = 0.3989422804014327f * __builtin_amdgcn_exp2f(-0.7213475204444817f * v * v);
-      return make_float2(v * h, __builtin_fmaf(v, d, h));
+      return make_float2(not_minus_inf(v) * h, __builtin_fmaf(not_inf(v), d, h));
     }
     case kActGeluTanh: {
       const float s = gelu_tanh_gate(v), u = near_zero(v);
       const float y = 2.0f * kGeluA * __builtin_fmaf(3.0f * kGeluB * u, u, 1.0f);
-      return make_float2(v * s, __builtin_fmaf(u * s * (1.0f - s), y, s));
+      return make_float2(not_minus_inf(v) * s, __builtin_fmaf(u * s * (1.0f - s), y, s));
     }
     default: return make_float2(v, 1.0f);
   }

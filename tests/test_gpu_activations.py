@@ -89,3 +89,35 @@ def test_slopes_and_the_multipliers_gradient(act):
     _, _, db, dt = h.backward(one, x, pre=v[None], times=one)
     within(dt[0], value, vbound + LEAST, act)
     within(db, slope, sbound + 2 * LEAST, act + "'")
+
+
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("typ", [torch.float32, torch.bfloat16])
+def test_infinities_have_their_limits(act, typ):
+    """A bias of -inf switches a feature off, one of inf gives inf; slopes are 0 and 1; a NaN
+    stays one."""
+    inf = math.inf
+    v = torch.tensor([-inf, inf, math.nan, -1e38, 1e38, 1.0, -inf, inf]).cuda()
+    want = torch.tensor([0, inf, math.nan, 0, 1e38, math.nan, 0, inf]).to(typ)
+    slope = torch.tensor([0, 1, math.nan, 0, 1, math.nan, 0, 1])
+
+    def same(got, want):
+        for g, e in zip(got.cpu().tolist(), want.tolist()):
+            if e == e:
+                assert g == e, (act, got, want)
+        assert got[2].isnan() and got[5].isfinite()
+
+    w = torch.zeros(8, 16, dtype=torch.bfloat16, device="cuda")
+    codes = torch.zeros(8 * 16, dtype=torch.uint8, device="cuda")
+    low = head.LowpLinear(pulse.FP8_E4M3, codes, None, 8, 16, bias=v, activation=act)
+    for tokens in (1, 5, 40):
+        x = torch.ones(tokens, 16, dtype=torch.bfloat16, device="cuda")
+        h = head.Linear(w, v, activation=act, max_tokens=tokens)
+        y, pre = h(x, out_dtype=typ, keep_pre=True)
+        one = torch.ones(tokens, 8, dtype=typ, device="cuda")
+        _, _, db, dt = h.backward(one, x, pre=pre, times=one)
+        for t in range(tokens):
+            same(y[t], want)
+            same(dt[t], want)
+        same(db / tokens, slope)
+        same(low(x, out_dtype=typ)[0], want)
