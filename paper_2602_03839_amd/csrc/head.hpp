@@ -156,12 +156,15 @@ struct LowpMatmulParams {
   Epilogue e;
 };
 
+constexpr uint32_t kBf16Tokens = 16;  // the most that a BF16 weight is multiplied with here
+
 // `epilogue`: e is looked at; always so for BF16 weights.
 hipError_t launch_lowp_matmul(WeightForm form, bool epilogue, const LowpMatmulParams& p, hipStream_t stream);
 
 // ---------------------------------------------------------------- linear
 
 constexpr uint32_t kLinearFewTokens = 16;  // up to here the forward pass needs no workspace
+static_assert(kLinearFewTokens <= kBf16Tokens, "they are launch_lowp_matmul's");
 
 struct LinearParams {
   const uint16_t* x;

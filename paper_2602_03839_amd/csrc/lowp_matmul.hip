@@ -641,7 +641,8 @@ bool launch_slabs(const LowpMatmulParams& p, bool epilogue, hipStream_t stream) 
   by_epilogue<FORM>(epilogue, [&](auto e) {
     constexpr bool E = decltype(e)::value;
     auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, lds, stream, p, z); };
-    constexpr int kMost = FORM == kWeightBf16 ? 1 : 2;  // tiles of tokens: BF16 has 16 tokens at most
+    static_assert(kBf16Tokens <= 16, "one tile of tokens");
+    constexpr int kMost = FORM == kWeightBf16 ? 1 : 2;  // tiles of tokens
     if (!xreg) launch(lowp_slab_kernel<FORM, 0, 1, E>);
     else if (z.slabs <= z.wk) launch(nt == 1 ? lowp_slab_kernel<FORM, 1, 1, E> : lowp_slab_kernel<FORM, 1, kMost, E>);
     else launch(nt == 1 ? lowp_slab_kernel<FORM, kEach, 1, E> : lowp_slab_kernel<FORM, kEach, kMost, E>);
@@ -670,6 +671,7 @@ void launch_type(const LowpMatmulParams& p, bool epilogue, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_lowp_matmul(WeightForm form, bool epilogue, const LowpMatmulParams& p, hipStream_t stream) {
+  if (form == kWeightBf16 && p.tokens > kBf16Tokens) return hipErrorInvalidValue;  // it has no such kernel
   const uint64_t size = p.y_bf16 ? 2 : 4;
   for (uint32_t first = 0; first < p.tokens; first += kTokensAtOnce) {
     LowpMatmulParams q = p;
