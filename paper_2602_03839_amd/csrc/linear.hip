@@ -556,7 +556,9 @@ void run_gradients(ProductParams x, ProductParams w, float* sums, hipStream_t st
 
 struct Plan {
   uint32_t ld, d_ld, chunk, chunks;
-  uint64_t w, x, d, partial, sums, total;
+  uint64_t w, x, d, partial, sums;
+  uint64_t low;  // d's lower parts: the forward pass's workspace ends here
+  uint64_t total;
 };
 
 Plan plan_of(uint32_t tokens, uint32_t rows, uint32_t cols) {
@@ -575,7 +577,7 @@ Plan plan_of(uint32_t tokens, uint32_t rows, uint32_t cols) {
   };
   q.w = take(cols % 8 ? (uint64_t)rows * q.ld * 2 : 0);
   q.x = take((uint64_t)tokens * q.ld * 2);
-  q.d = take((uint64_t)tokens * q.d_ld * 4);
+  q.d = take((uint64_t)tokens * q.d_ld * 2);
   q.partial = take((uint64_t)q.chunks * rows * 4);
   auto sums = [&](uint32_t m, uint32_t n, uint32_t k, uint32_t each) -> uint64_t {
     const Shape s = shape_of(m, n, k, each);
@@ -586,6 +588,7 @@ Plan plan_of(uint32_t tokens, uint32_t rows, uint32_t cols) {
     for (uint64_t v : {sums(cols, tokens, rows, each), sums(cols, rows, tokens, each)})
       if (v > most) most = v;
   q.sums = take(most);
+  q.low = take((uint64_t)tokens * q.d_ld * 2);
   q.total = at;
   return q;
 }
@@ -609,7 +612,9 @@ Tidy tidy(const uint16_t* from, uint64_t stride, uint64_t rows, uint32_t cols, u
 }  // namespace
 
 uint64_t linear_needs(bool forward, uint32_t tokens, uint32_t rows, uint32_t cols) {
-  return forward && tokens <= kFewTokens ? 0 : plan_of(tokens, rows, cols).total;
+  if (forward && tokens <= kFewTokens) return 0;
+  const Plan q = plan_of(tokens, rows, cols);
+  return forward ? q.low : q.total;
 }
 
 // A call of fewer tokens may take more splits, and shorter chunks: bounds on those parts.
@@ -626,7 +631,7 @@ uint64_t linear_bytes(uint32_t tokens, uint32_t rows, uint32_t cols) {
   product(cols, tokens, rows);
   product(cols, rows, tokens);
   if (sums > kSumBytes) sums = kSumBytes;
-  return q.partial + ((chunks * rows * 4 + 255) & ~255ull) + ((sums + 255) & ~255ull);
+  return q.partial + ((chunks * rows * 4 + 255) & ~255ull) + ((sums + 255) & ~255ull) + q.total - q.low;
 }
 
 hipError_t launch_linear(const LinearParams& c, char* ws, hipStream_t stream) {
@@ -685,7 +690,7 @@ hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t s
   s.dtimes_stride = c.dtimes_stride;
   s.d = serves ? nullptr : (uint16_t*)(ws + q.d);
   s.d_ld = q.d_ld;
-  s.low = exact ? 0 : (uint64_t)c.tokens * q.d_ld;
+  s.low = exact ? 0 : (q.low - q.d) / 2;
   s.partial = !c.dbias ? nullptr : q.chunks == 1 ? c.dbias : (float*)(ws + q.partial);
   s.tokens = c.tokens;
   s.rows = c.rows;
