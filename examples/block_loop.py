@@ -32,12 +32,12 @@ class Policy:
         w = self.bf16
         self.norm = head.LayerNorm(master["norm"], rms=True)
         self.join = head.BlockNorm(master["last"], post_weight=master["post"], residual_scale=SCALE)
-        layers = [head.Linear(w[k], max_tokens=max_tokens, activation="silu" if k == "gate" else None)
-                  for k in MATRICES]
-        ws = torch.empty(max(layer.workspace_bytes for layer in layers), dtype=torch.uint8, device="cuda")
-        for layer in layers:  # one workspace for all: their calls follow each other
-            layer.ws = ws
-        self.gate, self.up, self.down, self.head = layers
+        # one workspace for all: their calls follow each other
+        need = max(head.linear_workspace_bytes(max_tokens, *w[k].shape) for k in MATRICES)
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        self.gate, self.up, self.down, self.head = (
+            head.Linear(w[k], max_tokens=max_tokens, activation="silu" if k == "gate" else None, workspace=ws)
+            for k in MATRICES)
         self.ce = head.LinearCE(w["head"], max_tokens=max_tokens)
 
     def hidden(self, tokens, keep=False):

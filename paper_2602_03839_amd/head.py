@@ -499,6 +499,14 @@ def _activation(name) -> int:
         raise PulseError(f"activation must be one of {list(ACTIVATIONS)}, got {name!r}") from None
 
 
+def linear_workspace_bytes(max_tokens: int, rows: int, cols: int) -> int:
+    """What a Linear of a [rows, cols] weight and so many tokens needs, 0 for sizes that no
+    call handles: the largest of several is a workspace for all of them."""
+    if not all(0 <= v <= LINEAR_MAX_WIDTH for v in (max_tokens, rows, cols)):
+        return 0
+    return int(lib().pulse_linear_workspace_bytes(max_tokens, rows, cols))
+
+
 class Linear:
     """y = act(x W^T + bias) * times + residual for a BF16 weight [rows, cols], from one
     token to many, and its gradient.
@@ -507,7 +515,7 @@ class Linear:
     bfloat16, or None; ``activation`` None, "relu", "silu", "gelu" or "gelu_tanh".  One
     object serves up to ``max_tokens`` tokens a call.  Its workspace is allocated by the
     first call that needs one (forward, more than LINEAR_FEW_TOKENS tokens), or given: a
-    uint8 tensor of at least ``workspace_bytes``, which objects whose calls are ordered
+    uint8 tensor of at least ``linear_workspace_bytes`` of its sizes, which objects whose calls are ordered
     on one stream may share.
     """
 
@@ -526,7 +534,7 @@ class Linear:
         self._bias_dt = 0 if bias is None else _dtype(bias, "bias")
         self.weight, self.bias, self.activation, self.max_tokens = weight, bias, activation, max_tokens
         self._lib = lib()
-        self.workspace_bytes = int(self._lib.pulse_linear_workspace_bytes(max_tokens, self.rows, self.cols))
+        self.workspace_bytes = linear_workspace_bytes(max_tokens, self.rows, self.cols)
         self.ws = workspace
         if workspace is not None:
             _p(workspace, "workspace", dtype=torch.uint8, min_numel=self.workspace_bytes, device=self.device)
