@@ -537,8 +537,12 @@ void run_product(ProductParams p, float* sums, hipStream_t stream) {
   }
 }
 
-// dx and dW: where the smallest tiles of both are fewer than CUs, and dx's sums short,
-// one launch instead of two or three (each costs 3 us on the host and as much on the GPU).
+// dx and dW: where the smallest tiles of both are fewer than CUs, and the sums short, one
+// launch instead of two to four (each costs 3 us on the host and as much on the GPU), whose
+// blocks take a tile's steps one after the other.  us in one launch and in several, d of one
+// part: k up to 512 9.7 and 13.0 (128 x 512 x 512), 1,024 10.4 and 16.1, 2,048 17.4 and 16.2 to
+// 16.9 and 17.6 (2,048 x 128 x 128, 300 x 2,040 x 520); of two parts: 512 18.4 and 23.0, 1,024 25.3
+// and 26.2, 2,048 41.9 and 26.2.
 template <bool PAIRS>
 void run_gradients(ProductParams x, ProductParams w, float* sums, hipStream_t stream) {
   typedef TileS<true, false> TX;
@@ -546,7 +550,8 @@ void run_gradients(ProductParams x, ProductParams w, float* sums, hipStream_t st
   set_tiles<TX>(x);
   set_tiles<TW>(w);
   const uint64_t tiles = (uint64_t)x.tiles_m * x.tiles_n + (uint64_t)w.tiles_m * w.tiles_n;
-  if (tiles <= 256 && x.k <= 2048 && w.k <= 2048) {
+  constexpr uint32_t kMost = PAIRS ? 1024 : 2048;  // of k
+  if (tiles <= 256 && x.k <= kMost && w.k <= kMost) {
     hipLaunchKernelGGL((both_kernel<TX, TW, PAIRS>), dim3((uint32_t)tiles), dim3(TX::kThreads), 0, stream, x, w);
     return;
   }
