@@ -456,7 +456,14 @@ constexpr uint64_t kSumBytes = 32ull << 20;  // the most that splits' sums take
 constexpr uint32_t kMinSplit = 256;          // of k
 constexpr uint32_t kFewTokens = kLinearFewTokens;
 constexpr uint64_t kStreamBytes = 64ull << 20;  // results of more are written past the caches
-constexpr uint32_t kOneChunk = 128;  // tokens up to which dbias is summed by one block a strip
+
+// Few values before the gradient's products: a feature a lane, all tokens in one block's 16
+// waves and dbias summed there.  Else eight features a lane, chunks of tokens and a launch
+// that adds their sums.  us of a gradient with a weight of 64 columns, so and the other way,
+// BF16 silu and multiplier / FP32 gelu and bias: 17 tokens, 1,003 rows 21 and 32 / 21 and 34;
+// 128, 4,864 29.5 and 28.9 / 29.5 and 33.9; 17, 27,648 44 and 45 / 43 and 50; 64, 18,944 48 and 46 /
+// 47 and 51; 128, 27,648 66 and 53 / 58 and 58; 200, 200 22 and 16 / 20 and 21; 512, 1,003 44 and 34.
+bool few_values(uint64_t tokens, uint64_t rows) { return tokens <= 128 && tokens * rows <= 1u << 20; }
 
 // Time of a product in thousands of cycles: rounds of blocks, each with a fixed part and
 // one per 64 of k (which grows with the CUs that share the L2s), and, with splits, their
@@ -572,7 +579,7 @@ Plan plan_of(uint32_t tokens, uint32_t rows, uint32_t cols) {
   q.d_ld = up(rows, 8);
   // chunks of tokens for some eight blocks a CU; few tokens in one
   const uint32_t strips = parts(rows, 512), wanted = strips < 2048 ? 2048 / strips : 1;
-  q.chunk = tokens <= kOneChunk ? tokens : up(parts(tokens, wanted), 16);
+  q.chunk = few_values(tokens, rows) ? tokens : up(parts(tokens, wanted), 16);
   q.chunks = parts(tokens, q.chunk);
   uint64_t at = 0;
   auto take = [&](uint64_t bytes) {
@@ -677,7 +684,7 @@ hipError_t launch_linear(const LinearParams& c, char* ws, hipStream_t stream) {
 
 hipError_t launch_linear_grad(const LinearGradParams& c, char* ws, hipStream_t stream) {
   const Plan q = plan_of(c.tokens, c.rows, c.cols);
-  const bool few = c.tokens <= kOneChunk;
+  const bool few = few_values(c.tokens, c.rows);
   const uint32_t threads = few ? 1024 : 256;
   const Tidy w = tidy(c.weight, c.cols, c.rows, c.cols, (uint16_t*)(ws + q.w), q.ld, threads);
   const Tidy x = tidy(c.x, c.x_stride, c.tokens, c.cols, (uint16_t*)(ws + q.x), q.ld, threads);

@@ -151,3 +151,21 @@ def test_small_values():
             want = a @ b
             bound = 6 * REST * ((a * a) @ (b * b)).sqrt() + 100 * U * (a.abs() @ b.abs()) + 2.0 ** -125 * b.abs().sum(0)
             within(got, want, bound + HALF[BF16] * 1.01 * want.abs(), size)
+
+
+@pytest.mark.parametrize("tokens,rows", [(128, 8192), (128, 8193), (100, 18945), (17, 70001), (129, 8128), (1, 1 << 20)])
+def test_wide_rows_of_few_tokens(tokens, rows):
+    """On both sides of 2^20 values, where d, dtimes and dbias change their kernel: one launch's
+    sums over tokens, or chunks of them."""
+    for typ in (BF16, F32):
+        g = gen(rows)
+        w, x = normal(g, rows, 16).bfloat16(), normal(g, tokens, 16).bfloat16()
+        pre, times = (normal(g, tokens, rows).to(typ) for _ in range(2))
+        dy = normal(g, tokens, rows).to(typ)
+        h = head.Linear(w, torch.zeros(rows, device="cuda"), activation="silu", max_tokens=tokens)
+        check(h, x, w, dy, pre, times, "silu")
+        _, _, db, dt = h.backward(dy, x, pre=pre, times=times)
+        d, off = d64(dy, pre, times, "silu")
+        within(db, d.sum(0), off.sum(0) + (tokens + 20) * U * d.abs().sum(0) + 1e-37, "dbias")
+        value = act64("silu", pre.double())[0] * dy.double()
+        within(dt, value, (8 + 2 * pre.double().abs()) * U * value.abs() + HALF[typ] * 1.01 * value.abs() + 1e-37, "dtimes")
