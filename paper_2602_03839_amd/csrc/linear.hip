@@ -2,12 +2,12 @@
 // tokens, and its gradient.
 //
 // Up to 16 tokens the weight's way from HBM bounds it: lowp_matmul.hip, which reads it
-// once (18,944 x 3,584, 16 tokens: 27 us; 24 tokens there 35, 33 by tiles 28).  For more,
-// the matrix cores: tiles of gemm_tile.hpp, whose sums go through LDS as FP32 rows, so
+// once (18,944 x 3,584, 16 tokens: 27 us).  24 tokens took 35 us there, which reads the
+// weight twice, and 33 take 28 by tiles.  So for more than 16 the matrix cores: tiles of gemm_tile.hpp, whose sums go through LDS as FP32 rows, so
 // that multiplier, residual and results move 16 bytes a lane and whole lines at a time,
 // and the epilogue's code is there once, not once per accumulator.  4,096 tokens, 18,944 x
-// 3,584: forward 412 us (1.35 PFLOP/s), with silu, multiplier and pre-activation 477 to
-// 500 for the 466 MB that these move; dx 444 and dW 498 (1.25 and 1.12).
+// 3,584: forward 412 us (1.35 PFLOP/s), with silu, multiplier and pre-activation 500 to
+// 515 for the 466 MB that these move; dx 444 and dW 498 (1.25 and 1.12) for a d of one part.
 //
 // Backward, with d = dy * times * act'(pre):
 //   dx = d W,   dW = d^T x,   dbias = sum over tokens of d,   dtimes = dy * act(pre).
@@ -16,7 +16,7 @@
 // cancel in sums over d.  So d is two BF16 values, both products have twice the steps, and
 // 2^-16 of d is what is left out (4,096 tokens, 18,944 x 3,584: 1,930 us, 1,070 with one).
 // For a BF16 dy without multiplier, and no activation or relu, one holds it.
-// One elementwise kernel makes d, dtimes and parts of dbias (158 us there: 776 MB at 4.9
+// One elementwise kernel makes d, dtimes and parts of dbias (172 us there: 931 MB at 5.4
 // TB/s).
 //
 // Where the tiles are too few for the chip, k is split over blocks, whose FP32 sums are
@@ -467,7 +467,12 @@ bool few_values(uint64_t tokens, uint64_t rows) { return tokens <= 128 && tokens
 
 // Time of a product in thousands of cycles: rounds of blocks, each with a fixed part and
 // one per 64 of k (which grows with the CUs that share the L2s), and, with splits, their
-// sums' way and a launch.  The tiles' figures are those measured for the cross entropy's.
+// sums' way and a launch.  The tiles' figures are those measured for the cross entropy's,
+// whose epilogue is another.  us without splits by each tile, the chosen one first: forward with
+// silu, multiplier and pre-activation, 64 tokens, 18,944 x 3,584 31 (in splits; 30, 41, 68),
+// 1,024, 4,864 x 896 22 (256 x 128; 41, 33), 2,048, 18,944 x 3,584 279 (256 x 256; 266, 510),
+// 4,096, 4,864 x 896 84 (256 x 256; 68, 104); gradients of two parts 106 (346, 432, 699),
+// 75 (127, 138, 226), 1,003 (1,036, 2,062), 250 (232, 347).
 struct TileCost {
   uint32_t bm, bn;
   float fixed, step, shared;
