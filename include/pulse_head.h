@@ -306,8 +306,8 @@ int pulse_linear_forward(const uint16_t *x, uint64_t x_stride, const uint16_t *w
  * upstream dy (the residual's gradient is dy itself): with
  *   d = dy * times * act'(pre),
  *   dx = d W,   dweight = d^T x,   dbias = sum over tokens of d,   dtimes = dy * act(pre).
- * The two products take d as the sum of two BF16 values, which leaves 2^-16 of it at
- * most (nothing of a BF16 dy without multiplier and with no activation or relu); they
+ * The two products take d as the sum of two BF16 values, which leaves 2^-16 of it or
+ * 2^-126 at most (nothing of a BF16 dy without multiplier and with no activation or relu); they
  * are summed in FP32 and rounded once to BF16.  dbias is summed from d as it is.  relu's
  * derivative at 0 is 0.
  *   dtype     of dy, pre, times and dtimes: F32 or BF16.

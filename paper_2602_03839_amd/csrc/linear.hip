@@ -2,11 +2,11 @@
 // tokens, and its gradient.
 //
 // Up to 16 tokens the weight's way from HBM bounds it: lowp_matmul.hip, which reads it
-// once (18,944 x 3,584, 16 tokens: 27 us).  24 tokens took 35 us there, which reads the
-// weight twice, and 33 take 28 by tiles.  So for more than 16 the matrix cores: tiles of gemm_tile.hpp, whose sums go through LDS as FP32 rows, so
-// that multiplier, residual and results move 16 bytes a lane and whole lines at a time,
-// and the epilogue's code is there once, not once per accumulator.  4,096 tokens, 18,944 x
-// 3,584: forward 412 us (1.35 PFLOP/s), with silu, multiplier and pre-activation 500 to
+// once for every 16 (18,944 x 3,584, 16 tokens: 27 us; 24 tokens took 35 that way, and 33
+// tokens take 28 by tiles).  For more, the matrix cores: tiles of gemm_tile.hpp, whose sums
+// go through LDS as FP32 rows, so that multiplier, residual and results move 16 bytes a lane
+// and whole lines at a time, and the epilogue's code is there once, not once per
+// accumulator.  4,096 tokens, 18,944 x 3,584: forward 412 us (1.35 PFLOP/s), with silu, multiplier and pre-activation 500 to
 // 515 for the 466 MB that these move; dx 444 and dW 498 (1.25 and 1.12) for a d of one part.
 //
 // Backward, with d = dy * times * act'(pre):
@@ -14,7 +14,7 @@
 // The matrix cores take BF16, which would cut d to 8 bits: dx and dW 0.0023 off where
 // their own rounding is 0.0017, and a direction that the rows of W (or x) share would not
 // cancel in sums over d.  So d is two BF16 values, both products have twice the steps, and
-// 2^-16 of d is what is left out (4,096 tokens, 18,944 x 3,584: 1,930 us, 1,070 with one).
+// 2^-16 of d is what is left out (4,096 tokens, 18,944 x 3,584: 1,920 us, 1,020 with one).
 // For a BF16 dy without multiplier, and no activation or relu, one holds it.
 // One elementwise kernel makes d, dtimes and parts of dbias (172 us there: 931 MB at 5.4
 // TB/s).
@@ -315,7 +315,7 @@ __device__ __forceinline__ void pad_rows(const PadJob& j, uint32_t block, uint32
 // given back, whose rounding is off by 2^-16 of d at most.  Cut, not rounded, so that no
 // finite d becomes infinite, and never 0 but for d = 0: an infinite weight or token makes
 // of the second product the infinity that it makes of the first, not a NaN (where nothing
-// is left 2^-126 stands there, FP32's smallest).
+// is left 2^-126 stands there, FP32's smallest, which is more than 2^-16 of a d below 2^-110).
 __device__ __forceinline__ float take_upper(float& v) {
   v = __builtin_canonicalizef(v);  // a NaN's upper half is one then
   const float all = __builtin_fabsf(v);
@@ -468,11 +468,12 @@ bool few_values(uint64_t tokens, uint64_t rows) { return tokens <= 128 && tokens
 // Time of a product in thousands of cycles: rounds of blocks, each with a fixed part and
 // one per 64 of k (which grows with the CUs that share the L2s), and, with splits, their
 // sums' way and a launch.  The tiles' figures are those measured for the cross entropy's,
-// whose epilogue is another.  us without splits by each tile, the chosen one first: forward with
-// silu, multiplier and pre-activation, 64 tokens, 18,944 x 3,584 31 (in splits; 30, 41, 68),
-// 1,024, 4,864 x 896 22 (256 x 128; 41, 33), 2,048, 18,944 x 3,584 279 (256 x 256; 266, 510),
-// 4,096, 4,864 x 896 84 (256 x 256; 68, 104); gradients of two parts 106 (346, 432, 699),
-// 75 (127, 138, 226), 1,003 (1,036, 2,062), 250 (232, 347).
+// whose epilogue is another.  us as chosen, and by 256 x 256, 256 x 128 and 128 x 64 without
+// splits, BF16 with silu and multiplier, forward (pre-activation too) / gradient:
+//      64 tokens, 18,944 x 3,584    31, 68, 41, 30        106, 699, 432, 346
+//   1,024 tokens,  4,864 x   896    22, 41, 23, 33         75, 226, 138, 127
+//   2,048 tokens, 18,944 x 3,584   279, 281, 266, 510   1,003, 1,249, 1,036, 2,062
+//   4,096 tokens,  4,864 x   896    84, 85, 68, 104       250, 363, 232, 347
 struct TileCost {
   uint32_t bm, bn;
   float fixed, step, shared;

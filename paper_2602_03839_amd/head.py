@@ -515,8 +515,8 @@ class Linear:
     bfloat16, or None; ``activation`` None, "relu", "silu", "gelu" or "gelu_tanh".  One
     object serves up to ``max_tokens`` tokens a call.  Its workspace is allocated by the
     first call that needs one (forward, more than LINEAR_FEW_TOKENS tokens), or given: a
-    uint8 tensor of at least ``linear_workspace_bytes`` of its sizes, which objects whose calls are ordered
-    on one stream may share.
+    uint8 tensor of at least ``linear_workspace_bytes`` of its sizes, which objects whose
+    calls are ordered on one stream may share.
     """
 
     def __init__(self, weight: torch.Tensor, bias: Optional[torch.Tensor] = None,
@@ -587,7 +587,9 @@ class Linear:
         the forward pass's x, pre (needed with an activation or a multiplier) and times,
         all of dy's type but x.  dx and dweight are bfloat16, dbias float32, dtimes of
         dy's type; None where there is no bias or multiplier.  The residual's gradient is
-        dy itself."""
+        dy itself.  What is multiplied with weight and x, dy * times * act'(pre), keeps 16
+        bits, which costs twice the products (a bfloat16 dy without a multiplier, with no
+        activation or relu, once)."""
         dev = self.device
         px, sx, n, pws, nws = self._tokens(x, 0, stream)
         dt, typ = _dtype(dy, "dy"), dy.dtype
